@@ -475,6 +475,107 @@ int rtopk_get_stats(rtopk_ctx* ctx, int32_t slice, rtopk_stats* out, void* strea
  * A bookkeeping call with no counterpart in the paper.  *out is host memory.  Errors: INVALID_ARG. */
 int rtopk_get_launch_count(const rtopk_ctx* ctx, uint64_t* out);
 
+/*
+ * ---------------------------------------------------------------------------------------------
+ * Matrix operators of a training round.  They stand around the exchange of Algorithm 1 when the model's
+ * parameters are matrices: the master turns its momentum into an orthogonal update, the new weights go
+ * out as 8-bit codes, the workers multiply with the codes, and their weight gradients are the g that
+ * rtopk_sparsify / rtopk_step take.  The paper has no counterpart for them.
+ *
+ * They have a context of their own, which owns one block of device scratch.  rtopk_matrix_create
+ * allocates it (scratch_bytes: the largest that rtopk_orthogonalize_scratch / rtopk_coded_scratch
+ * give for the shapes to be used; a call that needs more returns INVALID_ARG); no other call
+ * allocates.  Calls that share a context must be ordered on one stream, as for rtopk_ctx.  They only
+ * enqueue work and may be captured into a CUDA graph.
+ *
+ * A view of `batch` matrices of m rows and n columns is a pointer, a row stride ld >= n and a
+ * distance `stride` from one matrix to the next (>= (m - 1) ld + n; not read when batch = 1), all in
+ * elements; it needs no alignment beyond its element's.
+ */
+typedef struct rtopk_matrix rtopk_matrix;
+
+int rtopk_matrix_create(rtopk_matrix** out, int device, int64_t scratch_bytes);
+int rtopk_matrix_destroy(rtopk_matrix* ctx);
+/* As rtopk_last_cuda_error, rtopk_get_launch_count and rtopk_poll_status, for this context. */
+int rtopk_matrix_last_cuda_error(const rtopk_matrix* ctx);
+int rtopk_matrix_get_launch_count(const rtopk_matrix* ctx, uint64_t* out);
+int rtopk_matrix_poll_status(rtopk_matrix* ctx, void* stream);
+
+/*
+ * The orthogonal factor of a matrix by Newton-Schulz steps: for every matrix U of the batch
+ *     X = U / (||U||_F + eps),   then `steps` times   X <- a X + b (X X^T) X + c (X X^T)^2 X
+ * (by the shorter side: X^T X for a tall U), which moves all singular values towards 1 and keeps the
+ * singular vectors.
+ *   src  [in]   batch x m x n of src_dtype;   out [out]  the same shape, out_dtype; may be src itself
+ *               when the two views are the same.
+ *   steps       1 .. 64;   coef  HOST array of steps triples (a, b, c), or null for
+ *               (3.4445, -4.7750, 2.0315) in every step.  Singular values must stay below 4 from step
+ *               to step (they do, below 1.3, with the default), else the 16-bit products overflow.
+ *   eps         >= 0.  A zero matrix gives zeros; one with a NaN or an infinity gives NaN.
+ * The products take 16-bit floating-point operands and 32-bit sums.  The diagonals of X X^T and of its
+ * polynomial and the low half of X stay outside the 16 bits: the result is within about 1e-3 of the
+ * exact iteration (2-norm of the difference over 2-norm of the result).
+ * Errors: INVALID_ARG, UNSUPPORTED (batch above 65535), CUDA.
+ */
+int rtopk_orthogonalize_scratch(int64_t batch, int64_t m, int64_t n, int64_t* bytes);
+int rtopk_orthogonalize(rtopk_matrix* ctx, const void* src, int src_dtype, int64_t ld_src, int64_t stride_src, void* out,
+                        int out_dtype, int64_t ld_out, int64_t stride_out, int64_t batch, int64_t m, int64_t n, int steps,
+                        const float* coef, float eps, void* stream);
+
+/*
+ * The master update of weight matrices with it (Algorithm 1's last line, with momentum):
+ *     v <- fp32(double(mu) v + g);   u = g + mu v with nesterov != 0, else v;
+ *     w <- (1 - eta decay) w - eta scale orth(u)
+ *   grad [in]  binary32, such as the dense average of rtopk_step (or a matrix inside it);
+ *   momentum, weights [in/out]  binary32;   the three views must not overlap.
+ *   eta, decay  finite, >= 0;   0 <= mu < 1;   scale  finite.   steps, coef, eps as above.
+ * Scratch: rtopk_orthogonalize_scratch.   Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+int rtopk_orthogonal_update(rtopk_matrix* ctx, const float* grad, int64_t ld_g, int64_t stride_g, float* momentum, int64_t ld_v,
+                            int64_t stride_v, float* weights, int64_t ld_w, int64_t stride_w, int64_t batch, int64_t m,
+                            int64_t n, float eta, float mu, int nesterov, float decay, float scale, int steps,
+                            const float* coef, float eps, void* stream);
+
+/*
+ * 8-bit codes.  A row v is coded as q = rint(v / s) clamped to +-127 with s = max |v| / 127 (both
+ * quotients rounded to binary32); an all-zero row has s = 0 and q = 0, a row with an infinity or a NaN has
+ * s = NaN and q = 0.
+ *
+ * rtopk_code_weights: W (n_out x n_in of dtype) -> codes for each output channel (row).
+ *   codes   [out]  n_out rows of ld_codes bytes;   scales [out]  n_out binary32;
+ *   codes_t [out]  the same codes transposed, n_in rows of ld_t bytes, for the gradient with respect to x;
+ *                  may be null.
+ * Bases of the code arrays 16-byte aligned, ld_codes and ld_t multiples of 16.  Needs no scratch.
+ */
+int rtopk_code_weights(rtopk_matrix* ctx, const void* weights, int dtype, int64_t ld_w, int64_t n_out, int64_t n_in,
+                       int8_t* codes, int64_t ld_codes, int8_t* codes_t, int64_t ld_t, float* scales, void* stream);
+
+/* Scratch of the two calls below for up to `tokens` tokens. */
+int rtopk_coded_scratch(int64_t tokens, int64_t n_out, int64_t n_in, int64_t* bytes);
+
+/*
+ * A linear layer on codes: x (tokens x n_in of dtype) is coded for each token, and
+ *     out[t][n] = s_t s_n sum_k q_x[t][k] q_w[n][k]        (tokens x n_out of dtype)
+ * The integer sums are exact.  tokens = 0 does nothing.
+ * Errors: INVALID_ARG, UNSUPPORTED (n_in above 131072, where a sum could leave 32 bits), CUDA.
+ */
+int rtopk_coded_product(rtopk_matrix* ctx, const void* x, int dtype, int64_t ld_x, const int8_t* codes, int64_t ld_codes,
+                        const float* scales, int64_t tokens, int64_t n_out, int64_t n_in, void* out, int64_t ld_out,
+                        void* stream);
+
+/*
+ * The gradients of that layer for dy (tokens x n_out of dtype), the rounding to codes taken as the identity:
+ *     dx[t][k] = s_t sum_n q(dy s_w)[t][n] q_w[n][k]       dy times the channel scales, coded for each token;
+ *     dw[n][k] = s_n s_k sum_t q(dy)[t][n] q(x)[t][k]      both coded for each channel, over the tokens.
+ *   dx  tokens x n_in of dtype, may be null (codes_t and scales are read for dx alone);
+ *   dw  n_out x n_in of dw_dtype, overwritten, may be null (x is read for dw alone): a worker's gradient as
+ *       rtopk_sparsify takes it.  With tokens = 0 it is zero.
+ * Errors: INVALID_ARG, UNSUPPORTED (n_out for dx, tokens for dw above 131072), CUDA.
+ */
+int rtopk_coded_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int dtype,
+                          const int8_t* codes_t, int64_t ld_t, const float* scales, int64_t tokens, int64_t n_out,
+                          int64_t n_in, void* dx, int64_t ld_dx, void* dw, int dw_dtype, int64_t ld_dw, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

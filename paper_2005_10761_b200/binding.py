@@ -70,6 +70,21 @@ EXPORTS = {
     "rtopk_get_phase_times": (_int, [_vp, _vp, _vp]),
     "rtopk_get_stats": (_int, [_vp, _i32, _vp, _vp]),
     "rtopk_get_launch_count": (_int, [_vp, _vp]),
+    "rtopk_matrix_create": (_int, [C.POINTER(_vp), _int, _i64]),
+    "rtopk_matrix_destroy": (_int, [_vp]),
+    "rtopk_matrix_last_cuda_error": (_int, [_vp]),
+    "rtopk_matrix_get_launch_count": (_int, [_vp, _vp]),
+    "rtopk_matrix_poll_status": (_int, [_vp, _vp]),
+    "rtopk_orthogonalize_scratch": (_int, [_i64, _i64, _i64, C.POINTER(_i64)]),
+    "rtopk_orthogonalize": (_int, [_vp, _vp, _int, _i64, _i64, _vp, _int, _i64, _i64, _i64, _i64, _i64, _int, _vp, C.c_float,
+                                   _vp]),
+    "rtopk_orthogonal_update": (_int, [_vp, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _i64, _i64, _i64, C.c_float,
+                                       C.c_float, _int, C.c_float, C.c_float, _int, _vp, C.c_float, _vp]),
+    "rtopk_code_weights": (_int, [_vp, _vp, _int, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
+    "rtopk_coded_scratch": (_int, [_i64, _i64, _i64, C.POINTER(_i64)]),
+    "rtopk_coded_product": (_int, [_vp, _vp, _int, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp]),
+    "rtopk_coded_gradients": (_int, [_vp, _vp, _i64, _vp, _i64, _int, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _int,
+                                     _i64, _vp]),
 }
 
 _lib: Optional[C.CDLL] = None

@@ -9,8 +9,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librtopk.so")
-SOURCES = ["rtopk.cu"]
-HEADERS = ["common.cuh", "element.cuh", "select.cuh", "stream.cuh", "sampler.cuh", "aggregate.cuh", "codec.cuh", "threshold.cuh", "finish.cuh"]
+SOURCES = ["rtopk.cu", "matrix.cu"]
+HEADERS = ["common.cuh", "element.cuh", "select.cuh", "stream.cuh", "sampler.cuh", "aggregate.cuh", "codec.cuh", "threshold.cuh", "finish.cuh",
+           "tensorcore.cuh", "gemm.cuh", "coded.cuh", "orthogonal.cuh"]
 
 
 def nvcc() -> str:
@@ -33,7 +34,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not stale():
         return LIB
     cmd = [nvcc(), "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-o", LIB]
+           "-Xcompiler", "-fPIC", "-shared", "-t", str(len(SOURCES)), "-o", LIB]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += [os.path.join(CSRC, s) for s in SOURCES]

@@ -1,0 +1,498 @@
+// Host side of the matrix operators: argument checks, the division of the scratch, tensor maps and the launch sequences.
+// All device work is enqueued on the caller's stream; only the documented status read synchronises.
+#include "../../include/rtopk.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "coded.cuh"
+#include "gemm.cuh"
+#include "orthogonal.cuh"
+
+using namespace rtopk::mat;
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+struct rtopk_matrix {
+  int device = 0, sms = 0;
+  int last_cuda_error = 0;
+  int64_t scratch_bytes = 0;
+  char* scratch = nullptr;
+  uint32_t* error = nullptr;
+  EncodeTiled encode = nullptr;
+  uint64_t launches = 0;
+};
+
+namespace {
+
+int fail(rtopk_matrix* ctx, cudaError_t e) {
+  ctx->last_cuda_error = (int)e;
+  return RTOPK_ERR_CUDA;
+}
+#define MAT_CUDA(call)                                  \
+  do {                                                  \
+    cudaError_t e__ = (call);                           \
+    if (e__ != cudaSuccess) return fail(ctx, e__);      \
+  } while (0)
+#define MAT_TRY(call)                                   \
+  do {                                                  \
+    const int s__ = (call);                             \
+    if (s__ != RTOPK_OK) return s__;                    \
+  } while (0)
+
+struct OnDevice {
+  int prev = -1;
+  bool ok = true;
+  explicit OnDevice(int dev) {
+    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
+    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+  }
+  ~OnDevice() { if (prev >= 0) cudaSetDevice(prev); }
+};
+
+constexpr int64_t kDimMax = 1 << 30;
+constexpr int64_t kBatchMax = 65535;
+constexpr int64_t kDepthMax = 131072;     // 127 * 127 * depth stays below 2^31
+
+int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+int64_t ceil_div(int64_t x, int64_t a) { return (x + a - 1) / a; }
+
+// Divides the scratch; with base = null it only counts.
+struct Carve {
+  char* base;
+  int64_t at = 0;
+  template <class T>
+  T* take(int64_t count) {
+    T* p = base ? (T*)(base + at) : nullptr;
+    at += up(count * (int64_t)sizeof(T), 1024);
+    return p;
+  }
+};
+
+struct OrthScratch {
+  __half *hi[2], *lo, *gram, *poly;
+  float *gram_d, *poly_d, *row_sums;
+  double* part;
+  int slots;
+  int64_t ld_x, ld_a, stride_x, stride_a, stride_d;
+  OrthScratch(Carve& c, int64_t batch, int64_t s, int64_t l) {
+    ld_x = up(l, 64), ld_a = up(s, 64);
+    stride_x = s * ld_x, stride_a = s * ld_a, stride_d = up(s, 64);
+    part = c.take<double>(batch * kNormBlocks);
+    for (auto& h : hi) h = c.take<__half>(batch * stride_x);
+    lo = c.take<__half>(batch * stride_x);
+    gram = c.take<__half>(batch * stride_a);
+    poly = c.take<__half>(batch * stride_a);
+    gram_d = c.take<float>(batch * stride_d);
+    poly_d = c.take<float>(batch * stride_d);
+    slots = (int)ceil_div(l, 32);
+    row_sums = c.take<float>(batch * slots * stride_d);
+  }
+};
+
+struct CodedScratch {
+  int8_t *x_rows, *dy_rows, *x_cols, *dy_cols;
+  float *x_row_s, *dy_row_s, *x_col_s, *dy_col_s;
+  uint32_t* col_max;      // n_in, then n_out
+  int64_t ld_in, ld_out, ld_tok;
+  CodedScratch(Carve& c, int64_t tokens, int64_t n_out, int64_t n_in) {
+    ld_in = up(n_in, 128), ld_out = up(n_out, 128), ld_tok = up(std::max<int64_t>(tokens, 1), 128);
+    x_rows = c.take<int8_t>(tokens * ld_in);
+    dy_rows = c.take<int8_t>(tokens * ld_out);
+    x_cols = c.take<int8_t>(n_in * ld_tok);
+    dy_cols = c.take<int8_t>(n_out * ld_tok);
+    x_row_s = c.take<float>(tokens);
+    dy_row_s = c.take<float>(tokens);
+    x_col_s = c.take<float>(n_in);
+    dy_col_s = c.take<float>(n_out);
+    col_max = c.take<uint32_t>(n_in + n_out);
+  }
+};
+
+// A kernel of a chain may start while the one before it ends (the kernels wait for it themselves); the first of a call
+// starts after all earlier work of the stream.
+template <class... P, class... A>
+int launch(rtopk_matrix* ctx, bool chained, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = chained ? 1 : 0;
+  MAT_CUDA(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
+  ++ctx->launches;
+  return RTOPK_OK;
+}
+
+// Tensor map of a [batch][rows][cols] array: boxes of box_rows rows of one 128-byte swizzle row.
+int tensor_map(rtopk_matrix* ctx, CUtensorMap* map, const void* base, bool int8, int64_t cols, int64_t rows, int64_t batch, int64_t ld, int64_t stride, int box_rows) {
+  const int64_t e = int8 ? 1 : 2;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch};
+  const cuuint64_t strides[2] = {(cuuint64_t)(ld * e), (cuuint64_t)((batch > 1 ? stride : rows * ld) * e)};
+  const cuuint32_t box[3] = {(cuuint32_t)(kDepthBytes / e), (cuuint32_t)box_rows, 1};
+  const cuuint32_t step[3] = {1, 1, 1};
+  const CUresult r = ctx->encode(map, int8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, step,
+                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? RTOPK_OK : fail(ctx, cudaErrorInvalidValue);
+}
+
+struct Operand { const void* p; int64_t cols, rows, ld, stride; };    // as stored: rows of `cols` contiguous elements
+
+template <int kCols, int kEpi>
+int gemm_tile(rtopk_matrix* ctx, bool chained, const Operand& p, const Operand& q, Gemm g, cudaStream_t st) {
+  constexpr bool kInt8 = kEpi == EPI_CODED;
+  constexpr bool kMnMajor = kEpi == EPI_APPLY || kEpi == EPI_OUT || kEpi == EPI_UPDATE;
+  g.tiles_l = (int)ceil_div(g.lanes, kLanes), g.tiles_c = (int)ceil_div(g.cols, kCols);
+  g.tiles = 0;
+  if (g.tri)
+    for (int c = 0; c < g.tiles_c; ++c) g.tiles += std::min(g.tiles_l, ((c + 1) * kCols - 1) / kLanes + 1);
+  else
+    g.tiles = g.tiles_l * g.tiles_c;
+  g.error = ctx->error;
+  CUtensorMap mp, mq;
+  MAT_TRY(tensor_map(ctx, &mp, p.p, kInt8, p.cols, p.rows, g.batch, p.ld, p.stride, kMnMajor ? 64 : kLanes));
+  MAT_TRY(tensor_map(ctx, &mq, q.p, kInt8, q.cols, q.rows, g.batch, q.ld, q.stride, kCols));
+  const int grid = (int)std::min<int64_t>((int64_t)g.tiles * g.batch, ctx->sms);
+  return launch(ctx, chained, k_gemm<kCols, kEpi>, dim3(grid), kGemmThreads, gemm_smem<kCols>(), st, mp, mq, g);
+}
+
+// The tile width: the one whose waves of tiles over the SMs take least, a tile costing its columns plus a fixed part.
+template <int kEpi>
+int gemm(rtopk_matrix* ctx, bool chained, const Operand& p, const Operand& q, const Gemm& g, cudaStream_t st) {
+  auto cost = [&](int cols) {
+    int64_t tiles = 0;
+    const int64_t tl = ceil_div(g.lanes, kLanes), tc = ceil_div(g.cols, cols);
+    if (g.tri)
+      for (int64_t c = 0; c < tc; ++c) tiles += std::min<int64_t>(tl, ((c + 1) * cols - 1) / kLanes + 1);
+    else
+      tiles = tl * tc;
+    return ceil_div(tiles * g.batch, ctx->sms) * (cols + 64);
+  };
+  const int64_t c64 = cost(64), c128 = cost(128), c256 = cost(256);
+  if (c256 <= c128 && c256 <= c64) return gemm_tile<256, kEpi>(ctx, chained, p, q, g, st);
+  if (c128 <= c64) return gemm_tile<128, kEpi>(ctx, chained, p, q, g, st);
+  return gemm_tile<64, kEpi>(ctx, chained, p, q, g, st);
+}
+
+template <int kEpi>
+cudaError_t allow_smem() {
+  cudaError_t e = cudaFuncSetAttribute(k_gemm<64, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, gemm_smem<64>());
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<128, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, gemm_smem<128>());
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<256, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, gemm_smem<256>());
+  return e;
+}
+
+constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
+
+bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+// Batches of matrices with `n` contiguous elements in rows `ld` apart.
+bool bad_view(const void* p, size_t elem, int64_t batch, int64_t m, int64_t n, int64_t ld, int64_t stride) {
+  return !p || !aligned_to(p, elem) || ld < n || (batch > 1 && stride < (m - 1) * ld + n);
+}
+
+struct Target {
+  int epi;                // EPI_OUT or EPI_UPDATE
+  void* out;
+  int bf16;
+  int64_t ld, stride;
+  float keep, rate;
+};
+
+int small_smem(int64_t l) { return (int)((up(l, 8) + 2 * kSmall) * kSmall * sizeof(float)); }
+constexpr int64_t kSmallLong = 256;      // X, its Gram matrix and the polynomial: 96 KB of shared memory
+
+int orthogonal_small(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, int64_t m, int64_t n, int steps, const float* coef, cudaStream_t st) {
+  src.m = (int)m, src.n = (int)n;
+  SmallOut o = {};
+  o.w = to.epi == EPI_UPDATE ? (float*)to.out : nullptr;
+  o.out = to.out, o.bf16 = to.bf16, o.ld = to.ld, o.stride = to.stride, o.keep = to.keep, o.rate = to.rate, o.steps = steps;
+  for (int i = 0; i < 3 * steps; ++i) o.coef[i] = coef ? coef[i] : kQuintic[i % 3];
+  return launch(ctx, false, k_orth_small, dim3((unsigned)batch), 256, small_smem(std::max(m, n)), st, src, o, m > n ? 1 : 0);
+}
+
+int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, int64_t m, int64_t n, int steps, const float* coef, cudaStream_t st) {
+  const int64_t s = std::min(m, n), l = std::max(m, n);
+  const bool tall = m > n;
+  Carve c{ctx->scratch};
+  OrthScratch w(c, batch, s, l);
+  if (c.at > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
+  if (s <= kSmall && l <= kSmallLong) return orthogonal_small(ctx, src, to, batch, m, n, steps, coef, st);
+  src.m = (int)m, src.n = (int)n;
+  src.part = w.part;
+  src.parts = (int)std::min<int64_t>(kNormBlocks, ceil_div(m * n, 2048));
+  MAT_TRY(launch(ctx, false, k_norm, dim3(src.parts, (unsigned)batch), 256, 0, st, src));
+  MAT_TRY(launch(ctx, true, k_split, dim3((unsigned)ceil_div(n, 64), (unsigned)ceil_div(m, 64), (unsigned)batch), 256, 0, st, src, w.hi[0], w.lo, w.ld_x, w.stride_x,
+                 w.row_sums, w.slots, w.stride_d, tall ? 1 : 0));
+  int cur = 0;
+  for (int i = 0; i < steps; ++i) {
+    const float* k = coef ? coef + 3 * i : kQuintic;
+    const Operand x = {w.hi[cur], l, s, w.ld_x, w.stride_x};
+    const Operand gram = {w.gram, s, s, w.ld_a, w.stride_a}, poly = {w.poly, s, s, w.ld_a, w.stride_a};
+    Gemm g = {};
+    g.batch = (int)batch;
+    g.d_stride = w.stride_d;
+    g.row_sums = w.row_sums, g.slots = w.slots;
+    g.a = k[0], g.b = k[1], g.c = k[2];
+    g.lanes = g.cols = (int)s, g.depth = (int)l, g.tri = 1;
+    g.h = w.gram, g.ld = w.ld_a, g.stride = w.stride_a, g.d_out = w.gram_d;
+    MAT_TRY(gemm<EPI_GRAM>(ctx, true, x, x, g, st));
+    g.depth = (int)s;
+    g.o = w.gram, g.d_in = w.gram_d, g.h = w.poly, g.d_out = w.poly_d;
+    MAT_TRY(gemm<EPI_POLY>(ctx, true, gram, gram, g, st));
+    g.lanes = (int)l, g.tri = 0;
+    g.o = w.hi[cur], g.lo = w.lo, g.ld = w.ld_x, g.stride = w.stride_x, g.d_in = w.poly_d;
+    if (i + 1 < steps) {
+      g.h = w.hi[cur ^ 1];
+      MAT_TRY(gemm<EPI_APPLY>(ctx, true, x, poly, g, st));
+      cur ^= 1;
+    } else {
+      g.out = to.out, g.out_bf16 = to.bf16, g.keep = to.keep, g.rate = to.rate;
+      g.out_col = tall ? 1 : to.ld, g.out_lane = tall ? to.ld : 1, g.out_batch = to.stride;
+      if (to.epi == EPI_OUT) MAT_TRY(gemm<EPI_OUT>(ctx, true, x, poly, g, st));
+      else MAT_TRY(gemm<EPI_UPDATE>(ctx, true, x, poly, g, st));
+    }
+  }
+  return RTOPK_OK;
+}
+
+int check_orth(const rtopk_matrix* ctx, int64_t batch, int64_t m, int64_t n, int steps, const float* coef, float eps) {
+  if (!ctx || batch < 1 || m < 1 || n < 1 || m > kDimMax || n > kDimMax || steps < 1 || steps > 64) return RTOPK_ERR_INVALID_ARG;
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return RTOPK_ERR_INVALID_ARG;
+  if (coef)
+    for (int i = 0; i < 3 * steps; ++i)
+      if (!std::isfinite(coef[i])) return RTOPK_ERR_INVALID_ARG;
+  if (batch > kBatchMax || m > 64 * kBatchMax) return RTOPK_ERR_UNSUPPORTED;
+  return RTOPK_OK;
+}
+
+template <class T>
+int code_cols(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, uint32_t* max_bits, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
+  const int per = (int)std::max<int64_t>(16, ceil_div(rows, 64));
+  MAT_TRY(launch(ctx, false, k_col_max<T>, dim3((unsigned)ceil_div(cols, 256), (unsigned)ceil_div(rows, per)), 256, 0, st, src, ld, rows, cols, per, max_bits));
+  return launch(ctx, true, k_code_cols<T>, dim3((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(rows, 64)), 256, 0, st, src, ld, rows, cols, max_bits, codes, ld_codes, scales);
+}
+
+int coded_gemm(rtopk_matrix* ctx, const int8_t* lane_codes, int64_t ld_lane, const float* lane_scale, int64_t lanes, const int8_t* col_codes, int64_t ld_col,
+               const float* col_scale, int64_t cols, int64_t depth, void* out, int bf16, int64_t ld_out, cudaStream_t st) {
+  Gemm g = {};
+  g.lanes = (int)lanes, g.cols = (int)cols, g.depth = (int)depth, g.batch = 1;
+  g.out = out, g.out_bf16 = bf16, g.out_col = ld_out, g.out_lane = 1;
+  g.scale_col = col_scale, g.scale_lane = lane_scale;
+  return gemm<EPI_CODED>(ctx, true, {lane_codes, depth, lanes, ld_lane, 0}, {col_codes, depth, cols, ld_col, 0}, g, st);
+}
+
+bool bad_codes(const int8_t* p, int64_t ld, int64_t cols) { return !p || !aligned_to(p, 16) || ld < cols || ld % 16; }
+bool bad_dtype(int t) { return t != RTOPK_F32 && t != RTOPK_BF16; }
+size_t elem(int t) { return t == RTOPK_F32 ? 4 : 2; }
+
+int check_coded(const rtopk_matrix* ctx, int64_t tokens, int64_t n_out, int64_t n_in) {
+  if (!ctx || tokens < 0 || n_out < 1 || n_in < 1 || tokens > kDimMax || n_out > kDimMax || n_in > kDimMax) return RTOPK_ERR_INVALID_ARG;
+  return RTOPK_OK;
+}
+
+template <class T>
+int product(rtopk_matrix* ctx, const T* x, int64_t ld_x, const int8_t* codes, int64_t ld_codes, const float* scales, int64_t tokens, int64_t n_out, int64_t n_in,
+            T* out, int64_t ld_out, cudaStream_t st) {
+  Carve c{ctx->scratch};
+  CodedScratch w(c, tokens, n_out, n_in);
+  MAT_TRY(launch(ctx, false, k_code_rows<T>, dim3((unsigned)tokens), 256, 0, st, x, ld_x, n_in, (const float*)nullptr, w.x_rows, w.ld_in, w.x_row_s));
+  return coded_gemm(ctx, codes, ld_codes, scales, n_out, w.x_rows, w.ld_in, w.x_row_s, tokens, n_in, out, sizeof(T) == 2, ld_out, st);
+}
+
+template <class T>
+int gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const int8_t* codes_t, int64_t ld_t, const float* scales, int64_t tokens,
+              int64_t n_out, int64_t n_in, T* dx, int64_t ld_dx, void* dw, int dw_dtype, int64_t ld_dw, cudaStream_t st) {
+  Carve c{ctx->scratch};
+  CodedScratch w(c, tokens, n_out, n_in);
+  if (dx) {
+    MAT_TRY(launch(ctx, false, k_code_rows<T>, dim3((unsigned)tokens), 256, 0, st, dy, ld_dy, n_out, scales, w.dy_rows, w.ld_out, w.dy_row_s));
+    MAT_TRY(coded_gemm(ctx, codes_t, ld_t, nullptr, n_in, w.dy_rows, w.ld_out, w.dy_row_s, tokens, n_out, dx, sizeof(T) == 2, ld_dx, st));
+  }
+  if (dw) {
+    MAT_CUDA(cudaMemsetAsync(w.col_max, 0, (n_in + n_out) * sizeof(uint32_t), st));
+    MAT_TRY(code_cols(ctx, x, ld_x, tokens, n_in, w.col_max, w.x_cols, w.ld_tok, w.x_col_s, st));
+    MAT_TRY(code_cols(ctx, dy, ld_dy, tokens, n_out, w.col_max + n_in, w.dy_cols, w.ld_tok, w.dy_col_s, st));
+    MAT_TRY(coded_gemm(ctx, w.x_cols, w.ld_tok, w.x_col_s, n_in, w.dy_cols, w.ld_tok, w.dy_col_s, n_out, tokens, dw, dw_dtype == RTOPK_BF16, ld_dw, st));
+  }
+  return RTOPK_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int rtopk_matrix_create(rtopk_matrix** out, int device, int64_t scratch_bytes) {
+  if (!out) return RTOPK_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (scratch_bytes < 0 || device < 0) return RTOPK_ERR_INVALID_ARG;
+  rtopk_matrix* ctx = new (std::nothrow) rtopk_matrix;
+  if (!ctx) return RTOPK_ERR_ALLOC;
+  ctx->device = device;
+  ctx->scratch_bytes = scratch_bytes;
+  OnDevice on(device);
+  int status = on.ok ? RTOPK_OK : RTOPK_ERR_CUDA;
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (status == RTOPK_OK && (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+                             found != cudaDriverEntryPointSuccess || cudaDeviceGetAttribute(&ctx->sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
+                             allow_smem<EPI_GRAM>() != cudaSuccess || allow_smem<EPI_POLY>() != cudaSuccess || allow_smem<EPI_APPLY>() != cudaSuccess ||
+                             allow_smem<EPI_OUT>() != cudaSuccess || allow_smem<EPI_UPDATE>() != cudaSuccess || allow_smem<EPI_CODED>() != cudaSuccess ||
+                             cudaFuncSetAttribute(k_orth_small, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(kSmallLong)) != cudaSuccess))
+    status = RTOPK_ERR_CUDA;
+  ctx->encode = (EncodeTiled)fn;
+  if (status == RTOPK_OK && (cudaMalloc(&ctx->error, 256) != cudaSuccess || cudaMemset(ctx->error, 0, 256) != cudaSuccess ||
+                             (scratch_bytes && cudaMalloc(&ctx->scratch, scratch_bytes) != cudaSuccess)))
+    status = RTOPK_ERR_ALLOC;
+  if (status != RTOPK_OK) {
+    cudaGetLastError();
+    rtopk_matrix_destroy(ctx);
+    return status;
+  }
+  *out = ctx;
+  return RTOPK_OK;
+}
+
+int rtopk_matrix_destroy(rtopk_matrix* ctx) {
+  if (!ctx) return RTOPK_OK;
+  OnDevice on(ctx->device);
+  if (ctx->scratch) cudaFree(ctx->scratch);
+  if (ctx->error) cudaFree(ctx->error);
+  delete ctx;
+  return RTOPK_OK;
+}
+
+int rtopk_matrix_last_cuda_error(const rtopk_matrix* ctx) { return ctx ? ctx->last_cuda_error : 0; }
+
+int rtopk_matrix_get_launch_count(const rtopk_matrix* ctx, uint64_t* out) {
+  if (!ctx || !out) return RTOPK_ERR_INVALID_ARG;
+  *out = ctx->launches;
+  return RTOPK_OK;
+}
+
+int rtopk_matrix_poll_status(rtopk_matrix* ctx, void* stream) {
+  if (!ctx) return RTOPK_ERR_INVALID_ARG;
+  OnDevice on(ctx->device);
+  cudaStream_t st = (cudaStream_t)stream;
+  uint32_t e = 0;
+  MAT_CUDA(cudaMemcpyAsync(&e, ctx->error, sizeof e, cudaMemcpyDeviceToHost, st));
+  MAT_CUDA(cudaStreamSynchronize(st));
+  if (!e) return RTOPK_OK;
+  MAT_CUDA(cudaMemsetAsync(ctx->error, 0, sizeof e, st));
+  return RTOPK_ERR_INTERNAL;
+}
+
+int rtopk_orthogonalize_scratch(int64_t batch, int64_t m, int64_t n, int64_t* bytes) {
+  if (!bytes || batch < 1 || m < 1 || n < 1 || batch > kBatchMax || m > kDimMax || n > kDimMax) return RTOPK_ERR_INVALID_ARG;
+  Carve c{nullptr};
+  OrthScratch w(c, batch, std::min(m, n), std::max(m, n));
+  *bytes = c.at;
+  return RTOPK_OK;
+}
+
+int rtopk_orthogonalize(rtopk_matrix* ctx, const void* src, int src_dtype, int64_t ld_src, int64_t stride_src, void* out, int out_dtype, int64_t ld_out,
+                        int64_t stride_out, int64_t batch, int64_t m, int64_t n, int steps, const float* coef, float eps, void* stream) {
+  MAT_TRY(check_orth(ctx, batch, m, n, steps, coef, eps));
+  if (bad_dtype(src_dtype) || bad_dtype(out_dtype) || bad_view(src, elem(src_dtype), batch, m, n, ld_src, stride_src) ||
+      bad_view(out, elem(out_dtype), batch, m, n, ld_out, stride_out))
+    return RTOPK_ERR_INVALID_ARG;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  Source s = {};
+  s.src = src, s.bf16 = src_dtype == RTOPK_BF16, s.ld = ld_src, s.stride = stride_src, s.eps = eps;
+  const Target to = {EPI_OUT, out, out_dtype == RTOPK_BF16, ld_out, stride_out, 0.f, 0.f};
+  return orthogonal(ctx, s, to, batch, m, n, steps, coef, (cudaStream_t)stream);
+}
+
+int rtopk_orthogonal_update(rtopk_matrix* ctx, const float* grad, int64_t ld_g, int64_t stride_g, float* momentum, int64_t ld_v, int64_t stride_v, float* weights,
+                            int64_t ld_w, int64_t stride_w, int64_t batch, int64_t m, int64_t n, float eta, float mu, int nesterov, float decay, float scale,
+                            int steps, const float* coef, float eps, void* stream) {
+  MAT_TRY(check_orth(ctx, batch, m, n, steps, coef, eps));
+  if (bad_view(grad, 4, batch, m, n, ld_g, stride_g) || bad_view(momentum, 4, batch, m, n, ld_v, stride_v) || bad_view(weights, 4, batch, m, n, ld_w, stride_w))
+    return RTOPK_ERR_INVALID_ARG;
+  if (!(eta >= 0.f) || !std::isfinite(eta) || !(mu >= 0.f && mu < 1.f) || !(decay >= 0.f) || !std::isfinite(decay) || !std::isfinite(scale)) return RTOPK_ERR_INVALID_ARG;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  Source s = {};
+  s.src = grad, s.ld = ld_g, s.stride = stride_g, s.eps = eps;
+  s.v = momentum, s.v_ld = ld_v, s.v_stride = stride_v, s.mu = mu, s.nesterov = nesterov != 0;
+  const Target to = {EPI_UPDATE, weights, 0, ld_w, stride_w, (float)(1.0 - (double)eta * (double)decay), (float)((double)eta * (double)scale)};
+  return orthogonal(ctx, s, to, batch, m, n, steps, coef, (cudaStream_t)stream);
+}
+
+int rtopk_code_weights(rtopk_matrix* ctx, const void* weights, int dtype, int64_t ld_w, int64_t n_out, int64_t n_in, int8_t* codes, int64_t ld_codes, int8_t* codes_t,
+                       int64_t ld_t, float* scales, void* stream) {
+  MAT_TRY(check_coded(ctx, 0, n_out, n_in));
+  if (bad_dtype(dtype) || bad_view(weights, elem(dtype), 1, n_out, n_in, ld_w, 0) || bad_codes(codes, ld_codes, n_in) || (codes_t && bad_codes(codes_t, ld_t, n_out)) ||
+      !scales || !aligned_to(scales, 4))
+    return RTOPK_ERR_INVALID_ARG;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dtype == RTOPK_F32)
+    MAT_TRY(launch(ctx, false, k_code_rows<float>, dim3((unsigned)n_out), 256, 0, st, (const float*)weights, ld_w, n_in, (const float*)nullptr, codes, ld_codes, scales));
+  else
+    MAT_TRY(launch(ctx, false, k_code_rows<__nv_bfloat16>, dim3((unsigned)n_out), 256, 0, st, (const __nv_bfloat16*)weights, ld_w, n_in, (const float*)nullptr, codes, ld_codes, scales));
+  if (codes_t)
+    MAT_TRY(launch(ctx, true, k_codes_transpose, dim3((unsigned)ceil_div(n_in, 64), (unsigned)ceil_div(n_out, 64)), 256, 0, st, codes, ld_codes, n_out, n_in, codes_t, ld_t));
+  return RTOPK_OK;
+}
+
+int rtopk_coded_scratch(int64_t tokens, int64_t n_out, int64_t n_in, int64_t* bytes) {
+  if (!bytes || tokens < 0 || n_out < 1 || n_in < 1 || tokens > kDimMax || n_out > kDimMax || n_in > kDimMax) return RTOPK_ERR_INVALID_ARG;
+  Carve c{nullptr};
+  CodedScratch w(c, tokens, n_out, n_in);
+  *bytes = c.at;
+  return RTOPK_OK;
+}
+
+int rtopk_coded_product(rtopk_matrix* ctx, const void* x, int dtype, int64_t ld_x, const int8_t* codes, int64_t ld_codes, const float* scales, int64_t tokens,
+                        int64_t n_out, int64_t n_in, void* out, int64_t ld_out, void* stream) {
+  MAT_TRY(check_coded(ctx, tokens, n_out, n_in));
+  if (bad_dtype(dtype) || bad_codes(codes, ld_codes, n_in) || !scales || !aligned_to(scales, 4)) return RTOPK_ERR_INVALID_ARG;
+  if (tokens && (bad_view(x, elem(dtype), 1, tokens, n_in, ld_x, 0) || bad_view(out, elem(dtype), 1, tokens, n_out, ld_out, 0))) return RTOPK_ERR_INVALID_ARG;
+  if (n_in > kDepthMax) return RTOPK_ERR_UNSUPPORTED;
+  int64_t need = 0;
+  rtopk_coded_scratch(tokens, n_out, n_in, &need);
+  if (need > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
+  if (!tokens) return RTOPK_OK;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  if (dtype == RTOPK_F32) return product(ctx, (const float*)x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, (float*)out, ld_out, (cudaStream_t)stream);
+  return product(ctx, (const __nv_bfloat16*)x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, (__nv_bfloat16*)out, ld_out, (cudaStream_t)stream);
+}
+
+int rtopk_coded_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int dtype, const int8_t* codes_t, int64_t ld_t,
+                          const float* scales, int64_t tokens, int64_t n_out, int64_t n_in, void* dx, int64_t ld_dx, void* dw, int dw_dtype, int64_t ld_dw, void* stream) {
+  MAT_TRY(check_coded(ctx, tokens, n_out, n_in));
+  if (bad_dtype(dtype) || (!dx && !dw) || (tokens && bad_view(dy, elem(dtype), 1, tokens, n_out, ld_dy, 0))) return RTOPK_ERR_INVALID_ARG;
+  if (dx && ((tokens && bad_view(dx, elem(dtype), 1, tokens, n_in, ld_dx, 0)) || bad_codes(codes_t, ld_t, n_out) || !scales || !aligned_to(scales, 4)))
+    return RTOPK_ERR_INVALID_ARG;
+  if (dw && (bad_dtype(dw_dtype) || bad_view(dw, elem(dw_dtype), 1, n_out, n_in, ld_dw, 0) || (tokens && bad_view(x, elem(dtype), 1, tokens, n_in, ld_x, 0))))
+    return RTOPK_ERR_INVALID_ARG;
+  if ((dx && n_out > kDepthMax) || (dw && tokens > kDepthMax)) return RTOPK_ERR_UNSUPPORTED;
+  int64_t need = 0;
+  rtopk_coded_scratch(tokens, n_out, n_in, &need);
+  if (need > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (!tokens) {      // an empty sum
+    if (dw) MAT_CUDA(cudaMemset2DAsync(dw, ld_dw * elem(dw_dtype), 0, n_in * elem(dw_dtype), n_out, st));
+    return RTOPK_OK;
+  }
+  if (dtype == RTOPK_F32)
+    return gradients(ctx, (const float*)dy, ld_dy, (const float*)x, ld_x, codes_t, ld_t, scales, tokens, n_out, n_in, (float*)dx, ld_dx, dw, dw_dtype, ld_dw, st);
+  return gradients(ctx, (const __nv_bfloat16*)dy, ld_dy, (const __nv_bfloat16*)x, ld_x, codes_t, ld_t, scales, tokens, n_out, n_in, (__nv_bfloat16*)dx, ld_dx, dw, dw_dtype, ld_dw, st);
+}
+
+}  // extern "C"
