@@ -524,7 +524,7 @@ int rtopk_orthogonalize(rtopk_matrix* ctx, const void* src, int src_dtype, int64
 
 /*
  * The master update of weight matrices with it (Algorithm 1's last line, with momentum):
- *     v <- fp32(double(mu) v + g);   u = g + mu v with nesterov != 0, else v;
+ *     v <- mu v + g (rounded once);   u = g + mu v with nesterov != 0, else v;
  *     w <- (1 - eta decay) w - eta scale orth(u)
  *   grad [in]  binary32, such as the dense average of rtopk_step (or a matrix inside it);
  *   momentum, weights [in/out]  binary32;   the three views must not overlap.

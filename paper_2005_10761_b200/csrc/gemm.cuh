@@ -1,8 +1,8 @@
 // The tensor-core product of the matrix operators: D[lane][col] = sum_k P[lane][k] Q[col][k], 16-bit floating point
 // with 32-bit sums or 8-bit integers with 32-bit integer sums, and what is done with D before it leaves the SM.
 //
-// One persistent block per SM, six warps: one thread feeds a ring of shared-memory stages by TMA, one thread issues
-// the products (128 x kCols tiles, the accumulators twice in tensor memory), four warps turn finished tiles into
+// One persistent block per SM, ten warps: one thread feeds a ring of shared-memory stages by TMA, one thread issues
+// the products (128 x kCols tiles, the accumulators twice in tensor memory), eight warps turn finished tiles into
 // results while the next tile is being multiplied.  D is always laid out so that the 32 lanes of a warp are
 // neighbours in the result's rows: the stores are coalesced without a pass through shared memory.
 #pragma once
@@ -15,7 +15,8 @@
 namespace rtopk {
 namespace mat {
 
-constexpr int kGemmThreads = 192;
+constexpr int kEpiWarps = 8;                // two for each quarter of the accumulator's lanes, taking its column chunks in turn
+constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
 constexpr int kLanes = 128;                 // rows of an accumulator tile (tensor-memory lanes)
 constexpr int kDepthBytes = 128;            // bytes of the contraction index per stage and row: one swizzle row
 constexpr int kSmemLimit = 227 * 1024;
@@ -91,14 +92,36 @@ __device__ __forceinline__ void store_half8(__half* p, const float* v) {
   *reinterpret_cast<uint4*>(p) = *reinterpret_cast<uint4*>(h);
 }
 
+// The entry of the Gram matrix's diagonal that belongs to `lane`, from the partial sums of squares; taken before the
+// tile's products are waited for.
+__device__ __forceinline__ float gram_diagonal(const Gemm& g, int z, int lane) {
+  if (lane >= g.lanes) return 0.f;
+  const float* sums = g.row_sums + (int64_t)z * g.slots * g.d_stride + lane;
+  float d = 0.f;
+#pragma unroll 16
+  for (int i = 0; i < g.slots; ++i) d += sums[i * g.d_stride];
+  return d * (1.f / kAScale);
+}
+
+// 32 entries of one lane, columns col0 .. (those past the edge read the last one): all loads are under way before the
+// first is used.
+__device__ __forceinline__ void load_column(const __half* p, int col0, int ncol, int64_t ld, __half (&v)[32]) {
+  p += col0 * ld;
+#pragma unroll
+  for (int c = 0; c < 32; ++c) v[c] = p[min(c, ncol - 1) * ld];
+}
+
 // 32 columns (col0 ..) of lane `lane` of one tile.
 template <int kEpi>
-__device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col0, const uint32_t (&acc)[32]) {
+__device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col0, float diag, const uint32_t (&acc)[32]) {
   const int ncol = min(32, g.cols - col0);
   if (kEpi == EPI_GRAM || kEpi == EPI_POLY) {
     // Symmetric result: a 128-wide block of columns left of this lane's block is the mirror image of another tile.
     const int lb = lane / kLanes, cb = col0 / kLanes;
-    if (cb < lb || lane >= g.lanes) return;
+    if (cb < lb) return;
+    const bool in = lane < g.lanes;
+    lane = min(lane, g.lanes - 1);
+    constexpr uint32_t active = 0xFFFFFFFFu;
     const float* d_in = g.d_in + z * g.d_stride;
     const __half* o = g.o + z * g.stride;
     __half* h = g.h + z * g.stride;
@@ -107,35 +130,30 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
 #pragma unroll
       for (int c = 0; c < 32; ++c) v[c] = __uint_as_float(acc[c]);
     } else {
-      const float dl = d_in[lane];
+      const float dl = d_in[lane], dc = d_in[col0 + min(threadIdx.x & 31, ncol - 1)];
+      __half oc[32];
+      load_column(o + lane, col0, ncol, g.ld, oc);
 #pragma unroll
-      for (int c = 0; c < 32; ++c)
-        if (c < ncol) {
-          const float oc = __half2float(o[(int64_t)(col0 + c) * g.ld + lane]);
-          v[c] = g.c * (__uint_as_float(acc[c]) * (1.f / kAScale)) + (g.b + g.c * (dl + d_in[col0 + c])) * oc;
-        } else {
-          v[c] = 0.f;
-        }
+      for (int c = 0; c < 32; ++c) {
+        const float d = __shfl_sync(active, dc, c);
+        v[c] = c < ncol ? g.c * (__uint_as_float(acc[c]) * (1.f / kAScale)) + (g.b + g.c * (dl + d)) * __half2float(oc[c]) : 0.f;
+      }
     }
-    if (lane >= col0 && lane < col0 + ncol) {
+    if (in && lane >= col0 && lane < col0 + ncol) {
+      float q = 0.f;
 #pragma unroll
       for (int c = 0; c < 32; ++c)
         if (lane == col0 + c) {
-          float d;
-          if (kEpi == EPI_GRAM) {
-            const float* sums = g.row_sums + z * g.slots * g.d_stride + lane;
-            d = 0.f;
-            for (int i = 0; i < g.slots; ++i) d += sums[i * g.d_stride];
-            d *= 1.f / kAScale;
-          } else {
-            const float q = __uint_as_float(acc[c]) * (1.f / kAScale);
-            const float x = d_in[lane];
-            d = g.a + g.b * x + g.c * (x * x + q * (1.f / kAScale));
-          }
-          g.d_out[z * g.d_stride + lane] = d;
+          q = __uint_as_float(acc[c]) * (1.f / kAScale);
           v[c] = 0.f;
         }
+      if (kEpi == EPI_POLY) {
+        const float x = d_in[lane];
+        diag = g.a + g.b * x + g.c * (x * x + q * (1.f / kAScale));
+      }
+      g.d_out[z * g.d_stride + lane] = diag;
     }
+    if (!in) return;
     // row `lane`, columns col0 ..: the row stride is a multiple of 8, so the padding takes whole vectors
     __half* row = h + (int64_t)lane * g.ld + col0;
 #pragma unroll
@@ -148,33 +166,34 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
     }
     return;
   }
+  const bool in = lane < g.lanes;
+  const int safe = min(lane, g.lanes - 1);      // loads of lanes past the edge read a neighbour's values and drop them
+  const int me = threadIdx.x & 31;
   if (kEpi == EPI_CODED) {
-    if (lane >= g.lanes) return;
-    const float sl = g.scale_lane ? g.scale_lane[lane] : 1.f;
-    const int64_t at = (int64_t)lane * g.out_lane;
+    const float sl = g.scale_lane ? g.scale_lane[safe] : 1.f;
+    const float sc = g.scale_col[col0 + min(me, ncol - 1)];
+    const int64_t at = (int64_t)lane * g.out_lane + (int64_t)col0 * g.out_col;
 #pragma unroll
-    for (int c = 0; c < 32; ++c)
-      if (c < ncol) {
-        const float v = (float)(int)acc[c] * g.scale_col[col0 + c] * sl;
-        const int64_t i = at + (int64_t)(col0 + c) * g.out_col;
-        if (g.out_bf16) ((__nv_bfloat16*)g.out)[i] = __float2bfloat16_rn(v);
-        else ((float*)g.out)[i] = v;
-      }
+    for (int c = 0; c < 32; ++c) {
+      const float v = (float)(int)acc[c] * __shfl_sync(0xFFFFFFFFu, sc, c) * sl;
+      if (!in || c >= ncol) continue;
+      if (g.out_bf16) ((__nv_bfloat16*)g.out)[at + c * g.out_col] = __float2bfloat16_rn(v);
+      else ((float*)g.out)[at + c * g.out_col] = v;
+    }
     return;
   }
   // X' = diag X + offdiag X: the product carries only the part off the diagonal, times kAScale * kXScale
-  const bool in = lane < g.lanes;
-  const float* d_in = g.d_in + z * g.d_stride;
-  const __half* o = g.o + z * g.stride + lane;
+  const float dc = g.d_in[z * g.d_stride + col0 + min(me, ncol - 1)];
   __half* lo = g.lo + z * g.stride + lane;
   float v[32];
+  {
+    __half oc[32], lc[32];
+    load_column(g.o + z * g.stride + safe, col0, ncol, g.ld, oc);
+    load_column(g.lo + z * g.stride + safe, col0, ncol, g.ld, lc);
 #pragma unroll
-  for (int c = 0; c < 32; ++c) {
-    v[c] = 0.f;
-    if (in && c < ncol) {
-      const int64_t i = (int64_t)(col0 + c) * g.ld;
-      const float x = __half2float(o[i]) + __half2float(lo[i]) * (1.f / kLoScale);
-      v[c] = d_in[col0 + c] * x + __uint_as_float(acc[c]) * (1.f / kAScale);
+    for (int c = 0; c < 32; ++c) {
+      const float x = __half2float(oc[c]) + __half2float(lc[c]) * (1.f / kLoScale);
+      v[c] = __shfl_sync(0xFFFFFFFFu, dc, c) * x + __uint_as_float(acc[c]) * (1.f / kAScale);
     }
   }
   if (kEpi == EPI_APPLY) {
@@ -187,10 +206,9 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
         h[i] = hi;
         lo[i] = to_half((v[c] - __half2float(hi)) * kLoScale);
       }
-      v[c] *= v[c];
+      v[c] = in ? v[c] * v[c] : 0.f;
     }
     // sums over the warp's 32 lanes, column c's in thread c
-    const int me = threadIdx.x & 31;
 #pragma unroll
     for (int n = 16; n; n >>= 1)
 #pragma unroll
@@ -204,20 +222,21 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
     return;
   }
   if (!in) return;
-  const int64_t at = z * g.out_batch + (int64_t)lane * g.out_lane;
+  const int64_t at = z * g.out_batch + (int64_t)lane * g.out_lane + (int64_t)col0 * g.out_col;
+  if (kEpi == EPI_UPDATE) {
+    float w[32];
+#pragma unroll
+    for (int c = 0; c < 32; ++c) w[c] = c < ncol ? ((const float*)g.out)[at + c * g.out_col] : 0.f;
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+      if (c < ncol) ((float*)g.out)[at + c * g.out_col] = g.keep * w[c] - g.rate * (v[c] * (1.f / kXScale));
+    return;
+  }
 #pragma unroll
   for (int c = 0; c < 32; ++c)
     if (c < ncol) {
-      const int64_t i = at + (int64_t)(col0 + c) * g.out_col;
-      const float x = v[c] * (1.f / kXScale);
-      if (kEpi == EPI_UPDATE) {
-        float* w = (float*)g.out + i;
-        *w = g.keep * *w - g.rate * x;
-      } else if (g.out_bf16) {
-        ((__nv_bfloat16*)g.out)[i] = __float2bfloat16_rn(x);
-      } else {
-        ((float*)g.out)[i] = x;
-      }
+      if (g.out_bf16) ((__nv_bfloat16*)g.out)[at + c * g.out_col] = __float2bfloat16_rn(v[c] * (1.f / kXScale));
+      else ((float*)g.out)[at + c * g.out_col] = v[c] * (1.f / kXScale);
     }
 }
 
@@ -247,7 +266,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { bar_init(full + 8 * s, 1); bar_init(empty + 8 * s, 1); }
-    for (int b = 0; b < 2; ++b) { bar_init(tm_full + 8 * b, 1); bar_init(tm_empty + 8 * b, 4); }
+    for (int b = 0; b < 2; ++b) { bar_init(tm_full + 8 * b, 1); bar_init(tm_empty + 8 * b, kEpiWarps); }
     bar_init(drain, 1);
     words[1] = 0u;
     bar_init_fence();
@@ -319,19 +338,23 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     __syncwarp();
   } else {
     const int quarter = warp & 3;       // the lanes of tensor memory that this warp may read
+    const int first = (warp - 2) / 4 * 32;
     uint32_t n = 0;
     for (int t = blockIdx.x; t < total; t += gridDim.x, ++n) {
       const uint32_t b = n & 1;
       const Tile q = tile_at<kCols>(g, t);
+      const int row = q.l * kLanes + quarter * 32 + lane;
+      float diag = 0.f;
+      if (kEpi == EPI_GRAM && q.l == q.c * kCols / kLanes) diag = gram_diagonal(g, q.z, row);
+      if (kEpi == EPI_GRAM && kCols > kLanes && q.l == q.c * kCols / kLanes + 1) diag = gram_diagonal(g, q.z, row);
       if (!__all_sync(0xFFFFFFFFu, bar_wait(tm_full + 8 * b, (n / 2) & 1, give))) break;
       tc_fence_after();
-      const int row = q.l * kLanes + quarter * 32 + lane;
 #pragma unroll 1
-      for (int c = 0; c < kCols; c += 32) {
+      for (int c = first; c < kCols; c += 32 * (kEpiWarps / 4)) {
         if (q.c * kCols + c >= g.cols) break;
         uint32_t acc[32];
         tmem_load32(tmem + b * kCols + c + ((uint32_t)(quarter * 32) << 16), acc);
-        epilogue<kEpi>(g, q.z, row, q.c * kCols + c, acc);
+        epilogue<kEpi>(g, q.z, row, q.c * kCols + c, diag, acc);
         __syncwarp();
       }
       tc_fence_before();

@@ -194,6 +194,10 @@ cudaError_t allow_smem() {
 constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 
 bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+// Rows that start on multiples of `bytes`, wherever in the batch.
+bool rows_aligned(const void* p, size_t elem, int64_t batch, int64_t ld, int64_t stride, size_t bytes) {
+  return aligned_to(p, bytes) && ld * elem % bytes == 0 && (batch == 1 || stride * elem % bytes == 0);
+}
 
 // Batches of matrices with `n` contiguous elements in rows `ld` apart.
 bool bad_view(const void* p, size_t elem, int64_t batch, int64_t m, int64_t n, int64_t ld, int64_t stride) {
@@ -229,7 +233,7 @@ int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, i
   if (s <= kSmall && l <= kSmallLong) return orthogonal_small(ctx, src, to, batch, m, n, steps, coef, st);
   src.m = (int)m, src.n = (int)n;
   src.part = w.part;
-  src.parts = (int)std::min<int64_t>(kNormBlocks, ceil_div(m * n, 2048));
+  src.parts = (int)std::min<int64_t>(kNormBlocks, ceil_div(m * ceil_div(n, kNormSpan), 8));
   MAT_TRY(launch(ctx, false, k_norm, dim3(src.parts, (unsigned)batch), 256, 0, st, src));
   MAT_TRY(launch(ctx, true, k_split, dim3((unsigned)ceil_div(n, 64), (unsigned)ceil_div(m, 64), (unsigned)batch), 256, 0, st, src, w.hi[0], w.lo, w.ld_x, w.stride_x,
                  w.row_sums, w.slots, w.stride_d, tall ? 1 : 0));
@@ -275,11 +279,25 @@ int check_orth(const rtopk_matrix* ctx, int64_t batch, int64_t m, int64_t n, int
   return RTOPK_OK;
 }
 
+// Rows of up to 1024 elements take a warp each, up to 4096 four warps, longer ones a block: what a row's threads hold in
+// registers is read once.
 template <class T>
-int code_cols(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, uint32_t* max_bits, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
-  const int per = (int)std::max<int64_t>(16, ceil_div(rows, 64));
-  MAT_TRY(launch(ctx, false, k_col_max<T>, dim3((unsigned)ceil_div(cols, 256), (unsigned)ceil_div(rows, per)), 256, 0, st, src, ld, rows, cols, per, max_bits));
-  return launch(ctx, true, k_code_cols<T>, dim3((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(rows, 64)), 256, 0, st, src, ld, rows, cols, max_bits, codes, ld_codes, scales);
+int code_rows(rtopk_matrix* ctx, bool chained, const T* src, int64_t ld, int64_t rows, int64_t cols, const float* mul, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
+  const int vec = rows_aligned(src, sizeof(T), 1, ld, 0, 16);
+  auto go = [&](auto kernel, int warps) {
+    return launch(ctx, chained, kernel, dim3((unsigned)ceil_div(rows, 8 / warps)), 256, 0, st, src, ld, rows, cols, vec, mul, codes, ld_codes, scales);
+  };
+  if (cols <= 1024) return go(k_code_rows<T, 1>, 1);
+  if (cols <= 4096) return go(k_code_rows<T, 4>, 4);
+  return go(k_code_rows<T, 8>, 8);
+}
+
+template <class T>
+int code_cols(rtopk_matrix* ctx, bool chained, const T* src, int64_t ld, int64_t rows, int64_t cols, uint32_t* max_bits, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
+  const int vec = rows_aligned(src, sizeof(T), 1, ld, 0, 16);
+  const int per = (int)std::max<int64_t>(32, ceil_div(rows, 64));
+  MAT_TRY(launch(ctx, chained, k_col_max<T>, dim3((unsigned)ceil_div(cols, 256), (unsigned)ceil_div(rows, per)), 256, 0, st, src, ld, rows, cols, vec, per, max_bits));
+  return launch(ctx, true, k_code_cols<T>, dim3((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(rows, 128)), 256, 0, st, src, ld, rows, cols, vec, max_bits, codes, ld_codes, scales);
 }
 
 int coded_gemm(rtopk_matrix* ctx, const int8_t* lane_codes, int64_t ld_lane, const float* lane_scale, int64_t lanes, const int8_t* col_codes, int64_t ld_col,
@@ -305,7 +323,7 @@ int product(rtopk_matrix* ctx, const T* x, int64_t ld_x, const int8_t* codes, in
             T* out, int64_t ld_out, cudaStream_t st) {
   Carve c{ctx->scratch};
   CodedScratch w(c, tokens, n_out, n_in);
-  MAT_TRY(launch(ctx, false, k_code_rows<T>, dim3((unsigned)tokens), 256, 0, st, x, ld_x, n_in, (const float*)nullptr, w.x_rows, w.ld_in, w.x_row_s));
+  MAT_TRY(code_rows(ctx, false, x, ld_x, tokens, n_in, nullptr, w.x_rows, w.ld_in, w.x_row_s, st));
   return coded_gemm(ctx, codes, ld_codes, scales, n_out, w.x_rows, w.ld_in, w.x_row_s, tokens, n_in, out, sizeof(T) == 2, ld_out, st);
 }
 
@@ -315,13 +333,13 @@ int gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, int64_t
   Carve c{ctx->scratch};
   CodedScratch w(c, tokens, n_out, n_in);
   if (dx) {
-    MAT_TRY(launch(ctx, false, k_code_rows<T>, dim3((unsigned)tokens), 256, 0, st, dy, ld_dy, n_out, scales, w.dy_rows, w.ld_out, w.dy_row_s));
+    MAT_TRY(code_rows(ctx, false, dy, ld_dy, tokens, n_out, scales, w.dy_rows, w.ld_out, w.dy_row_s, st));
     MAT_TRY(coded_gemm(ctx, codes_t, ld_t, nullptr, n_in, w.dy_rows, w.ld_out, w.dy_row_s, tokens, n_out, dx, sizeof(T) == 2, ld_dx, st));
   }
   if (dw) {
     MAT_CUDA(cudaMemsetAsync(w.col_max, 0, (n_in + n_out) * sizeof(uint32_t), st));
-    MAT_TRY(code_cols(ctx, x, ld_x, tokens, n_in, w.col_max, w.x_cols, w.ld_tok, w.x_col_s, st));
-    MAT_TRY(code_cols(ctx, dy, ld_dy, tokens, n_out, w.col_max + n_in, w.dy_cols, w.ld_tok, w.dy_col_s, st));
+    MAT_TRY(code_cols(ctx, false, x, ld_x, tokens, n_in, w.col_max, w.x_cols, w.ld_tok, w.x_col_s, st));
+    MAT_TRY(code_cols(ctx, true, dy, ld_dy, tokens, n_out, w.col_max + n_in, w.dy_cols, w.ld_tok, w.dy_col_s, st));
     MAT_TRY(coded_gemm(ctx, w.x_cols, w.ld_tok, w.x_col_s, n_in, w.dy_cols, w.ld_tok, w.dy_col_s, n_out, tokens, dw, dw_dtype == RTOPK_BF16, ld_dw, st));
   }
   return RTOPK_OK;
@@ -409,6 +427,7 @@ int rtopk_orthogonalize(rtopk_matrix* ctx, const void* src, int src_dtype, int64
   if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
   Source s = {};
   s.src = src, s.bf16 = src_dtype == RTOPK_BF16, s.ld = ld_src, s.stride = stride_src, s.eps = eps;
+  s.vec = rows_aligned(src, elem(src_dtype), batch, ld_src, stride_src, 4 * elem(src_dtype));
   const Target to = {EPI_OUT, out, out_dtype == RTOPK_BF16, ld_out, stride_out, 0.f, 0.f};
   return orthogonal(ctx, s, to, batch, m, n, steps, coef, (cudaStream_t)stream);
 }
@@ -424,6 +443,7 @@ int rtopk_orthogonal_update(rtopk_matrix* ctx, const float* grad, int64_t ld_g, 
   if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
   Source s = {};
   s.src = grad, s.ld = ld_g, s.stride = stride_g, s.eps = eps;
+  s.vec = rows_aligned(grad, 4, batch, ld_g, stride_g, 16), s.v_vec = rows_aligned(momentum, 4, batch, ld_v, stride_v, 16);
   s.v = momentum, s.v_ld = ld_v, s.v_stride = stride_v, s.mu = mu, s.nesterov = nesterov != 0;
   const Target to = {EPI_UPDATE, weights, 0, ld_w, stride_w, (float)(1.0 - (double)eta * (double)decay), (float)((double)eta * (double)scale)};
   return orthogonal(ctx, s, to, batch, m, n, steps, coef, (cudaStream_t)stream);
@@ -438,10 +458,8 @@ int rtopk_code_weights(rtopk_matrix* ctx, const void* weights, int dtype, int64_
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
   cudaStream_t st = (cudaStream_t)stream;
-  if (dtype == RTOPK_F32)
-    MAT_TRY(launch(ctx, false, k_code_rows<float>, dim3((unsigned)n_out), 256, 0, st, (const float*)weights, ld_w, n_in, (const float*)nullptr, codes, ld_codes, scales));
-  else
-    MAT_TRY(launch(ctx, false, k_code_rows<__nv_bfloat16>, dim3((unsigned)n_out), 256, 0, st, (const __nv_bfloat16*)weights, ld_w, n_in, (const float*)nullptr, codes, ld_codes, scales));
+  if (dtype == RTOPK_F32) MAT_TRY(code_rows(ctx, false, (const float*)weights, ld_w, n_out, n_in, nullptr, codes, ld_codes, scales, st));
+  else MAT_TRY(code_rows(ctx, false, (const __nv_bfloat16*)weights, ld_w, n_out, n_in, nullptr, codes, ld_codes, scales, st));
   if (codes_t)
     MAT_TRY(launch(ctx, true, k_codes_transpose, dim3((unsigned)ceil_div(n_in, 64), (unsigned)ceil_div(n_out, 64)), 256, 0, st, codes, ld_codes, n_out, n_in, codes_t, ld_t));
   return RTOPK_OK;

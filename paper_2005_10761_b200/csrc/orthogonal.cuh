@@ -19,6 +19,7 @@ struct Source {
   float mu;
   int nesterov;
   int m, n;
+  int vec, v_vec;        // rows allow loads of four
   float eps;
   double* part;          // [batch][kNormBlocks]
   int parts;
@@ -30,27 +31,69 @@ __device__ __forceinline__ float source_at(const Source& s, int64_t i) {
 // u from the momentum after its update
 __device__ __forceinline__ float update_of(const Source& s, float g, float v) { return s.nesterov ? fmaf(s.mu, v, g) : v; }
 
+// Four neighbours of a row, those past its end zero.
+__device__ __forceinline__ float4 load4(const float* p, int left, bool vec) {
+  if (vec && left >= 4) return *(const float4*)p;
+  return make_float4(left > 0 ? p[0] : 0.f, left > 1 ? p[1] : 0.f, left > 2 ? p[2] : 0.f, left > 3 ? p[3] : 0.f);
+}
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p, int left, bool vec) {
+  if (vec && left >= 4) {
+    const uint2 a = *(const uint2*)p;
+    return make_float4(__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xFFFF0000u), __uint_as_float(a.y << 16), __uint_as_float(a.y & 0xFFFF0000u));
+  }
+  return make_float4(left > 0 ? widen(p[0]) : 0.f, left > 1 ? widen(p[1]) : 0.f, left > 2 ? widen(p[2]) : 0.f, left > 3 ? widen(p[3]) : 0.f);
+}
+__device__ __forceinline__ float4 source4(const Source& s, int64_t i, int left) {
+  return s.bf16 ? load4((const __nv_bfloat16*)s.src + i, left, s.vec) : load4((const float*)s.src + i, left, s.vec);
+}
+
 // Sums of squares, in binary64 so that neither large nor small gradients leave the range; one partial sum per block, added
-// up in a fixed order by the readers.
+// up in a fixed order by the readers.  A warp takes 1024 neighbours of a row at a time.
+constexpr int kNormSpan = 1024;
 __global__ void __launch_bounds__(256) k_norm(const __grid_constant__ Source s) {
   __shared__ double part[8];
-  const int z = blockIdx.y;
+  const int z = blockIdx.y, lane = threadIdx.x & 31;
   launch_next();
+  const int pieces = (s.n + kNormSpan - 1) / kNormSpan;
+  const int64_t units = (int64_t)s.m * pieces;
   double sum = 0.0;
-  const int64_t count = (int64_t)s.m * s.n, step = (int64_t)gridDim.x * 256;
-  for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < count; k += step) {
-    const int64_t r = k / s.n, c = k - r * s.n;
-    float u = source_at(s, z * s.stride + r * s.ld + c);
-    if (s.v) {
-      float* v = s.v + z * s.v_stride + r * s.v_ld + c;
-      const float nv = (float)((double)s.mu * (double)*v + (double)u);
-      *v = nv;
-      u = update_of(s, u, nv);
+  for (int64_t k = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); k < units; k += (int64_t)gridDim.x * 8) {
+    const int64_t r = k / pieces;
+    const int c0 = (int)(k - r * pieces) * kNormSpan + lane * 4;
+    const int64_t at = z * s.stride + r * s.ld, at_v = z * s.v_stride + r * s.v_ld;
+    float4 u[8], v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int c = c0 + i * 128;
+      u[i] = c < s.n ? source4(s, at + c, s.n - c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      if (s.v) v[i] = c < s.n ? load4(s.v + at_v + c, s.n - c, s.v_vec) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    sum += (double)u * (double)u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int c = c0 + i * 128, left = s.n - c;
+      if (left <= 0) break;
+      if (s.v) {
+        const float4 g = u[i];
+        const float4 nv = make_float4(fmaf(s.mu, v[i].x, g.x), fmaf(s.mu, v[i].y, g.y), fmaf(s.mu, v[i].z, g.z), fmaf(s.mu, v[i].w, g.w));
+        float* p = s.v + at_v + c;
+        if (s.v_vec && left >= 4) {
+          *(float4*)p = nv;
+        } else {
+          p[0] = nv.x;
+          if (left > 1) p[1] = nv.y;
+          if (left > 2) p[2] = nv.z;
+          if (left > 3) p[3] = nv.w;
+        }
+        u[i] = make_float4(update_of(s, g.x, nv.x), update_of(s, g.y, nv.y), update_of(s, g.z, nv.z), update_of(s, g.w, nv.w));
+      }
+      sum += (double)u[i].x * (double)u[i].x;
+      sum += (double)u[i].y * (double)u[i].y;
+      sum += (double)u[i].z * (double)u[i].z;
+      sum += (double)u[i].w * (double)u[i].w;
+    }
   }
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = sum;
+  if (lane == 0) part[threadIdx.x >> 5] = sum;
   __syncthreads();
   if (threadIdx.x == 0) {
     sum = 0.0;
@@ -59,20 +102,8 @@ __global__ void __launch_bounds__(256) k_norm(const __grid_constant__ Source s) 
   }
 }
 
-// One element of X as its halves; the warp's 32 neighbours of a row give one partial sum of squares.
-__device__ __forceinline__ void split_store(float u, bool in, __half* hi, __half* lo, float* sum) {
-  if (in) {
-    const __half h = to_half(u);
-    *hi = h;
-    *lo = to_half((u - __half2float(h)) * kLoScale);
-  }
-  u *= u;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(0xFFFFFFFFu, u, o);
-  if ((threadIdx.x & 31) == 0) *sum = u;
-}
-
-// X, 64 x 64 elements of U per block, transposed when U is tall.
+// X, 64 x 64 elements of U per block, transposed when U is tall.  A thread writes eight neighbours of a row of X as their
+// halves; four threads together give one partial sum of squares.
 __global__ void __launch_bounds__(256)
 k_split(const __grid_constant__ Source s, __half* hi, __half* lo, int64_t ld, int64_t stride, float* row_sums, int slots, int64_t d_stride, int transpose) {
   __shared__ float tile[64][65];
@@ -86,26 +117,47 @@ k_split(const __grid_constant__ Source s, __half* hi, __half* lo, int64_t ld, in
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
     if (threadIdx.x == 0) inv_s = sum == 0.0 ? 0.f : (float)((double)kXScale / (sqrt(sum) + (double)s.eps));
   }
+  {
+    const int c = (threadIdx.x & 15) * 4, left = s.n - c0 - c;
+    float4 u[4], v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = r0 + (threadIdx.x >> 4) + 16 * i;
+      const bool in = r < s.m && left > 0;
+      u[i] = in ? source4(s, z * s.stride + r * s.ld + c0 + c, left) : make_float4(0.f, 0.f, 0.f, 0.f);
+      if (s.v) v[i] = in ? load4(s.v + z * s.v_stride + r * s.v_ld + c0 + c, left, s.v_vec) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (s.v) u[i] = make_float4(update_of(s, u[i].x, v[i].x), update_of(s, u[i].y, v[i].y), update_of(s, u[i].z, v[i].z), update_of(s, u[i].w, v[i].w));
+      float* t = tile[(threadIdx.x >> 4) + 16 * i] + c;
+      t[0] = u[i].x, t[1] = u[i].y, t[2] = u[i].z, t[3] = u[i].w;
+    }
+  }
   __syncthreads();
   const float inv = inv_s;
-  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
   hi += z * stride, lo += z * stride, row_sums += (int64_t)z * slots * d_stride;
-  for (int r = y; r < 64; r += 4) {
-    const int row = r0 + r, col = c0 + x;
-    float u = 0.f;
-    if (row < s.m && col < s.n) {
-      u = source_at(s, z * s.stride + row * s.ld + col);
-      if (s.v) u = update_of(s, u, s.v[z * s.v_stride + row * s.v_ld + col]);
-      u *= inv;
+  const int ns = transpose ? s.n : s.m, nl = transpose ? s.m : s.n;
+  const int a0 = transpose ? c0 : r0, b0 = transpose ? r0 : c0;      // of X: rows and columns
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int a = (threadIdx.x >> 3) + 32 * i, b = (threadIdx.x & 7) * 8;
+    float h[8], l[8], sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float u = (transpose ? tile[b + j][a] : tile[a][b + j]) * inv;
+      h[j] = __half2float(to_half(u));
+      l[j] = (u - h[j]) * kLoScale;
+      sum = fmaf(u, u, sum);
     }
-    if (transpose) tile[x][r] = u;
-    else if (row < s.m && (col & ~31) < s.n) split_store(u, col < s.n, hi + row * ld + col, lo + row * ld + col, row_sums + (col / 32) * d_stride + row);
-  }
-  if (!transpose) return;
-  __syncthreads();
-  for (int c = y; c < 64; c += 4) {
-    const int row = c0 + c, col = r0 + x;      // of X
-    if (row < s.n && (col & ~31) < s.m) split_store(tile[c][x], col < s.m, hi + row * ld + col, lo + row * ld + col, row_sums + (col / 32) * d_stride + row);
+    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+    if (a0 + a >= ns || b0 + (b & ~31) >= nl) continue;
+    if ((b & 31) == 0) row_sums[(int64_t)((b0 + b) / 32) * d_stride + a0 + a] = sum;
+    if (b0 + b < nl) {      // the rows' padding takes whole vectors
+      store_half8(hi + (a0 + a) * ld + b0 + b, h);
+      store_half8(lo + (a0 + a) * ld + b0 + b, l);
+    }
   }
 }
 
@@ -154,7 +206,7 @@ __global__ void __launch_bounds__(256) k_orth_small(const __grid_constant__ Sour
     float u = source_at(s, z * s.stride + r * s.ld + c);
     if (s.v) {
       float* v = s.v + z * s.v_stride + r * s.v_ld + c;
-      const float nv = (float)((double)s.mu * (double)*v + (double)u);
+      const float nv = fmaf(s.mu, *v, u);
       *v = nv;
       u = update_of(s, u, nv);
     }
