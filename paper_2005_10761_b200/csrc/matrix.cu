@@ -24,6 +24,8 @@ struct rtopk_matrix {
   int64_t scratch_bytes = 0;
   char* scratch = nullptr;
   uint32_t* error = nullptr;
+  uint32_t* arrived = nullptr;      // of split products, beside the error word
+  uint32_t* parts = nullptr;
   EncodeTiled encode = nullptr;
   uint64_t launches = 0;
 };
@@ -58,6 +60,10 @@ struct OnDevice {
 constexpr int64_t kDimMax = 1 << 30;
 constexpr int64_t kBatchMax = 65535;
 constexpr int64_t kDepthMax = 131072;     // 127 * 127 * depth stays below 2^31
+
+constexpr int kSplitTiles = 1024;         // tiles of a split product: counters
+constexpr int64_t kPartBytes = kLanes * 128 * 4;       // partial sums of one block: as many parts as there are SMs, at most
+constexpr int kErrorBytes = 1024 + 2 * kSplitTiles * 4;
 
 int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 int64_t ceil_div(int64_t x, int64_t a) { return (x + a - 1) / a; }
@@ -117,20 +123,32 @@ struct CodedScratch {
 // A kernel of a chain may start while the one before it ends (the kernels wait for it themselves); the first of a call
 // starts after all earlier work of the stream.
 template <class... P, class... A>
-int launch(rtopk_matrix* ctx, bool chained, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A... args) {
+int launch_cluster(rtopk_matrix* ctx, bool chained, int cluster, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute at;
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = chained ? 1 : 0;
+  cudaLaunchAttribute at[2];
+  int n = 0;
+  if (chained) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster > 1) {
+    at[n].id = cudaLaunchAttributeClusterDimension;
+    at[n].val.clusterDim.x = cluster, at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = n;
   MAT_CUDA(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
   ++ctx->launches;
   return RTOPK_OK;
+}
+template <class... P, class... A>
+int launch(rtopk_matrix* ctx, bool chained, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A... args) {
+  return launch_cluster(ctx, chained, 1, kernel, grid, threads, smem, st, args...);
 }
 
 // Tensor map of a [batch][rows][cols] array: boxes of box_rows rows of one 128-byte swizzle row.
@@ -147,47 +165,71 @@ int tensor_map(rtopk_matrix* ctx, CUtensorMap* map, const void* base, bool int8,
 
 struct Operand { const void* p; int64_t cols, rows, ld, stride; };    // as stored: rows of `cols` contiguous elements
 
-template <int kCols, int kEpi>
-int gemm_tile(rtopk_matrix* ctx, bool chained, const Operand& p, const Operand& q, Gemm g, cudaStream_t st) {
-  constexpr bool kInt8 = kEpi == EPI_CODED;
-  constexpr bool kMnMajor = kEpi == EPI_APPLY || kEpi == EPI_OUT || kEpi == EPI_UPDATE;
-  g.tiles_l = (int)ceil_div(g.lanes, kLanes), g.tiles_c = (int)ceil_div(g.cols, kCols);
-  g.tiles = 0;
-  if (g.tri)
-    for (int c = 0; c < g.tiles_c; ++c) g.tiles += std::min(g.tiles_l, ((c + 1) * kCols - 1) / kLanes + 1);
-  else
-    g.tiles = g.tiles_l * g.tiles_c;
-  g.error = ctx->error;
-  CUtensorMap mp, mq;
-  MAT_TRY(tensor_map(ctx, &mp, p.p, kInt8, p.cols, p.rows, g.batch, p.ld, p.stride, kMnMajor ? 64 : kLanes));
-  MAT_TRY(tensor_map(ctx, &mq, q.p, kInt8, q.cols, q.rows, g.batch, q.ld, q.stride, kCols));
-  const int grid = (int)std::min<int64_t>((int64_t)g.tiles * g.batch, ctx->sms);
-  return launch(ctx, chained, k_gemm<kCols, kEpi>, dim3(grid), kGemmThreads, gemm_smem<kCols>(), st, mp, mq, g);
+template <int kCols, bool kPair>
+int64_t gemm_tiles(const Gemm& g) {
+  using S = GemmShape<kCols, kPair>;
+  const int tiles_l = (int)ceil_div(g.lanes, S::kTileLanes), tiles_c = (int)ceil_div(g.cols, kCols);
+  if (!g.tri) return (int64_t)tiles_l * tiles_c;
+  int64_t n = 0;
+  for (int c = 0; c < tiles_c; ++c) n += tri_lane_tiles<kCols, S::kTileLanes>(tiles_l, c);
+  return n;
 }
 
-// The tile width: the one whose waves of tiles over the SMs take least, a tile costing its columns plus a fixed part.
+template <int kCols, bool kPair, int kEpi>
+int gemm_tile(rtopk_matrix* ctx, bool chained, const Operand& p, const Operand& q, Gemm g, int split, cudaStream_t st) {
+  using S = GemmShape<kCols, kPair>;
+  constexpr bool kInt8 = kEpi == EPI_CODED;
+  constexpr bool kMnMajor = kEpi == EPI_APPLY || kEpi == EPI_OUT || kEpi == EPI_UPDATE;
+  constexpr int kBlocks = kPair ? 2 : 1;
+  g.tiles_l = (int)ceil_div(g.lanes, S::kTileLanes), g.tiles_c = (int)ceil_div(g.cols, kCols);
+  g.tiles = (int)gemm_tiles<kCols, kPair>(g);
+  g.split = split;
+  g.parts = ctx->parts, g.arrived = ctx->arrived, g.error = ctx->error;
+  CUtensorMap mp, mq;
+  MAT_TRY(tensor_map(ctx, &mp, p.p, kInt8, p.cols, p.rows, g.batch, p.ld, p.stride, kMnMajor ? 64 : kLanes));
+  MAT_TRY(tensor_map(ctx, &mq, q.p, kInt8, q.cols, q.rows, g.batch, q.ld, q.stride, S::kQRows));
+  const int grid = kBlocks * (int)std::min<int64_t>((int64_t)g.tiles * g.batch * split, ctx->sms / kBlocks);
+  return launch_cluster(ctx, chained, kBlocks, k_gemm<kCols, kPair, kEpi>, dim3(grid), kGemmThreads, S::kSmem, st, mp, mq, g);
+}
+
+// Which tile, and in how many parts: the one for which this estimate of the time, in cycles, is least.  Per step of 128 bytes of the
+// contraction index a block takes what its stage needs from L2 (56 bytes a cycle and SM), or the tensor core's time; the last
+// tile of a block leaves its results behind the products; parts are written and read again.
 template <int kEpi>
 int gemm(rtopk_matrix* ctx, bool chained, const Operand& p, const Operand& q, const Gemm& g, cudaStream_t st) {
-  auto cost = [&](int cols) {
-    int64_t tiles = 0;
-    const int64_t tl = ceil_div(g.lanes, kLanes), tc = ceil_div(g.cols, cols);
-    if (g.tri)
-      for (int64_t c = 0; c < tc; ++c) tiles += std::min<int64_t>(tl, ((c + 1) * cols - 1) / kLanes + 1);
-    else
-      tiles = tl * tc;
-    return ceil_div(tiles * g.batch, ctx->sms) * (cols + 64);
+  const int64_t steps = ceil_div((int64_t)g.depth * (kEpi == EPI_CODED ? 1 : 2), kDepthBytes);
+  double best = 1e300;
+  int which = 0, parts = 1;
+  auto consider = [&](int id, int64_t tiles, int cols, int blocks, int stage_bytes) {
+    const int64_t sms = ctx->sms / blocks;
+    for (int split = 1; split <= 8; ++split) {
+      if (split > 1 && (tiles * g.batch * split > sms || steps < 4 * split || tiles * g.batch > kSplitTiles || cols > 128)) break;
+      if ((split - 1) * ceil_div(steps, split) >= steps) continue;      // a part without any step
+      const double per_step = std::max(stage_bytes / 56.0, cols * 2.0);
+      const double main = (double)ceil_div(steps, split) * per_step + 1000, tail = cols * 12.0 + (split > 1 ? cols * (6.0 + 6.0 * split) + 2500 : 0);
+      const double waves = (double)ceil_div(tiles * g.batch * split, sms);
+      const double t = waves * std::max(main, cols * 12.0) + tail;
+      if (t < best) best = t, which = id, parts = split;
+    }
   };
-  const int64_t c64 = cost(64), c128 = cost(128), c256 = cost(256);
-  if (c256 <= c128 && c256 <= c64) return gemm_tile<256, kEpi>(ctx, chained, p, q, g, st);
-  if (c128 <= c64) return gemm_tile<128, kEpi>(ctx, chained, p, q, g, st);
-  return gemm_tile<64, kEpi>(ctx, chained, p, q, g, st);
+  consider(0, gemm_tiles<64, false>(g), 64, 1, GemmShape<64, false>::kStageBytes);
+  consider(1, gemm_tiles<128, false>(g), 128, 1, GemmShape<128, false>::kStageBytes);
+  consider(2, gemm_tiles<128, true>(g), 128, 2, GemmShape<128, true>::kStageBytes);
+  consider(3, gemm_tiles<256, true>(g), 256, 2, GemmShape<256, true>::kStageBytes);
+  switch (which) {
+    case 0: return gemm_tile<64, false, kEpi>(ctx, chained, p, q, g, parts, st);
+    case 1: return gemm_tile<128, false, kEpi>(ctx, chained, p, q, g, parts, st);
+    case 2: return gemm_tile<128, true, kEpi>(ctx, chained, p, q, g, parts, st);
+    default: return gemm_tile<256, true, kEpi>(ctx, chained, p, q, g, parts, st);
+  }
 }
 
 template <int kEpi>
 cudaError_t allow_smem() {
-  cudaError_t e = cudaFuncSetAttribute(k_gemm<64, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, gemm_smem<64>());
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<128, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, gemm_smem<128>());
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<256, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, gemm_smem<256>());
+  cudaError_t e = cudaFuncSetAttribute(k_gemm<64, false, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<64, false>::kSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<128, false, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<128, false>::kSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<128, true, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<128, true>::kSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<256, true, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<256, true>::kSmem);
   return e;
 }
 
@@ -368,9 +410,14 @@ int rtopk_matrix_create(rtopk_matrix** out, int device, int64_t scratch_bytes) {
                              cudaFuncSetAttribute(k_orth_small, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(kSmallLong)) != cudaSuccess))
     status = RTOPK_ERR_CUDA;
   ctx->encode = (EncodeTiled)fn;
-  if (status == RTOPK_OK && (cudaMalloc(&ctx->error, 256) != cudaSuccess || cudaMemset(ctx->error, 0, 256) != cudaSuccess ||
-                             (scratch_bytes && cudaMalloc(&ctx->scratch, scratch_bytes) != cudaSuccess)))
+  if (status == RTOPK_OK && (cudaMalloc(&ctx->error, kErrorBytes + ctx->sms * kPartBytes + scratch_bytes) != cudaSuccess ||
+                             cudaMemset(ctx->error, 0, kErrorBytes) != cudaSuccess))
     status = RTOPK_ERR_ALLOC;
+  if (ctx->error) {
+    ctx->arrived = ctx->error + 64;
+    ctx->parts = ctx->error + kErrorBytes / 4;
+    ctx->scratch = (char*)ctx->parts + ctx->sms * kPartBytes;
+  }
   if (status != RTOPK_OK) {
     cudaGetLastError();
     rtopk_matrix_destroy(ctx);
@@ -383,7 +430,6 @@ int rtopk_matrix_create(rtopk_matrix** out, int device, int64_t scratch_bytes) {
 int rtopk_matrix_destroy(rtopk_matrix* ctx) {
   if (!ctx) return RTOPK_OK;
   OnDevice on(ctx->device);
-  if (ctx->scratch) cudaFree(ctx->scratch);
   if (ctx->error) cudaFree(ctx->error);
   delete ctx;
   return RTOPK_OK;
@@ -405,7 +451,7 @@ int rtopk_matrix_poll_status(rtopk_matrix* ctx, void* stream) {
   MAT_CUDA(cudaMemcpyAsync(&e, ctx->error, sizeof e, cudaMemcpyDeviceToHost, st));
   MAT_CUDA(cudaStreamSynchronize(st));
   if (!e) return RTOPK_OK;
-  MAT_CUDA(cudaMemsetAsync(ctx->error, 0, sizeof e, st));
+  MAT_CUDA(cudaMemsetAsync(ctx->error, 0, kErrorBytes, st));      // the counters too: a block that gave up may have left them
   return RTOPK_ERR_INTERNAL;
 }
 
