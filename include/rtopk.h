@@ -512,8 +512,8 @@ int rtopk_matrix_poll_status(rtopk_matrix* ctx, void* stream);
  *               (3.4445, -4.7750, 2.0315) in every step.  Singular values must stay below 4 from step
  *               to step (they do, below 1.3, with the default), else the 16-bit products overflow.
  *   eps         >= 0.  A zero matrix gives zeros; one with a NaN or an infinity gives NaN.
- * The products take 16-bit floating-point operands and 32-bit sums.  The diagonals of X X^T and of its
- * polynomial and the low half of X stay outside the 16 bits: the result is within about 1e-3 of the
+ * The products take 16-bit floating-point operands and 32-bit sums.  X itself and the diagonals of X X^T
+ * and of its polynomial are kept in 32 bits beside them: the result is within about 1e-3 of the
  * exact iteration (2-norm of the difference over 2-norm of the result).
  * Errors: INVALID_ARG, UNSUPPORTED (batch above 65535), CUDA.
  */

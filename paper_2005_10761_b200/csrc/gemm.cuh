@@ -32,12 +32,12 @@ constexpr int kSmemMisc = 1024 + 1024;      // alignment slack, barriers
 // Scales that keep 16-bit entries away from the subnormal range: X is held times 32 and its Gram matrix and the
 // polynomial of it times 1024.  ||X||_F = 1 at the start, so an entry of a 10000 x 1500 X is about 2.6e-4; afterwards
 // singular values stay below about 1.3, so nothing comes near the largest 16-bit number.
-constexpr float kXScale = 32.f, kAScale = 1024.f, kLoScale = 2048.f;
+constexpr float kXScale = 32.f, kAScale = 1024.f;
 
 enum Epi : int {
   EPI_GRAM = 0,    // A = X X^T: entries off the diagonal in 16 bits, the diagonal (from the unrounded X) in 32
   EPI_POLY = 1,    // a + b A + c A^2, in the same form
-  EPI_APPLY = 2,   // X <- (that) X, as high and low halves
+  EPI_APPLY = 2,   // X <- (that) X, in 32 bits and in 16
   EPI_OUT = 3,     // the last X, into the caller's matrix
   EPI_UPDATE = 4,  // the last X, into the caller's weights
   EPI_CODED = 5    // 8-bit codes: times the two scales
@@ -52,10 +52,10 @@ struct Gemm {
   uint32_t* arrived;         // split: blocks that have left their part, per tile and block of a pair; zero between launches
   uint32_t* error;
   // epilogue operands
-  const __half* o;           // POLY: A off the diagonal; APPLY / OUT / UPDATE: high halves of X
-  __half* lo;                // APPLY / OUT / UPDATE: low halves of X (APPLY: replaced in place)
+  const __half* o;           // POLY: A off the diagonal
+  float* x;                  // APPLY / OUT / UPDATE: X in 32 bits (APPLY: replaced in place)
   __half* h;                 // 16-bit result
-  int64_t ld, stride;        // of o, lo, h
+  int64_t ld, stride;        // of o, x, h
   const float* d_in;         // diagonal of the left operand [batch][cols]
   float* d_out;
   int64_t d_stride;
@@ -121,43 +121,48 @@ __device__ __forceinline__ float gram_diagonal(const Gemm& g, int z, int lane) {
   return d * (1.f / kAScale);
 }
 
-// 32 entries of one lane, columns col0 .. (those past the edge read the last one): all loads are under way before the
-// first is used.
-__device__ __forceinline__ void load_column(const __half* p, int col0, int ncol, int64_t ld, __half (&v)[32]) {
-  p += col0 * ld;
+// 32 entries of one lane, `step` apart (past the edge the last one again): all loads are under way before the first is used.
+template <bool kFull, class T>
+__device__ __forceinline__ void load_strip(const T* p, int n, int64_t step, T (&v)[32]) {
 #pragma unroll
-  for (int c = 0; c < 32; ++c) v[c] = p[min(c, ncol - 1) * ld];
+  for (int c = 0; c < 32; ++c) {
+    v[c] = *p;
+    if (kFull || c + 1 < n) p += step;
+  }
+}
+template <bool kFull, class T, class F>
+__device__ __forceinline__ void store_strip(T* p, int n, int64_t step, F value) {
+#pragma unroll
+  for (int c = 0; c < 32; ++c) {
+    if (kFull || c < n) *p = value(c);
+    p += step;
+  }
 }
 
-// 32 columns (col0 ..) of lane `lane` of one tile.
-template <int kEpi>
-__device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col0, float diag, const uint32_t (&acc)[32]) {
-  const int ncol = min(32, g.cols - col0);
-  if (kEpi == EPI_GRAM || kEpi == EPI_POLY) {
+// 32 columns (col0 ..) of lane `lane` of one tile; all 32 threads of the warp come here, each with its lane.  kFull: the
+// warp's lanes and columns all exist.  `n` of the columns do; loads of lanes that do not read a neighbour's values.
+template <int kEpi, bool kFull>
+__device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col0, int n, float diag, const uint32_t (&acc)[32]) {
+  const int me = threadIdx.x & 31;
+  bool in = kFull || lane < g.lanes;
+  const int safe = kFull ? lane : min(lane, g.lanes - 1), my_col = col0 + (kFull ? me : min(me, n - 1));
+  float v[32];
+  if constexpr (kEpi == EPI_GRAM || kEpi == EPI_POLY) {
     // Symmetric result: a 128-wide block of columns left of this lane's block is the mirror image of another tile.
     const int lb = lane / kLanes, cb = col0 / kLanes;
     if (cb < lb) return;
-    const bool in = lane < g.lanes;
-    lane = min(lane, g.lanes - 1);
-    constexpr uint32_t active = 0xFFFFFFFFu;
     const float* d_in = g.d_in + z * g.d_stride;
-    const __half* o = g.o + z * g.stride;
-    __half* h = g.h + z * g.stride;
-    float v[32];
-    if (kEpi == EPI_GRAM) {
+    if constexpr (kEpi == EPI_GRAM) {
 #pragma unroll
       for (int c = 0; c < 32; ++c) v[c] = __uint_as_float(acc[c]);
     } else {
-      const float dl = d_in[lane], dc = d_in[col0 + min(threadIdx.x & 31, ncol - 1)];
-      __half oc[32];
-      load_column(o + lane, col0, ncol, g.ld, oc);
+      __half o[32];
+      load_strip<kFull>(g.o + z * g.stride + (int64_t)col0 * g.ld + safe, n, g.ld, o);
+      const float dl = g.b + g.c * d_in[safe], dc = g.c * d_in[my_col], scale = g.c * (1.f / kAScale);
 #pragma unroll
-      for (int c = 0; c < 32; ++c) {
-        const float d = __shfl_sync(active, dc, c);
-        v[c] = c < ncol ? g.c * (__uint_as_float(acc[c]) * (1.f / kAScale)) + (g.b + g.c * (dl + d)) * __half2float(oc[c]) : 0.f;
-      }
+      for (int c = 0; c < 32; ++c) v[c] = scale * __uint_as_float(acc[c]) + (dl + __shfl_sync(0xFFFFFFFFu, dc, c)) * __half2float(o[c]);
     }
-    if (in && lane >= col0 && lane < col0 + ncol) {
+    if (cb == lb && in && lane >= col0 && lane < col0 + n) {
       float q = 0.f;
 #pragma unroll
       for (int c = 0; c < 32; ++c)
@@ -173,105 +178,74 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
     }
     if (!in) return;
     // row `lane`, columns col0 ..: the row stride is a multiple of 8, so the padding takes whole vectors
-    __half* row = h + (int64_t)lane * g.ld + col0;
+    __half* row = g.h + z * g.stride + lane * g.ld + col0;
 #pragma unroll
     for (int c = 0; c < 32; c += 8)
-      if (c < ncol) store_half8(row + c, v + c);
-    if (cb > lb) {
+      if (kFull || c < n) store_half8(row + c, v + c);
+    if (cb > lb) store_strip<kFull>(g.h + z * g.stride + col0 * g.ld + lane, n, g.ld, [&](int c) { return to_half(v[c]); });
+  } else if constexpr (kEpi == EPI_CODED) {
+    const float sl = g.scale_lane ? g.scale_lane[safe] : 1.f, sc = g.scale_col[my_col];
 #pragma unroll
-      for (int c = 0; c < 32; ++c)
-        if (c < ncol) h[(int64_t)(col0 + c) * g.ld + lane] = to_half(v[c]);
-    }
-    return;
-  }
-  bool in = lane < g.lanes;
-  const int safe = min(lane, g.lanes - 1);      // loads of lanes past the edge read a neighbour's values and drop them
-  const int me = threadIdx.x & 31;
-  if (kEpi == EPI_CODED) {
-    const float sl = g.scale_lane ? g.scale_lane[safe] : 1.f;
-    const float sc = g.scale_col[col0 + min(me, ncol - 1)];
-    const int64_t at = (int64_t)lane * g.out_lane + (int64_t)col0 * g.out_col;
+    for (int c = 0; c < 32; ++c) v[c] = (float)(int)acc[c] * __shfl_sync(0xFFFFFFFFu, sc, c) * sl;
+    if (!in) return;
+    const int64_t at = lane + col0 * g.out_col;
+    if (g.out_bf16) store_strip<kFull>((__nv_bfloat16*)g.out + at, n, g.out_col, [&](int c) { return __float2bfloat16_rn(v[c]); });
+    else store_strip<kFull>((float*)g.out + at, n, g.out_col, [&](int c) { return v[c]; });
+  } else {
+    // X' = diag X + offdiag X: the product carries only the part off the diagonal, times kAScale * kXScale
+    float* x = g.x + z * g.stride + col0 * g.ld;
+    load_strip<kFull>(x + safe, n, g.ld, v);
+    const float dc = g.d_in[z * g.d_stride + my_col];
 #pragma unroll
-    for (int c = 0; c < 32; ++c) {
-      const float v = (float)(int)acc[c] * __shfl_sync(0xFFFFFFFFu, sc, c) * sl;
-      if (!in || c >= ncol) continue;
-      if (g.out_bf16) ((__nv_bfloat16*)g.out)[at + c * g.out_col] = __float2bfloat16_rn(v);
-      else ((float*)g.out)[at + c * g.out_col] = v;
-    }
-    return;
-  }
-  // X' = diag X + offdiag X: the product carries only the part off the diagonal, times kAScale * kXScale
-  const float dc = g.d_in[z * g.d_stride + col0 + min(me, ncol - 1)];
-  __half* lo = g.lo + z * g.stride + lane;
-  float v[32];
-  {
-    __half oc[32], lc[32];
-    load_column(g.o + z * g.stride + safe, col0, ncol, g.ld, oc);
-    load_column(g.lo + z * g.stride + safe, col0, ncol, g.ld, lc);
-#pragma unroll
-    for (int c = 0; c < 32; ++c) {
-      const float x = __half2float(oc[c]) + __half2float(lc[c]) * (1.f / kLoScale);
-      v[c] = __shfl_sync(0xFFFFFFFFu, dc, c) * x + __uint_as_float(acc[c]) * (1.f / kAScale);
-    }
-  }
-  if (kEpi == EPI_APPLY) {
-    __half* h = g.h + z * g.stride + lane;
-#pragma unroll
-    for (int c = 0; c < 32; ++c) {
-      if (in && c < ncol) {
-        const int64_t i = (int64_t)(col0 + c) * g.ld;
-        const __half hi = to_half(v[c]);
-        h[i] = hi;
-        lo[i] = to_half((v[c] - __half2float(hi)) * kLoScale);
+    for (int c = 0; c < 32; ++c) v[c] = __shfl_sync(0xFFFFFFFFu, dc, c) * v[c] + __uint_as_float(acc[c]) * (1.f / kAScale);
+    if constexpr (kEpi == EPI_APPLY) {
+      if (in) {
+        store_strip<kFull>(x + lane, n, g.ld, [&](int c) { return v[c]; });
+        store_strip<kFull>(g.h + z * g.stride + col0 * g.ld + lane, n, g.ld, [&](int c) { return to_half(v[c]); });
       }
-      v[c] = in ? v[c] * v[c] : 0.f;
-    }
-    // sums over the warp's 32 lanes, column c's in thread c
 #pragma unroll
-    for (int n = 16; n; n >>= 1)
+      for (int c = 0; c < 32; ++c) v[c] = in ? v[c] * v[c] : 0.f;
+      // sums over the warp's 32 lanes, column c's in thread c
 #pragma unroll
-      for (int i = 0; i < n; ++i) {
-        const bool upper = me & n;
-        const float give = upper ? v[i] : v[i + n], keep = upper ? v[i + n] : v[i];
-        v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, n);
-      }
-    const int slot = (lane - me) / 32;
-    if (me < ncol && slot < g.slots) g.row_sums[((int64_t)z * g.slots + slot) * g.d_stride + col0 + me] = v[0];
-    return;
-  }
-  int n = ncol;
-  int64_t at = z * g.out_batch + (int64_t)lane * g.out_lane + (int64_t)col0 * g.out_col, step = g.out_col;
-  if (g.out_lane != 1) {      // the result's rows run along the columns: turn the 32 x 32 block round
-    in = me < ncol;
-    n = min(32, g.lanes - (lane - me));
-    at = z * g.out_batch + (int64_t)(lane - me) * g.out_lane + (int64_t)(col0 + me) * g.out_col, step = g.out_lane;
+      for (int k = 16; k; k >>= 1)
 #pragma unroll
-    for (int k = 16; k; k >>= 1)
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (!(i & k)) {
+        for (int i = 0; i < k; ++i) {
           const bool upper = me & k;
-          const float got = __shfl_xor_sync(0xFFFFFFFFu, upper ? v[i] : v[i | k], k);
-          if (upper) v[i] = got;
-          else v[i | k] = got;
+          const float give = upper ? v[i] : v[i + k], keep = upper ? v[i + k] : v[i];
+          v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, k);
         }
-  }
-  if (!in) return;
-  if (kEpi == EPI_UPDATE) {
-    float w[32];
+      const int slot = (lane - me) / 32;
+      if (kFull || (me < n && slot < g.slots)) g.row_sums[((int64_t)z * g.slots + slot) * g.d_stride + col0 + me] = v[0];
+    } else {
+      int64_t at = z * g.out_batch + lane * g.out_lane + col0 * g.out_col, step = g.out_col;
+      if (g.out_lane != 1) {      // the result's rows run along the columns: turn the 32 x 32 block round
+        in = kFull || me < n;
+        n = kFull ? 32 : min(32, g.lanes - (lane - me));
+        at = z * g.out_batch + (lane - me) * g.out_lane + (col0 + me) * g.out_col, step = g.out_lane;
 #pragma unroll
-    for (int c = 0; c < 32; ++c) w[c] = ((const float*)g.out)[at + min(c, n - 1) * step];
+        for (int k = 16; k; k >>= 1)
 #pragma unroll
-    for (int c = 0; c < 32; ++c)
-      if (c < n) ((float*)g.out)[at + c * step] = g.keep * w[c] - g.rate * (v[c] * (1.f / kXScale));
-    return;
-  }
-#pragma unroll
-  for (int c = 0; c < 32; ++c)
-    if (c < n) {
-      if (g.out_bf16) ((__nv_bfloat16*)g.out)[at + c * step] = __float2bfloat16_rn(v[c] * (1.f / kXScale));
-      else ((float*)g.out)[at + c * step] = v[c] * (1.f / kXScale);
+          for (int i = 0; i < 32; ++i)
+            if (!(i & k)) {
+              const bool upper = me & k;
+              const float got = __shfl_xor_sync(0xFFFFFFFFu, upper ? v[i] : v[i | k], k);
+              if (upper) v[i] = got;
+              else v[i | k] = got;
+            }
+      }
+      if (!in || n <= 0) return;
+      if constexpr (kEpi == EPI_UPDATE) {
+        float w[32];
+        load_strip<kFull>((const float*)g.out + at, n, step, w);
+        const float rate = g.rate * (1.f / kXScale);
+        store_strip<kFull>((float*)g.out + at, n, step, [&](int c) { return g.keep * w[c] - rate * v[c]; });
+      } else if (g.out_bf16) {
+        store_strip<kFull>((__nv_bfloat16*)g.out + at, n, step, [&](int c) { return __float2bfloat16_rn(v[c] * (1.f / kXScale)); });
+      } else {
+        store_strip<kFull>((float*)g.out + at, n, step, [&](int c) { return v[c] * (1.f / kXScale); });
+      }
     }
+  }
 }
 
 template <int kCols, bool kPair>
@@ -412,13 +386,18 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       tc_fence_after();
       const uint32_t from = tmem + b * kCols + ((uint32_t)(quarter * 32) << 16);
       const int cols = min(kCols, g.cols - q.c * kCols);
+      const bool lanes_full = row0 + kLanes <= g.lanes;
+      auto finish = [&](int c, const uint32_t(&acc)[32]) {
+        if (lanes_full && c + 32 <= cols) epilogue<kEpi, true>(g, q.z, row, q.c * kCols + c, 32, diag, acc);
+        else epilogue<kEpi, false>(g, q.z, row, q.c * kCols + c, min(32, cols - c), diag, acc);
+        __syncwarp();
+      };
       if (g.split == 1) {
 #pragma unroll 1
         for (int c = chunk0; c < cols; c += 32 * (kEpiWarps / 4)) {
           uint32_t acc[32];
           tmem_load32(from + c, acc);
-          epilogue<kEpi>(g, q.z, row, q.c * kCols + c, diag, acc);
-          __syncwarp();
+          finish(c, acc);
         }
         tc_fence_before();
         __syncwarp();
@@ -470,8 +449,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
           for (int i = 0; i < 32; ++i)
             acc[i] = kInt8 ? acc[i] + w[i] : __float_as_uint(__uint_as_float(acc[i]) + __uint_as_float(w[i]));
         }
-        epilogue<kEpi>(g, q.z, row, q.c * kCols + c, diag, acc);
-        __syncwarp();
+        finish(c, acc);
       }
     }
     __syncwarp();

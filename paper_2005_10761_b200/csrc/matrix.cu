@@ -81,7 +81,8 @@ struct Carve {
 };
 
 struct OrthScratch {
-  __half *hi[2], *lo, *gram, *poly;
+  float* x;               // X in 32 bits; its 16-bit form is read by a product while the next one is written
+  __half *hi[2], *gram, *poly;
   float *gram_d, *poly_d, *row_sums;
   double* part;
   int slots;
@@ -91,7 +92,7 @@ struct OrthScratch {
     stride_x = s * ld_x, stride_a = s * ld_a, stride_d = up(s, 64);
     part = c.take<double>(batch * kNormBlocks);
     for (auto& h : hi) h = c.take<__half>(batch * stride_x);
-    lo = c.take<__half>(batch * stride_x);
+    x = c.take<float>(batch * stride_x);
     gram = c.take<__half>(batch * stride_a);
     poly = c.take<__half>(batch * stride_a);
     gram_d = c.take<float>(batch * stride_d);
@@ -277,7 +278,7 @@ int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, i
   src.part = w.part;
   src.parts = (int)std::min<int64_t>(kNormBlocks, ceil_div(m * ceil_div(n, kNormSpan), 8));
   MAT_TRY(launch(ctx, false, k_norm, dim3(src.parts, (unsigned)batch), 256, 0, st, src));
-  MAT_TRY(launch(ctx, true, k_split, dim3((unsigned)ceil_div(n, 64), (unsigned)ceil_div(m, 64), (unsigned)batch), 256, 0, st, src, w.hi[0], w.lo, w.ld_x, w.stride_x,
+  MAT_TRY(launch(ctx, true, k_split, dim3((unsigned)ceil_div(n, 64), (unsigned)ceil_div(m, 64), (unsigned)batch), 256, 0, st, src, w.x, w.hi[0], w.ld_x, w.stride_x,
                  w.row_sums, w.slots, w.stride_d, tall ? 1 : 0));
   int cur = 0;
   for (int i = 0; i < steps; ++i) {
@@ -296,7 +297,7 @@ int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, i
     g.o = w.gram, g.d_in = w.gram_d, g.h = w.poly, g.d_out = w.poly_d;
     MAT_TRY(gemm<EPI_POLY>(ctx, true, gram, gram, g, st));
     g.lanes = (int)l, g.tri = 0;
-    g.o = w.hi[cur], g.lo = w.lo, g.ld = w.ld_x, g.stride = w.stride_x, g.d_in = w.poly_d;
+    g.x = w.x, g.ld = w.ld_x, g.stride = w.stride_x, g.d_in = w.poly_d;
     if (i + 1 < steps) {
       g.h = w.hi[cur ^ 1];
       MAT_TRY(gemm<EPI_APPLY>(ctx, true, x, poly, g, st));

@@ -1,5 +1,5 @@
-// What comes before the products of the orthogonalisation: momentum, the Frobenius norm, and X = U / (||U||_F + eps) as high
-// and low halves, short side first.
+// What comes before the products of the orthogonalisation: momentum, the Frobenius norm, and X = U / (||U||_F + eps) in
+// 32 and in 16 bits, short side first.
 #pragma once
 
 #include "coded.cuh"
@@ -102,10 +102,9 @@ __global__ void __launch_bounds__(256) k_norm(const __grid_constant__ Source s) 
   }
 }
 
-// X, 64 x 64 elements of U per block, transposed when U is tall.  A thread writes eight neighbours of a row of X as their
-// halves; four threads together give one partial sum of squares.
+// X, 64 x 64 elements of U per block, transposed when U is tall.  A thread writes eight neighbours of a row of X; four threads together give one partial sum of squares.
 __global__ void __launch_bounds__(256)
-k_split(const __grid_constant__ Source s, __half* hi, __half* lo, int64_t ld, int64_t stride, float* row_sums, int slots, int64_t d_stride, int transpose) {
+k_split(const __grid_constant__ Source s, float* x, __half* h, int64_t ld, int64_t stride, float* row_sums, int slots, int64_t d_stride, int transpose) {
   __shared__ float tile[64][65];
   __shared__ float inv_s;
   const int z = blockIdx.z, c0 = blockIdx.x * 64, r0 = blockIdx.y * 64;
@@ -136,27 +135,27 @@ k_split(const __grid_constant__ Source s, __half* hi, __half* lo, int64_t ld, in
   }
   __syncthreads();
   const float inv = inv_s;
-  hi += z * stride, lo += z * stride, row_sums += (int64_t)z * slots * d_stride;
+  x += z * stride, h += z * stride, row_sums += (int64_t)z * slots * d_stride;
   const int ns = transpose ? s.n : s.m, nl = transpose ? s.m : s.n;
   const int a0 = transpose ? c0 : r0, b0 = transpose ? r0 : c0;      // of X: rows and columns
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int a = (threadIdx.x >> 3) + 32 * i, b = (threadIdx.x & 7) * 8;
-    float h[8], l[8], sum = 0.f;
+    float u[8], sum = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float u = (transpose ? tile[b + j][a] : tile[a][b + j]) * inv;
-      h[j] = __half2float(to_half(u));
-      l[j] = (u - h[j]) * kLoScale;
-      sum = fmaf(u, u, sum);
+      u[j] = (transpose ? tile[b + j][a] : tile[a][b + j]) * inv;
+      sum = fmaf(u[j], u[j], sum);
     }
     sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
     sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
     if (a0 + a >= ns || b0 + (b & ~31) >= nl) continue;
     if ((b & 31) == 0) row_sums[(int64_t)((b0 + b) / 32) * d_stride + a0 + a] = sum;
     if (b0 + b < nl) {      // the rows' padding takes whole vectors
-      store_half8(hi + (a0 + a) * ld + b0 + b, h);
-      store_half8(lo + (a0 + a) * ld + b0 + b, l);
+      const int64_t at = (a0 + a) * ld + b0 + b;
+      *(float4*)(x + at) = make_float4(u[0], u[1], u[2], u[3]);
+      *(float4*)(x + at + 4) = make_float4(u[4], u[5], u[6], u[7]);
+      store_half8(h + at, u);
     }
   }
 }
