@@ -24,18 +24,35 @@ __device__ __forceinline__ float code_scale(uint32_t max_magnitude) {
   if (max_magnitude >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
   return __fdiv_rn(__uint_as_float(max_magnitude), 127.f);
 }
-// rint(v / s) for finite v and s.  The product with the reciprocal r is within 2^-23 of the quotient, 2e-5 at 127: unless
-// it lies that near to the middle between two codes, it rounds to the same one; otherwise the quotient is formed.
-__device__ __forceinline__ int code(float v, float s, float r) {
-  const float t = v * r;
-  float q = rintf(t);
-  if (!(fabsf(fabsf(t - q) - 0.5f) > 1e-4f)) q = rintf(__fdiv_rn(v, s));
-  return max(-127, min(127, (int)q));
+// rint(v / s), the quotient formed.
+__device__ __forceinline__ int code_exactly(float v, float s) { return max(-127, min(127, __float2int_rn(__fdiv_rn(v, s)))); }
+
+// Codes without a division: adding 1.5 * 2^23 to v * r, r the reciprocal of s, rounds the exact product to a whole number and
+// leaves it in the low byte of the sum.  The product is within 2^-23 of the quotient, 2e-5 at 127, so both round to the same
+// code unless the product lies that near to the middle between two: `off` collects how far the products are from their codes,
+// and where that comes to 0.4999 the quotients are formed after all.
+constexpr float kToByte = 12582912.f;
+__device__ __forceinline__ uint32_t code_byte(float v, float r, float& off) {
+  const float t = fmaf(v, r, kToByte);
+  off = fmaxf(off, fabsf(fmaf(v, r, kToByte - t)));
+  return __float_as_uint(t);
 }
-// The reciprocal for code(): NaN where the quotient has to be formed every time, 0 (with s = 1) where all codes are 0.
+__device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+// The reciprocal for code_byte().  All codes are 0 without a positive scale (s = 1 then, r = 0); scales near the subnormal
+// range have no usable reciprocal: infinity, which makes `off` NaN or infinite.
 __device__ __forceinline__ float code_reciprocal(float& s) {
   if (!(s > 0.f)) { s = 1.f; return 0.f; }
-  return s < 1e-36f ? __uint_as_float(0x7FC00000u) : __fdiv_rn(1.f, s);
+  return s < 1e-36f ? __uint_as_float(0x7F800000u) : __fdiv_rn(1.f, s);
+}
+// Four codes in a word.  With r = 0 the values may be anything, infinities and NaN too.
+__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d, float s, float r) {
+  if (r == 0.f) return 0u;
+  float off = 0.f;
+  const uint32_t w = pack_bytes(code_byte(a, r, off), code_byte(b, r, off), code_byte(c, r, off), code_byte(d, r, off));
+  if (off < 0.4999f && r < 1e37f) return w;
+  return pack_bytes(code_exactly(a, s), code_exactly(b, s), code_exactly(c, s), code_exactly(d, s));
 }
 
 // Eight neighbours of a row; those past the end are zero.  `vec`: the row allows 16-byte loads.
@@ -65,9 +82,7 @@ __device__ __forceinline__ void times8(const float* mul, int left, float (&v)[8]
     if (i < left) v[i] *= mul[i];
 }
 __device__ __forceinline__ void code8(const float (&v)[8], int left, float s, float r, int8_t* out) {
-  uint32_t w[2] = {0u, 0u};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)(uint8_t)code(v[i], s, r) << (8 * (i & 3));
+  const uint32_t w[2] = {code4(v[0], v[1], v[2], v[3], s, r), code4(v[4], v[5], v[6], v[7], s, r)};
   if (left >= 8) {
     *(uint2*)out = make_uint2(w[0], w[1]);
   } else {
@@ -147,7 +162,7 @@ __global__ void __launch_bounds__(256) k_col_max(const T* src, int64_t ld, int r
   launch_next();
   uint32_t m[8] = {};
   if (c < cols) {
-#pragma unroll 4
+#pragma unroll 8
     for (int r = r0 + y; r < r1; r += 8) {
       float v[8];
       load8(src + r * ld + c, cols - c, vec, v);
@@ -171,6 +186,7 @@ template <class T>
 __global__ void __launch_bounds__(256)
 k_code_cols(const T* src, int64_t ld, int rows, int cols, int vec, const uint32_t* max_bits, int8_t* codes, int64_t ld_codes, float* scales) {
   __shared__ uint32_t tile[64][33];
+  __shared__ float2 scale[64];
   const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 128;
   const int cg = (threadIdx.x & 7) * 8, rg = threadIdx.x >> 3;
   launch_wait();
@@ -180,22 +196,21 @@ k_code_cols(const T* src, int64_t ld, int rows, int cols, int vec, const uint32_
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = r0 + rg * 4 + i;
-    if (left > 0 && r < rows) load8(src + (int64_t)r * ld + c0 + cg, left, vec, v[i]);
-    else
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+    load8(src + (int64_t)min(r, rows - 1) * ld + c0 + cg, r < rows ? left : 0, vec, v[i]);
   }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    if (j >= left) break;
-    float s = code_scale(max_bits[c0 + cg + j]);
-    if (blockIdx.y == 0 && rg == 0) scales[c0 + cg + j] = s;
+  if (threadIdx.x < 64 && c0 + threadIdx.x < cols) {
+    float s = code_scale(max_bits[c0 + threadIdx.x]);
+    if (blockIdx.y == 0) scales[c0 + threadIdx.x] = s;
     const float r = code_reciprocal(s);
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w |= (uint32_t)(uint8_t)code(v[i][j], s, r) << (8 * i);
-    tile[cg + j][rg] = w;
+    scale[threadIdx.x] = make_float2(s, r);
   }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < left) {
+      const float2 q = scale[cg + j];
+      tile[cg + j][rg] = code4(v[0][j], v[1][j], v[2][j], v[3][j], q.x, q.y);
+    }
   __syncthreads();
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
   const int n = min(4, rows - r0 - x * 4);
@@ -221,6 +236,86 @@ __global__ void __launch_bounds__(256) k_codes_transpose(const int8_t* codes, in
   __syncthreads();
   for (int c = y; c < 64; c += 4)
     if (c0 + c < cols && r0 + x < rows) out[(int64_t)(c0 + c) * ld_out + r0 + x] = tile[c][x];
+}
+
+// A linear layer for a few tokens: reading the codes of W once is all the work, so one launch does everything.  Each block
+// codes the tokens for itself (they are small, and come from L2), then each warp takes two output channels at a time: 16 codes
+// of W a thread, four-way integer dot products with the tokens' codes in shared memory.
+constexpr int kFewThreads = 256;
+constexpr int kFewBytes = 48 * 1024;       // codes of all tokens in shared memory, at most
+__host__ __device__ constexpr int few_row(int n_in) { return (n_in + 511) / 512 * 512; }
+
+template <class T, int kTokens>
+__global__ void __launch_bounds__(kFewThreads)
+k_product_few(const T* x, int64_t ld_x, int vec, const int8_t* codes, int64_t ld_codes, const float* scales, int tokens, int n_out, int n_in, T* out, int64_t ld_out) {
+  extern __shared__ __align__(16) char few_smem[];
+  __shared__ uint32_t part[8][kTokens];
+  __shared__ float token_scale[kTokens];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = few_row(n_in);
+  launch_wait();
+  launch_next();
+  uint32_t m[kTokens] = {};
+  for (int c = threadIdx.x * 8; c < n_in; c += kFewThreads * 8)
+#pragma unroll
+    for (int t = 0; t < kTokens; ++t) {
+      float v[8];
+      load8(x + min(t, tokens - 1) * ld_x + c, n_in - c, vec, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[t] = max(m[t], magnitude(v[i]));
+    }
+#pragma unroll
+  for (int t = 0; t < kTokens; ++t) {
+    m[t] = __reduce_max_sync(0xFFFFFFFFu, m[t]);
+    if (lane == 0) part[warp][t] = m[t];
+  }
+  __syncthreads();
+  float s[kTokens], r[kTokens];
+#pragma unroll
+  for (int t = 0; t < kTokens; ++t) {
+    uint32_t best = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) best = max(best, part[i][t]);
+    s[t] = code_scale(best);
+    if (threadIdx.x == 0) token_scale[t] = s[t];
+    r[t] = code_reciprocal(s[t]);
+  }
+  for (int c = threadIdx.x * 8; c < row; c += kFewThreads * 8)
+#pragma unroll
+    for (int t = 0; t < kTokens; ++t) {
+      float v[8];
+      load8(x + min(t, tokens - 1) * ld_x + min(c, n_in - 1), max(n_in - c, 0), vec, v);
+      *(uint2*)(few_smem + t * row + c) = make_uint2(code4(v[0], v[1], v[2], v[3], s[t], r[t]), code4(v[4], v[5], v[6], v[7], s[t], r[t]));
+    }
+  __syncthreads();
+  const int pairs = (n_out + 1) / 2;
+  for (int k = blockIdx.x * 8 + warp; k < pairs; k += gridDim.x * 8) {
+    const int n0 = 2 * k, n1 = min(n0 + 1, n_out - 1);
+    const int8_t *w0 = codes + n0 * ld_codes, *w1 = codes + n1 * ld_codes;
+    int acc[2][kTokens] = {};
+    // past the end of a row the tokens' codes are zero, so that the last 16 codes read there count for nothing
+#pragma unroll 4
+    for (int c = lane * 16; c < n_in; c += 512) {
+      const int4 a = __ldg((const int4*)(w0 + c)), b = __ldg((const int4*)(w1 + c));
+#pragma unroll
+      for (int t = 0; t < kTokens; ++t) {
+        const int4 q = *(const int4*)(few_smem + t * row + c);
+        acc[0][t] = __dp4a(a.x, q.x, __dp4a(a.y, q.y, __dp4a(a.z, q.z, __dp4a(a.w, q.w, acc[0][t]))));
+        acc[1][t] = __dp4a(b.x, q.x, __dp4a(b.y, q.y, __dp4a(b.z, q.z, __dp4a(b.w, q.w, acc[1][t]))));
+      }
+    }
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < 2 * kTokens; ++i) {
+      const int sum = __reduce_add_sync(0xFFFFFFFFu, acc[i & 1][i >> 1]);
+      if (lane == i) mine = sum;
+    }
+    const int t = lane >> 1, n = n0 + (lane & 1);
+    if (t < tokens && t < kTokens && n < n_out) {
+      const float v = (float)mine * token_scale[t] * scales[n];
+      if (sizeof(T) == 2) ((__nv_bfloat16*)out)[t * ld_out + n] = __float2bfloat16_rn(v);
+      else ((float*)out)[t * ld_out + n] = v;
+    }
+  }
 }
 
 }  // namespace mat

@@ -47,6 +47,7 @@ struct Gemm {
   int lanes, cols, depth;    // D is lanes x cols; depth in elements
   int batch, tiles_l, tiles_c, tiles;   // tiles per batch entry
   int tri;                   // only tiles that reach the upper triangle (col >= lane)
+  int p_early;               // P is not written by the kernel before this one: its first stages are loaded ahead of launch_wait()
   int split;                 // parts of the contraction, 1: whole
   uint32_t* parts;           // split: partial sums, [unit][col][lane]
   uint32_t* arrived;         // split: blocks that have left their part, per tile and block of a pair; zero between launches
@@ -295,12 +296,29 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
   else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = words[0];
-  launch_wait();
-  launch_next();
 
   const int total = g.tiles * g.batch * g.split;
   const int first = blockIdx.x / kBlocks, step = gridDim.x / kBlocks;
   const int all_k = (g.depth + kDepth - 1) / kDepth, part_k = (all_k + g.split - 1) / g.split;
+  auto load_p = [&](uint32_t s, const Tile& q, int kb) {
+    const uint32_t dst = base + s * S::kStageBytes, bar = kPair ? first_of_pair(full + 8 * s) : full + 8 * s;
+    const int row = q.l * S::kTileLanes + rank * kLanes;
+    if (rank == 0) bar_expect(full + 8 * s, kBlocks * S::kStageBytes);
+    if (kMnMajor) {
+      tma_load<kPair>(dst, &map_p, row, kb * kDepth, q.z, bar);
+      tma_load<kPair>(dst + S::kPBytes / 2, &map_p, row + 64, kb * kDepth, q.z, bar);
+    } else {
+      tma_load<kPair>(dst, &map_p, kb * kDepth, row, q.z, bar);
+    }
+  };
+  uint32_t early = 0;      // stages whose P is under way
+  if (kInt8 && g.p_early && threadIdx.x == 0 && first < total) {
+    const Tile q = tile_at<kCols, S::kTileLanes>(g, first);
+    const int k0 = q.part * part_k, n = min(kStages, min(all_k, k0 + part_k) - k0);
+    for (; early < (uint32_t)n; ++early) load_p(early, q, k0 + early);
+  }
+  launch_wait();
+  launch_next();
   if (warp == 0) {
     if (lane == 0) {
       uint32_t it = 0;
@@ -308,20 +326,11 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       for (int u = first; u < total && ok; u += step) {
         const Tile q = tile_at<kCols, S::kTileLanes>(g, u);
         const int k1 = min(all_k, (q.part + 1) * part_k);
-        const int p_row = q.l * S::kTileLanes + rank * kLanes, q_row = q.c * kCols + rank * S::kQRows;
         for (int kb = q.part * part_k; kb < k1; ++kb, ++it) {
           const uint32_t s = it % kStages;
           if (it >= (uint32_t)kStages && !(ok = bar_wait(empty + 8 * s, (it / kStages - 1) & 1, give))) break;
-          const uint32_t dst = base + s * S::kStageBytes;
-          if (rank == 0) bar_expect(full + 8 * s, kBlocks * S::kStageBytes);
-          const uint32_t bar = kPair ? first_of_pair(full + 8 * s) : full + 8 * s;
-          if (kMnMajor) {
-            tma_load<kPair>(dst, &map_p, p_row, kb * kDepth, q.z, bar);
-            tma_load<kPair>(dst + S::kPBytes / 2, &map_p, p_row + 64, kb * kDepth, q.z, bar);
-          } else {
-            tma_load<kPair>(dst, &map_p, kb * kDepth, p_row, q.z, bar);
-          }
-          tma_load<kPair>(dst + S::kPBytes, &map_q, kb * kDepth, q_row, q.z, bar);
+          if (it >= early) load_p(s, q, kb);
+          tma_load<kPair>(base + s * S::kStageBytes + S::kPBytes, &map_q, kb * kDepth, q.c * kCols + rank * S::kQRows, q.z, kPair ? first_of_pair(full + 8 * s) : full + 8 * s);
         }
       }
       if (!ok) {

@@ -121,10 +121,9 @@ struct CodedScratch {
   }
 };
 
-// A kernel of a chain may start while the one before it ends (the kernels wait for it themselves); the first of a call
-// starts after all earlier work of the stream.
+// A kernel may start while the one before it in the stream ends; the kernels wait for it themselves.
 template <class... P, class... A>
-int launch_cluster(rtopk_matrix* ctx, bool chained, int cluster, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A... args) {
+int launch_cluster(rtopk_matrix* ctx, int cluster, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
@@ -132,10 +131,8 @@ int launch_cluster(rtopk_matrix* ctx, bool chained, int cluster, void (*kernel)(
   cfg.stream = st;
   cudaLaunchAttribute at[2];
   int n = 0;
-  if (chained) {
-    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[n++].val.programmaticStreamSerializationAllowed = 1;
-  }
+  at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[n++].val.programmaticStreamSerializationAllowed = 1;
   if (cluster > 1) {
     at[n].id = cudaLaunchAttributeClusterDimension;
     at[n].val.clusterDim.x = cluster, at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
@@ -148,8 +145,8 @@ int launch_cluster(rtopk_matrix* ctx, bool chained, int cluster, void (*kernel)(
   return RTOPK_OK;
 }
 template <class... P, class... A>
-int launch(rtopk_matrix* ctx, bool chained, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A... args) {
-  return launch_cluster(ctx, chained, 1, kernel, grid, threads, smem, st, args...);
+int launch(rtopk_matrix* ctx, void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, A... args) {
+  return launch_cluster(ctx, 1, kernel, grid, threads, smem, st, args...);
 }
 
 // Tensor map of a [batch][rows][cols] array: boxes of box_rows rows of one 128-byte swizzle row.
@@ -177,7 +174,7 @@ int64_t gemm_tiles(const Gemm& g) {
 }
 
 template <int kCols, bool kPair, int kEpi>
-int gemm_tile(rtopk_matrix* ctx, bool chained, const Operand& p, const Operand& q, Gemm g, int split, cudaStream_t st) {
+int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int split, cudaStream_t st) {
   using S = GemmShape<kCols, kPair>;
   constexpr bool kInt8 = kEpi == EPI_CODED;
   constexpr bool kMnMajor = kEpi == EPI_APPLY || kEpi == EPI_OUT || kEpi == EPI_UPDATE;
@@ -190,14 +187,14 @@ int gemm_tile(rtopk_matrix* ctx, bool chained, const Operand& p, const Operand& 
   MAT_TRY(tensor_map(ctx, &mp, p.p, kInt8, p.cols, p.rows, g.batch, p.ld, p.stride, kMnMajor ? 64 : kLanes));
   MAT_TRY(tensor_map(ctx, &mq, q.p, kInt8, q.cols, q.rows, g.batch, q.ld, q.stride, S::kQRows));
   const int grid = kBlocks * (int)std::min<int64_t>((int64_t)g.tiles * g.batch * split, ctx->sms / kBlocks);
-  return launch_cluster(ctx, chained, kBlocks, k_gemm<kCols, kPair, kEpi>, dim3(grid), kGemmThreads, S::kSmem, st, mp, mq, g);
+  return launch_cluster(ctx, kBlocks, k_gemm<kCols, kPair, kEpi>, dim3(grid), kGemmThreads, S::kSmem, st, mp, mq, g);
 }
 
 // Which tile, and in how many parts: the one for which this estimate of the time, in cycles, is least.  Per step of 128 bytes of the
 // contraction index a block takes what its stage needs from L2 (56 bytes a cycle and SM), or the tensor core's time; the last
 // tile of a block leaves its results behind the products; parts are written and read again.
 template <int kEpi>
-int gemm(rtopk_matrix* ctx, bool chained, const Operand& p, const Operand& q, const Gemm& g, cudaStream_t st) {
+int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, cudaStream_t st) {
   const int64_t steps = ceil_div((int64_t)g.depth * (kEpi == EPI_CODED ? 1 : 2), kDepthBytes);
   double best = 1e300;
   int which = 0, parts = 1;
@@ -218,10 +215,10 @@ int gemm(rtopk_matrix* ctx, bool chained, const Operand& p, const Operand& q, co
   consider(2, gemm_tiles<128, true>(g), 128, 2, GemmShape<128, true>::kStageBytes);
   consider(3, gemm_tiles<256, true>(g), 256, 2, GemmShape<256, true>::kStageBytes);
   switch (which) {
-    case 0: return gemm_tile<64, false, kEpi>(ctx, chained, p, q, g, parts, st);
-    case 1: return gemm_tile<128, false, kEpi>(ctx, chained, p, q, g, parts, st);
-    case 2: return gemm_tile<128, true, kEpi>(ctx, chained, p, q, g, parts, st);
-    default: return gemm_tile<256, true, kEpi>(ctx, chained, p, q, g, parts, st);
+    case 0: return gemm_tile<64, false, kEpi>(ctx, p, q, g, parts, st);
+    case 1: return gemm_tile<128, false, kEpi>(ctx, p, q, g, parts, st);
+    case 2: return gemm_tile<128, true, kEpi>(ctx, p, q, g, parts, st);
+    default: return gemm_tile<256, true, kEpi>(ctx, p, q, g, parts, st);
   }
 }
 
@@ -264,7 +261,7 @@ int orthogonal_small(rtopk_matrix* ctx, Source src, const Target& to, int64_t ba
   o.w = to.epi == EPI_UPDATE ? (float*)to.out : nullptr;
   o.out = to.out, o.bf16 = to.bf16, o.ld = to.ld, o.stride = to.stride, o.keep = to.keep, o.rate = to.rate, o.steps = steps;
   for (int i = 0; i < 3 * steps; ++i) o.coef[i] = coef ? coef[i] : kQuintic[i % 3];
-  return launch(ctx, false, k_orth_small, dim3((unsigned)batch), 256, small_smem(std::max(m, n)), st, src, o, m > n ? 1 : 0);
+  return launch(ctx, k_orth_small, dim3((unsigned)batch), 256, small_smem(std::max(m, n)), st, src, o, m > n ? 1 : 0);
 }
 
 int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, int64_t m, int64_t n, int steps, const float* coef, cudaStream_t st) {
@@ -277,8 +274,8 @@ int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, i
   src.m = (int)m, src.n = (int)n;
   src.part = w.part;
   src.parts = (int)std::min<int64_t>(kNormBlocks, ceil_div(m * ceil_div(n, kNormSpan), 8));
-  MAT_TRY(launch(ctx, false, k_norm, dim3(src.parts, (unsigned)batch), 256, 0, st, src));
-  MAT_TRY(launch(ctx, true, k_split, dim3((unsigned)ceil_div(n, 64), (unsigned)ceil_div(m, 64), (unsigned)batch), 256, 0, st, src, w.x, w.hi[0], w.ld_x, w.stride_x,
+  MAT_TRY(launch(ctx, k_norm, dim3(src.parts, (unsigned)batch), 256, 0, st, src));
+  MAT_TRY(launch(ctx, k_split, dim3((unsigned)ceil_div(n, 64), (unsigned)ceil_div(m, 64), (unsigned)batch), 256, 0, st, src, w.x, w.hi[0], w.ld_x, w.stride_x,
                  w.row_sums, w.slots, w.stride_d, tall ? 1 : 0));
   int cur = 0;
   for (int i = 0; i < steps; ++i) {
@@ -292,21 +289,21 @@ int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, i
     g.a = k[0], g.b = k[1], g.c = k[2];
     g.lanes = g.cols = (int)s, g.depth = (int)l, g.tri = 1;
     g.h = w.gram, g.ld = w.ld_a, g.stride = w.stride_a, g.d_out = w.gram_d;
-    MAT_TRY(gemm<EPI_GRAM>(ctx, true, x, x, g, st));
+    MAT_TRY(gemm<EPI_GRAM>(ctx, x, x, g, st));
     g.depth = (int)s;
     g.o = w.gram, g.d_in = w.gram_d, g.h = w.poly, g.d_out = w.poly_d;
-    MAT_TRY(gemm<EPI_POLY>(ctx, true, gram, gram, g, st));
+    MAT_TRY(gemm<EPI_POLY>(ctx, gram, gram, g, st));
     g.lanes = (int)l, g.tri = 0;
     g.x = w.x, g.ld = w.ld_x, g.stride = w.stride_x, g.d_in = w.poly_d;
     if (i + 1 < steps) {
       g.h = w.hi[cur ^ 1];
-      MAT_TRY(gemm<EPI_APPLY>(ctx, true, x, poly, g, st));
+      MAT_TRY(gemm<EPI_APPLY>(ctx, x, poly, g, st));
       cur ^= 1;
     } else {
       g.out = to.out, g.out_bf16 = to.bf16, g.keep = to.keep, g.rate = to.rate;
       g.out_col = tall ? 1 : to.ld, g.out_lane = tall ? to.ld : 1, g.out_batch = to.stride;
-      if (to.epi == EPI_OUT) MAT_TRY(gemm<EPI_OUT>(ctx, true, x, poly, g, st));
-      else MAT_TRY(gemm<EPI_UPDATE>(ctx, true, x, poly, g, st));
+      if (to.epi == EPI_OUT) MAT_TRY(gemm<EPI_OUT>(ctx, x, poly, g, st));
+      else MAT_TRY(gemm<EPI_UPDATE>(ctx, x, poly, g, st));
     }
   }
   return RTOPK_OK;
@@ -325,10 +322,10 @@ int check_orth(const rtopk_matrix* ctx, int64_t batch, int64_t m, int64_t n, int
 // Rows of up to 1024 elements take a warp each, up to 4096 four warps, longer ones a block: what a row's threads hold in
 // registers is read once.
 template <class T>
-int code_rows(rtopk_matrix* ctx, bool chained, const T* src, int64_t ld, int64_t rows, int64_t cols, const float* mul, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
+int code_rows(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, const float* mul, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
   const int vec = rows_aligned(src, sizeof(T), 1, ld, 0, 16);
   auto go = [&](auto kernel, int warps) {
-    return launch(ctx, chained, kernel, dim3((unsigned)ceil_div(rows, 8 / warps)), 256, 0, st, src, ld, rows, cols, vec, mul, codes, ld_codes, scales);
+    return launch(ctx, kernel, dim3((unsigned)ceil_div(rows, 8 / warps)), 256, 0, st, src, ld, rows, cols, vec, mul, codes, ld_codes, scales);
   };
   if (cols <= 1024) return go(k_code_rows<T, 1>, 1);
   if (cols <= 4096) return go(k_code_rows<T, 4>, 4);
@@ -336,20 +333,21 @@ int code_rows(rtopk_matrix* ctx, bool chained, const T* src, int64_t ld, int64_t
 }
 
 template <class T>
-int code_cols(rtopk_matrix* ctx, bool chained, const T* src, int64_t ld, int64_t rows, int64_t cols, uint32_t* max_bits, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
+int code_cols(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, uint32_t* max_bits, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
   const int vec = rows_aligned(src, sizeof(T), 1, ld, 0, 16);
   const int per = (int)std::max<int64_t>(32, ceil_div(rows, 64));
-  MAT_TRY(launch(ctx, chained, k_col_max<T>, dim3((unsigned)ceil_div(cols, 256), (unsigned)ceil_div(rows, per)), 256, 0, st, src, ld, rows, cols, vec, per, max_bits));
-  return launch(ctx, true, k_code_cols<T>, dim3((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(rows, 128)), 256, 0, st, src, ld, rows, cols, vec, max_bits, codes, ld_codes, scales);
+  MAT_TRY(launch(ctx, k_col_max<T>, dim3((unsigned)ceil_div(cols, 256), (unsigned)ceil_div(rows, per)), 256, 0, st, src, ld, rows, cols, vec, per, max_bits));
+  return launch(ctx, k_code_cols<T>, dim3((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(rows, 128)), 256, 0, st, src, ld, rows, cols, vec, max_bits, codes, ld_codes, scales);
 }
 
-int coded_gemm(rtopk_matrix* ctx, const int8_t* lane_codes, int64_t ld_lane, const float* lane_scale, int64_t lanes, const int8_t* col_codes, int64_t ld_col,
+int coded_gemm(rtopk_matrix* ctx, bool lanes_early, const int8_t* lane_codes, int64_t ld_lane, const float* lane_scale, int64_t lanes, const int8_t* col_codes, int64_t ld_col,
                const float* col_scale, int64_t cols, int64_t depth, void* out, int bf16, int64_t ld_out, cudaStream_t st) {
   Gemm g = {};
   g.lanes = (int)lanes, g.cols = (int)cols, g.depth = (int)depth, g.batch = 1;
   g.out = out, g.out_bf16 = bf16, g.out_col = ld_out, g.out_lane = 1;
   g.scale_col = col_scale, g.scale_lane = lane_scale;
-  return gemm<EPI_CODED>(ctx, true, {lane_codes, depth, lanes, ld_lane, 0}, {col_codes, depth, cols, ld_col, 0}, g, st);
+  g.p_early = lanes_early;
+  return gemm<EPI_CODED>(ctx, {lane_codes, depth, lanes, ld_lane, 0}, {col_codes, depth, cols, ld_col, 0}, g, st);
 }
 
 bool bad_codes(const int8_t* p, int64_t ld, int64_t cols) { return !p || !aligned_to(p, 16) || ld < cols || ld % 16; }
@@ -361,13 +359,29 @@ int check_coded(const rtopk_matrix* ctx, int64_t tokens, int64_t n_out, int64_t 
   return RTOPK_OK;
 }
 
+template <class T, int kTokens>
+int product_few(rtopk_matrix* ctx, const T* x, int64_t ld_x, const int8_t* codes, int64_t ld_codes, const float* scales, int64_t tokens, int64_t n_out, int64_t n_in,
+                T* out, int64_t ld_out, cudaStream_t st) {
+  const int smem = kTokens * few_row((int)n_in);
+  const int64_t fit = std::max<int64_t>(1, std::min<int64_t>(4, kSmemLimit / (smem + 2048)));
+  const int grid = (int)std::min<int64_t>(ceil_div(n_out, 16), ctx->sms * fit);
+  return launch(ctx, k_product_few<T, kTokens>, dim3(grid), kFewThreads, smem, st, x, ld_x, rows_aligned(x, sizeof(T), 1, ld_x, 0, 16) ? 1 : 0, codes, ld_codes, scales, tokens,
+                n_out, n_in, out, ld_out);
+}
+
 template <class T>
 int product(rtopk_matrix* ctx, const T* x, int64_t ld_x, const int8_t* codes, int64_t ld_codes, const float* scales, int64_t tokens, int64_t n_out, int64_t n_in,
             T* out, int64_t ld_out, cudaStream_t st) {
+  if (tokens <= 8 && (tokens <= 1 ? 1 : tokens <= 2 ? 2 : tokens <= 4 ? 4 : 8) * few_row((int)n_in) <= kFewBytes) {
+    if (tokens == 1) return product_few<T, 1>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
+    if (tokens == 2) return product_few<T, 2>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
+    if (tokens <= 4) return product_few<T, 4>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
+    return product_few<T, 8>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
+  }
   Carve c{ctx->scratch};
   CodedScratch w(c, tokens, n_out, n_in);
-  MAT_TRY(code_rows(ctx, false, x, ld_x, tokens, n_in, nullptr, w.x_rows, w.ld_in, w.x_row_s, st));
-  return coded_gemm(ctx, codes, ld_codes, scales, n_out, w.x_rows, w.ld_in, w.x_row_s, tokens, n_in, out, sizeof(T) == 2, ld_out, st);
+  MAT_TRY(code_rows(ctx, x, ld_x, tokens, n_in, nullptr, w.x_rows, w.ld_in, w.x_row_s, st));
+  return coded_gemm(ctx, true, codes, ld_codes, scales, n_out, w.x_rows, w.ld_in, w.x_row_s, tokens, n_in, out, sizeof(T) == 2, ld_out, st);
 }
 
 template <class T>
@@ -376,14 +390,14 @@ int gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, int64_t
   Carve c{ctx->scratch};
   CodedScratch w(c, tokens, n_out, n_in);
   if (dx) {
-    MAT_TRY(code_rows(ctx, false, dy, ld_dy, tokens, n_out, scales, w.dy_rows, w.ld_out, w.dy_row_s, st));
-    MAT_TRY(coded_gemm(ctx, codes_t, ld_t, nullptr, n_in, w.dy_rows, w.ld_out, w.dy_row_s, tokens, n_out, dx, sizeof(T) == 2, ld_dx, st));
+    MAT_TRY(code_rows(ctx, dy, ld_dy, tokens, n_out, scales, w.dy_rows, w.ld_out, w.dy_row_s, st));
+    MAT_TRY(coded_gemm(ctx, true, codes_t, ld_t, nullptr, n_in, w.dy_rows, w.ld_out, w.dy_row_s, tokens, n_out, dx, sizeof(T) == 2, ld_dx, st));
   }
   if (dw) {
     MAT_CUDA(cudaMemsetAsync(w.col_max, 0, (n_in + n_out) * sizeof(uint32_t), st));
-    MAT_TRY(code_cols(ctx, false, x, ld_x, tokens, n_in, w.col_max, w.x_cols, w.ld_tok, w.x_col_s, st));
-    MAT_TRY(code_cols(ctx, true, dy, ld_dy, tokens, n_out, w.col_max + n_in, w.dy_cols, w.ld_tok, w.dy_col_s, st));
-    MAT_TRY(coded_gemm(ctx, w.x_cols, w.ld_tok, w.x_col_s, n_in, w.dy_cols, w.ld_tok, w.dy_col_s, n_out, tokens, dw, dw_dtype == RTOPK_BF16, ld_dw, st));
+    MAT_TRY(code_cols(ctx, x, ld_x, tokens, n_in, w.col_max, w.x_cols, w.ld_tok, w.x_col_s, st));
+    MAT_TRY(code_cols(ctx, dy, ld_dy, tokens, n_out, w.col_max + n_in, w.dy_cols, w.ld_tok, w.dy_col_s, st));
+    MAT_TRY(coded_gemm(ctx, false, w.x_cols, w.ld_tok, w.x_col_s, n_in, w.dy_cols, w.ld_tok, w.dy_col_s, n_out, tokens, dw, dw_dtype == RTOPK_BF16, ld_dw, st));
   }
   return RTOPK_OK;
 }
@@ -505,10 +519,10 @@ int rtopk_code_weights(rtopk_matrix* ctx, const void* weights, int dtype, int64_
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
   cudaStream_t st = (cudaStream_t)stream;
-  if (dtype == RTOPK_F32) MAT_TRY(code_rows(ctx, false, (const float*)weights, ld_w, n_out, n_in, nullptr, codes, ld_codes, scales, st));
-  else MAT_TRY(code_rows(ctx, false, (const __nv_bfloat16*)weights, ld_w, n_out, n_in, nullptr, codes, ld_codes, scales, st));
+  if (dtype == RTOPK_F32) MAT_TRY(code_rows(ctx, (const float*)weights, ld_w, n_out, n_in, nullptr, codes, ld_codes, scales, st));
+  else MAT_TRY(code_rows(ctx, (const __nv_bfloat16*)weights, ld_w, n_out, n_in, nullptr, codes, ld_codes, scales, st));
   if (codes_t)
-    MAT_TRY(launch(ctx, true, k_codes_transpose, dim3((unsigned)ceil_div(n_in, 64), (unsigned)ceil_div(n_out, 64)), 256, 0, st, codes, ld_codes, n_out, n_in, codes_t, ld_t));
+    MAT_TRY(launch(ctx, k_codes_transpose, dim3((unsigned)ceil_div(n_in, 64), (unsigned)ceil_div(n_out, 64)), 256, 0, st, codes, ld_codes, n_out, n_in, codes_t, ld_t));
   return RTOPK_OK;
 }
 

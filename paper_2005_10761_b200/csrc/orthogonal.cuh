@@ -53,6 +53,7 @@ constexpr int kNormSpan = 1024;
 __global__ void __launch_bounds__(256) k_norm(const __grid_constant__ Source s) {
   __shared__ double part[8];
   const int z = blockIdx.y, lane = threadIdx.x & 31;
+  launch_wait();
   launch_next();
   const int pieces = (s.n + kNormSpan - 1) / kNormSpan;
   const int64_t units = (int64_t)s.m * pieces;
@@ -198,6 +199,8 @@ __global__ void __launch_bounds__(256) k_orth_small(const __grid_constant__ Sour
   float* g = x + rows * kSmall;                   // [64][64]
   float* b = g + kSmall * kSmall;
   for (int i = t; i < rows * kSmall; i += 256) x[i] = 0.f;
+  launch_wait();
+  launch_next();
   __syncthreads();
   double sum = 0.0;
   for (int k = t; k < s.m * s.n; k += 256) {

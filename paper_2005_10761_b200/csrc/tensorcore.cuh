@@ -176,8 +176,10 @@ __host__ __device__ constexpr uint32_t instr_desc(bool int8, bool a_mn_major, ui
 }
 
 // ----------------------------------------------------------------------------- launch order
-// A kernel launched with the programmatic attribute may start while its predecessor still runs; nothing of the
-// predecessor's output may be read, and nothing it reads may be written, before launch_wait().
+// Every kernel here is launched with the programmatic attribute: it may start while its predecessor in the stream still runs,
+// as soon as all of that one's blocks have called launch_next() or ended.  Nothing of the predecessor's output may be read, and
+// nothing it reads may be written, before launch_wait(), which returns when the predecessor is complete.  Every kernel calls
+// launch_next() after its own launch_wait(), so all that came before the predecessor is complete from the start.
 __device__ __forceinline__ void launch_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
