@@ -252,16 +252,13 @@ struct Target {
   float keep, rate;
 };
 
-int small_smem(int64_t l) { return (int)((up(l, 8) + 2 * kSmall) * kSmall * sizeof(float)); }
-constexpr int64_t kSmallLong = 256;      // X, its Gram matrix and the polynomial: 96 KB of shared memory
-
 int orthogonal_small(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, int64_t m, int64_t n, int steps, const float* coef, cudaStream_t st) {
   src.m = (int)m, src.n = (int)n;
   SmallOut o = {};
   o.w = to.epi == EPI_UPDATE ? (float*)to.out : nullptr;
   o.out = to.out, o.bf16 = to.bf16, o.ld = to.ld, o.stride = to.stride, o.keep = to.keep, o.rate = to.rate, o.steps = steps;
   for (int i = 0; i < 3 * steps; ++i) o.coef[i] = coef ? coef[i] : kQuintic[i % 3];
-  return launch(ctx, k_orth_small, dim3((unsigned)batch), 256, small_smem(std::max(m, n)), st, src, o, m > n ? 1 : 0);
+  return launch(ctx, k_orth_small, dim3((unsigned)batch), kSmallThreads, small_bytes((int)std::max(m, n)), st, src, o, m > n ? 1 : 0);
 }
 
 int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, int64_t m, int64_t n, int steps, const float* coef, cudaStream_t st) {
@@ -422,7 +419,7 @@ int rtopk_matrix_create(rtopk_matrix** out, int device, int64_t scratch_bytes) {
                              found != cudaDriverEntryPointSuccess || cudaDeviceGetAttribute(&ctx->sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
                              allow_smem<EPI_GRAM>() != cudaSuccess || allow_smem<EPI_POLY>() != cudaSuccess || allow_smem<EPI_APPLY>() != cudaSuccess ||
                              allow_smem<EPI_OUT>() != cudaSuccess || allow_smem<EPI_UPDATE>() != cudaSuccess || allow_smem<EPI_CODED>() != cudaSuccess ||
-                             cudaFuncSetAttribute(k_orth_small, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(kSmallLong)) != cudaSuccess))
+                             cudaFuncSetAttribute(k_orth_small, cudaFuncAttributeMaxDynamicSharedMemorySize, small_bytes(kSmallLong)) != cudaSuccess))
     status = RTOPK_ERR_CUDA;
   ctx->encode = (EncodeTiled)fn;
   if (status == RTOPK_OK && (cudaMalloc(&ctx->error, kErrorBytes + ctx->sms * kPartBytes + scratch_bytes) != cudaSuccess ||

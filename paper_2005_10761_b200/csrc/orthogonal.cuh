@@ -161,10 +161,16 @@ k_split(const __grid_constant__ Source s, float* x, __half* h, int64_t ld, int64
   }
 }
 
-// Small matrices (the shorter side at most kSmall): the whole operator in one block per matrix, everything in shared memory
-// and binary32.  A chain of launches would spend its time starting them: at 64 x 64 a step's three products are
-// 1.6 million operations.  X is held transposed, [long][64], so that all products read rows of 64.
-constexpr int kSmall = 64;
+// Small matrices (the shorter side at most 64, the longer at most 256): the whole operator in one block per matrix, everything in
+// shared memory.  A chain of launches would spend its time starting them: at 64 x 64 a step's three products are 1.6 million
+// operations.  What bounds this kernel is the chain of dependent products inside one SM, so they are mma.sync products of the
+// block's sixteen warps, 16 x 16 entries each, with no trip through tensor memory between them.  Every factor is the sum of two
+// 16-bit numbers, high and low, and three of the four partial products are formed: 2^-21 of the result is lost, so
+// that a matrix too small for errors to average out is as exact as a large one.
+constexpr int kSmall = 64, kSmallLong = 256, kSmallThreads = 512;
+constexpr int kSmallKeep = kSmall * kSmallLong / kSmallThreads;      // elements of U in a thread's registers
+constexpr int kSmallLd = kSmall + 8;
+constexpr float kSmallScale = 32.f;                                  // of X, its Gram matrix and the polynomial
 
 struct SmallOut {
   float* w;                // update: the weights; null: out
@@ -176,107 +182,155 @@ struct SmallOut {
   int steps;
 };
 
-// acc[i][j] += sum_k p[k][i0 + i] q[k][j0 + j], rows of kSmall floats
-__device__ __forceinline__ void small_product(const float* p, const float* q, int depth, int i0, int j0, float (&acc)[4][4]) {
-#pragma unroll 4
-  for (int k = 0; k < depth; ++k) {
-    const float4 a = *(const float4*)(p + k * kSmall + i0), b = *(const float4*)(q + k * kSmall + j0);
-    const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(av[i], bv[j], acc[i][j]);
-  }
+__host__ __device__ constexpr int small_ld(int nl) { return (nl + 63) / 64 * 64 + 8; }      // rows 16 bytes off a multiple of 128
+__host__ __device__ constexpr int small_bytes(int nl) { return 2 * 2 * kSmall * (small_ld(nl) + 2 * kSmallLd); }
+
+struct Halves { __half *hi, *lo; int ld; };
+
+__device__ __forceinline__ void ld_matrix(uint32_t (&r)[4], const __half* p) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(smem_addr(p)) : "memory");
+}
+__device__ __forceinline__ void ld_matrix_trans(uint32_t (&r)[4], const __half* p) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(smem_addr(p)) : "memory");
+}
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-__global__ void __launch_bounds__(256) k_orth_small(const __grid_constant__ Source s, const __grid_constant__ SmallOut to, int transpose) {
-  extern __shared__ float small_smem[];
-  __shared__ double part[8];
-  const int z = blockIdx.x, t = threadIdx.x;
-  const int ns = transpose ? s.n : s.m, nl = transpose ? s.m : s.n;
-  const int rows = (nl + 7) & ~7;             // both halves of a warp have rows to work on, or neither
-  float* x = small_smem;                          // [rows][64]
-  float* g = x + rows * kSmall;                   // [64][64]
-  float* b = g + kSmall * kSmall;
-  for (int i = t; i < rows * kSmall; i += 256) x[i] = 0.f;
+// acc = the warp's 16 x 16 entries, rows i0 .. and columns j0 .., of P Q^T (rows of both along the contraction index), or with
+// kTrans of P Q (Q's rows are the contraction index).
+template <bool kTrans>
+__device__ __forceinline__ void small_product(const Halves& p, const Halves& q, int depth, int i0, int j0, float (&acc)[2][4]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
+  const int at_p = (i0 + (lane & 15)) * p.ld + (lane >> 4) * 8;
+  const int at_q = kTrans ? (lane & 15) * q.ld + j0 + (lane >> 4) * 8 : (j0 + (lane & 7) + (lane >> 4) * 8) * q.ld + ((lane >> 3) & 1) * 8;
+  const int step_q = kTrans ? 16 * q.ld : 16;
+#pragma unroll 4
+  for (int k = 0; k < depth; k += 16) {
+    uint32_t ph[4], pl[4], qh[4], ql[4];
+    ld_matrix(ph, p.hi + at_p + k);
+    ld_matrix(pl, p.lo + at_p + k);
+    const int iq = at_q + k / 16 * step_q;
+    if (kTrans) {
+      ld_matrix_trans(qh, q.hi + iq);
+      ld_matrix_trans(ql, q.lo + iq);
+    } else {
+      ld_matrix(qh, q.hi + iq);
+      ld_matrix(ql, q.lo + iq);
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      mma_16x8x16(acc[n], pl, qh[2 * n], qh[2 * n + 1]);
+      mma_16x8x16(acc[n], ph, ql[2 * n], ql[2 * n + 1]);
+      mma_16x8x16(acc[n], ph, qh[2 * n], qh[2 * n + 1]);
+    }
+  }
+}
+__device__ __forceinline__ void small_split(float a, float b, __half2& hi, __half2& lo) {
+  hi = __floats2half2_rn(a, b);
+  const float2 h = __half22float2(hi);
+  lo = __floats2half2_rn(a - h.x, b - h.y);
+}
+// Entries (row, col) and (row, col + 1).
+__device__ __forceinline__ void small_store(const Halves& m, int row, int col, float a, float b) {
+  __half2 hi, lo;
+  small_split(a, b, hi, lo);
+  *(__half2*)(m.hi + row * m.ld + col) = hi;
+  *(__half2*)(m.lo + row * m.ld + col) = lo;
+}
+__device__ __forceinline__ float2 small_load(const Halves& m, int row, int col) {
+  const float2 h = __half22float2(*(const __half2*)(m.hi + row * m.ld + col)), l = __half22float2(*(const __half2*)(m.lo + row * m.ld + col));
+  return make_float2(h.x + l.x, h.y + l.y);
+}
+
+__global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_constant__ Source s, const __grid_constant__ SmallOut to, int transpose) {
+  extern __shared__ __align__(16) __half small_smem[];
+  __shared__ double part[kSmallThreads / 32];
+  const int z = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int ns = transpose ? s.n : s.m, nl = transpose ? s.m : s.n, ld = small_ld(nl), count = s.m * s.n;
+  const int chunks = (nl + 63) / 64, ks = (ns + 15) / 16 * 16, kl = (nl + 15) / 16 * 16;
+  const Halves x = {small_smem, small_smem + kSmall * ld, ld};
+  const Halves g = {x.lo + kSmall * ld, x.lo + kSmall * (ld + kSmallLd), kSmallLd};
+  const Halves b = {g.lo + kSmall * kSmallLd, g.lo + 2 * kSmall * kSmallLd, kSmallLd};
+  for (int i = t; i < kSmall * ld; i += kSmallThreads) *((uint32_t*)x.hi + i) = 0u;      // both halves
   launch_wait();
   launch_next();
-  __syncthreads();
+  float u[kSmallKeep];
   double sum = 0.0;
-  for (int k = t; k < s.m * s.n; k += 256) {
+#pragma unroll
+  for (int i = 0; i < kSmallKeep; ++i) {
+    const int k = t + i * kSmallThreads;
+    u[i] = 0.f;
+    if (k >= count) continue;
     const int r = k / s.n, c = k - r * s.n;
-    float u = source_at(s, z * s.stride + r * s.ld + c);
+    u[i] = source_at(s, z * s.stride + r * s.ld + c);
     if (s.v) {
       float* v = s.v + z * s.v_stride + r * s.v_ld + c;
-      const float nv = fmaf(s.mu, *v, u);
+      const float nv = fmaf(s.mu, *v, u[i]);
       *v = nv;
-      u = update_of(s, u, nv);
+      u[i] = update_of(s, u[i], nv);
     }
-    sum += (double)u * (double)u;
-    x[transpose ? r * kSmall + c : c * kSmall + r] = u;
+    sum += (double)u[i] * (double)u[i];
   }
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-  if ((t & 31) == 0) part[t >> 5] = sum;
+  if (lane == 0) part[warp] = sum;
   __syncthreads();
   sum = 0.0;
-  for (int i = 0; i < 8; ++i) sum += part[i];
-  const float inv = sum == 0.0 ? 0.f : (float)(1.0 / (sqrt(sum) + (double)s.eps));
-  for (int i = t; i < rows * kSmall; i += 256) x[i] *= inv;
+  for (int i = 0; i < kSmallThreads / 32; ++i) sum += part[i];
+  const float inv = sum == 0.0 ? 0.f : (float)((double)kSmallScale / (sqrt(sum) + (double)s.eps));
+#pragma unroll
+  for (int i = 0; i < kSmallKeep; ++i) {
+    const int k = t + i * kSmallThreads;
+    if (k >= count) continue;
+    const int r = k / s.n, c = k - r * s.n, at = transpose ? c * ld + r : r * ld + c;
+    const float v = u[i] * inv;
+    const __half h = to_half(v);
+    x.hi[at] = h;
+    x.lo[at] = to_half(v - __half2float(h));
+  }
   __syncthreads();
-  const int i0 = (t & 15) * 4, j0 = (t >> 4) * 4;
+  const int i0 = (warp & 3) * 16, j0 = (warp >> 2) * 16;
+  const int row = i0 + lane / 4, col = j0 + (lane & 3) * 2;      // of acc[n][0]: column + 8 n; acc[n][2]: row + 8
+  float acc[2][4];
   for (int step = 0; step < to.steps; ++step) {
-    const float ca = to.coef[3 * step], cb = to.coef[3 * step + 1], cc = to.coef[3 * step + 2];
-    {
-      float acc[4][4] = {};
-      small_product(x, x, nl, i0, j0, acc);
+    const float ca = to.coef[3 * step] * kSmallScale, cb = to.coef[3 * step + 1], cc = to.coef[3 * step + 2] * (1.f / kSmallScale);
+    small_product<false>(x, x, kl, i0, j0, acc);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) *(float4*)(g + (j0 + j) * kSmall + i0) = make_float4(acc[0][j], acc[1][j], acc[2][j], acc[3][j]);
-    }
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        small_store(g, row + 8 * h, col + 8 * n, acc[n][2 * h] * (1.f / kSmallScale), acc[n][2 * h + 1] * (1.f / kSmallScale));
     __syncthreads();
-    {
-      float acc[4][4] = {};
-      small_product(g, g, ns, i0, j0, acc);
+    small_product<false>(g, g, ks, i0, j0, acc);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float4 a = *(const float4*)(g + (j0 + j) * kSmall + i0);
-        const float av[4] = {a.x, a.y, a.z, a.w};
-        float v[4];
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = cc * acc[i][j] + cb * av[i] + (i0 + i == j0 + j ? ca : 0.f);
-        *(float4*)(b + (j0 + j) * kSmall + i0) = make_float4(v[0], v[1], v[2], v[3]);
+      for (int h = 0; h < 2; ++h) {
+        const int r = row + 8 * h, c = col + 8 * n;
+        const float2 a = small_load(g, r, c);
+        small_store(b, r, c, cc * acc[n][2 * h] + cb * a.x + (r == c ? ca : 0.f), cc * acc[n][2 * h + 1] + cb * a.y + (r == c + 1 ? ca : 0.f));
       }
-    }
     __syncthreads();
-    // a thread's four rows of X are read by its whole group of 16 before they are written: the rows of one group belong to
-    // one half of a warp
-    for (int r0 = (t >> 4) * 4; r0 < rows; r0 += 64) {
-      float acc[4][4] = {};
-      for (int k = 0; k < ns; k += 4) {
-        float4 xr[4];
+    for (int k = 0; k < chunks; ++k) {
+      small_product<true>(b, x, ks, i0, k * 64 + j0, acc);
+      __syncthreads();      // these 64 columns of X have been read
 #pragma unroll
-        for (int j = 0; j < 4; ++j) xr[j] = *(const float4*)(x + (r0 + j) * kSmall + k);
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          const float4 p = *(const float4*)(b + (k + kk) * kSmall + i0);
-          const float pv[4] = {p.x, p.y, p.z, p.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float xv = kk == 0 ? xr[j].x : kk == 1 ? xr[j].y : kk == 2 ? xr[j].z : xr[j].w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i][j] = fmaf(pv[i], xv, acc[i][j]);
-          }
-        }
-      }
-      __syncwarp();
-#pragma unroll
-      for (int j = 0; j < 4; ++j) *(float4*)(x + (r0 + j) * kSmall + i0) = make_float4(acc[0][j], acc[1][j], acc[2][j], acc[3][j]);
-      __syncwarp();
+        for (int h = 0; h < 2; ++h)
+          small_store(x, row + 8 * h, k * 64 + col + 8 * n, acc[n][2 * h] * (1.f / kSmallScale), acc[n][2 * h + 1] * (1.f / kSmallScale));
     }
     __syncthreads();
   }
-  for (int k = t; k < s.m * s.n; k += 256) {
-    const int r = k / s.n, c = k - r * s.n;
-    const float v = x[transpose ? r * kSmall + c : c * kSmall + r];
+  for (int k = t; k < count; k += kSmallThreads) {
+    const int r = k / s.n, c = k - r * s.n, from = transpose ? c * ld + r : r * ld + c;
+    const float v = (__half2float(x.hi[from]) + __half2float(x.lo[from])) * (1.f / kSmallScale);
     const int64_t at = z * to.stride + r * to.ld + c;
     if (to.w) to.w[at] = to.keep * to.w[at] - to.rate * v;
     else if (to.bf16) ((__nv_bfloat16*)to.out)[at] = __float2bfloat16_rn(v);

@@ -7,7 +7,9 @@ from typing import Optional, Sequence
 
 import torch
 
-from .binding import GRAD_BF16, GRAD_F32, RTopKError, _i64, _stream, _vp, load_library
+from .binding import GRAD_BF16, GRAD_F32, RTopKError, _i64, _vp, load_library
+
+_DTYPES = {torch.float32: GRAD_F32, torch.bfloat16: GRAD_BF16}
 
 
 def _scratch(what: str, *sizes: int) -> int:
@@ -29,11 +31,10 @@ def coded_scratch(tokens: int, n_out: int, n_in: int) -> int:
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:
-    if t.dtype == torch.float32:
-        return GRAD_F32
-    if t.dtype == torch.bfloat16:
-        return GRAD_BF16
-    raise TypeError(f"{what} must be float32 or bfloat16")
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be float32 or bfloat16")
+    return code
 
 
 class CodedWeights:
@@ -47,6 +48,10 @@ class CodedWeights:
         self.codes = torch.zeros((n_out, -(-n_in // 128) * 128), dtype=torch.int8, device=device)
         self.codes_t = torch.zeros((n_in, -(-n_out // 128) * 128), dtype=torch.int8, device=device) if transposed else None
         self.scales = torch.zeros(n_out, dtype=torch.float32, device=device)
+        # (pointer, row stride) of both arrays and the scales' pointer, as the calls take them
+        self._codes = (self.codes.data_ptr(), self.codes.stride(0))
+        self._codes_t = (self.codes_t.data_ptr(), self.codes_t.stride(0)) if transposed else (None, 0)
+        self._scales = self.scales.data_ptr()
 
     def dense(self) -> torch.Tensor:
         """The values that the codes stand for."""
@@ -68,6 +73,10 @@ class MatrixContext:
         if rc != 0:
             raise RTopKError(rc, "rtopk_matrix_create", self._lib.rtopk_status_string(rc).decode())
         self._h = h
+        self._raw_stream = torch._C._cuda_getCurrentRawStream      # the handle alone: a Stream object takes microseconds
+
+    def _stream(self) -> int:
+        return self._raw_stream(self.device)
 
     def close(self) -> None:
         if getattr(self, "_h", None):
@@ -90,11 +99,12 @@ class MatrixContext:
     @staticmethod
     def _rows(t: torch.Tensor, what: str, shape=None):
         """(pointer, row stride) of a matrix with contiguous rows."""
-        if shape is not None and tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
+        sizes, strides = t.shape, t.stride()
+        if shape is not None and sizes != shape:
+            raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(sizes)}")
+        if strides[-1] != 1 and sizes[-1] > 1:
             raise ValueError(f"the rows of {what} must be contiguous")
-        return t.data_ptr(), (t.stride(-2) if t.shape[-2] > 1 else t.shape[-1])
+        return t.data_ptr(), (strides[-2] if sizes[-2] > 1 else sizes[-1])
 
     @classmethod
     def _batch(cls, t: torch.Tensor, what: str, shape=None):
@@ -122,7 +132,7 @@ class MatrixContext:
         p, ld, stride = self._batch(src, "src")
         po, ldo, strideo = self._batch(out, "out", src.shape)
         rc = self._lib.rtopk_orthogonalize(self._h, p, _dtype(src, "src"), ld, stride, po, _dtype(out, "out"), ldo, strideo,
-                                           *self._sizes(src), steps, self._coef(coef, steps), eps, _stream())
+                                           *self._sizes(src), steps, self._coef(coef, steps), eps, self._stream())
         self._check(rc, "rtopk_orthogonalize")
 
     def orthogonal_update(self, grad, momentum, weights, eta, mu, nesterov=True, decay=0.0, scale=1.0, steps=5, coef=None,
@@ -136,27 +146,26 @@ class MatrixContext:
         w, ldw, sw = self._batch(weights, "weights", grad.shape)
         rc = self._lib.rtopk_orthogonal_update(self._h, g, ldg, sg, v, ldv, sv, w, ldw, sw, *self._sizes(grad), eta, mu,
                                                1 if nesterov else 0, decay, scale, steps, self._coef(coef, steps), eps,
-                                               _stream())
+                                               self._stream())
         self._check(rc, "rtopk_orthogonal_update")
 
     def code_weights(self, weights, coded: CodedWeights) -> None:
         """coded <- the codes of weights ([n_out, n_in], float32 or bfloat16), one scale for each row."""
         p, ld = self._rows(weights, "weights", (coded.n_out, coded.n_in))
-        t = coded.codes_t
-        rc = self._lib.rtopk_code_weights(self._h, p, _dtype(weights, "weights"), ld, coded.n_out, coded.n_in,
-                                          coded.codes.data_ptr(), coded.codes.stride(0), t.data_ptr() if t is not None else None,
-                                          t.stride(0) if t is not None else 0, coded.scales.data_ptr(), _stream())
+        rc = self._lib.rtopk_code_weights(self._h, p, _dtype(weights, "weights"), ld, coded.n_out, coded.n_in, *coded._codes,
+                                          *coded._codes_t, coded._scales, self._stream())
         self._check(rc, "rtopk_code_weights")
 
     def coded_product(self, x, coded: CodedWeights, out) -> None:
         """out[t, n] <- x W^T with W as codes and x ([tokens, n_in], float32 or bfloat16) coded for each token."""
-        p, ld = self._rows(x, "x", (x.shape[0], coded.n_in))
-        po, ldo = self._rows(out, "out", (x.shape[0], coded.n_out))
-        dt = _dtype(x, "x")
+        tokens, n_in, n_out = x.shape[0], coded.n_in, coded.n_out
+        p, ld = self._rows(x, "x", (tokens, n_in))
+        po, ldo = self._rows(out, "out", (tokens, n_out))
         if out.dtype != x.dtype:
             raise TypeError("out must have the type of x")
-        rc = self._lib.rtopk_coded_product(self._h, p, dt, ld, coded.codes.data_ptr(), coded.codes.stride(0),
-                                           coded.scales.data_ptr(), x.shape[0], coded.n_out, coded.n_in, po, ldo, _stream())
+        codes, ld_codes = coded._codes
+        rc = self._lib.rtopk_coded_product(self._h, p, _dtype(x, "x"), ld, codes, ld_codes, coded._scales, tokens, n_out, n_in,
+                                           po, ldo, self._stream())
         self._check(rc, "rtopk_coded_product")
 
     def coded_gradients(self, dy, x, coded: CodedWeights, dx=None, dw=None) -> None:
@@ -179,14 +188,12 @@ class MatrixContext:
                 raise TypeError("dx must have the type of dy")
             if coded.codes_t is None:
                 raise ValueError("these weights were made without their transposed codes")
-        t = coded.codes_t
-        rc = self._lib.rtopk_coded_gradients(self._h, py, ldy, px, ldx, dt, t.data_ptr() if t is not None else None,
-                                             t.stride(0) if t is not None else 0, coded.scales.data_ptr(), tokens, coded.n_out,
-                                             coded.n_in, pdx, lddx, pdw, wt, lddw, _stream())
+        rc = self._lib.rtopk_coded_gradients(self._h, py, ldy, px, ldx, dt, *coded._codes_t, coded._scales, tokens, coded.n_out,
+                                             coded.n_in, pdx, lddx, pdw, wt, lddw, self._stream())
         self._check(rc, "rtopk_coded_gradients")
 
     def poll_status(self) -> None:
-        self._check(self._lib.rtopk_matrix_poll_status(self._h, _stream()), "rtopk_matrix_poll_status")
+        self._check(self._lib.rtopk_matrix_poll_status(self._h, self._stream()), "rtopk_matrix_poll_status")
 
     def launch_count(self) -> int:
         n = C.c_uint64(0)
