@@ -17,6 +17,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "tensorcore.cuh"
 
 namespace rtopk {
@@ -140,28 +142,47 @@ __device__ __forceinline__ void store_strip(T* p, int n, int64_t step, F value) 
   }
 }
 
+// What the results of 32 columns need beside the products.  Read ahead: for a tile's first columns while its products are
+// still being formed, then for the next columns while the present ones are finished.
+template <int kEpi>
+struct Ahead {
+  typename std::conditional<kEpi == EPI_POLY, __half, float>::type at[kEpi == EPI_POLY || kEpi == EPI_APPLY || kEpi == EPI_OUT || kEpi == EPI_UPDATE ? 32 : 1];
+  float col;             // of column `threadIdx & 31`: its entry of the diagonal, or its scale
+};
+
+template <int kEpi, bool kFull>
+__device__ __forceinline__ void read_ahead(const Gemm& g, int z, int lane, int col0, int n, Ahead<kEpi>& ahead) {
+  const int me = threadIdx.x & 31;
+  const int safe = kFull ? lane : min(lane, g.lanes - 1), my_col = col0 + (kFull ? me : min(me, n - 1));
+  if constexpr (kEpi == EPI_POLY) {
+    if (col0 / kLanes < lane / kLanes) return;
+    load_strip<kFull>(g.o + z * g.stride + col0 * g.ld + safe, n, g.ld, ahead.at);
+  } else if constexpr (kEpi == EPI_APPLY || kEpi == EPI_OUT || kEpi == EPI_UPDATE) {
+    load_strip<kFull>((const float*)g.x + z * g.stride + col0 * g.ld + safe, n, g.ld, ahead.at);
+  }
+  if constexpr (kEpi == EPI_CODED) ahead.col = g.scale_col[my_col];
+  else if constexpr (kEpi != EPI_GRAM) ahead.col = g.d_in[z * g.d_stride + my_col];
+}
+
 // 32 columns (col0 ..) of lane `lane` of one tile; all 32 threads of the warp come here, each with its lane.  kFull: the
 // warp's lanes and columns all exist.  `n` of the columns do; loads of lanes that do not read a neighbour's values.
+// `of_lane`: the lane's entry of the diagonal (GRAM: of the result's), or its scale.
 template <int kEpi, bool kFull>
-__device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col0, int n, float diag, const uint32_t (&acc)[32]) {
+__device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col0, int n, float of_lane, const Ahead<kEpi>& ahead, const uint32_t (&acc)[32]) {
   const int me = threadIdx.x & 31;
   bool in = kFull || lane < g.lanes;
-  const int safe = kFull ? lane : min(lane, g.lanes - 1), my_col = col0 + (kFull ? me : min(me, n - 1));
   float v[32];
   if constexpr (kEpi == EPI_GRAM || kEpi == EPI_POLY) {
     // Symmetric result: a 128-wide block of columns left of this lane's block is the mirror image of another tile.
     const int lb = lane / kLanes, cb = col0 / kLanes;
     if (cb < lb) return;
-    const float* d_in = g.d_in + z * g.d_stride;
     if constexpr (kEpi == EPI_GRAM) {
 #pragma unroll
       for (int c = 0; c < 32; ++c) v[c] = __uint_as_float(acc[c]);
     } else {
-      __half o[32];
-      load_strip<kFull>(g.o + z * g.stride + (int64_t)col0 * g.ld + safe, n, g.ld, o);
-      const float dl = g.b + g.c * d_in[safe], dc = g.c * d_in[my_col], scale = g.c * (1.f / kAScale);
+      const float dl = g.b + g.c * of_lane, dc = g.c * ahead.col, scale = g.c * (1.f / kAScale);
 #pragma unroll
-      for (int c = 0; c < 32; ++c) v[c] = scale * __uint_as_float(acc[c]) + (dl + __shfl_sync(0xFFFFFFFFu, dc, c)) * __half2float(o[c]);
+      for (int c = 0; c < 32; ++c) v[c] = scale * __uint_as_float(acc[c]) + (dl + __shfl_sync(0xFFFFFFFFu, dc, c)) * __half2float(ahead.at[c]);
     }
     if (cb == lb && in && lane >= col0 && lane < col0 + n) {
       float q = 0.f;
@@ -171,11 +192,7 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
           q = __uint_as_float(acc[c]) * (1.f / kAScale);
           v[c] = 0.f;
         }
-      if (kEpi == EPI_POLY) {
-        const float x = d_in[lane];
-        diag = g.a + g.b * x + g.c * (x * x + q * (1.f / kAScale));
-      }
-      g.d_out[z * g.d_stride + lane] = diag;
+      g.d_out[z * g.d_stride + lane] = kEpi == EPI_GRAM ? of_lane : g.a + g.b * of_lane + g.c * (of_lane * of_lane + q * (1.f / kAScale));
     }
     if (!in) return;
     // row `lane`, columns col0 ..: the row stride is a multiple of 8, so the padding takes whole vectors
@@ -185,9 +202,8 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
       if (kFull || c < n) store_half8(row + c, v + c);
     if (cb > lb) store_strip<kFull>(g.h + z * g.stride + col0 * g.ld + lane, n, g.ld, [&](int c) { return to_half(v[c]); });
   } else if constexpr (kEpi == EPI_CODED) {
-    const float sl = g.scale_lane ? g.scale_lane[safe] : 1.f, sc = g.scale_col[my_col];
 #pragma unroll
-    for (int c = 0; c < 32; ++c) v[c] = (float)(int)acc[c] * __shfl_sync(0xFFFFFFFFu, sc, c) * sl;
+    for (int c = 0; c < 32; ++c) v[c] = (float)(int)acc[c] * __shfl_sync(0xFFFFFFFFu, ahead.col, c) * of_lane;
     if (!in) return;
     const int64_t at = lane + col0 * g.out_col;
     if (g.out_bf16) store_strip<kFull>((__nv_bfloat16*)g.out + at, n, g.out_col, [&](int c) { return __float2bfloat16_rn(v[c]); });
@@ -195,10 +211,8 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
   } else {
     // X' = diag X + offdiag X: the product carries only the part off the diagonal, times kAScale * kXScale
     float* x = g.x + z * g.stride + col0 * g.ld;
-    load_strip<kFull>(x + safe, n, g.ld, v);
-    const float dc = g.d_in[z * g.d_stride + my_col];
 #pragma unroll
-    for (int c = 0; c < 32; ++c) v[c] = __shfl_sync(0xFFFFFFFFu, dc, c) * v[c] + __uint_as_float(acc[c]) * (1.f / kAScale);
+    for (int c = 0; c < 32; ++c) v[c] = __shfl_sync(0xFFFFFFFFu, ahead.col, c) * ahead.at[c] + __uint_as_float(acc[c]) * (1.f / kAScale);
     if constexpr (kEpi == EPI_APPLY) {
       if (in) {
         store_strip<kFull>(x + lane, n, g.ld, [&](int c) { return v[c]; });
@@ -389,24 +403,41 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       const Tile q = tile_at<kCols, S::kTileLanes>(g, u);
       const int in_tile = quarter * 32 + lane;
       const int row0 = q.l * S::kTileLanes + rank * kLanes, row = row0 + in_tile;
-      float diag = 0.f;
-      if (kEpi == EPI_GRAM && q.c * kCols < row0 + kLanes && row0 < (q.c + 1) * kCols) diag = gram_diagonal(g, q.z, row);
+      constexpr int kNext = 32 * (kEpiWarps / 4);
+      const int cols = min(kCols, g.cols - q.c * kCols);
+      const bool lanes_full = row0 + kLanes <= g.lanes;
+      float of_lane = 1.f;
+      if (kEpi == EPI_GRAM) {
+        if (q.c * kCols < row0 + kLanes && row0 < (q.c + 1) * kCols) of_lane = gram_diagonal(g, q.z, row);
+      } else if (kEpi == EPI_POLY) {
+        of_lane = g.d_in[q.z * g.d_stride + min(row, g.lanes - 1)];
+      } else if (kEpi == EPI_CODED) {
+        if (g.scale_lane) of_lane = g.scale_lane[min(row, g.lanes - 1)];
+      }
+      auto read = [&](int c, Ahead<kEpi>& ahead) {
+        if (c >= cols) return;
+        if (lanes_full && c + 32 <= cols) read_ahead<kEpi, true>(g, q.z, row, q.c * kCols + c, 32, ahead);
+        else read_ahead<kEpi, false>(g, q.z, row, q.c * kCols + c, min(32, cols - c), ahead);
+      };
+      auto finish = [&](int c, const Ahead<kEpi>& ahead, const uint32_t(&acc)[32]) {
+        if (lanes_full && c + 32 <= cols) epilogue<kEpi, true>(g, q.z, row, q.c * kCols + c, 32, of_lane, ahead, acc);
+        else epilogue<kEpi, false>(g, q.z, row, q.c * kCols + c, min(32, cols - c), of_lane, ahead, acc);
+        __syncwarp();
+      };
+      Ahead<kEpi> ahead;
+      read(chunk0, ahead);
       if (!__all_sync(0xFFFFFFFFu, bar_wait(tm_full + 8 * b, (n / 2) & 1, give))) break;
       tc_fence_after();
       const uint32_t from = tmem + b * kCols + ((uint32_t)(quarter * 32) << 16);
-      const int cols = min(kCols, g.cols - q.c * kCols);
-      const bool lanes_full = row0 + kLanes <= g.lanes;
-      auto finish = [&](int c, const uint32_t(&acc)[32]) {
-        if (lanes_full && c + 32 <= cols) epilogue<kEpi, true>(g, q.z, row, q.c * kCols + c, 32, diag, acc);
-        else epilogue<kEpi, false>(g, q.z, row, q.c * kCols + c, min(32, cols - c), diag, acc);
-        __syncwarp();
-      };
       if (g.split == 1) {
 #pragma unroll 1
-        for (int c = chunk0; c < cols; c += 32 * (kEpiWarps / 4)) {
+        for (int c = chunk0; c < cols; c += kNext) {
           uint32_t acc[32];
           tmem_load32(from + c, acc);
-          finish(c, acc);
+          Ahead<kEpi> next;
+          read(c + kNext, next);
+          finish(c, ahead, acc);
+          ahead = next;
         }
         tc_fence_before();
         __syncwarp();
@@ -419,7 +450,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       const int64_t part_words = (int64_t)kCols * S::kTileLanes;
       uint32_t* mine = g.parts + u * part_words + rank * kLanes + in_tile;
 #pragma unroll 1
-      for (int c = chunk0; c < cols; c += 32 * (kEpiWarps / 4)) {
+      for (int c = chunk0; c < cols; c += kNext) {
         uint32_t acc[32];
         tmem_load32(from + c, acc);
 #pragma unroll
@@ -445,7 +476,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       __threadfence();
       const uint32_t* parts = g.parts + (u - q.part) * part_words + rank * kLanes + in_tile;
 #pragma unroll 1
-      for (int c = chunk0; c < cols; c += 32 * (kEpiWarps / 4)) {
+      for (int c = chunk0; c < cols; c += kNext) {
         uint32_t acc[32];
 #pragma unroll
         for (int i = 0; i < 32; ++i) acc[i] = __ldcg(parts + (c + i) * S::kTileLanes);
@@ -458,7 +489,8 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
           for (int i = 0; i < 32; ++i)
             acc[i] = kInt8 ? acc[i] + w[i] : __float_as_uint(__uint_as_float(acc[i]) + __uint_as_float(w[i]));
         }
-        finish(c, acc);
+        if (c > chunk0) read(c, ahead);
+        finish(c, ahead, acc);
       }
     }
     __syncwarp();
