@@ -24,13 +24,21 @@ __device__ __forceinline__ float code_scale(uint32_t max_magnitude) {
   if (max_magnitude >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
   return __fdiv_rn(__uint_as_float(max_magnitude), 127.f);
 }
-// rint(v / s), the quotient formed.
-__device__ __forceinline__ int code_exactly(float v, float s) { return max(-127, min(127, __float2int_rn(__fdiv_rn(v, s)))); }
-
-// Codes without a division: adding 1.5 * 2^23 to v * r, r the reciprocal of s, rounds the exact product to a whole number and
-// leaves it in the low byte of the sum.  The product is within 2^-23 of the quotient, 2e-5 at 127, so both round to the same
-// code unless the product lies that near to the middle between two: `off` collects how far the products are from their codes,
-// and where that comes to 0.4999 the quotients are formed after all.
+// What coding with one scale needs.
+struct Coder {
+  float s, r;        // the scale and its reciprocal
+  float limit;       // of the distance below; negative: the quotients are formed every time
+};
+__device__ __forceinline__ Coder coder_of(float s) {
+  // Nothing but zeros, or a row with no number for a scale: code 0.  Scales near the subnormal range have no usable reciprocal.
+  if (s == 0.f) return {1.f, 0.f, 0.5f};
+  if (!(s > 1e-36f)) return {s, 0.f, -1.f};
+  return {s, __fdiv_rn(1.f, s), 0.49997f};
+}
+// Codes without a division: adding 1.5 * 2^23 to v * r rounds the exact product to a whole number and leaves it in the low byte
+// of the sum.  The product is within 2^-24 of the exact quotient and that within 2^-24 of the rounded one, 1.6e-5 at 127, so
+// both round to the same code unless the product lies that near to the middle between two: `off` collects how far the
+// products are from their codes, and where that passes the limit the quotients are formed after all.
 constexpr float kToByte = 12582912.f;
 __device__ __forceinline__ uint32_t code_byte(float v, float r, float& off) {
   const float t = fmaf(v, r, kToByte);
@@ -40,63 +48,79 @@ __device__ __forceinline__ uint32_t code_byte(float v, float r, float& off) {
 __device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
-// The reciprocal for code_byte().  All codes are 0 without a positive scale (s = 1 then, r = 0); scales near the subnormal
-// range have no usable reciprocal: infinity, which makes `off` NaN or infinite.
-__device__ __forceinline__ float code_reciprocal(float& s) {
-  if (!(s > 0.f)) { s = 1.f; return 0.f; }
-  return s < 1e-36f ? __uint_as_float(0x7F800000u) : __fdiv_rn(1.f, s);
+__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d, const Coder& q, float& off) {
+  return pack_bytes(code_byte(a, q.r, off), code_byte(b, q.r, off), code_byte(c, q.r, off), code_byte(d, q.r, off));
 }
-// Four codes in a word.  With r = 0 the values may be anything, infinities and NaN too.
-__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d, float s, float r) {
-  if (r == 0.f) return 0u;
-  float off = 0.f;
-  const uint32_t w = pack_bytes(code_byte(a, r, off), code_byte(b, r, off), code_byte(c, r, off), code_byte(d, r, off));
-  if (off < 0.4999f && r < 1e37f) return w;
+__device__ __forceinline__ int code_exactly(float v, float s) { return s > 0.f ? max(-127, min(127, __float2int_rn(__fdiv_rn(v, s)))) : 0; }
+// Kept out of line: one group in a thousand comes here.
+__device__ __noinline__ uint32_t code4_exactly(float a, float b, float c, float d, float s) {
   return pack_bytes(code_exactly(a, s), code_exactly(b, s), code_exactly(c, s), code_exactly(d, s));
 }
 
-// Eight neighbours of a row; those past the end are zero.  `vec`: the row allows 16-byte loads.
-__device__ __forceinline__ void load8(const float* p, int left, bool vec, float (&v)[8]) {
-  if (vec && left >= 8) {
-    const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.f;
+// Eight neighbours of a row as they are in memory; those past the end are zero.  `vec`: the row allows 16-byte loads.
+template <class T>
+struct Eight;
+template <>
+struct Eight<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p, int left, bool vec) {
+    if (vec && left >= 8) {
+      a = *(const float4*)p, b = *(const float4*)(p + 4);
+    } else {
+      a = make_float4(left > 0 ? p[0] : 0.f, left > 1 ? p[1] : 0.f, left > 2 ? p[2] : 0.f, left > 3 ? p[3] : 0.f);
+      b = make_float4(left > 4 ? p[4] : 0.f, left > 5 ? p[5] : 0.f, left > 6 ? p[6] : 0.f, left > 7 ? p[7] : 0.f);
+    }
   }
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, int left, bool vec, float (&v)[8]) {
-  if (vec && left >= 8) {
-    const uint4 a = *(const uint4*)p;
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+  __device__ __forceinline__ void widen_to(float (&v)[8]) const {
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  }
+};
+template <>
+struct Eight<__nv_bfloat16> {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int left, bool vec) {
+    if (vec && left >= 8) {
+      const uint4 a = *(const uint4*)p;
+      w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+    } else {
+      const uint16_t* u = (const uint16_t*)p;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (left > 2 * i ? u[2 * i] : 0u) | (left > 2 * i + 1 ? (uint32_t)u[2 * i + 1] << 16 : 0u);
+    }
+  }
+  __device__ __forceinline__ void widen_to(float (&v)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < left ? widen(p[i]) : 0.f;
   }
+};
+template <class T>
+__device__ __forceinline__ void load8(const T* p, int left, bool vec, float (&v)[8]) {
+  Eight<T> e;
+  e.load(p, left, vec);
+  e.widen_to(v);
 }
-__device__ __forceinline__ void times8(const float* mul, int left, float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < left) v[i] *= mul[i];
+__device__ __forceinline__ uint2 code8(const float (&v)[8], const Coder& q) {
+  float off = 0.f;
+  uint2 w = make_uint2(code4(v[0], v[1], v[2], v[3], q, off), code4(v[4], v[5], v[6], v[7], q, off));
+  if (!(off <= q.limit)) w = make_uint2(code4_exactly(v[0], v[1], v[2], v[3], q.s), code4_exactly(v[4], v[5], v[6], v[7], q.s));
+  return w;
 }
-__device__ __forceinline__ void code8(const float (&v)[8], int left, float s, float r, int8_t* out) {
-  const uint32_t w[2] = {code4(v[0], v[1], v[2], v[3], s, r), code4(v[4], v[5], v[6], v[7], s, r)};
+__device__ __forceinline__ void store8(uint2 w, int left, int8_t* out) {
   if (left >= 8) {
-    *(uint2*)out = make_uint2(w[0], w[1]);
+    *(uint2*)out = w;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i < left) out[i] = (int8_t)(w[i >> 2] >> (8 * (i & 3)));
+      if (i < left) out[i] = (int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
   }
 }
 
-// Codes along the rows; kWarps warps per row.  `mul` (may be null) multiplies column c first.  Rows of up to
-// kWarps * 1024 elements are read once and kept in registers, longer ones are read again for their codes.
-template <class T, int kWarps>
-__global__ void __launch_bounds__(256) k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* mul, int8_t* codes, int64_t ld_codes, float* scales) {
-  constexpr int kKeep = 4, kSpan = kWarps * 32 * 8;
+// Codes along the rows; kWarps warps per row.  A row is read once and kept in registers as it is in memory (256 bytes a thread);
+// what is beyond that is read again for its codes.  With kMul column c is multiplied by mul[c] first.
+template <class T, int kWarps, bool kMul>
+__global__ void __launch_bounds__(256)
+k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* mul, int mul_vec, int8_t* codes, int64_t ld_codes, float* scales) {
+  constexpr int kKeep = 32 / sizeof(T), kSpan = kWarps * 32 * 8;
   __shared__ uint32_t part[8];
   const int group = threadIdx.x / (32 * kWarps), t = threadIdx.x % (32 * kWarps);
   const int row = blockIdx.x * (8 / kWarps) + group;
@@ -104,50 +128,62 @@ __global__ void __launch_bounds__(256) k_code_rows(const T* src, int64_t ld, int
   launch_wait();
   launch_next();
   const T* p = src + (int64_t)(in ? row : 0) * ld;
-  float v[kKeep][8];
-  uint32_t m = 0;
+  auto values = [&](const Eight<T>& e, int c, float (&v)[8]) {
+    e.widen_to(v);
+    if constexpr (kMul) {
+      float f[8];
+      load8(mul + c, cols - c, mul_vec, f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= f[j];
+    }
+  };
+  Eight<T> kept[kKeep];
 #pragma unroll
   for (int i = 0; i < kKeep; ++i) {
     const int c = i * kSpan + t * 8;
-    if (c < cols) load8(p + c, cols - c, vec, v[i]);
+    if (c < cols) kept[i].load(p + c, cols - c, vec);
   }
+  uint32_t m = 0;
+  float v[8];
 #pragma unroll
   for (int i = 0; i < kKeep; ++i) {
     const int c = i * kSpan + t * 8;
-    if (c >= cols) continue;
-    if (mul) times8(mul + c, cols - c, v[i]);
+    if (c >= cols) break;
+    values(kept[i], c, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, magnitude(v[i][j]));
+    for (int j = 0; j < 8; ++j) m = max(m, magnitude(v[j]));
   }
   for (int c = kKeep * kSpan + t * 8; c < cols; c += kSpan) {
-    float u[8];
-    load8(p + c, cols - c, vec, u);
-    if (mul) times8(mul + c, cols - c, u);
+    Eight<T> e;
+    e.load(p + c, cols - c, vec);
+    values(e, c, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, magnitude(u[j]));
+    for (int j = 0; j < 8; ++j) m = max(m, magnitude(v[j]));
   }
   m = __reduce_max_sync(0xFFFFFFFFu, m);
-  if (kWarps > 1) {
+  if constexpr (kWarps > 1) {
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
     __syncthreads();
     m = part[group * kWarps + (threadIdx.x & (kWarps - 1))];
     m = __reduce_max_sync(0xFFFFFFFFu, m);
   }
   if (!in) return;
-  float s = code_scale(m);
+  const float s = code_scale(m);
   if (t == 0) scales[row] = s;
-  const float r = code_reciprocal(s);
+  const Coder q = coder_of(s);
   int8_t* out = codes + row * ld_codes;
 #pragma unroll
   for (int i = 0; i < kKeep; ++i) {
     const int c = i * kSpan + t * 8;
-    if (c < cols) code8(v[i], cols - c, s, r, out + c);
+    if (c >= cols) break;
+    values(kept[i], c, v);
+    store8(code8(v, q), cols - c, out + c);
   }
   for (int c = kKeep * kSpan + t * 8; c < cols; c += kSpan) {
-    float u[8];
-    load8(p + c, cols - c, vec, u);
-    if (mul) times8(mul + c, cols - c, u);
-    code8(u, cols - c, s, r, out + c);
+    Eight<T> e;
+    e.load(p + c, cols - c, vec);
+    values(e, c, v);
+    store8(code8(v, q), cols - c, out + c);
   }
 }
 
@@ -186,30 +222,45 @@ template <class T>
 __global__ void __launch_bounds__(256)
 k_code_cols(const T* src, int64_t ld, int rows, int cols, int vec, const uint32_t* max_bits, int8_t* codes, int64_t ld_codes, float* scales) {
   __shared__ uint32_t tile[64][33];
-  __shared__ float2 scale[64];
+  __shared__ Coder coder[64];
   const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 128;
   const int cg = (threadIdx.x & 7) * 8, rg = threadIdx.x >> 3;
   launch_wait();
   launch_next();
   const int left = cols - c0 - cg;
-  float v[4][8];
+  Eight<T> e[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = r0 + rg * 4 + i;
-    load8(src + (int64_t)min(r, rows - 1) * ld + c0 + cg, r < rows ? left : 0, vec, v[i]);
+    e[i].load(src + (int64_t)min(r, rows - 1) * ld + c0 + cg, r < rows ? left : 0, vec);
   }
-  if (threadIdx.x < 64 && c0 + threadIdx.x < cols) {
-    float s = code_scale(max_bits[c0 + threadIdx.x]);
-    if (blockIdx.y == 0) scales[c0 + threadIdx.x] = s;
-    const float r = code_reciprocal(s);
-    scale[threadIdx.x] = make_float2(s, r);
+  if (threadIdx.x < 64) {
+    const bool in = c0 + threadIdx.x < cols;
+    const float s = in ? code_scale(max_bits[c0 + threadIdx.x]) : 0.f;
+    if (in && blockIdx.y == 0) scales[c0 + threadIdx.x] = s;
+    coder[threadIdx.x] = coder_of(s);
   }
   __syncthreads();
+  float v[4][8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (j < left) {
-      const float2 q = scale[cg + j];
-      tile[cg + j][rg] = code4(v[0][j], v[1][j], v[2][j], v[3][j], q.x, q.y);
+  for (int i = 0; i < 4; ++i) e[i].widen_to(v[i]);
+  float off = 0.f, limit = 0.5f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const Coder q = coder[cg + j];
+    limit = fminf(limit, q.limit);
+    tile[cg + j][rg] = code4(v[0][j], v[1][j], v[2][j], v[3][j], q, off);
+  }
+  if (!(off <= limit))
+#pragma unroll 1
+    for (int j = 0; j < 8; ++j) {
+      float u[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = r0 + rg * 4 + i;
+        u[i] = r < rows && j < left ? widen(src[(int64_t)r * ld + c0 + cg + j]) : 0.f;
+      }
+      tile[cg + j][rg] = code4_exactly(u[0], u[1], u[2], u[3], coder[cg + j].s);
     }
   __syncthreads();
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
@@ -269,22 +320,22 @@ k_product_few(const T* x, int64_t ld_x, int vec, const int8_t* codes, int64_t ld
     if (lane == 0) part[warp][t] = m[t];
   }
   __syncthreads();
-  float s[kTokens], r[kTokens];
+  Coder q[kTokens];
 #pragma unroll
   for (int t = 0; t < kTokens; ++t) {
     uint32_t best = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) best = max(best, part[i][t]);
-    s[t] = code_scale(best);
-    if (threadIdx.x == 0) token_scale[t] = s[t];
-    r[t] = code_reciprocal(s[t]);
+    const float s = code_scale(best);
+    if (threadIdx.x == 0) token_scale[t] = s;
+    q[t] = coder_of(s);
   }
   for (int c = threadIdx.x * 8; c < row; c += kFewThreads * 8)
 #pragma unroll
     for (int t = 0; t < kTokens; ++t) {
       float v[8];
       load8(x + min(t, tokens - 1) * ld_x + min(c, n_in - 1), max(n_in - c, 0), vec, v);
-      *(uint2*)(few_smem + t * row + c) = make_uint2(code4(v[0], v[1], v[2], v[3], s[t], r[t]), code4(v[4], v[5], v[6], v[7], s[t], r[t]));
+      *(uint2*)(few_smem + t * row + c) = code8(v, q[t]);
     }
   __syncthreads();
   const int pairs = (n_out + 1) / 2;

@@ -316,24 +316,23 @@ int check_orth(const rtopk_matrix* ctx, int64_t batch, int64_t m, int64_t n, int
   return RTOPK_OK;
 }
 
-// Rows of up to 1024 elements take a warp each, up to 4096 four warps, longer ones a block: what a row's threads hold in
-// registers is read once.
+// A row that a warp's registers hold takes a warp, a longer one, or one of too few to fill the SMs, eight.
 template <class T>
 int code_rows(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, const float* mul, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
-  const int vec = rows_aligned(src, sizeof(T), 1, ld, 0, 16);
-  auto go = [&](auto kernel, int warps) {
-    return launch(ctx, kernel, dim3((unsigned)ceil_div(rows, 8 / warps)), 256, 0, st, src, ld, rows, cols, vec, mul, codes, ld_codes, scales);
+  const int vec = rows_aligned(src, sizeof(T), 1, ld, 0, 16), mul_vec = aligned_to(mul, 16);
+  auto go = [&](auto kernel, auto kernel_mul, int warps) {
+    return launch(ctx, mul ? kernel_mul : kernel, dim3((unsigned)ceil_div(rows, 8 / warps)), 256, 0, st, src, ld, rows, cols, vec, mul, mul_vec, codes, ld_codes, scales);
   };
-  if (cols <= 1024) return go(k_code_rows<T, 1>, 1);
-  if (cols <= 4096) return go(k_code_rows<T, 4>, 4);
-  return go(k_code_rows<T, 8>, 8);
+  if (cols <= 256 || (cols * sizeof(T) <= 32 * 256 && rows > 8 * ctx->sms)) return go(k_code_rows<T, 1, false>, k_code_rows<T, 1, true>, 1);
+  return go(k_code_rows<T, 8, false>, k_code_rows<T, 8, true>, 8);
 }
 
 template <class T>
 int code_cols(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, uint32_t* max_bits, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
   const int vec = rows_aligned(src, sizeof(T), 1, ld, 0, 16);
-  const int per = (int)std::max<int64_t>(32, ceil_div(rows, 64));
-  MAT_TRY(launch(ctx, k_col_max<T>, dim3((unsigned)ceil_div(cols, 256), (unsigned)ceil_div(rows, per)), 256, 0, st, src, ld, rows, cols, vec, per, max_bits));
+  const int64_t across = ceil_div(cols, 256);
+  const int per = (int)std::max<int64_t>(32, ceil_div(rows, std::max<int64_t>(1, 6 * ctx->sms / across)));      // all blocks at once
+  MAT_TRY(launch(ctx, k_col_max<T>, dim3((unsigned)across, (unsigned)ceil_div(rows, per)), 256, 0, st, src, ld, rows, cols, vec, per, max_bits));
   return launch(ctx, k_code_cols<T>, dim3((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(rows, 128)), 256, 0, st, src, ld, rows, cols, vec, max_bits, codes, ld_codes, scales);
 }
 
