@@ -24,37 +24,39 @@ __device__ __forceinline__ float code_scale(uint32_t max_magnitude) {
   if (max_magnitude >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
   return __fdiv_rn(__uint_as_float(max_magnitude), 127.f);
 }
-// What coding with one scale needs.
+// Codes without a division for each: with r the correctly rounded reciprocal of s and q = v r, the remainder v - q s is exact in a
+// fused multiply-add and q + r (v - q s) is the correctly rounded quotient (Markstein, IBM J. Res. Dev. 34, 1990); adding
+// 1.5 * 2^23 to it rounds it to a whole number and leaves that in the low byte of the sum.  (Testing how near a plain product
+// comes to the middle between two codes does not pay: bfloat16 values over a bfloat16 maximum are quotients of small whole
+// numbers, one in three hundred is such a tie.)
 struct Coder {
-  float s, r;        // the scale and its reciprocal
-  float limit;       // of the distance below; negative: the quotients are formed every time
+  float s, r;        // the scale and its reciprocal, both times 2^-64 and 2^64 where the scale is small
+  float up;          // 1, or 2^64: values are multiplied by it first
+  uint32_t mask;     // 0 where the scale is no number: all codes are 0
 };
+constexpr float kUp = 18446744073709551616.f;
 __device__ __forceinline__ Coder coder_of(float s) {
-  // Nothing but zeros, or a row with no number for a scale: code 0.  Scales near the subnormal range have no usable reciprocal.
-  if (s == 0.f) return {1.f, 0.f, 0.5f};
-  if (!(s > 1e-36f)) return {s, 0.f, -1.f};
-  return {s, __fdiv_rn(1.f, s), 0.49997f};
+  if (!(s >= 0.f)) return {0.f, 0.f, 1.f, 0u};
+  if (s == 0.f) return {0.f, 0.f, 1.f, ~0u};
+  const float up = s < 1e-18f ? kUp : 1.f;
+  s *= up;
+  return {s, __fdiv_rn(1.f, s), up, ~0u};
 }
-// Codes without a division: adding 1.5 * 2^23 to v * r rounds the exact product to a whole number and leaves it in the low byte
-// of the sum.  The product is within 2^-24 of the exact quotient and that within 2^-24 of the rounded one, 1.6e-5 at 127, so
-// both round to the same code unless the product lies that near to the middle between two: `off` collects how far the
-// products are from their codes, and where that passes the limit the quotients are formed after all.
 constexpr float kToByte = 12582912.f;
-__device__ __forceinline__ uint32_t code_byte(float v, float r, float& off) {
-  const float t = fmaf(v, r, kToByte);
-  off = fmaxf(off, fabsf(fmaf(v, r, kToByte - t)));
-  return __float_as_uint(t);
+__device__ __forceinline__ uint32_t code_byte(float v, float s, float r) {
+  const float q = v * r;
+  return __float_as_uint(fmaf(fmaf(-q, s, v), r, q) + kToByte);
 }
 __device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
-__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d, const Coder& q, float& off) {
-  return pack_bytes(code_byte(a, q.r, off), code_byte(b, q.r, off), code_byte(c, q.r, off), code_byte(d, q.r, off));
-}
-__device__ __forceinline__ int code_exactly(float v, float s) { return s > 0.f ? max(-127, min(127, __float2int_rn(__fdiv_rn(v, s)))) : 0; }
-// Kept out of line: one group in a thousand comes here.
-__device__ __noinline__ uint32_t code4_exactly(float a, float b, float c, float d, float s) {
-  return pack_bytes(code_exactly(a, s), code_exactly(b, s), code_exactly(c, s), code_exactly(d, s));
+__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d, const Coder& q) {
+  if (q.up != 1.f) {      // a subnormal scale may be so coarse that the largest value is more than 127 of it
+    const float top = 127.f * q.s;
+    a = fminf(fmaxf(a * q.up, -top), top), b = fminf(fmaxf(b * q.up, -top), top);
+    c = fminf(fmaxf(c * q.up, -top), top), d = fminf(fmaxf(d * q.up, -top), top);
+  }
+  return q.mask & pack_bytes(code_byte(a, q.s, q.r), code_byte(b, q.s, q.r), code_byte(c, q.s, q.r), code_byte(d, q.s, q.r));
 }
 
 // Eight neighbours of a row as they are in memory; those past the end are zero.  `vec`: the row allows 16-byte loads.
@@ -100,10 +102,7 @@ __device__ __forceinline__ void load8(const T* p, int left, bool vec, float (&v)
   e.widen_to(v);
 }
 __device__ __forceinline__ uint2 code8(const float (&v)[8], const Coder& q) {
-  float off = 0.f;
-  uint2 w = make_uint2(code4(v[0], v[1], v[2], v[3], q, off), code4(v[4], v[5], v[6], v[7], q, off));
-  if (!(off <= q.limit)) w = make_uint2(code4_exactly(v[0], v[1], v[2], v[3], q.s), code4_exactly(v[4], v[5], v[6], v[7], q.s));
-  return w;
+  return make_uint2(code4(v[0], v[1], v[2], v[3], q), code4(v[4], v[5], v[6], v[7], q));
 }
 __device__ __forceinline__ void store8(uint2 w, int left, int8_t* out) {
   if (left >= 8) {
@@ -115,12 +114,12 @@ __device__ __forceinline__ void store8(uint2 w, int left, int8_t* out) {
   }
 }
 
-// Codes along the rows; kWarps warps per row.  A row is read once and kept in registers as it is in memory (256 bytes a thread);
+// Codes along the rows; kWarps warps per row.  A row is read once and kept in registers as it is in memory (128 bytes a thread);
 // what is beyond that is read again for its codes.  With kMul column c is multiplied by mul[c] first.
 template <class T, int kWarps, bool kMul>
 __global__ void __launch_bounds__(256)
 k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* mul, int mul_vec, int8_t* codes, int64_t ld_codes, float* scales) {
-  constexpr int kKeep = 32 / sizeof(T), kSpan = kWarps * 32 * 8;
+  constexpr int kKeep = 16 / sizeof(T), kSpan = kWarps * 32 * 8;
   __shared__ uint32_t part[8];
   const int group = threadIdx.x / (32 * kWarps), t = threadIdx.x % (32 * kWarps);
   const int row = blockIdx.x * (8 / kWarps) + group;
@@ -238,30 +237,14 @@ k_code_cols(const T* src, int64_t ld, int rows, int cols, int vec, const uint32_
     const bool in = c0 + threadIdx.x < cols;
     const float s = in ? code_scale(max_bits[c0 + threadIdx.x]) : 0.f;
     if (in && blockIdx.y == 0) scales[c0 + threadIdx.x] = s;
-    coder[threadIdx.x] = coder_of(s);
+    coder[(threadIdx.x & 7) * 8 + (threadIdx.x >> 3)] = coder_of(s);      // the eight threads of a row read neighbours
   }
   __syncthreads();
   float v[4][8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) e[i].widen_to(v[i]);
-  float off = 0.f, limit = 0.5f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const Coder q = coder[cg + j];
-    limit = fminf(limit, q.limit);
-    tile[cg + j][rg] = code4(v[0][j], v[1][j], v[2][j], v[3][j], q, off);
-  }
-  if (!(off <= limit))
-#pragma unroll 1
-    for (int j = 0; j < 8; ++j) {
-      float u[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = r0 + rg * 4 + i;
-        u[i] = r < rows && j < left ? widen(src[(int64_t)r * ld + c0 + cg + j]) : 0.f;
-      }
-      tile[cg + j][rg] = code4_exactly(u[0], u[1], u[2], u[3], coder[cg + j].s);
-    }
+  for (int j = 0; j < 8; ++j) tile[cg + j][rg] = code4(v[0][j], v[1][j], v[2][j], v[3][j], coder[j * 8 + (threadIdx.x & 7)]);
   __syncthreads();
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
   const int n = min(4, rows - r0 - x * 4);
@@ -275,18 +258,35 @@ k_code_cols(const T* src, int64_t ld, int rows, int cols, int vec, const uint32_
   }
 }
 
-// codes_t[c][r] = codes[r][c].
+// codes_t[c][r] = codes[r][c]: 128 rows x 64 columns per block, four codes of a column in a word.
 __global__ void __launch_bounds__(256) k_codes_transpose(const int8_t* codes, int64_t ld, int rows, int cols, int8_t* out, int64_t ld_out) {
-  __shared__ int8_t tile[64][65];
-  const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 64;
+  __shared__ uint32_t tile[64][33];
+  const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 128;
+  const int cg = (threadIdx.x & 7) * 8, rg = threadIdx.x >> 3;
   launch_wait();
   launch_next();
-  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-  for (int r = y; r < 64; r += 4)
-    if (r0 + r < rows && c0 + x < cols) tile[x][r] = codes[(int64_t)(r0 + r) * ld + c0 + x];
+  uint2 v[4];      // eight columns of four rows; the row stride is a multiple of 16, so whole vectors exist
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = r0 + rg * 4 + i;
+    v[i] = r < rows && c0 + cg < cols ? *(const uint2*)(codes + (int64_t)r * ld + c0 + cg) : make_uint2(0u, 0u);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    auto byte = [&](const uint2& w) { return (j < 4 ? w.x : w.y) >> (8 * (j & 3)); };
+    tile[cg + j][rg] = pack_bytes(byte(v[0]), byte(v[1]), byte(v[2]), byte(v[3]));
+  }
   __syncthreads();
-  for (int c = y; c < 64; c += 4)
-    if (c0 + c < cols && r0 + x < rows) out[(int64_t)(c0 + c) * ld_out + r0 + x] = tile[c][x];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const int n = min(4, rows - r0 - x * 4);
+  for (int c = y; c < 64; c += 8) {
+    if (c0 + c >= cols || n <= 0) continue;
+    int8_t* p = out + (int64_t)(c0 + c) * ld_out + r0 + x * 4;
+    const uint32_t w = tile[c][x];
+    if (n == 4) *(uint32_t*)p = w;
+    else
+      for (int i = 0; i < n; ++i) p[i] = (int8_t)(w >> (8 * i));
+  }
 }
 
 // A linear layer for a few tokens: reading the codes of W once is all the work, so one launch does everything.  Each block

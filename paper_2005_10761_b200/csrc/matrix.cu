@@ -316,14 +316,17 @@ int check_orth(const rtopk_matrix* ctx, int64_t batch, int64_t m, int64_t n, int
   return RTOPK_OK;
 }
 
-// A row that a warp's registers hold takes a warp, a longer one, or one of too few to fill the SMs, eight.
+// As many warps as hold a row in their registers, 4096 bytes each; eight where there are too few rows to fill the SMs.
 template <class T>
 int code_rows(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, const float* mul, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
   const int vec = rows_aligned(src, sizeof(T), 1, ld, 0, 16), mul_vec = aligned_to(mul, 16);
   auto go = [&](auto kernel, auto kernel_mul, int warps) {
     return launch(ctx, mul ? kernel_mul : kernel, dim3((unsigned)ceil_div(rows, 8 / warps)), 256, 0, st, src, ld, rows, cols, vec, mul, mul_vec, codes, ld_codes, scales);
   };
-  if (cols <= 256 || (cols * sizeof(T) <= 32 * 256 && rows > 8 * ctx->sms)) return go(k_code_rows<T, 1, false>, k_code_rows<T, 1, true>, 1);
+  const int64_t warps = rows <= 4 * ctx->sms ? ceil_div(cols, 256) : ceil_div(cols * sizeof(T), 4096);
+  if (warps <= 1) return go(k_code_rows<T, 1, false>, k_code_rows<T, 1, true>, 1);
+  if (warps <= 2) return go(k_code_rows<T, 2, false>, k_code_rows<T, 2, true>, 2);
+  if (warps <= 4) return go(k_code_rows<T, 4, false>, k_code_rows<T, 4, true>, 4);
   return go(k_code_rows<T, 8, false>, k_code_rows<T, 8, true>, 8);
 }
 
@@ -518,7 +521,7 @@ int rtopk_code_weights(rtopk_matrix* ctx, const void* weights, int dtype, int64_
   if (dtype == RTOPK_F32) MAT_TRY(code_rows(ctx, (const float*)weights, ld_w, n_out, n_in, nullptr, codes, ld_codes, scales, st));
   else MAT_TRY(code_rows(ctx, (const __nv_bfloat16*)weights, ld_w, n_out, n_in, nullptr, codes, ld_codes, scales, st));
   if (codes_t)
-    MAT_TRY(launch(ctx, k_codes_transpose, dim3((unsigned)ceil_div(n_in, 64), (unsigned)ceil_div(n_out, 64)), 256, 0, st, codes, ld_codes, n_out, n_in, codes_t, ld_t));
+    MAT_TRY(launch(ctx, k_codes_transpose, dim3((unsigned)ceil_div(n_in, 64), (unsigned)ceil_div(n_out, 128)), 256, 0, st, codes, ld_codes, n_out, n_in, codes_t, ld_t));
   return RTOPK_OK;
 }
 
