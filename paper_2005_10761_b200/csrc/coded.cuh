@@ -115,10 +115,12 @@ __device__ __forceinline__ void store8(uint2 w, int left, int8_t* out) {
 }
 
 // Codes along the rows; kWarps warps per row.  A row is read once and kept in registers as it is in memory (128 bytes a thread);
-// what is beyond that is read again for its codes.  With kMul column c is multiplied by mul[c] first.
+// what is beyond that is read again for its codes.  With kMul column c is multiplied by mul[c] first.  `clear`: words that a later
+// launch wants zeroed.
 template <class T, int kWarps, bool kMul>
 __global__ void __launch_bounds__(256)
-k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* mul, int mul_vec, int8_t* codes, int64_t ld_codes, float* scales) {
+k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* mul, int mul_vec, int8_t* codes, int64_t ld_codes, float* scales, uint32_t* clear,
+            int clear_words) {
   constexpr int kKeep = 16 / sizeof(T), kSpan = kWarps * 32 * 8;
   __shared__ uint32_t part[8];
   const int group = threadIdx.x / (32 * kWarps), t = threadIdx.x % (32 * kWarps);
@@ -126,6 +128,7 @@ k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* 
   const bool in = row < rows;
   launch_wait();
   launch_next();
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < clear_words; i += gridDim.x * 256) clear[i] = 0u;
   const T* p = src + (int64_t)(in ? row : 0) * ld;
   auto values = [&](const Eight<T>& e, int c, float (&v)[8]) {
     e.widen_to(v);
@@ -186,17 +189,34 @@ k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* 
   }
 }
 
+// Up to two matrices of the same number of rows in one launch: the first `tiles` blocks along x take the first.
+template <class T>
+struct Columns {
+  const T* src;
+  int64_t ld;
+  int cols, vec, tiles;
+  uint32_t* max_bits;
+  int8_t* codes;       // [cols][ld_codes]
+  float* scales;
+};
+
 // Largest magnitude of every column (max_bits zeroed before): 256 columns per block, eight threads deep.
 template <class T>
-__global__ void __launch_bounds__(256) k_col_max(const T* src, int64_t ld, int rows, int cols, int vec, int rows_per_block, uint32_t* max_bits) {
+__global__ void __launch_bounds__(256) k_col_max(const __grid_constant__ Columns<T> first, const __grid_constant__ Columns<T> second, int rows, int rows_per_block) {
   __shared__ uint32_t part[8][256];
+  const bool in_first = (int)blockIdx.x < first.tiles;
+  const Columns<T>& q = in_first ? first : second;
+  const int tile = in_first ? blockIdx.x : blockIdx.x - first.tiles;
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-  const int c = blockIdx.x * 256 + x * 8;
+  const int c = tile * 256 + x * 8, cols = q.cols;
   const int r0 = blockIdx.y * rows_per_block, r1 = min(rows, r0 + rows_per_block);
   launch_wait();
   launch_next();
   uint32_t m[8] = {};
   if (c < cols) {
+    const T* src = q.src;
+    const int64_t ld = q.ld;
+    const bool vec = q.vec;
 #pragma unroll 8
     for (int r = r0 + y; r < r1; r += 8) {
       float v[8];
@@ -211,18 +231,25 @@ __global__ void __launch_bounds__(256) k_col_max(const T* src, int64_t ld, int r
   uint32_t best = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) best = max(best, part[i][threadIdx.x]);
-  const int col = blockIdx.x * 256 + x * 8 + y;     // entry y * 32 + x
-  if (col < cols && best) atomicMax(max_bits + col, best);
+  const int col = tile * 256 + x * 8 + y;     // entry y * 32 + x
+  if (col < cols && best) atomicMax(q.max_bits + col, best);
 }
 
 // Codes for each column, written transposed: codes[c][r], scales[c].  128 rows x 64 columns per block; four codes of a
 // column are one word, so that a row of the result leaves in 128-byte pieces.
 template <class T>
-__global__ void __launch_bounds__(256)
-k_code_cols(const T* src, int64_t ld, int rows, int cols, int vec, const uint32_t* max_bits, int8_t* codes, int64_t ld_codes, float* scales) {
+__global__ void __launch_bounds__(256) k_code_cols(const __grid_constant__ Columns<T> first, const __grid_constant__ Columns<T> second, int rows, int64_t ld_codes) {
   __shared__ uint32_t tile[64][33];
   __shared__ Coder coder[64];
-  const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 128;
+  const bool in_first = (int)blockIdx.x < first.tiles;
+  const Columns<T>& job = in_first ? first : second;
+  const T* src = job.src;
+  const int64_t ld = job.ld;
+  const int cols = job.cols, vec = job.vec;
+  const uint32_t* max_bits = job.max_bits;
+  int8_t* codes = job.codes;
+  float* scales = job.scales;
+  const int c0 = (in_first ? blockIdx.x : blockIdx.x - first.tiles) * 64, r0 = blockIdx.y * 128;
   const int cg = (threadIdx.x & 7) * 8, rg = threadIdx.x >> 3;
   launch_wait();
   launch_next();

@@ -318,25 +318,18 @@ int check_orth(const rtopk_matrix* ctx, int64_t batch, int64_t m, int64_t n, int
 
 // As many warps as hold a row in their registers, 4096 bytes each; eight where there are too few rows to fill the SMs.
 template <class T>
-int code_rows(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, const float* mul, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
+int code_rows(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, const float* mul, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st,
+              uint32_t* clear = nullptr, int64_t clear_words = 0) {
   const int vec = rows_aligned(src, sizeof(T), 1, ld, 0, 16), mul_vec = aligned_to(mul, 16);
   auto go = [&](auto kernel, auto kernel_mul, int warps) {
-    return launch(ctx, mul ? kernel_mul : kernel, dim3((unsigned)ceil_div(rows, 8 / warps)), 256, 0, st, src, ld, rows, cols, vec, mul, mul_vec, codes, ld_codes, scales);
+    return launch(ctx, mul ? kernel_mul : kernel, dim3((unsigned)ceil_div(rows, 8 / warps)), 256, 0, st, src, ld, rows, cols, vec, mul, mul_vec, codes, ld_codes, scales,
+                  clear, clear_words);
   };
   const int64_t warps = rows <= 4 * ctx->sms ? ceil_div(cols, 256) : ceil_div(cols * sizeof(T), 4096);
   if (warps <= 1) return go(k_code_rows<T, 1, false>, k_code_rows<T, 1, true>, 1);
   if (warps <= 2) return go(k_code_rows<T, 2, false>, k_code_rows<T, 2, true>, 2);
   if (warps <= 4) return go(k_code_rows<T, 4, false>, k_code_rows<T, 4, true>, 4);
   return go(k_code_rows<T, 8, false>, k_code_rows<T, 8, true>, 8);
-}
-
-template <class T>
-int code_cols(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, uint32_t* max_bits, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st) {
-  const int vec = rows_aligned(src, sizeof(T), 1, ld, 0, 16);
-  const int64_t across = ceil_div(cols, 256);
-  const int per = (int)std::max<int64_t>(32, ceil_div(rows, std::max<int64_t>(1, 6 * ctx->sms / across)));      // all blocks at once
-  MAT_TRY(launch(ctx, k_col_max<T>, dim3((unsigned)across, (unsigned)ceil_div(rows, per)), 256, 0, st, src, ld, rows, cols, vec, per, max_bits));
-  return launch(ctx, k_code_cols<T>, dim3((unsigned)ceil_div(cols, 64), (unsigned)ceil_div(rows, 128)), 256, 0, st, src, ld, rows, cols, vec, max_bits, codes, ld_codes, scales);
 }
 
 int coded_gemm(rtopk_matrix* ctx, bool lanes_early, const int8_t* lane_codes, int64_t ld_lane, const float* lane_scale, int64_t lanes, const int8_t* col_codes, int64_t ld_col,
@@ -389,13 +382,18 @@ int gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, int64_t
   Carve c{ctx->scratch};
   CodedScratch w(c, tokens, n_out, n_in);
   if (dx) {
-    MAT_TRY(code_rows(ctx, dy, ld_dy, tokens, n_out, scales, w.dy_rows, w.ld_out, w.dy_row_s, st));
+    MAT_TRY(code_rows(ctx, dy, ld_dy, tokens, n_out, scales, w.dy_rows, w.ld_out, w.dy_row_s, st, w.col_max, dw ? n_in + n_out : 0));
     MAT_TRY(coded_gemm(ctx, true, codes_t, ld_t, nullptr, n_in, w.dy_rows, w.ld_out, w.dy_row_s, tokens, n_out, dx, sizeof(T) == 2, ld_dx, st));
   }
   if (dw) {
-    MAT_CUDA(cudaMemsetAsync(w.col_max, 0, (n_in + n_out) * sizeof(uint32_t), st));
-    MAT_TRY(code_cols(ctx, x, ld_x, tokens, n_in, w.col_max, w.x_cols, w.ld_tok, w.x_col_s, st));
-    MAT_TRY(code_cols(ctx, dy, ld_dy, tokens, n_out, w.col_max + n_in, w.dy_cols, w.ld_tok, w.dy_col_s, st));
+    if (!dx) MAT_CUDA(cudaMemsetAsync(w.col_max, 0, (n_in + n_out) * sizeof(uint32_t), st));
+    Columns<T> cx = {x, ld_x, (int)n_in, rows_aligned(x, sizeof(T), 1, ld_x, 0, 16), (int)ceil_div(n_in, 256), w.col_max, w.x_cols, w.x_col_s};
+    Columns<T> cy = {dy, ld_dy, (int)n_out, rows_aligned(dy, sizeof(T), 1, ld_dy, 0, 16), (int)ceil_div(n_out, 256), w.col_max + n_in, w.dy_cols, w.dy_col_s};
+    const int64_t across = cx.tiles + cy.tiles;
+    const int per = (int)std::max<int64_t>(32, ceil_div(tokens, std::max<int64_t>(1, 6 * ctx->sms / across)));      // all blocks at once
+    MAT_TRY(launch(ctx, k_col_max<T>, dim3((unsigned)across, (unsigned)ceil_div(tokens, per)), 256, 0, st, cx, cy, tokens, per));
+    cx.tiles = (int)ceil_div(n_in, 64), cy.tiles = (int)ceil_div(n_out, 64);
+    MAT_TRY(launch(ctx, k_code_cols<T>, dim3((unsigned)(cx.tiles + cy.tiles), (unsigned)ceil_div(tokens, 128)), 256, 0, st, cx, cy, tokens, w.ld_tok));
     MAT_TRY(coded_gemm(ctx, false, w.x_cols, w.ld_tok, w.x_col_s, n_in, w.dy_cols, w.ld_tok, w.dy_col_s, n_out, tokens, dw, dw_dtype == RTOPK_BF16, ld_dw, st));
   }
   return RTOPK_OK;
