@@ -162,15 +162,20 @@ k_split(const __grid_constant__ Source s, float* x, __half* h, int64_t ld, int64
 }
 
 // Small matrices (the shorter side at most 64, the longer at most 256): the whole operator in one block per matrix, everything in
-// shared memory.  A chain of launches would spend its time starting them: at 64 x 64 a step's three products are 1.6 million
-// operations.  What bounds this kernel is the chain of dependent products inside one SM, so they are mma.sync products of the
-// block's sixteen warps, 16 x 16 entries each, with no trip through tensor memory between them.  Every factor is the sum of two
-// 16-bit numbers, high and low, and three of the four partial products are formed: 2^-21 of the result is lost, so
-// that a matrix too small for errors to average out is as exact as a large one.
+// shared and tensor memory.  A chain of launches would spend its time starting them: at 64 x 64 a step's three products are 1.6
+// million operations.  What bounds this kernel is the chain of fifteen dependent products, each of which goes from shared
+// memory through the tensor core and tensor memory back to shared memory.  Every factor is the sum of two 16-bit numbers, high
+// and low, and three of the four partial products are formed: 2^-21 of the result is lost, so that a matrix too small for
+// errors to average out is as exact as a large one.
+//
+// A tile is 64 x 64 16-bit numbers in rows of 128 bytes, swizzled; X is a row of them.  The same bytes serve as a K-major
+// operand (its rows along the contraction index) and as an MN-major one (its rows are the contraction index).  The tensor core's 128
+// lanes reach 64 rows past a tile; what they make of those is not read.
 constexpr int kSmall = 64, kSmallLong = 256, kSmallThreads = 512;
 constexpr int kSmallKeep = kSmall * kSmallLong / kSmallThreads;      // elements of U in a thread's registers
-constexpr int kSmallLd = kSmall + 8;
+constexpr int kSmallBatch = 8;                                       // of them whose loads are under way together
 constexpr float kSmallScale = 32.f;                                  // of X, its Gram matrix and the polynomial
+constexpr int kTileBytes = kSmall * kDepthBytes;
 
 struct SmallOut {
   float* w;                // update: the weights; null: out
@@ -182,159 +187,220 @@ struct SmallOut {
   int steps;
 };
 
-__host__ __device__ constexpr int small_ld(int nl) { return (nl + 63) / 64 * 64 + 8; }      // rows 16 bytes off a multiple of 128
-__host__ __device__ constexpr int small_bytes(int nl) { return 2 * 2 * kSmall * (small_ld(nl) + 2 * kSmallLd); }
+__host__ __device__ constexpr int small_chunks(int nl) { return (nl + kSmall - 1) / kSmall; }
+// X's, the Gram matrix's and the polynomial's tiles, high and low; the rows past the last one; alignment
+__host__ __device__ constexpr int small_bytes(int nl) { return (2 * small_chunks(nl) + 4 + 1) * kTileBytes + 1024; }
 
-struct Halves { __half *hi, *lo; int ld; };
+// Byte of entry (row, col) of a tile.
+__device__ __forceinline__ int tile_byte(int row, int col) { return row * kDepthBytes + (((col >> 3) ^ (row & 7)) << 4) + (col & 7) * 2; }
 
-__device__ __forceinline__ void ld_matrix(uint32_t (&r)[4], const __half* p) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(smem_addr(p)) : "memory");
-}
-__device__ __forceinline__ void ld_matrix_trans(uint32_t (&r)[4], const __half* p) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(smem_addr(p)) : "memory");
-}
-__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// acc = the warp's 16 x 16 entries, rows i0 .. and columns j0 .., of P Q^T (rows of both along the contraction index), or with
-// kTrans of P Q (Q's rows are the contraction index).
-template <bool kTrans>
-__device__ __forceinline__ void small_product(const Halves& p, const Halves& q, int depth, int i0, int j0, float (&acc)[2][4]) {
-  const int lane = threadIdx.x & 31;
+// Sixteen neighbours of a row of a tile, as high and low halves.
+__device__ __forceinline__ void small_store(char* hi, char* lo, int row, int col, const float (&v)[16]) {
 #pragma unroll
-  for (int n = 0; n < 2; ++n)
+  for (int c = 0; c < 16; c += 8) {
+    __half2 h[4], l[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
-  const int at_p = (i0 + (lane & 15)) * p.ld + (lane >> 4) * 8;
-  const int at_q = kTrans ? (lane & 15) * q.ld + j0 + (lane >> 4) * 8 : (j0 + (lane & 7) + (lane >> 4) * 8) * q.ld + ((lane >> 3) & 1) * 8;
-  const int step_q = kTrans ? 16 * q.ld : 16;
-#pragma unroll 4
-  for (int k = 0; k < depth; k += 16) {
-    uint32_t ph[4], pl[4], qh[4], ql[4];
-    ld_matrix(ph, p.hi + at_p + k);
-    ld_matrix(pl, p.lo + at_p + k);
-    const int iq = at_q + k / 16 * step_q;
-    if (kTrans) {
-      ld_matrix_trans(qh, q.hi + iq);
-      ld_matrix_trans(ql, q.lo + iq);
-    } else {
-      ld_matrix(qh, q.hi + iq);
-      ld_matrix(ql, q.lo + iq);
+    for (int i = 0; i < 4; ++i) {
+      h[i] = __floats2half2_rn(v[c + 2 * i], v[c + 2 * i + 1]);
+      const float2 f = __half22float2(h[i]);
+      l[i] = __floats2half2_rn(v[c + 2 * i] - f.x, v[c + 2 * i + 1] - f.y);
     }
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      mma_16x8x16(acc[n], pl, qh[2 * n], qh[2 * n + 1]);
-      mma_16x8x16(acc[n], ph, ql[2 * n], ql[2 * n + 1]);
-      mma_16x8x16(acc[n], ph, qh[2 * n], qh[2 * n + 1]);
-    }
+    const int at = tile_byte(row, col + c);
+    *(uint4*)(hi + at) = *(uint4*)h;
+    *(uint4*)(lo + at) = *(uint4*)l;
   }
 }
-__device__ __forceinline__ void small_split(float a, float b, __half2& hi, __half2& lo) {
-  hi = __floats2half2_rn(a, b);
-  const float2 h = __half22float2(hi);
-  lo = __floats2half2_rn(a - h.x, b - h.y);
-}
-// Entries (row, col) and (row, col + 1).
-__device__ __forceinline__ void small_store(const Halves& m, int row, int col, float a, float b) {
-  __half2 hi, lo;
-  small_split(a, b, hi, lo);
-  *(__half2*)(m.hi + row * m.ld + col) = hi;
-  *(__half2*)(m.lo + row * m.ld + col) = lo;
-}
-__device__ __forceinline__ float2 small_load(const Halves& m, int row, int col) {
-  const float2 h = __half22float2(*(const __half2*)(m.hi + row * m.ld + col)), l = __half22float2(*(const __half2*)(m.lo + row * m.ld + col));
-  return make_float2(h.x + l.x, h.y + l.y);
+
+// d (+)= P Q^T, or with kTrans P Q, of one pair of tiles with their low halves.
+template <bool kTrans>
+__device__ __forceinline__ void small_product(uint32_t d, uint32_t p_hi, uint32_t p_lo, uint32_t q_hi, uint32_t q_lo, bool accumulate) {
+  constexpr uint32_t kDesc = instr_desc(false, false, 128, kSmall, kTrans);
+  constexpr int kStep = kTrans ? 2048 >> 4 : 2;
+  const uint64_t ph = smem_desc(p_hi, 16), pl = smem_desc(p_lo, 16), qh = smem_desc(q_hi, kTileBytes), ql = smem_desc(q_lo, kTileBytes);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    tc_mma<false, false>(d, pl + k * 2, qh + k * kStep, kDesc, accumulate || k);
+    tc_mma<false, false>(d, ph + k * 2, ql + k * kStep, kDesc, 1);
+    tc_mma<false, false>(d, ph + k * 2, qh + k * kStep, kDesc, 1);
+  }
 }
 
-__global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_constant__ Source s, const __grid_constant__ SmallOut to, int transpose) {
-  extern __shared__ __align__(16) __half small_smem[];
+__global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_constant__ Source s, const __grid_constant__ SmallOut to, int transpose, uint32_t* error) {
+  extern __shared__ char small_smem[];
   __shared__ double part[kSmallThreads / 32];
+  __shared__ __align__(8) uint64_t done;
+  __shared__ volatile uint32_t words[2];      // tensor-memory address, give-up word
   const int z = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
-  const int ns = transpose ? s.n : s.m, nl = transpose ? s.m : s.n, ld = small_ld(nl), count = s.m * s.n;
-  const int chunks = (nl + 63) / 64, ks = (ns + 15) / 16 * 16, kl = (nl + 15) / 16 * 16;
-  const Halves x = {small_smem, small_smem + kSmall * ld, ld};
-  const Halves g = {x.lo + kSmall * ld, x.lo + kSmall * (ld + kSmallLd), kSmallLd};
-  const Halves b = {g.lo + kSmall * kSmallLd, g.lo + 2 * kSmall * kSmallLd, kSmallLd};
-  for (int i = t; i < kSmall * ld; i += kSmallThreads) *((uint32_t*)x.hi + i) = 0u;      // both halves
+  const int nl = transpose ? s.m : s.n;
+  const int chunks = small_chunks(nl), bytes = chunks * kTileBytes;
+  const uint32_t at_smem = smem_addr(small_smem), base = (at_smem + 1023u) & ~1023u;
+  char* x_hi = small_smem + (base - at_smem);
+  char *x_lo = x_hi + bytes, *g_hi = x_lo + bytes, *g_lo = g_hi + kTileBytes, *b_hi = g_lo + kTileBytes, *b_lo = b_hi + kTileBytes;
+  const uint32_t x = base, g = base + 2 * bytes, b = g + 2 * kTileBytes, bar = smem_addr(&done);
+  const uint32_t tmem_cols = chunks <= 1 ? 64 : chunks <= 2 ? 128 : 256;
+  const GiveUp give{words + 1, error};
+  if (t == 0) {
+    bar_init(bar, 1);
+    words[1] = 0u;
+    bar_init_fence();
+  }
+  if (warp == 0) tmem_alloc<false>(smem_addr((const void*)words), tmem_cols);
+  for (int i = t * 16; i < 2 * bytes; i += kSmallThreads * 16) *(uint4*)(x_hi + i) = make_uint4(0u, 0u, 0u, 0u);
   launch_wait();
   launch_next();
+  // Element i of a thread: entry t + 512 i of U with its rows padded to a power of two; entries outside U read its first one.
+  const int shift = s.n <= 32 ? 5 : 32 - __clz(s.n - 1), turns = ((s.m << shift) + kSmallThreads - 1) / kSmallThreads;
+  auto entry = [&](int i, int& r, int& c) {
+    const int k = t + i * kSmallThreads;
+    r = k >> shift, c = k & ((1 << shift) - 1);
+    return r < s.m && c < s.n;
+  };
   float u[kSmallKeep];
   double sum = 0.0;
 #pragma unroll
-  for (int i = 0; i < kSmallKeep; ++i) {
-    const int k = t + i * kSmallThreads;
-    u[i] = 0.f;
-    if (k >= count) continue;
-    const int r = k / s.n, c = k - r * s.n;
-    u[i] = source_at(s, z * s.stride + r * s.ld + c);
-    if (s.v) {
-      float* v = s.v + z * s.v_stride + r * s.v_ld + c;
-      const float nv = fmaf(s.mu, *v, u[i]);
-      *v = nv;
-      u[i] = update_of(s, u[i], nv);
+  for (int i0 = 0; i0 < kSmallKeep; i0 += kSmallBatch) {
+    if (i0 >= turns) break;
+    float v[kSmallBatch];
+#pragma unroll
+    for (int i = 0; i < kSmallBatch; ++i) {
+      int r, c;
+      const bool in = entry(i0 + i, r, c);
+      u[i0 + i] = source_at(s, z * s.stride + (in ? r * s.ld + c : 0));
+      if (s.v) v[i] = s.v[z * s.v_stride + (in ? r * s.v_ld + c : 0)];
     }
-    sum += (double)u[i] * (double)u[i];
+#pragma unroll
+    for (int i = 0; i < kSmallBatch; ++i) {
+      int r, c;
+      const bool in = entry(i0 + i, r, c);
+      float& e = u[i0 + i];
+      if (s.v) {
+        const float nv = fmaf(s.mu, v[i], e);
+        if (in) s.v[z * s.v_stride + r * s.v_ld + c] = nv;
+        e = update_of(s, e, nv);
+      }
+      if (in) sum += (double)e * (double)e;
+    }
   }
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
   if (lane == 0) part[warp] = sum;
+  tc_fence_before();
   __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = words[0];
   sum = 0.0;
   for (int i = 0; i < kSmallThreads / 32; ++i) sum += part[i];
   const float inv = sum == 0.0 ? 0.f : (float)((double)kSmallScale / (sqrt(sum) + (double)s.eps));
 #pragma unroll
   for (int i = 0; i < kSmallKeep; ++i) {
-    const int k = t + i * kSmallThreads;
-    if (k >= count) continue;
-    const int r = k / s.n, c = k - r * s.n, at = transpose ? c * ld + r : r * ld + c;
+    if (i >= turns) break;
+    int r, c;
+    if (!entry(i, r, c)) continue;
+    const int row = transpose ? c : r, col = transpose ? r : c, at = col / kSmall * kTileBytes + tile_byte(row, col & (kSmall - 1));
     const float v = u[i] * inv;
     const __half h = to_half(v);
-    x.hi[at] = h;
-    x.lo[at] = to_half(v - __half2float(h));
+    *(__half*)(x_hi + at) = h;
+    *(__half*)(x_lo + at) = to_half(v - __half2float(h));
   }
+  smem_publish();
   __syncthreads();
-  const int i0 = (warp & 3) * 16, j0 = (warp >> 2) * 16;
-  const int row = i0 + lane / 4, col = j0 + (lane & 3) * 2;      // of acc[n][0]: column + 8 n; acc[n][2]: row + 8
-  float acc[2][4];
+  // tensor memory's lanes 0 .. 63 belong to the warps 0 and 1 of every four: eight warps at work, 32 rows x 16 columns each
+  const bool works = (warp & 3) < 2;
+  const int row = (warp & 3) * 32 + lane, col = (warp >> 2) * 16;
+  const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16) + col;
+  uint32_t phase = 0;
+  bool failed = false;
+  // ends a product: its results, once it is done
+  auto result = [&](int c0, float (&v)[16], float scale) {
+    uint32_t acc[16];
+    tmem_load16(from + c0, acc);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(acc[i]) * scale;
+  };
+  auto wait = [&]() {
+    if (works) {
+      if (!__all_sync(0xFFFFFFFFu, bar_wait(bar, phase, give))) failed = true;
+      tc_fence_after();
+    }
+    phase ^= 1;
+  };
+  auto publish = [&]() {
+    tc_fence_before();
+    smem_publish();
+    failed = __syncthreads_or(failed) != 0;
+    tc_fence_after();
+  };
   for (int step = 0; step < to.steps; ++step) {
     const float ca = to.coef[3 * step] * kSmallScale, cb = to.coef[3 * step + 1], cc = to.coef[3 * step + 2] * (1.f / kSmallScale);
-    small_product<false>(x, x, kl, i0, j0, acc);
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        small_store(g, row + 8 * h, col + 8 * n, acc[n][2 * h] * (1.f / kSmallScale), acc[n][2 * h + 1] * (1.f / kSmallScale));
-    __syncthreads();
-    small_product<false>(g, g, ks, i0, j0, acc);
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = row + 8 * h, c = col + 8 * n;
-        const float2 a = small_load(g, r, c);
-        small_store(b, r, c, cc * acc[n][2 * h] + cb * a.x + (r == c ? ca : 0.f), cc * acc[n][2 * h + 1] + cb * a.y + (r == c + 1 ? ca : 0.f));
+    float gram[16], v[16];
+    if (t == 0) {
+      for (int c = 0; c < chunks; ++c) {
+        const uint32_t at = x + c * kTileBytes;
+        small_product<false>(tmem, at, at + bytes, at, at + bytes, c > 0);
       }
-    __syncthreads();
-    for (int k = 0; k < chunks; ++k) {
-      small_product<true>(b, x, ks, i0, k * 64 + j0, acc);
-      __syncthreads();      // these 64 columns of X have been read
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          small_store(x, row + 8 * h, k * 64 + col + 8 * n, acc[n][2 * h] * (1.f / kSmallScale), acc[n][2 * h + 1] * (1.f / kSmallScale));
+      tc_commit<false>(bar);
     }
+    __syncwarp();
+    wait();
+    if (works) {
+      result(0, gram, 1.f / kSmallScale);
+      small_store(g_hi, g_lo, row, col, gram);
+    }
+    publish();
+    if (failed) break;
+    if (t == 0) {
+      small_product<false>(tmem, g, g + kTileBytes, g, g + kTileBytes, false);
+      tc_commit<false>(bar);
+    }
+    __syncwarp();
+    wait();
+    if (works) {
+      result(0, v, cc);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] += cb * gram[i] + (row == col + i ? ca : 0.f);
+      small_store(b_hi, b_lo, row, col, v);
+    }
+    publish();
+    if (failed) break;
+    if (t == 0) {
+      for (int c = 0; c < chunks; ++c) small_product<true>(tmem + c * kSmall, b, b + kTileBytes, x + c * kTileBytes, x + bytes + c * kTileBytes, false);
+      tc_commit<false>(bar);
+    }
+    __syncwarp();
+    wait();
+    if (works)
+      for (int c = 0; c < chunks; ++c) {
+        result(c * kSmall, v, 1.f / kSmallScale);
+        small_store(x_hi + c * kTileBytes, x_lo + c * kTileBytes, row, col, v);
+      }
+    publish();
+    if (failed) break;
+  }
+  if (failed) {
+    if (t == 0) bar_drain(bar, phase ^ 1);
     __syncthreads();
   }
-  for (int k = t; k < count; k += kSmallThreads) {
-    const int r = k / s.n, c = k - r * s.n, from = transpose ? c * ld + r : r * ld + c;
-    const float v = (__half2float(x.hi[from]) + __half2float(x.lo[from])) * (1.f / kSmallScale);
-    const int64_t at = z * to.stride + r * to.ld + c;
-    if (to.w) to.w[at] = to.keep * to.w[at] - to.rate * v;
-    else if (to.bf16) ((__nv_bfloat16*)to.out)[at] = __float2bfloat16_rn(v);
-    else ((float*)to.out)[at] = v;
+  if (warp == 0) tmem_free<false>(tmem, tmem_cols);
+  if (failed) return;
+#pragma unroll 1
+  for (int i0 = 0; i0 < turns; i0 += kSmallBatch) {
+    float w[kSmallBatch];
+#pragma unroll
+    for (int i = 0; i < kSmallBatch; ++i) {
+      int r, c;
+      const bool in = entry(i0 + i, r, c);
+      if (to.w) w[i] = to.w[z * to.stride + (in ? r * to.ld + c : 0)];
+    }
+#pragma unroll
+    for (int i = 0; i < kSmallBatch; ++i) {
+      int r, c;
+      if (!entry(i0 + i, r, c)) continue;
+      const int row = transpose ? c : r, col = transpose ? r : c, from_x = col / kSmall * kTileBytes + tile_byte(row, col & (kSmall - 1));
+      const float v = (__half2float(*(const __half*)(x_hi + from_x)) + __half2float(*(const __half*)(x_lo + from_x))) * (1.f / kSmallScale);
+      const int64_t at = z * to.stride + r * to.ld + c;
+      if (to.w) to.w[at] = to.keep * w[i] - to.rate * v;
+      else if (to.bf16) ((__nv_bfloat16*)to.out)[at] = __float2bfloat16_rn(v);
+      else ((float*)to.out)[at] = v;
+    }
   }
 }
 

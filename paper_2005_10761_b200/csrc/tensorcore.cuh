@@ -163,6 +163,19 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
       : "memory");
 }
 
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr)
+      : "memory");
+}
+// Ordinary stores to shared memory, seen by the tensor core and TMA after the next barrier.
+__device__ __forceinline__ void smem_publish() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // Shared-memory matrix descriptor, 128-byte swizzle.  K-major tiles: rows of 128 bytes, groups of 8 rows 1024 bytes
 // apart (the leading offset is not used).  MN-major tiles: slabs of 64 16-bit elements along the row index,
 // `slab_bytes` apart, in which 8 steps of the contraction index take 1024 bytes.
@@ -171,8 +184,8 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t slab_bytes
          (1ull << 46) | (2ull << 61);
 }
 // Instruction descriptor: f16 x f16 -> f32 or s8 x s8 -> s32, m x n.
-__host__ __device__ constexpr uint32_t instr_desc(bool int8, bool a_mn_major, uint32_t m, uint32_t n) {
-  return (int8 ? (2u << 4) | (1u << 7) | (1u << 10) : (1u << 4)) | (a_mn_major ? 1u << 15 : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
+__host__ __device__ constexpr uint32_t instr_desc(bool int8, bool a_mn_major, uint32_t m, uint32_t n, bool b_mn_major = false) {
+  return (int8 ? (2u << 4) | (1u << 7) | (1u << 10) : (1u << 4)) | (a_mn_major ? 1u << 15 : 0u) | (b_mn_major ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 
 // ----------------------------------------------------------------------------- launch order
