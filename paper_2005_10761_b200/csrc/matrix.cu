@@ -62,7 +62,7 @@ constexpr int64_t kBatchMax = 65535;
 constexpr int64_t kDepthMax = 131072;     // 127 * 127 * depth stays below 2^31
 
 constexpr int kSplitTiles = 1024;         // tiles of a split product: counters
-constexpr int64_t kPartBytes = kLanes * 128 * 4;       // partial sums of one block: as many parts as there are SMs, at most
+constexpr int64_t kPartBytes = kLanes * 256 * 4;       // partial sums of one block: as many parts as there are SMs, at most
 constexpr int kErrorBytes = 1024 + 2 * kSplitTiles * 4;
 
 int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
@@ -190,23 +190,23 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
   return launch_cluster(ctx, kBlocks, k_gemm<kCols, kPair, kEpi>, dim3(grid), kGemmThreads, S::kSmem, st, mp, mq, g);
 }
 
-// Which tile, and in how many parts: the one for which this estimate of the time, in cycles, is least.  Per step of 128 bytes of the
-// contraction index a block takes what its stage needs from L2 (56 bytes a cycle and SM), or the tensor core's time; the last
-// tile of a block leaves its results behind the products; parts are written and read again.
+// Which tile, and in how many parts: the one for which this estimate of the time, in cycles, is least.  A step of 128 bytes of
+// the contraction index takes the tensor core's time or what its stage needs from L2 (44 bytes a cycle and SM, measured);
+// the results of a tile take so many cycles a column, beside the next tile's products or, for the last one, after them; parts
+// are written and read again.
 template <int kEpi>
 int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, cudaStream_t st) {
+  constexpr double kColumn = kEpi == EPI_CODED ? 25 : kEpi == EPI_GRAM ? 35 : kEpi == EPI_OUT ? 45 : kEpi == EPI_POLY ? 52 : 60;
   const int64_t steps = ceil_div((int64_t)g.depth * (kEpi == EPI_CODED ? 1 : 2), kDepthBytes);
   double best = 1e300;
   int which = 0, parts = 1;
   auto consider = [&](int id, int64_t tiles, int cols, int blocks, int stage_bytes) {
-    const int64_t sms = ctx->sms / blocks;
+    const int64_t sms = ctx->sms / blocks, all = tiles * g.batch;
     for (int split = 1; split <= 8; ++split) {
-      if (split > 1 && (tiles * g.batch * split > sms || steps < 4 * split || tiles * g.batch > kSplitTiles || cols > 128)) break;
+      if (split > 1 && (all * split > sms || steps < 4 * split || all > kSplitTiles)) break;
       if ((split - 1) * ceil_div(steps, split) >= steps) continue;      // a part without any step
-      const double per_step = std::max(stage_bytes / 56.0, cols * 2.0);
-      const double main = (double)ceil_div(steps, split) * per_step + 1000, tail = cols * 12.0 + (split > 1 ? cols * (6.0 + 6.0 * split) + 2500 : 0);
-      const double waves = (double)ceil_div(tiles * g.batch * split, sms);
-      const double t = waves * std::max(main, cols * 12.0) + tail;
+      const double main = (double)ceil_div(steps, split) * std::max(stage_bytes / 44.0, cols * 2.0) + 500, tail = cols * kColumn;
+      const double t = ceil_div(all * split, sms) * std::max(main, tail) + tail + (split > 1 ? cols * (16.0 + 16.0 * split) + 3000 : 0);
       if (t < best) best = t, which = id, parts = split;
     }
   };
@@ -258,7 +258,7 @@ int orthogonal_small(rtopk_matrix* ctx, Source src, const Target& to, int64_t ba
   o.w = to.epi == EPI_UPDATE ? (float*)to.out : nullptr;
   o.out = to.out, o.bf16 = to.bf16, o.ld = to.ld, o.stride = to.stride, o.keep = to.keep, o.rate = to.rate, o.steps = steps;
   for (int i = 0; i < 3 * steps; ++i) o.coef[i] = coef ? coef[i] : kQuintic[i % 3];
-  return launch(ctx, k_orth_small, dim3((unsigned)batch), kSmallThreads, small_bytes((int)std::max(m, n)), st, src, o, m > n ? 1 : 0);
+  return launch(ctx, k_orth_small, dim3((unsigned)batch), kSmallThreads, small_bytes((int)std::max(m, n)), st, src, o, m > n ? 1 : 0, ctx->error);
 }
 
 int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, int64_t m, int64_t n, int steps, const float* coef, cudaStream_t st) {
