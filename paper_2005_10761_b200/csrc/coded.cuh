@@ -115,12 +115,12 @@ __device__ __forceinline__ void store8(uint2 w, int left, int8_t* out) {
 }
 
 // Codes along the rows; kWarps warps per row.  A row is read once and kept in registers as it is in memory (128 bytes a thread);
-// what is beyond that is read again for its codes.  With kMul column c is multiplied by mul[c] first.  `clear`: words that a later
-// launch wants zeroed.
+// what is beyond that is read again for its codes.  With kMul column c is multiplied by mul[c] first.  `padded`: that many codes of a
+// row are written, those past its end zero.  `clear`: words that a later launch wants zeroed.
 template <class T, int kWarps, bool kMul>
 __global__ void __launch_bounds__(256)
-k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* mul, int mul_vec, int8_t* codes, int64_t ld_codes, float* scales, uint32_t* clear,
-            int clear_words) {
+k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* mul, int mul_vec, int8_t* codes, int64_t ld_codes, int padded, float* scales,
+            uint32_t* clear, int clear_words) {
   constexpr int kKeep = 16 / sizeof(T), kSpan = kWarps * 32 * 8;
   __shared__ uint32_t part[8];
   const int group = threadIdx.x / (32 * kWarps), t = threadIdx.x % (32 * kWarps);
@@ -179,14 +179,15 @@ k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* 
     const int c = i * kSpan + t * 8;
     if (c >= cols) break;
     values(kept[i], c, v);
-    store8(code8(v, q), cols - c, out + c);
+    store8(code8(v, q), padded - c, out + c);
   }
   for (int c = kKeep * kSpan + t * 8; c < cols; c += kSpan) {
     Eight<T> e;
     e.load(p + c, cols - c, vec);
     values(e, c, v);
-    store8(code8(v, q), cols - c, out + c);
+    store8(code8(v, q), padded - c, out + c);
   }
+  for (int c = (cols + 7) / 8 * 8 + t * 8; c < padded; c += kSpan) store8(make_uint2(0u, 0u), padded - c, out + c);
 }
 
 // Up to two matrices of the same number of rows in one launch: the first `tiles` blocks along x take the first.
@@ -393,6 +394,73 @@ k_product_few(const T* x, int64_t ld_x, int vec, const int8_t* codes, int64_t ld
       if (sizeof(T) == 2) ((__nv_bfloat16*)out)[t * ld_out + n] = __float2bfloat16_rn(v);
       else ((float*)out)[t * ld_out + n] = v;
     }
+  }
+}
+
+// The same for up to eight tokens, whose codes come from a launch before (rows of whole 64s, zero past n_in): 32 output channels a
+// block, the contraction dealt out to its eight warps in pieces of 64 codes, integer matrix instructions (16 channels x 8
+// tokens x 32 codes) straight from registers.  Reading W is what takes the time here, so nothing of it goes through shared
+// memory: a thread's 16 consecutive codes of a channel are two instructions' operands, in an order of the contraction index that
+// the tokens' codes follow.  The warps' sums meet in shared memory.
+constexpr int kTokThreads = 256, kTokChannels = 32;
+
+__device__ __forceinline__ void mma_codes(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <class T>
+__global__ void __launch_bounds__(kTokThreads, 2)
+k_product_tokens(const int8_t* x, int64_t ld_x, const float* token_scales, const int8_t* codes, int64_t ld_codes, const float* scales, int tokens, int n_out, int n_in, T* out,
+                 int64_t ld_out) {
+  __shared__ int sums[8][8][kTokChannels + 1];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const int n0 = blockIdx.x * kTokChannels;
+  const int8_t* w[4];      // channels g, g + 8, g + 16, g + 24; those past the last one read it again
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = codes + min(n0 + g + 8 * i, n_out - 1) * ld_codes;
+  const int8_t* p = x + min(g, tokens - 1) * ld_x;
+  auto read_w = [&](int k, uint4 (&a)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = k < n_in ? __ldg((const uint4*)(w[i] + k)) : make_uint4(0u, 0u, 0u, 0u);
+  };
+  constexpr int kAhead = 3, kStep = 8 * 64;
+  uint4 a[kAhead][4];
+  int k = warp * 64 + q * 16;
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) read_w(k + j * kStep, a[j]);      // W is not written by the launch before
+  launch_wait();
+  launch_next();
+  int acc[2][4] = {};
+  for (int j0 = 0; j0 * kStep + warp * 64 < n_in; j0 += kAhead)
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int kk = k + (j0 + j) * kStep;
+      if ((j0 + j) * kStep + warp * 64 >= n_in) break;
+      const uint4 b = *(const uint4*)(p + kk);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        mma_codes(acc[m], a[j][2 * m].x, a[j][2 * m + 1].x, a[j][2 * m].y, a[j][2 * m + 1].y, b.x, b.y);
+        mma_codes(acc[m], a[j][2 * m].z, a[j][2 * m + 1].z, a[j][2 * m].w, a[j][2 * m + 1].w, b.z, b.w);
+      }
+      read_w(kk + kAhead * kStep, a[j]);
+    }
+  // acc[m]: channels 16 m + g and + 8, tokens 2 q and + 1
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[warp][2 * q + (e & 1)][16 * m + g + 8 * (e >> 1)] = acc[m][e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < tokens * kTokChannels; i += kTokThreads) {
+    const int t = i / kTokChannels, c = i % kTokChannels, n = n0 + c;
+    if (n >= n_out) continue;
+    int sum = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += sums[j][t][c];
+    const float v = (float)sum * token_scales[t] * scales[n];
+    if (sizeof(T) == 2) ((__nv_bfloat16*)out)[t * ld_out + n] = __float2bfloat16_rn(v);
+    else ((float*)out)[t * ld_out + n] = v;
   }
 }
 

@@ -319,11 +319,11 @@ int check_orth(const rtopk_matrix* ctx, int64_t batch, int64_t m, int64_t n, int
 // As many warps as hold a row in their registers, 4096 bytes each; eight where there are too few rows to fill the SMs.
 template <class T>
 int code_rows(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, const float* mul, int8_t* codes, int64_t ld_codes, float* scales, cudaStream_t st,
-              uint32_t* clear = nullptr, int64_t clear_words = 0) {
+              int64_t padded = 0, uint32_t* clear = nullptr, int64_t clear_words = 0) {
   const int vec = rows_aligned(src, sizeof(T), 1, ld, 0, 16), mul_vec = aligned_to(mul, 16);
   auto go = [&](auto kernel, auto kernel_mul, int warps) {
-    return launch(ctx, mul ? kernel_mul : kernel, dim3((unsigned)ceil_div(rows, 8 / warps)), 256, 0, st, src, ld, rows, cols, vec, mul, mul_vec, codes, ld_codes, scales,
-                  clear, clear_words);
+    return launch(ctx, mul ? kernel_mul : kernel, dim3((unsigned)ceil_div(rows, 8 / warps)), 256, 0, st, src, ld, rows, cols, vec, mul, mul_vec, codes, ld_codes,
+                  std::max(cols, padded), scales, clear, clear_words);
   };
   const int64_t warps = rows <= 4 * ctx->sms ? ceil_div(cols, 256) : ceil_div(cols * sizeof(T), 4096);
   if (warps <= 1) return go(k_code_rows<T, 1, false>, k_code_rows<T, 1, true>, 1);
@@ -364,15 +364,20 @@ int product_few(rtopk_matrix* ctx, const T* x, int64_t ld_x, const int8_t* codes
 template <class T>
 int product(rtopk_matrix* ctx, const T* x, int64_t ld_x, const int8_t* codes, int64_t ld_codes, const float* scales, int64_t tokens, int64_t n_out, int64_t n_in,
             T* out, int64_t ld_out, cudaStream_t st) {
-  if (tokens <= 8 && (tokens <= 1 ? 1 : tokens <= 2 ? 2 : tokens <= 4 ? 4 : 8) * few_row((int)n_in) <= kFewBytes) {
-    if (tokens == 1) return product_few<T, 1>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
-    if (tokens == 2) return product_few<T, 2>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
-    if (tokens <= 4) return product_few<T, 4>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
-    return product_few<T, 8>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
+  // One launch saves 2 us over two, but its dot products take longer than reading W once there are many: 4 tokens through
+  // 1500 -> 6000 6.9 us against 7.5, through 4096 -> 4096 9.2 against 7.4; 8 tokens through 8192 -> 8192 19 against 17.
+  const int64_t few = tokens <= 1 ? 1 : tokens <= 2 ? 2 : 4;
+  if (tokens <= 4 && few * few_row((int)n_in) <= kFewBytes && (tokens == 1 || tokens * n_in * n_out <= 40000000)) {
+    if (few == 1) return product_few<T, 1>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
+    if (few == 2) return product_few<T, 2>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
+    return product_few<T, 4>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
   }
   Carve c{ctx->scratch};
   CodedScratch w(c, tokens, n_out, n_in);
-  MAT_TRY(code_rows(ctx, x, ld_x, tokens, n_in, nullptr, w.x_rows, w.ld_in, w.x_row_s, st));
+  MAT_TRY(code_rows(ctx, x, ld_x, tokens, n_in, nullptr, w.x_rows, w.ld_in, w.x_row_s, st, w.ld_in));
+  if (tokens <= 8)      // above, the product kernel is as fast or faster: 16 tokens through 8192 -> 8192 18.7 us against 19.9
+    return launch(ctx, k_product_tokens<T>, dim3((unsigned)ceil_div(n_out, kTokChannels)), kTokThreads, 0, st, w.x_rows, w.ld_in, w.x_row_s, codes, ld_codes, scales, tokens, n_out,
+                  n_in, out, ld_out);
   return coded_gemm(ctx, true, codes, ld_codes, scales, n_out, w.x_rows, w.ld_in, w.x_row_s, tokens, n_in, out, sizeof(T) == 2, ld_out, st);
 }
 
@@ -382,7 +387,7 @@ int gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, int64_t
   Carve c{ctx->scratch};
   CodedScratch w(c, tokens, n_out, n_in);
   if (dx) {
-    MAT_TRY(code_rows(ctx, dy, ld_dy, tokens, n_out, scales, w.dy_rows, w.ld_out, w.dy_row_s, st, w.col_max, dw ? n_in + n_out : 0));
+    MAT_TRY(code_rows(ctx, dy, ld_dy, tokens, n_out, scales, w.dy_rows, w.ld_out, w.dy_row_s, st, 0, w.col_max, dw ? n_in + n_out : 0));
     MAT_TRY(coded_gemm(ctx, true, codes_t, ld_t, nullptr, n_in, w.dy_rows, w.ld_out, w.dy_row_s, tokens, n_out, dx, sizeof(T) == 2, ld_dx, st));
   }
   if (dw) {
