@@ -482,11 +482,13 @@ int rtopk_get_launch_count(const rtopk_ctx* ctx, uint64_t* out);
  * out as 8-bit codes, the workers multiply with the codes, and their weight gradients are the g that
  * rtopk_sparsify / rtopk_step take.  The paper has no counterpart for them.
  *
- * They have a context of their own, which owns one block of device scratch.  rtopk_matrix_create
- * allocates it (scratch_bytes: the largest that rtopk_orthogonalize_scratch / rtopk_coded_scratch
- * give for the shapes to be used; a call that needs more returns INVALID_ARG); no other call
- * allocates.  Calls that share a context must be ordered on one stream, as for rtopk_ctx.  They only
- * enqueue work and may be captured into a CUDA graph.
+ * They have a context of their own with one block of device scratch: the caller's (`scratch`, 256-byte
+ * aligned, scratch_bytes long, his until rtopk_matrix_destroy), or with scratch = null one that the context
+ * allocates.  scratch_bytes is the largest that rtopk_orthogonalize_scratch / rtopk_coded_scratch give
+ * for the shapes to be used; a call that needs more returns INVALID_ARG, and none allocates.
+ * rtopk_matrix_create clears the context's error words on `stream`; calls that share a context must be
+ * ordered on one stream, as for rtopk_ctx, the first after that.  They only enqueue work and may be
+ * captured into a CUDA graph.
  *
  * A view of `batch` matrices of m rows and n columns is a pointer, a row stride ld >= n and a
  * distance `stride` from one matrix to the next (>= (m - 1) ld + n; not read when batch = 1), all in
@@ -494,7 +496,7 @@ int rtopk_get_launch_count(const rtopk_ctx* ctx, uint64_t* out);
  */
 typedef struct rtopk_matrix rtopk_matrix;
 
-int rtopk_matrix_create(rtopk_matrix** out, int device, int64_t scratch_bytes);
+int rtopk_matrix_create(rtopk_matrix** out, int device, void* scratch, int64_t scratch_bytes, void* stream);
 int rtopk_matrix_destroy(rtopk_matrix* ctx);
 /* As rtopk_last_cuda_error, rtopk_get_launch_count and rtopk_poll_status, for this context. */
 int rtopk_matrix_last_cuda_error(const rtopk_matrix* ctx);

@@ -23,9 +23,10 @@ struct rtopk_matrix {
   int last_cuda_error = 0;
   int64_t scratch_bytes = 0;
   char* scratch = nullptr;
+  bool owns_scratch = false;
   uint32_t* error = nullptr;
   uint32_t* arrived = nullptr;      // of split products, beside the error word
-  uint32_t* parts = nullptr;
+  uint32_t* parts = nullptr;        // partial sums of split products, at the scratch's start
   EncodeTiled encode = nullptr;
   uint64_t launches = 0;
 };
@@ -62,7 +63,9 @@ constexpr int64_t kBatchMax = 65535;
 constexpr int64_t kDepthMax = 131072;     // 127 * 127 * depth stays below 2^31
 
 constexpr int kSplitTiles = 1024;         // tiles of a split product: counters
-constexpr int64_t kPartBytes = kLanes * 256 * 4;       // partial sums of one block: as many parts as there are SMs, at most
+constexpr int64_t kPartBytes = kLanes * 256 * 4;       // partial sums of one block
+constexpr int kPartBlocks = 160;                       // blocks with a part, at most
+constexpr int64_t kPartsBytes = kPartBlocks * kPartBytes;
 constexpr int kErrorBytes = 1024 + 2 * kSplitTiles * 4;
 
 int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
@@ -90,6 +93,7 @@ struct OrthScratch {
   OrthScratch(Carve& c, int64_t batch, int64_t s, int64_t l) {
     ld_x = up(l, 64), ld_a = up(s, 64);
     stride_x = s * ld_x, stride_a = s * ld_a, stride_d = up(s, 64);
+    c.take<char>(kPartsBytes);
     part = c.take<double>(batch * kNormBlocks);
     for (auto& h : hi) h = c.take<__half>(batch * stride_x);
     x = c.take<float>(batch * stride_x);
@@ -109,6 +113,7 @@ struct CodedScratch {
   int64_t ld_in, ld_out, ld_tok;
   CodedScratch(Carve& c, int64_t tokens, int64_t n_out, int64_t n_in) {
     ld_in = up(n_in, 128), ld_out = up(n_out, 128), ld_tok = up(std::max<int64_t>(tokens, 1), 128);
+    c.take<char>(kPartsBytes);
     x_rows = c.take<int8_t>(tokens * ld_in);
     dy_rows = c.take<int8_t>(tokens * ld_out);
     x_cols = c.take<int8_t>(n_in * ld_tok);
@@ -201,7 +206,7 @@ int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, c
   double best = 1e300;
   int which = 0, parts = 1;
   auto consider = [&](int id, int64_t tiles, int cols, int blocks, int stage_bytes) {
-    const int64_t sms = ctx->sms / blocks, all = tiles * g.batch;
+    const int64_t sms = std::min(ctx->sms, kPartBlocks) / blocks, all = tiles * g.batch;
     for (int split = 1; split <= 8; ++split) {
       if (split > 1 && (all * split > sms || steps < 4 * split || all > kSplitTiles)) break;
       if ((split - 1) * ceil_div(steps, split) >= steps) continue;      // a part without any step
@@ -408,10 +413,10 @@ int gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, int64_t
 
 extern "C" {
 
-int rtopk_matrix_create(rtopk_matrix** out, int device, int64_t scratch_bytes) {
+int rtopk_matrix_create(rtopk_matrix** out, int device, void* scratch, int64_t scratch_bytes, void* stream) {
   if (!out) return RTOPK_ERR_INVALID_ARG;
   *out = nullptr;
-  if (scratch_bytes < 0 || device < 0) return RTOPK_ERR_INVALID_ARG;
+  if (scratch_bytes < 0 || device < 0 || !aligned_to(scratch, 256)) return RTOPK_ERR_INVALID_ARG;
   rtopk_matrix* ctx = new (std::nothrow) rtopk_matrix;
   if (!ctx) return RTOPK_ERR_ALLOC;
   ctx->device = device;
@@ -427,19 +432,22 @@ int rtopk_matrix_create(rtopk_matrix** out, int device, int64_t scratch_bytes) {
                              cudaFuncSetAttribute(k_orth_small, cudaFuncAttributeMaxDynamicSharedMemorySize, small_bytes(kSmallLong)) != cudaSuccess))
     status = RTOPK_ERR_CUDA;
   ctx->encode = (EncodeTiled)fn;
-  if (status == RTOPK_OK && (cudaMalloc(&ctx->error, kErrorBytes + ctx->sms * kPartBytes + scratch_bytes) != cudaSuccess ||
-                             cudaMemset(ctx->error, 0, kErrorBytes) != cudaSuccess))
-    status = RTOPK_ERR_ALLOC;
-  if (ctx->error) {
-    ctx->arrived = ctx->error + 64;
-    ctx->parts = ctx->error + kErrorBytes / 4;
-    ctx->scratch = (char*)ctx->parts + ctx->sms * kPartBytes;
+  ctx->scratch = (char*)scratch;
+  if (status == RTOPK_OK) {
+    if (cudaMalloc(&ctx->error, kErrorBytes) != cudaSuccess) status = RTOPK_ERR_ALLOC;
+    else if (cudaMemsetAsync(ctx->error, 0, kErrorBytes, (cudaStream_t)stream) != cudaSuccess) status = RTOPK_ERR_CUDA;
+    else if (!scratch && scratch_bytes) {
+      ctx->owns_scratch = cudaMalloc(&ctx->scratch, scratch_bytes) == cudaSuccess;
+      if (!ctx->owns_scratch) status = RTOPK_ERR_ALLOC;
+    }
   }
   if (status != RTOPK_OK) {
     cudaGetLastError();
     rtopk_matrix_destroy(ctx);
     return status;
   }
+  ctx->arrived = ctx->error + 64;
+  ctx->parts = (uint32_t*)ctx->scratch;
   *out = ctx;
   return RTOPK_OK;
 }
@@ -447,6 +455,7 @@ int rtopk_matrix_create(rtopk_matrix** out, int device, int64_t scratch_bytes) {
 int rtopk_matrix_destroy(rtopk_matrix* ctx) {
   if (!ctx) return RTOPK_OK;
   OnDevice on(ctx->device);
+  if (ctx->owns_scratch) cudaFree(ctx->scratch);
   if (ctx->error) cudaFree(ctx->error);
   delete ctx;
   return RTOPK_OK;

@@ -68,20 +68,30 @@ class MatrixContext:
         self._lib = load_library()
         self._h = None
         self.device = torch.cuda.current_device() if device is None else int(device)
+        self._raw_stream = torch._C._cuda_getCurrentRawStream      # the handle alone: a Stream object takes microseconds
+        # from torch's allocator, which knows the stream that the scratch was made on; others are made known to it as they come
+        self._scratch = torch.empty(scratch_bytes, dtype=torch.uint8, device=f"cuda:{self.device}") if scratch_bytes > 0 else None
+        self._streams = {self._raw_stream(self.device)}
         h = _vp()
-        rc = self._lib.rtopk_matrix_create(C.byref(h), self.device, scratch_bytes)
+        rc = self._lib.rtopk_matrix_create(C.byref(h), self.device, self._scratch.data_ptr() if scratch_bytes > 0 else None,
+                                           scratch_bytes, self._stream())
         if rc != 0:
             raise RTopKError(rc, "rtopk_matrix_create", self._lib.rtopk_status_string(rc).decode())
         self._h = h
-        self._raw_stream = torch._C._cuda_getCurrentRawStream      # the handle alone: a Stream object takes microseconds
 
     def _stream(self) -> int:
-        return self._raw_stream(self.device)
+        s = self._raw_stream(self.device)
+        if s not in self._streams:
+            self._streams.add(s)
+            if self._scratch is not None:
+                self._scratch.record_stream(torch.cuda.current_stream(self.device))
+        return s
 
     def close(self) -> None:
         if getattr(self, "_h", None):
             self._lib.rtopk_matrix_destroy(self._h)
             self._h = None
+            self._scratch = None
 
     def __del__(self):
         try:
