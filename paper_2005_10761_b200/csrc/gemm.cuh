@@ -289,7 +289,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
   // [0] tensor-memory address, [1] give-up word, [2] whether this block came last to a split tile
   volatile uint32_t* words = (volatile uint32_t*)(gen + 16 * kStages + 64);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = kPair ? rank_in_pair() : 0;
+  const uint32_t rank = kPair ? rank_in_cluster() : 0;
   const GiveUp give{words + 1, g.error};
 
   if (threadIdx.x == 0) {
@@ -304,7 +304,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
   }
   if (warp == 1) tmem_alloc<kPair>(smem_addr((const void*)words), kTmemCols);
   tc_fence_before();
-  if (kPair) pair_sync();
+  if (kPair) cluster_sync();
   else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = words[0];
@@ -494,7 +494,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     __syncwarp();
   }
   tc_fence_before();
-  if (kPair) pair_sync();
+  if (kPair) cluster_sync();
   else __syncthreads();
   tc_fence_after();
   if (warp == 1) tmem_free<kPair>(tmem, kTmemCols);

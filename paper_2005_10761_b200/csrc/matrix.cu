@@ -263,6 +263,13 @@ int orthogonal_small(rtopk_matrix* ctx, Source src, const Target& to, int64_t ba
   o.w = to.epi == EPI_UPDATE ? (float*)to.out : nullptr;
   o.out = to.out, o.bf16 = to.bf16, o.ld = to.ld, o.stride = to.stride, o.keep = to.keep, o.rate = to.rate, o.steps = steps;
   for (int i = 0; i < 3 * steps; ++i) o.coef[i] = coef ? coef[i] : kQuintic[i % 3];
+  const int64_t s = std::min(m, n), l = std::max(m, n);
+  if (s > kSmall || l > kSmallLong) {
+    int blocks = 1;
+    while (blocks * kMidChunks * kSmall < l) blocks *= 2;
+    return launch_cluster(ctx, blocks, k_orth_cluster, dim3((unsigned)(batch * blocks)), kMidThreads, kMidBytes, st, src, o, m > n ? 1 : 0,
+                          (int)ceil_div(ceil_div(l, kSmall), blocks), ctx->error);
+  }
   return launch(ctx, k_orth_small, dim3((unsigned)batch), kSmallThreads, small_bytes((int)std::max(m, n)), st, src, o, m > n ? 1 : 0, ctx->error);
 }
 
@@ -272,7 +279,7 @@ int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, i
   Carve c{ctx->scratch};
   OrthScratch w(c, batch, s, l);
   if (c.at > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
-  if (s <= kSmall && l <= kSmallLong) return orthogonal_small(ctx, src, to, batch, m, n, steps, coef, st);
+  if ((s <= kSmall && l <= kSmallLong) || (s <= kMid && l <= kMidLong)) return orthogonal_small(ctx, src, to, batch, m, n, steps, coef, st);
   src.m = (int)m, src.n = (int)n;
   src.part = w.part;
   src.parts = (int)std::min<int64_t>(kNormBlocks, ceil_div(m * ceil_div(n, kNormSpan), 8));
@@ -429,7 +436,8 @@ int rtopk_matrix_create(rtopk_matrix** out, int device, void* scratch, int64_t s
                              found != cudaDriverEntryPointSuccess || cudaDeviceGetAttribute(&ctx->sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
                              allow_smem<EPI_GRAM>() != cudaSuccess || allow_smem<EPI_POLY>() != cudaSuccess || allow_smem<EPI_APPLY>() != cudaSuccess ||
                              allow_smem<EPI_OUT>() != cudaSuccess || allow_smem<EPI_UPDATE>() != cudaSuccess || allow_smem<EPI_CODED>() != cudaSuccess ||
-                             cudaFuncSetAttribute(k_orth_small, cudaFuncAttributeMaxDynamicSharedMemorySize, small_bytes(kSmallLong)) != cudaSuccess))
+                             cudaFuncSetAttribute(k_orth_small, cudaFuncAttributeMaxDynamicSharedMemorySize, small_bytes(kSmallLong)) != cudaSuccess ||
+                             cudaFuncSetAttribute(k_orth_cluster, cudaFuncAttributeMaxDynamicSharedMemorySize, kMidBytes) != cudaSuccess))
     status = RTOPK_ERR_CUDA;
   ctx->encode = (EncodeTiled)fn;
   ctx->scratch = (char*)scratch;

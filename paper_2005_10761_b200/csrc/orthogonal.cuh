@@ -404,5 +404,248 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
   }
 }
 
+// The shorter side at most 128, the longer at most 2048: one cluster of up to eight blocks per matrix, 256 columns of X a block.  A
+// launch for each product would take 5 to 7 us here, most of it for starting and for the first bytes to arrive; in the
+// cluster X never leaves the SMs (in 32 bits in registers, in 16 bits as the products' operand in shared memory), each block
+// forms the polynomial for itself, and only the blocks' shares of the Gram matrix meet, through distributed shared memory: each
+// block adds up its part of the entries in the blocks' order and hands the sum to all.  The arithmetic is that of the
+// product kernel: 16-bit operands, X and the diagonals in 32 bits.
+constexpr int kMid = 128, kMidThreads = 512, kMidChunks = 4, kMidCluster = 8, kMidLong = kMidCluster * kMidChunks * kSmall;
+constexpr int kMidTile = kMid * kDepthBytes;                          // 128 rows of 64 16-bit numbers
+constexpr int kMidPart = kMid * kMid * 4;
+constexpr int kMidBytes = (kMidChunks + 2 + 2) * kMidTile + kMidPart + 1024;      // X, the Gram matrix, the polynomial, the block's share
+
+__global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_constant__ Source s, const __grid_constant__ SmallOut to, int transpose, int chunks, uint32_t* error) {
+  extern __shared__ char mid_smem[];
+  __shared__ double warp_sum[kMidThreads / 32], norms[kMidCluster];
+  __shared__ float gram_d[kMid], poly_d[kMid], row_part[4][kMid], row_sums[kMidCluster][kMid];
+  __shared__ __align__(8) uint64_t done;
+  __shared__ volatile uint32_t words[2];      // tensor-memory address, give-up word
+  uint32_t blocks;
+  asm volatile("mov.u32 %0, %cluster_nctaid.x;" : "=r"(blocks));
+  const uint32_t rank = rank_in_cluster();
+  const int z = blockIdx.x / blocks, t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int ns = transpose ? s.n : s.m, nl = transpose ? s.m : s.n;
+  const uint32_t at_smem = smem_addr(mid_smem), x_at = (at_smem + 1023u) & ~1023u;
+  char* x_tile = mid_smem + (x_at - at_smem);
+  char *g_tile = x_tile + kMidChunks * kMidTile, *b_tile = g_tile + 2 * kMidTile;
+  float4* share = (float4*)(b_tile + 2 * kMidTile);                   // [column / 4][row]
+  const uint32_t g_at = x_at + kMidChunks * kMidTile, b_at = g_at + 2 * kMidTile, share_at = b_at + 2 * kMidTile, bar = smem_addr(&done);
+  const GiveUp give{words + 1, error};
+  if (t == 0) {
+    bar_init(bar, 1);
+    words[1] = 0u;
+    bar_init_fence();
+  }
+  if (warp == 0) tmem_alloc<false>(smem_addr((const void*)words), 512);
+  launch_wait();
+  launch_next();
+  // a thread's part of X: its lane's row, 16 columns of each of the block's chunks
+  const int quarter = warp & 3, group = warp >> 2, row = quarter * 32 + lane;
+  const int col0 = rank * chunks * kSmall + group * 16;
+  const int64_t step_src = transpose ? s.ld : 1, step_v = transpose ? s.v_ld : 1, step_out = transpose ? to.ld : 1;
+  const int64_t at_src = z * s.stride + (transpose ? row : row * s.ld), at_v = z * s.v_stride + (transpose ? row : row * s.v_ld);
+  float x[kMidChunks][16];
+  double sum = 0.0;
+#pragma unroll
+  for (int c = 0; c < kMidChunks; ++c) {
+    const int col = col0 + c * kSmall, n = c < chunks && row < ns ? min(16, nl - col) : 0;
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      x[c][i] = i < n ? source_at(s, at_src + (col + i) * step_src) : 0.f;
+      if (s.v) v[i] = i < n ? s.v[at_v + (col + i) * step_v] : 0.f;
+    }
+    if (s.v)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float nv = fmaf(s.mu, v[i], x[c][i]);
+        if (i < n) s.v[at_v + (col + i) * step_v] = nv;
+        x[c][i] = update_of(s, x[c][i], nv);
+      }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += (double)x[c][i] * (double)x[c][i];
+  }
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  if (lane == 0) warp_sum[warp] = sum;
+  tc_fence_before();
+  cluster_sync();      // every block of the cluster has started
+  tc_fence_after();
+  const uint32_t tmem = words[0];
+  if (t < (int)blocks) {
+    sum = 0.0;
+    for (int i = 0; i < kMidThreads / 32; ++i) sum += warp_sum[i];
+    cluster_store(at_rank(smem_addr(norms + rank), t), sum);
+  }
+  cluster_sync();
+  sum = 0.0;
+  for (uint32_t i = 0; i < blocks; ++i) sum += norms[i];
+  const float inv = sum == 0.0 ? 0.f : (float)((double)kXScale / (sqrt(sum) + (double)s.eps));
+#pragma unroll
+  for (int c = 0; c < kMidChunks; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[c][i] *= inv;
+
+  // Sixteen neighbours of a row of a tile.
+  auto store16 = [&](char* tile, int col, const float* v) {
+    store_half8((__half*)(tile + tile_byte(row, col)), v);
+    store_half8((__half*)(tile + tile_byte(row, col + 8)), v + 8);
+  };
+  auto publish = [&]() {
+    tc_fence_before();
+    smem_publish();
+    __syncthreads();
+    tc_fence_after();
+  };
+  uint32_t phase = 0;
+  auto wait = [&]() {      // a block that gives up goes on, so that the others' barriers are met; its results mean nothing
+    __syncwarp();
+    bar_wait(bar, phase, give);
+    phase ^= 1;
+    __syncwarp();
+    tc_fence_after();
+  };
+  const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
+  const int own = 32 / blocks;      // groups of four columns of the Gram matrix that this block adds up
+  for (int step = 0; step < to.steps; ++step) {
+    const float ca = to.coef[3 * step], cb = to.coef[3 * step + 1], cc = to.coef[3 * step + 2];
+    // X as the products' operand, and the squares of its rows
+    float squares = 0.f;
+#pragma unroll
+    for (int c = 0; c < kMidChunks; ++c) {
+      if (c >= chunks) break;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) squares = fmaf(x[c][i], x[c][i], squares);
+      store16(x_tile + c * kMidTile, group * 16, x[c]);
+    }
+    row_part[group][row] = squares;
+    publish();
+    // the Gram matrix
+    if (t == 0) {
+      constexpr uint32_t kDesc = instr_desc(false, false, kMid, kMid);
+      for (int k = 0; k < 4 * chunks; ++k) {
+        const uint64_t d = smem_desc(x_at + k / 4 * kMidTile, 16) + k % 4 * 2;
+        tc_mma<false, false>(tmem, d, d, kDesc, k > 0);
+      }
+      tc_commit<false>(bar);
+    }
+    if (t >= 32 && t < 32 + (int)(blocks * 16)) {      // eight rows' sums to one block each
+      const uint32_t peer = (t - 32) >> 4;
+      for (int r = ((t - 32) & 15) * 8, e = r + 8; r < e; ++r)
+        cluster_store(at_rank(smem_addr(&row_sums[rank][r]), peer), (row_part[0][r] + row_part[1][r]) + (row_part[2][r] + row_part[3][r]));
+    }
+    wait();
+    {
+      uint32_t acc[32];
+      tmem_load32(from + group * 32, acc);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        share[(group * 8 + i) * kMid + row] =
+            make_float4(__uint_as_float(acc[4 * i]), __uint_as_float(acc[4 * i + 1]), __uint_as_float(acc[4 * i + 2]), __uint_as_float(acc[4 * i + 3]));
+    }
+    tc_fence_before();
+    cluster_sync();
+    for (int i = t; i < own * kMid; i += kMidThreads) {
+      const int col4 = rank * own + i / kMid, r = i % kMid;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (uint32_t p = 0; p < blocks; ++p) {
+        const float4 w = cluster_load4(at_rank(share_at + (col4 * kMid + r) * 16, p));
+        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+      }
+      const int off = r - col4 * 4;      // the diagonal is kept apart
+      __half2 h[2] = {__floats2half2_rn(off == 0 ? 0.f : v.x, off == 1 ? 0.f : v.y), __floats2half2_rn(off == 2 ? 0.f : v.z, off == 3 ? 0.f : v.w)};
+      const uint32_t at = g_at + (col4 / 16) * kMidTile + tile_byte(r, col4 % 16 * 4);
+      for (uint32_t p = 0; p < blocks; ++p) cluster_store(at_rank(at, p), *(uint2*)h);
+    }
+    if (t < kMid) {
+      float d = 0.f;
+      for (uint32_t p = 0; p < blocks; ++p) d += row_sums[p][t];
+      gram_d[t] = d * (1.f / kAScale);
+    }
+    cluster_publish();
+    cluster_sync();
+    cluster_publish();
+    tc_fence_after();
+    // the polynomial
+    if (t == 0) {
+      constexpr uint32_t kDesc = instr_desc(false, false, kMid, kMid);
+      for (int k = 0; k < 8; ++k) {
+        const uint64_t d = smem_desc(g_at + k / 4 * kMidTile, 16) + k % 4 * 2;
+        tc_mma<false, false>(tmem, d, d, kDesc, k > 0);
+      }
+      tc_commit<false>(bar);
+    }
+    wait();
+    {
+      uint32_t acc[32];
+      tmem_load32(from + group * 32, acc);
+      const float dl = gram_d[row];
+#pragma unroll
+      for (int c = 0; c < 32; c += 8) {
+        const int col = group * 32 + c, tile = col / kSmall * kMidTile, at = tile + tile_byte(row, col % kSmall);
+        const uint4 w = *(const uint4*)(g_tile + at);
+        const __half2* g = (const __half2*)&w;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float o = i & 1 ? __high2float(g[i / 2]) : __low2float(g[i / 2]);
+          const float q = __uint_as_float(acc[c + i]) * (1.f / kAScale);
+          v[i] = cc * q + (cb + cc * (dl + gram_d[col + i])) * o;
+          if (row == col + i) {
+            poly_d[row] = ca + cb * dl + cc * (dl * dl + q * (1.f / kAScale));
+            v[i] = 0.f;
+          }
+        }
+        store_half8((__half*)(b_tile + at), v);
+      }
+    }
+    publish();
+    // X <- (that) X
+    if (t == 0) {
+      const uint32_t desc = instr_desc(false, false, kMid, chunks * kSmall, true);
+      for (int k = 0; k < 8; ++k)
+        tc_mma<false, false>(tmem + kMid, smem_desc(b_at + k / 4 * kMidTile, 16) + k % 4 * 2, smem_desc(x_at, kMidTile) + k * (2048 >> 4), desc, k > 0);
+      tc_commit<false>(bar);
+    }
+    wait();
+    const float d = poly_d[row];
+#pragma unroll
+    for (int c = 0; c < kMidChunks; ++c) {
+      if (c >= chunks) break;
+      uint32_t acc[16];
+      tmem_load16(from + kMid + c * kSmall + group * 16, acc);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[c][i] = d * x[c][i] + __uint_as_float(acc[i]) * (1.f / kAScale);
+    }
+  }
+  if (words[1] && t == 0) bar_drain(bar, phase ^ 1);
+  tc_fence_before();
+  cluster_sync();
+  tc_fence_after();
+  if (warp == 0) tmem_free<false>(tmem, 512);
+#pragma unroll
+  for (int c = 0; c < kMidChunks; ++c) {
+    const int col = col0 + c * kSmall, n = c < chunks && row < ns ? min(16, nl - col) : 0;
+    if (n <= 0) continue;
+    const int64_t at = z * to.stride + (transpose ? row : row * to.ld) + col * step_out;
+    if (to.w) {
+      float w[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = i < n ? to.w[at + i * step_out] : 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (i < n) to.w[at + i * step_out] = to.keep * w[i] - to.rate * (x[c][i] * (1.f / kXScale));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (i < n) {
+          const float v = x[c][i] * (1.f / kXScale);
+          if (to.bf16) ((__nv_bfloat16*)to.out)[at + i * step_out] = __float2bfloat16_rn(v);
+          else ((float*)to.out)[at + i * step_out] = v;
+        }
+    }
+  }
+}
+
 }  // namespace mat
 }  // namespace rtopk
