@@ -412,13 +412,14 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
 // product kernel: 16-bit operands, X and the diagonals in 32 bits.
 constexpr int kMid = 128, kMidThreads = 512, kMidChunks = 4, kMidCluster = 8, kMidLong = kMidCluster * kMidChunks * kSmall;
 constexpr int kMidTile = kMid * kDepthBytes;                          // 128 rows of 64 16-bit numbers
-constexpr int kMidPart = kMid * kMid * 4;
+constexpr int kMidPart = kMid * kMid * 4, kMidPitch = kSmall + 1;
 constexpr int kMidBytes = (kMidChunks + 2 + 2) * kMidTile + kMidPart + 1024;      // X, the Gram matrix, the polynomial, the block's share
 
 __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_constant__ Source s, const __grid_constant__ SmallOut to, int transpose, int chunks, uint32_t* error) {
   extern __shared__ char mid_smem[];
   __shared__ double warp_sum[kMidThreads / 32], norms[kMidCluster];
-  __shared__ float gram_d[kMid], poly_d[kMid], row_part[4][kMid], row_sums[kMidCluster][kMid];
+  __shared__ __align__(16) float gram_d[kMid];
+  __shared__ float poly_d[kMid], row_part[4][kMid], row_sums[kMidCluster][kMid];
   __shared__ __align__(8) uint64_t done;
   __shared__ volatile uint32_t words[2];      // tensor-memory address, give-up word
   uint32_t blocks;
@@ -440,31 +441,41 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
   if (warp == 0) tmem_alloc<false>(smem_addr((const void*)words), 512);
   launch_wait();
   launch_next();
-  // a thread's part of X: its lane's row, 16 columns of each of the block's chunks
+  // A thread's part of X: its lane's row, 16 columns of each of the block's chunks.  It comes by way of the tiles' room, where
+  // a chunk takes 128 rows of 65 numbers, so that neighbours of a row of U are read together.
   const int quarter = warp & 3, group = warp >> 2, row = quarter * 32 + lane;
-  const int col0 = rank * chunks * kSmall + group * 16;
-  const int64_t step_src = transpose ? s.ld : 1, step_v = transpose ? s.v_ld : 1, step_out = transpose ? to.ld : 1;
-  const int64_t at_src = z * s.stride + (transpose ? row : row * s.ld), at_v = z * s.v_stride + (transpose ? row : row * s.v_ld);
-  float x[kMidChunks][16];
+  const int col0 = rank * chunks * kSmall;
+  float* stage = (float*)x_tile;
+  auto entry = [&](int c, int i, int& r, int& k) {      // entry i of a thread of chunk c: row and column of X; whether it exists
+    const int e = t + i * kMidThreads;
+    r = transpose ? e & (kMid - 1) : e >> 6, k = transpose ? e >> 7 : e & (kSmall - 1);
+    return r < ns && col0 + c * kSmall + k < nl;
+  };
+  auto offset = [&](int c, int r, int k, int64_t ld) { return transpose ? (int64_t)(col0 + c * kSmall + k) * ld + r : r * ld + col0 + c * kSmall + k; };
   double sum = 0.0;
-#pragma unroll
-  for (int c = 0; c < kMidChunks; ++c) {
-    const int col = col0 + c * kSmall, n = c < chunks && row < ns ? min(16, nl - col) : 0;
-    float v[16];
+#pragma unroll 1
+  for (int c = 0; c < chunks; ++c) {
+    float u[16], v[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      x[c][i] = i < n ? source_at(s, at_src + (col + i) * step_src) : 0.f;
-      if (s.v) v[i] = i < n ? s.v[at_v + (col + i) * step_v] : 0.f;
+      int r, k;
+      const bool in = entry(c, i, r, k);
+      u[i] = source_at(s, z * s.stride + (in ? offset(c, r, k, s.ld) : 0));
+      if (s.v) v[i] = s.v[z * s.v_stride + (in ? offset(c, r, k, s.v_ld) : 0)];
     }
-    if (s.v)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float nv = fmaf(s.mu, v[i], x[c][i]);
-        if (i < n) s.v[at_v + (col + i) * step_v] = nv;
-        x[c][i] = update_of(s, x[c][i], nv);
+    for (int i = 0; i < 16; ++i) {
+      int r, k;
+      const bool in = entry(c, i, r, k);
+      if (s.v) {
+        const float nv = fmaf(s.mu, v[i], u[i]);
+        if (in) s.v[z * s.v_stride + offset(c, r, k, s.v_ld)] = nv;
+        u[i] = update_of(s, u[i], nv);
       }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum += (double)x[c][i] * (double)x[c][i];
+      if (!in) u[i] = 0.f;
+      sum += (double)u[i] * (double)u[i];
+      stage[(c * kMid + r) * kMidPitch + k] = u[i];
+    }
   }
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
   if (lane == 0) warp_sum[warp] = sum;
@@ -481,10 +492,12 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
   sum = 0.0;
   for (uint32_t i = 0; i < blocks; ++i) sum += norms[i];
   const float inv = sum == 0.0 ? 0.f : (float)((double)kXScale / (sqrt(sum) + (double)s.eps));
+  float x[kMidChunks][16];
 #pragma unroll
   for (int c = 0; c < kMidChunks; ++c)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[c][i] *= inv;
+    for (int i = 0; i < 16; ++i) x[c][i] = c < chunks ? stage[(c * kMid + row) * kMidPitch + group * 16 + i] * inv : 0.f;
+  __syncthreads();
 
   // Sixteen neighbours of a row of a tile.
   auto store16 = [&](char* tile, int col, const float* v) {
@@ -529,43 +542,61 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
       }
       tc_commit<false>(bar);
     }
-    if (t >= 32 && t < 32 + (int)(blocks * 16)) {      // eight rows' sums to one block each
-      const uint32_t peer = (t - 32) >> 4;
-      for (int r = ((t - 32) & 15) * 8, e = r + 8; r < e; ++r)
-        cluster_store(at_rank(smem_addr(&row_sums[rank][r]), peer), (row_part[0][r] + row_part[1][r]) + (row_part[2][r] + row_part[3][r]));
-    }
-    wait();
-    {
+    if (blocks == 1) {
+      if (t < kMid) gram_d[t] = ((row_part[0][t] + row_part[1][t]) + (row_part[2][t] + row_part[3][t])) * (1.f / kAScale);
+      wait();
       uint32_t acc[32];
       tmem_load32(from + group * 32, acc);
+      float v[32];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        share[(group * 8 + i) * kMid + row] =
-            make_float4(__uint_as_float(acc[4 * i]), __uint_as_float(acc[4 * i + 1]), __uint_as_float(acc[4 * i + 2]), __uint_as_float(acc[4 * i + 3]));
-    }
-    tc_fence_before();
-    cluster_sync();
-    for (int i = t; i < own * kMid; i += kMidThreads) {
-      const int col4 = rank * own + i / kMid, r = i % kMid;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (uint32_t p = 0; p < blocks; ++p) {
-        const float4 w = cluster_load4(at_rank(share_at + (col4 * kMid + r) * 16, p));
-        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+      for (int i = 0; i < 32; ++i) v[i] = group == quarter && lane == i ? 0.f : __uint_as_float(acc[i]);      // the diagonal is kept apart
+      char* tile = g_tile + group * 32 / kSmall * kMidTile;
+      store16(tile, group * 32 % kSmall, v);
+      store16(tile, group * 32 % kSmall + 16, v + 16);
+      publish();
+    } else {
+      if (t >= 32 && t < 32 + (int)(blocks * 16)) {      // eight rows' sums to one block each
+        const uint32_t peer = (t - 32) >> 4;
+        for (int r = ((t - 32) & 15) * 8, e = r + 8; r < e; ++r)
+          cluster_store(at_rank(smem_addr(&row_sums[rank][r]), peer), (row_part[0][r] + row_part[1][r]) + (row_part[2][r] + row_part[3][r]));
       }
-      const int off = r - col4 * 4;      // the diagonal is kept apart
-      __half2 h[2] = {__floats2half2_rn(off == 0 ? 0.f : v.x, off == 1 ? 0.f : v.y), __floats2half2_rn(off == 2 ? 0.f : v.z, off == 3 ? 0.f : v.w)};
-      const uint32_t at = g_at + (col4 / 16) * kMidTile + tile_byte(r, col4 % 16 * 4);
-      for (uint32_t p = 0; p < blocks; ++p) cluster_store(at_rank(at, p), *(uint2*)h);
+      wait();
+      {
+        uint32_t acc[32];
+        tmem_load32(from + group * 32, acc);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          share[(group * 8 + i) * kMid + row] =
+              make_float4(__uint_as_float(acc[4 * i]), __uint_as_float(acc[4 * i + 1]), __uint_as_float(acc[4 * i + 2]), __uint_as_float(acc[4 * i + 3]));
+      }
+      tc_fence_before();
+      cluster_sync();
+      for (int i = t; i < own * kMid; i += kMidThreads) {
+        const int col4 = rank * own + i / kMid, r = i % kMid;
+        float4 w[kMidCluster], v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (uint32_t p = 0; p < kMidCluster; ++p)
+          if (p < blocks) w[p] = cluster_load4(at_rank(share_at + (col4 * kMid + r) * 16, p));
+#pragma unroll
+        for (uint32_t p = 0; p < kMidCluster; ++p)
+          if (p < blocks) v.x += w[p].x, v.y += w[p].y, v.z += w[p].z, v.w += w[p].w;
+        const int off = r - col4 * 4;      // the diagonal is kept apart
+        __half2 h[2] = {__floats2half2_rn(off == 0 ? 0.f : v.x, off == 1 ? 0.f : v.y), __floats2half2_rn(off == 2 ? 0.f : v.z, off == 3 ? 0.f : v.w)};
+        const uint32_t at = g_at + (col4 / 16) * kMidTile + tile_byte(r, col4 % 16 * 4);
+#pragma unroll
+        for (uint32_t p = 0; p < kMidCluster; ++p)
+          if (p < blocks) cluster_store(at_rank(at, p), *(uint2*)h);
+      }
+      if (t < kMid) {
+        float d = 0.f;
+        for (uint32_t p = 0; p < blocks; ++p) d += row_sums[p][t];
+        gram_d[t] = d * (1.f / kAScale);
+      }
+      cluster_publish();
+      cluster_sync();
+      cluster_publish();
+      tc_fence_after();
     }
-    if (t < kMid) {
-      float d = 0.f;
-      for (uint32_t p = 0; p < blocks; ++p) d += row_sums[p][t];
-      gram_d[t] = d * (1.f / kAScale);
-    }
-    cluster_publish();
-    cluster_sync();
-    cluster_publish();
-    tc_fence_after();
     // the polynomial
     if (t == 0) {
       constexpr uint32_t kDesc = instr_desc(false, false, kMid, kMid);
@@ -579,22 +610,29 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
     {
       uint32_t acc[32];
       tmem_load32(from + group * 32, acc);
-      const float dl = gram_d[row];
+      const float dl = gram_d[row], base = cb + cc * dl, scale = cc * (1.f / kAScale);
+      if (group == quarter) {      // the warps whose columns hold their rows' diagonal
+        float q = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          q = lane == i ? __uint_as_float(acc[i]) : q;
+          acc[i] = lane == i ? 0u : acc[i];      // the Gram matrix holds 0 there too
+        }
+        poly_d[row] = ca + cb * dl + cc * (dl * dl + q * (1.f / (kAScale * kAScale)));
+      }
 #pragma unroll
       for (int c = 0; c < 32; c += 8) {
-        const int col = group * 32 + c, tile = col / kSmall * kMidTile, at = tile + tile_byte(row, col % kSmall);
+        const int col = group * 32 + c, at = col / kSmall * kMidTile + tile_byte(row, col % kSmall);
         const uint4 w = *(const uint4*)(g_tile + at);
         const __half2* g = (const __half2*)&w;
+        const float4 d0 = *(const float4*)(gram_d + col), d1 = *(const float4*)(gram_d + col + 4);
+        const float dc[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float o = i & 1 ? __high2float(g[i / 2]) : __low2float(g[i / 2]);
-          const float q = __uint_as_float(acc[c + i]) * (1.f / kAScale);
-          v[i] = cc * q + (cb + cc * (dl + gram_d[col + i])) * o;
-          if (row == col + i) {
-            poly_d[row] = ca + cb * dl + cc * (dl * dl + q * (1.f / kAScale));
-            v[i] = 0.f;
-          }
+        for (int i = 0; i < 8; i += 2) {
+          const float2 o = __half22float2(g[i / 2]);
+          v[i] = fmaf(scale, __uint_as_float(acc[c + i]), fmaf(cc, dc[i], base) * o.x);
+          v[i + 1] = fmaf(scale, __uint_as_float(acc[c + i + 1]), fmaf(cc, dc[i + 1], base) * o.y);
         }
         store_half8((__half*)(b_tile + at), v);
       }
@@ -624,25 +662,30 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
   tc_fence_after();
   if (warp == 0) tmem_free<false>(tmem, 512);
 #pragma unroll
-  for (int c = 0; c < kMidChunks; ++c) {
-    const int col = col0 + c * kSmall, n = c < chunks && row < ns ? min(16, nl - col) : 0;
-    if (n <= 0) continue;
-    const int64_t at = z * to.stride + (transpose ? row : row * to.ld) + col * step_out;
-    if (to.w) {
-      float w[16];
+  for (int c = 0; c < kMidChunks; ++c)
+    if (c < chunks)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) w[i] = i < n ? to.w[at + i * step_out] : 0.f;
+      for (int i = 0; i < 16; ++i) stage[(c * kMid + row) * kMidPitch + group * 16 + i] = x[c][i] * (1.f / kXScale);
+  __syncthreads();
+#pragma unroll 1
+  for (int c = 0; c < chunks; ++c) {
+    float w[16];
+    if (to.w)
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i < n) to.w[at + i * step_out] = to.keep * w[i] - to.rate * (x[c][i] * (1.f / kXScale));
-    } else {
+      for (int i = 0; i < 16; ++i) {
+        int r, k;
+        const bool in = entry(c, i, r, k);
+        w[i] = to.w[z * to.stride + (in ? offset(c, r, k, to.ld) : 0)];
+      }
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i < n) {
-          const float v = x[c][i] * (1.f / kXScale);
-          if (to.bf16) ((__nv_bfloat16*)to.out)[at + i * step_out] = __float2bfloat16_rn(v);
-          else ((float*)to.out)[at + i * step_out] = v;
-        }
+    for (int i = 0; i < 16; ++i) {
+      int r, k;
+      if (!entry(c, i, r, k)) continue;
+      const float v = stage[(c * kMid + r) * kMidPitch + k];
+      const int64_t at = z * to.stride + offset(c, r, k, to.ld);
+      if (to.w) to.w[at] = to.keep * w[i] - to.rate * v;
+      else if (to.bf16) ((__nv_bfloat16*)to.out)[at] = __float2bfloat16_rn(v);
+      else ((float*)to.out)[at] = v;
     }
   }
 }
