@@ -511,13 +511,13 @@ int rtopk_matrix_poll_status(rtopk_matrix* ctx, void* stream);
  *   src  [in]   batch x m x n of src_dtype;   out [out]  the same shape, out_dtype; may be src itself
  *               when the two views are the same.
  *   steps       1 .. 64;   coef  HOST array of steps triples (a, b, c), or null for
- *               (3.4445, -4.7750, 2.0315) in every step.  Singular values must stay below 4 from step
- *               to step (they do, below 1.3, with the default), else the 16-bit products overflow.
+ *               (3.4445, -4.7750, 2.0315) in every step.  Singular values must stay below 2 from step
+ *               to step (they do, below 1.3, with the default), else 16-bit operands may overflow.
  *   eps         >= 0.  A zero matrix gives zeros; one with a NaN or an infinity gives NaN.
  * The products take 16-bit floating-point operands and 32-bit sums.  X itself and the diagonals of X X^T
  * and of its polynomial are kept in 32 bits beside them: the result is within about 1e-3 of the
  * exact iteration (2-norm of the difference over 2-norm of the result).
- * Errors: INVALID_ARG, UNSUPPORTED (batch above 65535), CUDA.
+ * Errors: INVALID_ARG, UNSUPPORTED (batch above 65535, m above 4194240), CUDA.
  */
 int rtopk_orthogonalize_scratch(int64_t batch, int64_t m, int64_t n, int64_t* bytes);
 int rtopk_orthogonalize(rtopk_matrix* ctx, const void* src, int src_dtype, int64_t ld_src, int64_t stride_src, void* out,
@@ -547,7 +547,8 @@ int rtopk_orthogonal_update(rtopk_matrix* ctx, const float* grad, int64_t ld_g, 
  *   codes   [out]  n_out rows of ld_codes bytes;   scales [out]  n_out binary32;
  *   codes_t [out]  the same codes transposed, n_in rows of ld_t bytes, for the gradient with respect to x;
  *                  may be null.
- * Bases of the code arrays 16-byte aligned, ld_codes and ld_t multiples of 16.  Needs no scratch.
+ * Bases of the code arrays 16-byte aligned, ld_codes and ld_t multiples of 16; bytes past the rows' ends
+ * are left alone.  Needs no scratch.  Errors: INVALID_ARG, UNSUPPORTED (codes_t with n_out above 8388480), CUDA.
  */
 int rtopk_code_weights(rtopk_matrix* ctx, const void* weights, int dtype, int64_t ld_w, int64_t n_out, int64_t n_in,
                        int8_t* codes, int64_t ld_codes, int8_t* codes_t, int64_t ld_t, float* scales, void* stream);

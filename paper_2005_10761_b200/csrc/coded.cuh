@@ -76,6 +76,11 @@ struct Eight<float> {
   __device__ __forceinline__ void widen_to(float (&v)[8]) const {
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
   }
+  __device__ __forceinline__ uint32_t largest(uint32_t m) const {
+    m = max(max(m, magnitude(a.x)), max(magnitude(a.y), max(magnitude(a.z), magnitude(a.w))));
+    return max(max(m, magnitude(b.x)), max(magnitude(b.y), max(magnitude(b.z), magnitude(b.w))));
+  }
+  static __device__ __forceinline__ uint32_t as_magnitude(uint32_t m) { return m; }
 };
 template <>
 struct Eight<__nv_bfloat16> {
@@ -94,6 +99,13 @@ struct Eight<__nv_bfloat16> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }
+  // two 16-bit maxima in a word
+  __device__ __forceinline__ uint32_t largest(uint32_t m) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+    return m;
+  }
+  static __device__ __forceinline__ uint32_t as_magnitude(uint32_t m) { return max(m << 16, m & 0xFFFF0000u); }
 };
 template <class T>
 __device__ __forceinline__ void load8(const T* p, int left, bool vec, float (&v)[8]) {
@@ -147,21 +159,27 @@ k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* 
   }
   uint32_t m = 0;
   float v[8];
+  auto widest = [&](const Eight<T>& e, int c) {
+    if constexpr (kMul) {
+      values(e, c, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = max(m, magnitude(v[j]));
+    } else {
+      m = e.largest(m);
+    }
+  };
 #pragma unroll
   for (int i = 0; i < kKeep; ++i) {
     const int c = i * kSpan + t * 8;
     if (c >= cols) break;
-    values(kept[i], c, v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, magnitude(v[j]));
+    widest(kept[i], c);
   }
   for (int c = kKeep * kSpan + t * 8; c < cols; c += kSpan) {
     Eight<T> e;
     e.load(p + c, cols - c, vec);
-    values(e, c, v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, magnitude(v[j]));
+    widest(e, c);
   }
+  if constexpr (!kMul) m = Eight<T>::as_magnitude(m);
   m = __reduce_max_sync(0xFFFFFFFFu, m);
   if constexpr (kWarps > 1) {
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
@@ -321,7 +339,7 @@ __global__ void __launch_bounds__(256) k_codes_transpose(const int8_t* codes, in
 // codes the tokens for itself (they are small, and come from L2), then each warp takes two output channels at a time: 16 codes
 // of W a thread, four-way integer dot products with the tokens' codes in shared memory.
 constexpr int kFewThreads = 256;
-constexpr int kFewBytes = 48 * 1024;       // codes of all tokens in shared memory, at most
+constexpr int kFewBytes = 47 * 1024;       // codes of all tokens in shared memory, at most (48 KB with the rest)
 __host__ __device__ constexpr int few_row(int n_in) { return (n_in + 511) / 512 * 512; }
 
 template <class T, int kTokens>

@@ -211,7 +211,7 @@ int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, c
       if (split > 1 && (all * split > sms || steps < 4 * split || all > kSplitTiles)) break;
       if ((split - 1) * ceil_div(steps, split) >= steps) continue;      // a part without any step
       const double main = (double)ceil_div(steps, split) * std::max(stage_bytes / 44.0, cols * 2.0) + 500, tail = cols * kColumn;
-      const double t = ceil_div(all * split, sms) * std::max(main, tail) + tail + (split > 1 ? cols * (16.0 + 16.0 * split) + 3000 : 0);
+      const double t = main + tail + (ceil_div(all * split, sms) - 1) * std::max(main, tail) + (split > 1 ? cols * (16.0 + 16.0 * split) + 3000 : 0);
       if (t < best) best = t, which = id, parts = split;
     }
   };
@@ -535,6 +535,7 @@ int rtopk_code_weights(rtopk_matrix* ctx, const void* weights, int dtype, int64_
   if (bad_dtype(dtype) || bad_view(weights, elem(dtype), 1, n_out, n_in, ld_w, 0) || bad_codes(codes, ld_codes, n_in) || (codes_t && bad_codes(codes_t, ld_t, n_out)) ||
       !scales || !aligned_to(scales, 4))
     return RTOPK_ERR_INVALID_ARG;
+  if (codes_t && n_out > 128 * kBatchMax) return RTOPK_ERR_UNSUPPORTED;
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
   cudaStream_t st = (cudaStream_t)stream;

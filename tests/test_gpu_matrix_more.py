@@ -1,0 +1,139 @@
+"""The matrix operators where their kernels change: shapes on both sides of every choice, views far apart in memory, the loop that
+uses them together.  Tolerances as derived in test_gpu_matrix.py."""
+import os
+import sys
+
+import pytest
+import torch
+
+from test_gpu_matrix import U16, code64, matrices, mu_exact, near, orth64, rel, rt, tokens_of  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+# one block, clusters of two to eight, just past them; tall, wide, batched
+EDGES = [(1, 64, 256), (1, 64, 257), (1, 65, 65), (1, 128, 128), (2, 128, 257), (3, 100, 513), (1, 128, 1025), (1, 90, 2048), (1, 2048, 90), (2, 128, 2049),
+         (1, 129, 300), (1, 300, 129), (20, 128, 300), (1, 3, 2000), (1, 512, 512), (2, 1500, 512), (1, 256, 4100)]
+
+
+@pytest.mark.parametrize("batch,m,n", EDGES)
+def test_orthogonalize_at_the_edges(rt, batch, m, n):  # noqa: F811
+    ctx = rt.MatrixContext(rt.orthogonalize_scratch(batch, m, n))
+    for kind in ("gauss", "low"):
+        u = matrices(kind, batch, m, n, 5)
+        out = torch.full((batch, m, n), 7.0, device="cuda")
+        ctx.orthogonalize(u, out)
+        ctx.poll_status()
+        want = orth64(u)
+        for z in range(batch):
+            assert rel(out[z], want[z]) <= 4 * U16, (kind, z)
+    ctx.close()
+
+
+@pytest.mark.parametrize("m,n", [(100, 700), (700, 100), (128, 200), (130, 600)])
+def test_orthogonal_update_at_the_edges(rt, m, n):  # noqa: F811
+    ctx = rt.MatrixContext(rt.orthogonalize_scratch(2, m, n))
+    g, v, w = (matrices(k, 2, m, n, i) * s for i, (k, s) in enumerate((("sparse", 1e-3), ("low", 1e-3), ("gauss", 0.05))))
+    big = torch.zeros((2, m, n + 3), device="cuda")
+    mom = big[..., 1:1 + n]                       # rows that allow no vector loads
+    mom.copy_(v)
+    weights = w.clone()
+    ctx.orthogonal_update(g, mom, weights, 0.02, 0.9, decay=0.1, scale=3.0)
+    v64 = mu_exact(0.9) * v.double() + g.double()
+    assert float((mom.double() - v64).abs().max() / (v64.abs() + g.abs().double()).max()) <= 2.0 ** -23
+    o = orth64(g.double() + mu_exact(0.9) * mom.double())
+    want = w.double() * (1 - 0.02 * 0.1) - 0.02 * 3.0 * o
+    for z in range(2):
+        assert float((weights[z].double() - want[z]).norm()) <= 3 * 2.0 ** -24 * float(want[z].norm()) + 0.02 * 3.0 * 4 * U16 * float(o[z].norm())
+    assert bool((big[..., 0] == 0).all()) and bool((big[..., 1 + n:] == 0).all())
+    ctx.close()
+
+
+def test_matrices_more_than_two_to_the_31_apart(rt):  # noqa: F811
+    m, n, far = 200, 300, (1 << 31) + 72
+    base = torch.empty(far + m * n, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty(far + m * n, dtype=torch.bfloat16, device="cuda")
+    src, dst = (t.as_strided((2, m, n), (far, n, 1)) for t in (base, out))
+    src.copy_(matrices("gauss", 2, m, n).bfloat16())
+    ctx = rt.MatrixContext(max(rt.orthogonalize_scratch(2, m, n), rt.coded_scratch(20, m, n)))
+    ctx.orthogonalize(src, dst)
+    want = orth64(src)
+    for z in range(2):
+        assert rel(dst[z], want[z]) <= 4 * U16 + 2.0 ** -8
+    # two, and twenty, tokens whose rows are that far apart
+    coded = rt.CodedWeights(m, n)
+    w = tokens_of(m, n, 1, torch.float32)
+    ctx.code_weights(w, coded)
+    qw, sw = code64(w, 1)
+    x, y = (t.as_strided((2, k), (far, 1)) for t, k in ((base, n), (out, m)))
+    ctx.coded_product(x, coded, y)
+    qx, sx = code64(x, 1)
+    near(y, (qx @ qw.t()) * sx * sw.t(), torch.bfloat16)
+    dx, dw = torch.empty((2, n), dtype=torch.bfloat16, device="cuda"), torch.empty((m, n), device="cuda")
+    ctx.coded_gradients(y, x, coded, dx, dw)
+    qy, sy = code64(y, 0)
+    qx, sx = code64(x, 0)
+    near(dw, (qy.t() @ qx) * sy.t() * sx, torch.float32)
+    ctx.close()
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 3, 4, 5, 8, 9])
+@pytest.mark.parametrize("n_in,n_out", [(64, 32), (63, 33), (65, 31), (512, 2000), (4099, 4000), (12000, 50), (20000, 500)])
+def test_coded_product_of_few_tokens(rt, tokens, n_in, n_out):  # noqa: F811
+    """One launch, integer matrix instructions and the product kernel meet here."""
+    ctx = rt.MatrixContext(rt.coded_scratch(tokens, n_out, n_in))
+    w, x = tokens_of(n_out, n_in, 1, torch.float32), tokens_of(tokens, n_in, 2, torch.bfloat16)
+    coded = rt.CodedWeights(n_out, n_in, transposed=False)
+    coded.codes.fill_(99)                          # what lies past the rows' ends must not count
+    ctx.code_weights(w, coded)
+    out = torch.zeros((tokens, n_out), dtype=torch.bfloat16, device="cuda")
+    ctx.coded_product(x, coded, out)
+    qx, sx = code64(x, 1)
+    qw, sw = code64(w, 1)
+    near(out, (qx @ qw.t()) * sx * sw.t(), torch.bfloat16)
+    assert n_in == coded.codes.shape[1] or bool((coded.codes[:, n_in:] == 99).all())
+    ctx.close()
+
+
+def test_codes_of_exact_middles_go_to_even(rt):  # noqa: F811
+    """max = 127 gives s = 1: every quotient is the value itself, and halves go to the even neighbour."""
+    v = torch.arange(-254, 255, device="cuda").float() / 2
+    w = torch.stack([v, v.flip(0), v * 2.0 ** -140])          # the last among the subnormal numbers
+    coded = rt.CodedWeights(3, v.numel())
+    ctx = rt.MatrixContext(0)
+    ctx.code_weights(w, coded)
+    q, s = code64(w, 1)
+    assert torch.equal(coded.codes[:, :v.numel()].double(), q) and torch.equal(coded.scales.double(), s.flatten())
+    assert torch.equal(coded.codes[0, :v.numel()].float(), v.round())
+    ctx.close()
+
+
+def test_a_context_on_the_library_s_own_scratch(rt):  # noqa: F811
+    """Through the C interface with scratch = null; a context that is too small refuses and writes nothing."""
+    import ctypes as C
+    lib, h, m, n = rt.load_library(), C.c_void_p(), 300, 400
+    assert lib.rtopk_matrix_create(C.byref(h), 0, None, rt.orthogonalize_scratch(1, m, n), None) == 0
+    u = matrices("gauss", 1, m, n)[0]
+    out = torch.zeros_like(u)
+    torch.cuda.synchronize()
+    call = lambda mm: lib.rtopk_orthogonalize(h, u.data_ptr(), 0, n, 0, out.data_ptr(), 0, n, 0, 1, mm, n, 5, None, 1e-7, None)  # noqa: E731
+    assert call(m) == 0 and lib.rtopk_matrix_poll_status(h, None) == 0
+    assert rel(out, orth64(u)) <= 4 * U16
+    assert lib.rtopk_matrix_destroy(h) == 0
+    assert lib.rtopk_matrix_create(C.byref(h), 0, u.data_ptr() + 4, 1024, None) == 1          # misaligned
+    assert lib.rtopk_matrix_create(C.byref(h), 0, None, -1, None) == 1 and not h.value
+    assert lib.rtopk_matrix_create(None, 0, None, 0, None) == 1
+
+
+def test_the_round_of_the_example_learns():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    sys.path.insert(0, os.path.join(root, "examples"))
+    try:
+        import coded_round
+    finally:
+        sys.path.pop(0)
+    losses = coded_round.train(rounds=60)
+    assert all(v == v for v in losses)
+    # a fit of the teacher, not its variance: the loss of predicting nothing is the starting loss's order
+    assert losses[-1] < 0.35 * losses[0], (losses[0], losses[-1])
+    again = coded_round.train(rounds=5)
+    assert again == losses[:5]                     # every kernel gives the same bits every time
