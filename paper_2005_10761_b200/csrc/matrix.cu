@@ -279,6 +279,7 @@ int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, i
   Carve c{ctx->scratch};
   OrthScratch w(c, batch, s, l);
   if (c.at > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
+  // one launch: 2.7 times as fast as a chain at 128 x 128, 1.3 times at 128 x 2048; beyond, X does not fit a cluster
   if ((s <= kSmall && l <= kSmallLong) || (s <= kMid && l <= kMidLong)) return orthogonal_small(ctx, src, to, batch, m, n, steps, coef, st);
   src.m = (int)m, src.n = (int)n;
   src.part = w.part;
