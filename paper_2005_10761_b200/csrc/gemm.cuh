@@ -328,7 +328,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     }
   };
   uint32_t early = 0;      // stages whose P is under way
-  if (kInt8 && g.p_early && threadIdx.x == 0 && first < total) {
+  if (g.p_early && threadIdx.x == 0 && first < total) {
     const Tile q = tile_at<kCols, S::kTileLanes>(g, first);
     const int k0 = q.part * part_k, n = min(kStages, min(all_k, k0 + part_k) - k0);
     for (; early < (uint32_t)n; ++early) load_p(early, q, k0 + early);
