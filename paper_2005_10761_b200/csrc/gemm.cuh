@@ -292,7 +292,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
   char* gen = smem_raw + (base - smem_addr(smem_raw)) + kStages * S::kStageBytes;
   // [0] tensor-memory address, [1] give-up word, [2] whether this block came last to a split tile
   volatile uint32_t* words = (volatile uint32_t*)(gen + 16 * kStages + 64);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // the same for all of a warp, and known to be
   const uint32_t rank = kPair ? rank_in_cluster() : 0;
   const GiveUp give{words + 1, g.error};
 
@@ -328,39 +328,42 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     }
   };
   uint32_t early = 0;      // stages whose P is under way
-  if (g.p_early && threadIdx.x == 0 && first < total) {
+  if (g.p_early && warp == 0 && first < total) {
     const Tile q = tile_at<kCols, S::kTileLanes>(g, first);
     const int k0 = q.part * part_k, n = min(kStages, min(all_k, k0 + part_k) - k0);
-    for (; early < (uint32_t)n; ++early) load_p(early, q, k0 + early);
+    for (; early < (uint32_t)n; ++early)
+      if (elect_one()) load_p(early, q, k0 + early);
   }
   launch_wait();
   launch_next();
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = true;
-      for (int u = first; u < total && ok; u += step) {
-        const Tile q = tile_at<kCols, S::kTileLanes>(g, u);
-        const int k1 = min(all_k, (q.part + 1) * part_k);
-        for (int kb = q.part * part_k; kb < k1; ++kb, ++it) {
-          const uint32_t s = it % kStages;
-          if (it >= (uint32_t)kStages && !(ok = bar_wait(empty + 8 * s, (it / kStages - 1) & 1, give))) break;
+    uint32_t it = 0;
+    bool ok = true;
+    for (int u = first; u < total && ok; u += step) {
+      const Tile q = tile_at<kCols, S::kTileLanes>(g, u);
+      const int k1 = min(all_k, (q.part + 1) * part_k);
+#pragma unroll 1
+      for (int kb = q.part * part_k; kb < k1; ++kb, ++it) {
+        const uint32_t s = it % kStages;
+        if (it >= (uint32_t)kStages && !(ok = __all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * s, (it / kStages - 1) & 1, give)))) break;
+        if (elect_one()) {
           if (it >= early) load_p(s, q, kb);
           tma_load<kPair>(base + s * S::kStageBytes + S::kPBytes, &map_q, kb * kDepth, q.c * kCols + rank * S::kQRows, q.z, kPair ? first_of_pair(full + 8 * s) : full + 8 * s);
         }
+        __syncwarp();
       }
-      if (!ok) {
-        if (rank == 0) {
-          for (uint32_t k = it > (uint32_t)kStages ? it - kStages : 0; k < it; ++k) bar_drain(full + 8 * (k % kStages), (k / kStages) & 1);
-        } else {      // this block's copies report to the other one: give them time
-          const uint64_t t0 = now_ns();
-          while (now_ns() - t0 < 1000000ull) {}
-        }
+    }
+    if (!ok && lane == 0) {
+      if (rank == 0) {
+        for (uint32_t k = it > (uint32_t)kStages ? it - kStages : 0; k < it; ++k) bar_drain(full + 8 * (k % kStages), (k / kStages) & 1);
+      } else {      // this block's copies report to the other one: give them time
+        const uint64_t t0 = now_ns();
+        while (now_ns() - t0 < 1000000ull) {}
       }
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
       constexpr uint32_t kDesc = instr_desc(kInt8, kMnMajor, S::kTileLanes, kCols);
       uint32_t it = 0, n = 0;
       bool ok = true;
@@ -368,25 +371,32 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
         const Tile q = tile_at<kCols, S::kTileLanes>(g, u);
         const int k0 = q.part * part_k, k1 = min(all_k, k0 + part_k);
         const uint32_t b = n & 1;
-        if (n >= 2 && !(ok = bar_wait(tm_empty + 8 * b, (n / 2 - 1) & 1, give))) break;
+        if (n >= 2 && !(ok = __all_sync(0xFFFFFFFFu, bar_wait(tm_empty + 8 * b, (n / 2 - 1) & 1, give)))) break;
         tc_fence_after();
+#pragma unroll 1
         for (int kb = k0; kb < k1; ++kb, ++it) {
           const uint32_t s = it % kStages;
-          if (!(ok = bar_wait(full + 8 * s, (it / kStages) & 1, give))) break;
+          if (!(ok = __all_sync(0xFFFFFFFFu, bar_wait(full + 8 * s, (it / kStages) & 1, give)))) break;
           tc_fence_after();
           const uint32_t src = base + s * S::kStageBytes;
           // one instruction takes 32 bytes of the contraction index: 16 steps of an MN-major tile are 2048 bytes on
           const uint64_t dp = smem_desc(src, kMnMajor ? S::kPBytes / 2 : 16), dq = smem_desc(src + S::kPBytes, 16);
+          if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            tc_mma<kPair, kInt8>(tmem + b * kCols, dp + (kMnMajor ? k * (2048 >> 4) : k * 2), dq + k * 2, kDesc, kb > k0 || k);
-          tc_commit<kPair>(empty + 8 * s);
+            for (int k = 0; k < 4; ++k)
+              tc_mma<kPair, kInt8>(tmem + b * kCols, dp + (kMnMajor ? k * (2048 >> 4) : k * 2), dq + k * 2, kDesc, kb > k0 || k);
+            tc_commit<kPair>(empty + 8 * s);
+          }
+          __syncwarp();
         }
-        if (ok) tc_commit<kPair>(tm_full + 8 * b);
+        if (ok && elect_one()) tc_commit<kPair>(tm_full + 8 * b);
+        __syncwarp();
       }
       if (!ok) {
-        tc_commit<kPair>(drain);
-        bar_drain(drain, 0);
+        if (elect_one()) {
+          tc_commit<kPair>(drain);
+          bar_drain(drain, 0);
+        }
       }
     }
     __syncwarp();

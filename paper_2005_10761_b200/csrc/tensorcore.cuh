@@ -17,6 +17,15 @@ __device__ __forceinline__ uint64_t now_ns() {
   return t;
 }
 
+// True in one thread of the converged warp, always the same one.  The warps that feed and issue products run their loops whole and let
+// one thread through here, so that addresses and descriptors stay in uniform registers, where these instructions take them
+// from; a loop that one thread runs alone moves each of them there first.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t is;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+  return is != 0;
+}
+
 // ----------------------------------------------------------------------------- mbarriers
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
