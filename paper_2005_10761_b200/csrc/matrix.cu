@@ -210,7 +210,7 @@ int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, c
     for (int split = 1; split <= 8; ++split) {
       if (split > 1 && (all * split > sms || steps < 4 * split || all > kSplitTiles)) break;
       if ((split - 1) * ceil_div(steps, split) >= steps) continue;      // a part without any step
-      const double main = (double)ceil_div(steps, split) * std::max(stage_bytes / 44.0, cols * 2.0) + 500, tail = cols * kColumn;
+      const double main = (double)ceil_div(steps, split) * std::max(stage_bytes / 64.0, cols * 2.0) + 500, tail = cols * kColumn;
       const double t = main + tail + (ceil_div(all * split, sms) - 1) * std::max(main, tail) + (split > 1 ? cols * (16.0 + 16.0 * split) + 3000 : 0);
       if (t < best) best = t, which = id, parts = split;
     }

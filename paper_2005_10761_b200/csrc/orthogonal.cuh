@@ -216,18 +216,21 @@ __device__ __forceinline__ void small_store(char* hi, char* lo, int row, int col
   }
 }
 
-// d (+)= P Q^T, or with kTrans P Q, of one pair of tiles with their low halves.
+// d (+)= P Q^T, or with kTrans P Q, of one pair of tiles with their low halves; by one whole warp.
 template <bool kTrans>
 __device__ __forceinline__ void small_product(uint32_t d, uint32_t p_hi, uint32_t p_lo, uint32_t q_hi, uint32_t q_lo, bool accumulate) {
   constexpr uint32_t kDesc = instr_desc(false, false, 128, kSmall, kTrans);
   constexpr int kStep = kTrans ? 2048 >> 4 : 2;
   const uint64_t ph = smem_desc(p_hi, 16), pl = smem_desc(p_lo, 16), qh = smem_desc(q_hi, kTileBytes), ql = smem_desc(q_lo, kTileBytes);
+  if (elect_one()) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    tc_mma<false, false>(d, pl + k * 2, qh + k * kStep, kDesc, accumulate || k);
-    tc_mma<false, false>(d, ph + k * 2, ql + k * kStep, kDesc, 1);
-    tc_mma<false, false>(d, ph + k * 2, qh + k * kStep, kDesc, 1);
+    for (int k = 0; k < 4; ++k) {
+      tc_mma<false, false>(d, pl + k * 2, qh + k * kStep, kDesc, accumulate || k);
+      tc_mma<false, false>(d, ph + k * 2, ql + k * kStep, kDesc, 1);
+      tc_mma<false, false>(d, ph + k * 2, qh + k * kStep, kDesc, 1);
+    }
   }
+  __syncwarp();
 }
 
 __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_constant__ Source s, const __grid_constant__ SmallOut to, int transpose, uint32_t* error) {
@@ -235,7 +238,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
   __shared__ double part[kSmallThreads / 32];
   __shared__ __align__(8) uint64_t done;
   __shared__ volatile uint32_t words[2];      // tensor-memory address, give-up word
-  const int z = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int z = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = __shfl_sync(0xFFFFFFFFu, t >> 5, 0);
   const int nl = transpose ? s.m : s.n;
   const int chunks = small_chunks(nl), bytes = chunks * kTileBytes;
   const uint32_t at_smem = smem_addr(small_smem), base = (at_smem + 1023u) & ~1023u;
@@ -337,14 +340,14 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
   for (int step = 0; step < to.steps; ++step) {
     const float ca = to.coef[3 * step] * kSmallScale, cb = to.coef[3 * step + 1], cc = to.coef[3 * step + 2] * (1.f / kSmallScale);
     float gram[16], v[16];
-    if (t == 0) {
+    if (warp == 0) {
       for (int c = 0; c < chunks; ++c) {
         const uint32_t at = x + c * kTileBytes;
         small_product<false>(tmem, at, at + bytes, at, at + bytes, c > 0);
       }
-      tc_commit<false>(bar);
+      if (elect_one()) tc_commit<false>(bar);
+      __syncwarp();
     }
-    __syncwarp();
     wait();
     if (works) {
       result(0, gram, 1.f / kSmallScale);
@@ -352,11 +355,11 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
     }
     publish();
     if (failed) break;
-    if (t == 0) {
+    if (warp == 0) {
       small_product<false>(tmem, g, g + kTileBytes, g, g + kTileBytes, false);
-      tc_commit<false>(bar);
+      if (elect_one()) tc_commit<false>(bar);
+      __syncwarp();
     }
-    __syncwarp();
     wait();
     if (works) {
       result(0, v, cc);
@@ -366,11 +369,11 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
     }
     publish();
     if (failed) break;
-    if (t == 0) {
+    if (warp == 0) {
       for (int c = 0; c < chunks; ++c) small_product<true>(tmem + c * kSmall, b, b + kTileBytes, x + c * kTileBytes, x + bytes + c * kTileBytes, false);
-      tc_commit<false>(bar);
+      if (elect_one()) tc_commit<false>(bar);
+      __syncwarp();
     }
-    __syncwarp();
     wait();
     if (works)
       for (int c = 0; c < chunks; ++c) {
@@ -434,7 +437,7 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
   uint32_t blocks;
   asm volatile("mov.u32 %0, %cluster_nctaid.x;" : "=r"(blocks));
   const uint32_t rank = rank_in_cluster();
-  const int z = blockIdx.x / blocks, t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int z = blockIdx.x / blocks, t = threadIdx.x, lane = t & 31, warp = __shfl_sync(0xFFFFFFFFu, t >> 5, 0);
   const int ns = transpose ? s.n : s.m, nl = transpose ? s.m : s.n;
   const uint32_t at_smem = smem_addr(mid_smem), x_at = (at_smem + 1023u) & ~1023u;
   char* x_tile = mid_smem + (x_at - at_smem);
@@ -543,13 +546,17 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
     row_part[group][row] = squares;
     publish();
     // the Gram matrix
-    if (t == 0) {
+    if (warp == 0) {
       constexpr uint32_t kDesc = instr_desc(false, false, kMid, kMid);
-      for (int k = 0; k < 4 * chunks; ++k) {
-        const uint64_t d = smem_desc(x_at + k / 4 * kMidTile, 16) + k % 4 * 2;
-        tc_mma<false, false>(tmem, d, d, kDesc, k > 0);
+      for (int c = 0; c < chunks; ++c) {
+        const uint64_t d = smem_desc(x_at + c * kMidTile, 16);
+        if (elect_one())
+#pragma unroll
+          for (int k = 0; k < 4; ++k) tc_mma<false, false>(tmem, d + k * 2, d + k * 2, kDesc, c > 0 || k);
+        __syncwarp();
       }
-      tc_commit<false>(bar);
+      if (elect_one()) tc_commit<false>(bar);
+      __syncwarp();
     }
     if (blocks == 1) {
       if (t < kMid) gram_d[t] = ((row_part[0][t] + row_part[1][t]) + (row_part[2][t] + row_part[3][t])) * (1.f / kAScale);
@@ -607,13 +614,18 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
       tc_fence_after();
     }
     // the polynomial
-    if (t == 0) {
+    if (warp == 0) {
       constexpr uint32_t kDesc = instr_desc(false, false, kMid, kMid);
-      for (int k = 0; k < 8; ++k) {
-        const uint64_t d = smem_desc(g_at + k / 4 * kMidTile, 16) + k % 4 * 2;
-        tc_mma<false, false>(tmem, d, d, kDesc, k > 0);
+      const uint64_t d = smem_desc(g_at, 16);
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint64_t at = d + k / 4 * (kMidTile >> 4) + k % 4 * 2;
+          tc_mma<false, false>(tmem, at, at, kDesc, k > 0);
+        }
+        tc_commit<false>(bar);
       }
-      tc_commit<false>(bar);
+      __syncwarp();
     }
     wait();
     {
@@ -648,11 +660,15 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
     }
     publish();
     // X <- (that) X
-    if (t == 0) {
+    if (warp == 0) {
       const uint32_t desc = instr_desc(false, false, kMid, chunks * kSmall, true);
-      for (int k = 0; k < 8; ++k)
-        tc_mma<false, false>(tmem + kMid, smem_desc(b_at + k / 4 * kMidTile, 16) + k % 4 * 2, smem_desc(x_at, kMidTile) + k * (2048 >> 4), desc, k > 0);
-      tc_commit<false>(bar);
+      const uint64_t dp = smem_desc(b_at, 16), dq = smem_desc(x_at, kMidTile);
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) tc_mma<false, false>(tmem + kMid, dp + k / 4 * (kMidTile >> 4) + k % 4 * 2, dq + k * (2048 >> 4), desc, k > 0);
+        tc_commit<false>(bar);
+      }
+      __syncwarp();
     }
     wait();
     const float d = poly_d[row];
