@@ -33,7 +33,7 @@ constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
 constexpr int kLanes = 128;                 // rows of an accumulator tile (tensor-memory lanes)
 constexpr int kDepthBytes = 128;            // bytes of the contraction index per stage and row: one swizzle row
 constexpr int kSmemLimit = 227 * 1024;
-constexpr int kSmemMisc = 1024 + 1024;      // alignment slack, barriers
+constexpr int kSmemMisc = 1024 + 2048;      // alignment slack, barriers, the epilogue's columns
 
 // Scales that keep 16-bit entries away from the subnormal range: X is held times 32 and its Gram matrix and the
 // polynomial of it times 1024.  ||X||_F = 1 at the start, so an entry of a 10000 x 1500 X is about 2.6e-4; afterwards
@@ -171,9 +171,19 @@ __device__ __forceinline__ void read_ahead(const Gemm& g, int z, int lane, int c
 // warp's lanes and columns all exist.  `n` of the columns do; loads of lanes that do not read a neighbour's values.
 // `of_lane`: the lane's entry of the diagonal (GRAM: of the result's), or its scale.
 template <int kEpi, bool kFull>
-__device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col0, int n, float of_lane, const Ahead<kEpi>& ahead, const uint32_t (&acc)[32]) {
+__device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col0, int n, float of_lane, float* cols, const Ahead<kEpi>& ahead, const uint32_t (&acc)[32]) {
   const int me = threadIdx.x & 31;
   bool in = kFull || lane < g.lanes;
+  float of_col[kEpi == EPI_GRAM ? 1 : 32];      // every column's number in every thread: by way of the warp's place in shared memory
+  if constexpr (kEpi != EPI_GRAM) {
+    cols[me] = ahead.col;
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 32; c += 4) {
+      const float4 q = *(const float4*)(cols + c);
+      of_col[c] = q.x, of_col[c + 1] = q.y, of_col[c + 2] = q.z, of_col[c + 3] = q.w;
+    }
+  }
   float v[32];
   if constexpr (kEpi == EPI_GRAM || kEpi == EPI_POLY) {
     // Symmetric result: a 128-wide block of columns left of this lane's block is the mirror image of another tile.
@@ -183,9 +193,9 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
 #pragma unroll
       for (int c = 0; c < 32; ++c) v[c] = __uint_as_float(acc[c]);
     } else {
-      const float dl = g.b + g.c * of_lane, dc = g.c * ahead.col, scale = g.c * (1.f / kAScale);
+      const float dl = g.b + g.c * of_lane, scale = g.c * (1.f / kAScale);
 #pragma unroll
-      for (int c = 0; c < 32; ++c) v[c] = scale * __uint_as_float(acc[c]) + (dl + __shfl_sync(0xFFFFFFFFu, dc, c)) * __half2float(ahead.at[c]);
+      for (int c = 0; c < 32; ++c) v[c] = scale * __uint_as_float(acc[c]) + fmaf(g.c, of_col[c], dl) * __half2float(ahead.at[c]);
     }
     if (cb == lb && in && lane >= col0 && lane < col0 + n) {
       float q = 0.f;
@@ -206,7 +216,7 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
     if (cb > lb) store_strip<kFull>(g.h + z * g.stride + col0 * g.ld + lane, n, g.ld, [&](int c) { return to_half(v[c]); });
   } else if constexpr (kEpi == EPI_CODED) {
 #pragma unroll
-    for (int c = 0; c < 32; ++c) v[c] = (float)(int)acc[c] * __shfl_sync(0xFFFFFFFFu, ahead.col, c) * of_lane;
+    for (int c = 0; c < 32; ++c) v[c] = (float)(int)acc[c] * of_col[c] * of_lane;
     if (!in) return;
     const int64_t at = lane + col0 * g.out_col;
     if (g.out_bf16) store_strip<kFull>((__nv_bfloat16*)g.out + at, n, g.out_col, [&](int c) { return __float2bfloat16_rn(v[c]); });
@@ -214,7 +224,7 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
   } else {
     // X' = diag X + offdiag X: the product carries only the part off the diagonal, times kAScale * kXScale
 #pragma unroll
-    for (int c = 0; c < 32; ++c) v[c] = __shfl_sync(0xFFFFFFFFu, ahead.col, c) * (float)ahead.at[c] + __uint_as_float(acc[c]) * (1.f / kAScale);
+    for (int c = 0; c < 32; ++c) v[c] = of_col[c] * (float)ahead.at[c] + __uint_as_float(acc[c]) * (1.f / kAScale);
     if constexpr (kEpi == EPI_APPLY) {
       if (in) {
         if (g.keep_x) store_strip<kFull>(g.x + z * g.stride + col0 * g.ld + lane, n, g.ld, [&](int c) { return v[c]; });
@@ -272,7 +282,7 @@ struct GemmShape {
   static constexpr int kPBytes = kLanes * kDepthBytes, kQBytes = kQRows * kDepthBytes, kStageBytes = kPBytes + kQBytes;
   static constexpr int kFit = (kSmemLimit - kSmemMisc) / kStageBytes;
   static constexpr int kStages = kFit > 8 ? 8 : kFit;
-  static constexpr int kSmem = kStages * kStageBytes + kSmemMisc;
+  static constexpr int kSmem = kStages * kStageBytes + 2048;      // the rest is static
 };
 
 template <int kCols, bool kPair, int kEpi>
@@ -287,6 +297,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
   constexpr uint32_t kTmemCols = 2 * kCols;
 
   extern __shared__ char smem_raw[];
+  __shared__ __align__(16) float epi_cols[kEpiWarps][32];
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
   const uint32_t full = base + kStages * S::kStageBytes, empty = full + 8 * kStages, tm_full = empty + 8 * kStages, tm_empty = tm_full + 16, drain = tm_empty + 16, meet = drain + 8;
   char* gen = smem_raw + (base - smem_addr(smem_raw)) + kStages * S::kStageBytes;
@@ -403,6 +414,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
   } else {
     const int quarter = warp & 3;       // the lanes of tensor memory that this warp may read
     const int chunk0 = (warp - 2) / 4 * 32;
+    float* cols_at = epi_cols[warp - 2];
     uint32_t n = 0, met = 0;
     // all epilogue warps, with the limit of every wait
     auto together = [&]() {
@@ -432,8 +444,8 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
         else read_ahead<kEpi, false>(g, q.z, row, q.c * kCols + c, min(32, cols - c), ahead);
       };
       auto finish = [&](int c, const Ahead<kEpi>& ahead, const uint32_t(&acc)[32]) {
-        if (lanes_full && c + 32 <= cols) epilogue<kEpi, true>(g, q.z, row, q.c * kCols + c, 32, of_lane, ahead, acc);
-        else epilogue<kEpi, false>(g, q.z, row, q.c * kCols + c, min(32, cols - c), of_lane, ahead, acc);
+        if (lanes_full && c + 32 <= cols) epilogue<kEpi, true>(g, q.z, row, q.c * kCols + c, 32, of_lane, cols_at, ahead, acc);
+        else epilogue<kEpi, false>(g, q.z, row, q.c * kCols + c, min(32, cols - c), of_lane, cols_at, ahead, acc);
         __syncwarp();
       };
       Ahead<kEpi> ahead;
