@@ -54,6 +54,7 @@ struct Gemm {
   int batch, tiles_l, tiles_c, tiles;   // tiles per batch entry
   int tri;                   // only tiles that reach the upper triangle (col >= lane)
   int p_early;               // P is not written by the kernel before this one: its first stages are loaded ahead of launch_wait()
+  int free_start;            // nothing here touches what the kernel before this one reads or writes: launch_wait() comes last
   int split;                 // parts of the contraction, 1: whole
   uint32_t* parts;           // split: partial sums, [unit][col][lane]
   uint32_t* arrived;         // split: blocks that have left their part, per tile and block of a pair; zero between launches
@@ -345,8 +346,10 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     for (; early < (uint32_t)n; ++early)
       if (elect_one()) load_p(early, q, k0 + early);
   }
-  launch_wait();
-  launch_next();
+  if (!g.free_start) {
+    launch_wait();
+    launch_next();
+  }
   if (warp == 0) {
     uint32_t it = 0;
     bool ok = true;
@@ -518,6 +521,10 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       }
     }
     __syncwarp();
+  }
+  if (g.free_start) {
+    launch_wait();
+    launch_next();
   }
   tc_fence_before();
   if (kPair) cluster_sync();

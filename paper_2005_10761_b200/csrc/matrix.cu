@@ -187,6 +187,7 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
   g.tiles_l = (int)ceil_div(g.lanes, S::kTileLanes), g.tiles_c = (int)ceil_div(g.cols, kCols);
   g.tiles = (int)gemm_tiles<kCols, kPair>(g);
   g.split = split;
+  if (split > 1) g.free_start = 0;      // the parts' room is the context's
   g.parts = ctx->parts, g.arrived = ctx->arrived, g.error = ctx->error;
   CUtensorMap mp, mq;
   MAT_TRY(tensor_map(ctx, &mp, p.p, kInt8, p.cols, p.rows, g.batch, p.ld, p.stride, kMnMajor ? 64 : kLanes));
@@ -346,13 +347,13 @@ int code_rows(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t
   return go(k_code_rows<T, 8, false>, k_code_rows<T, 8, true>, 8);
 }
 
-int coded_gemm(rtopk_matrix* ctx, bool lanes_early, const int8_t* lane_codes, int64_t ld_lane, const float* lane_scale, int64_t lanes, const int8_t* col_codes, int64_t ld_col,
+int coded_gemm(rtopk_matrix* ctx, bool lanes_early, bool free_start, const int8_t* lane_codes, int64_t ld_lane, const float* lane_scale, int64_t lanes, const int8_t* col_codes, int64_t ld_col,
                const float* col_scale, int64_t cols, int64_t depth, void* out, int bf16, int64_t ld_out, cudaStream_t st) {
   Gemm g = {};
   g.lanes = (int)lanes, g.cols = (int)cols, g.depth = (int)depth, g.batch = 1;
   g.out = out, g.out_bf16 = bf16, g.out_col = ld_out, g.out_lane = 1;
   g.scale_col = col_scale, g.scale_lane = lane_scale;
-  g.p_early = lanes_early;
+  g.p_early = lanes_early, g.free_start = free_start;
   return gemm<EPI_CODED>(ctx, {lane_codes, depth, lanes, ld_lane, 0}, {col_codes, depth, cols, ld_col, 0}, g, st);
 }
 
@@ -392,7 +393,7 @@ int product(rtopk_matrix* ctx, const T* x, int64_t ld_x, const int8_t* codes, in
   if (tokens <= 8)      // above, the product kernel is as fast or faster: 16 tokens through 8192 -> 8192 18.7 us against 19.9
     return launch(ctx, k_product_tokens<T>, dim3((unsigned)ceil_div(n_out, kTokChannels)), kTokThreads, 0, st, w.x_rows, w.ld_in, w.x_row_s, codes, ld_codes, scales, tokens, n_out,
                   n_in, out, ld_out);
-  return coded_gemm(ctx, true, codes, ld_codes, scales, n_out, w.x_rows, w.ld_in, w.x_row_s, tokens, n_in, out, sizeof(T) == 2, ld_out, st);
+  return coded_gemm(ctx, true, false, codes, ld_codes, scales, n_out, w.x_rows, w.ld_in, w.x_row_s, tokens, n_in, out, sizeof(T) == 2, ld_out, st);
 }
 
 template <class T>
@@ -400,10 +401,8 @@ int gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, int64_t
               int64_t n_out, int64_t n_in, T* dx, int64_t ld_dx, void* dw, int dw_dtype, int64_t ld_dw, cudaStream_t st) {
   Carve c{ctx->scratch};
   CodedScratch w(c, tokens, n_out, n_in);
-  if (dx) {
-    MAT_TRY(code_rows(ctx, dy, ld_dy, tokens, n_out, scales, w.dy_rows, w.ld_out, w.dy_row_s, st, 0, w.col_max, dw ? n_in + n_out : 0));
-    MAT_TRY(coded_gemm(ctx, true, codes_t, ld_t, nullptr, n_in, w.dy_rows, w.ld_out, w.dy_row_s, tokens, n_out, dx, sizeof(T) == 2, ld_dx, st));
-  }
+  // All coding first, then both products: the second does not depend on the first and starts as SMs fall free.
+  if (dx) MAT_TRY(code_rows(ctx, dy, ld_dy, tokens, n_out, scales, w.dy_rows, w.ld_out, w.dy_row_s, st, 0, w.col_max, dw ? n_in + n_out : 0));
   if (dw) {
     if (!dx) MAT_CUDA(cudaMemsetAsync(w.col_max, 0, (n_in + n_out) * sizeof(uint32_t), st));
     Columns<T> cx = {x, ld_x, (int)n_in, rows_aligned(x, sizeof(T), 1, ld_x, 0, 16), (int)ceil_div(n_in, 256), w.col_max, w.x_cols, w.x_col_s};
@@ -413,8 +412,10 @@ int gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, int64_t
     MAT_TRY(launch(ctx, k_col_max<T>, dim3((unsigned)across, (unsigned)ceil_div(tokens, per)), 256, 0, st, cx, cy, tokens, per));
     cx.tiles = (int)ceil_div(n_in, 64), cy.tiles = (int)ceil_div(n_out, 64);
     MAT_TRY(launch(ctx, k_code_cols<T>, dim3((unsigned)(cx.tiles + cy.tiles), (unsigned)ceil_div(tokens, 128)), 256, 0, st, cx, cy, tokens, w.ld_tok));
-    MAT_TRY(coded_gemm(ctx, false, w.x_cols, w.ld_tok, w.x_col_s, n_in, w.dy_cols, w.ld_tok, w.dy_col_s, n_out, tokens, dw, dw_dtype == RTOPK_BF16, ld_dw, st));
   }
+  if (dx) MAT_TRY(coded_gemm(ctx, true, false, codes_t, ld_t, nullptr, n_in, w.dy_rows, w.ld_out, w.dy_row_s, tokens, n_out, dx, sizeof(T) == 2, ld_dx, st));
+  if (dw)
+    MAT_TRY(coded_gemm(ctx, false, dx != nullptr, w.x_cols, w.ld_tok, w.x_col_s, n_in, w.dy_cols, w.ld_tok, w.dy_col_s, n_out, tokens, dw, dw_dtype == RTOPK_BF16, ld_dw, st));
   return RTOPK_OK;
 }
 
