@@ -1,21 +1,24 @@
 // The tensor-core product of the matrix operators: D[lane][col] = sum_k P[lane][k] Q[col][k], 16-bit floating point
 // with 32-bit sums or 8-bit integers with 32-bit integer sums, and what is done with D before it leaves the SM.
 //
-// One persistent block per SM, ten warps: one thread feeds a ring of shared-memory stages by TMA, one thread issues
-// the products, eight warps turn finished tiles into results while the next tile is being multiplied (the accumulators
-// lie twice in tensor memory).  D is always laid out so that the 32 lanes of a warp are neighbours in the result's rows:
-// the stores are coalesced without a pass through shared memory.
+// One persistent block per SM, ten warps: one feeds a ring of shared-memory stages by TMA, one issues the products, eight
+// turn finished tiles into results while the next tile is being multiplied (the accumulators lie twice in tensor memory).  D
+// is always laid out so that the 32 lanes of a warp are neighbours in the result's rows: the stores are coalesced without a
+// pass through shared memory.
 //
-// The mainloop is bound by what an SM gets from L2, 78 to 89 bytes a nanosecond (a step of 128 bytes of the contraction index:
-// 0.27 us for 24 KB, 0.41 us for 32 KB), not by the tensor cores: a block of 128 x 256 alone would read 48 KB for 512 cycles'
-// worth of products.  So large products run in pairs of blocks (two SMs, one 256 x kCols tile): each block loads its own 128
-// rows of P and half of Q's rows, and the pair's first block issues the products for both.  Measured: codes 8192 x 4096 by
-// 4096 x 8192 0.19 ms, 2.9 Pop/s; four matrices of 1500 x 6000: Gram product 75 us (70 % of the tensor cores' cycles), product with
-// X 117 us, polynomial 36 us (its two waves of tiles leave a third of the SMs idle).
+// An SM gets 64 bytes a cycle from L2 (a step of 128 bytes of the contraction index: 0.19 us for the 24 KB of a 128-column
+// stage), so a block of 128 x 256 alone would wait for its 48 KB half of the time.  Large products run in pairs of blocks (two SMs,
+// one 256 x kCols tile): each block loads its own 128 rows of P and half of Q's rows, and the pair's first block issues the
+// products for both; 256 columns then take 0.27 to 0.30 us a step, the tensor cores' 512 cycles.  Both figures need the loops of
+// the feeding and the issuing warp to keep their addresses in uniform registers; run by one thread they took 0.31 and 0.41 us.
+//
+// What bounds it: large products the tensor cores, and under load the card's power (codes 8192 x 4096 by 4096 x 8192 0.19 ms, 2.9
+// Pop/s, where a short burst does 3.6); products of one or two waves the first bytes (1.2 us), the results behind the last
+// products (256 columns of X 6 to 8 us: 10 bytes an entry, from and to L2, all SMs at once) and tiles that do not fill the SMs.
 //
 // Small products leave SMs idle with one tile per block; there the contraction is cut into g.split parts, each block leaves its
 // partial sums in scratch, and the block that comes last to a tile adds the parts in their order and goes on as usual (Gram
-// product of 1500 x 10000: 58 us whole, 39 us in three parts).
+// product of 1500 x 10000: 59 us whole, 39 us in three parts).
 #pragma once
 
 #include <cuda_bf16.h>

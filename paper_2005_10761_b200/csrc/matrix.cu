@@ -197,12 +197,12 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
 }
 
 // Which tile, and in how many parts: the one for which this estimate of the time, in cycles, is least.  A step of 128 bytes of
-// the contraction index takes the tensor core's time or what its stage needs from L2 (44 bytes a cycle and SM, measured);
-// the results of a tile take so many cycles a column, beside the next tile's products or, for the last one, after them; parts
+// the contraction index takes the tensor core's time or what its stage needs from L2 (64 bytes a cycle and SM, measured);
+// the results of a tile take so many cycles a column after the last products, six tenths of that beside the next tile's; parts
 // are written and read again.
 template <int kEpi>
 int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, cudaStream_t st) {
-  constexpr double kColumn = kEpi == EPI_CODED ? 25 : kEpi == EPI_GRAM ? 35 : kEpi == EPI_OUT ? 45 : kEpi == EPI_POLY ? 52 : 60;
+  constexpr double kColumn = kEpi == EPI_CODED ? 35 : kEpi == EPI_GRAM || kEpi == EPI_OUT ? 45 : 75;
   const int64_t steps = ceil_div((int64_t)g.depth * (kEpi == EPI_CODED ? 1 : 2), kDepthBytes);
   double best = 1e300;
   int which = 0, parts = 1;
@@ -212,7 +212,7 @@ int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, c
       if (split > 1 && (all * split > sms || steps < 4 * split || all > kSplitTiles)) break;
       if ((split - 1) * ceil_div(steps, split) >= steps) continue;      // a part without any step
       const double main = (double)ceil_div(steps, split) * std::max(stage_bytes / 64.0, cols * 2.0) + 500, tail = cols * kColumn;
-      const double t = main + tail + (ceil_div(all * split, sms) - 1) * std::max(main, tail) + (split > 1 ? cols * (16.0 + 16.0 * split) + 3000 : 0);
+      const double t = main + tail + (ceil_div(all * split, sms) - 1) * std::max(main, 0.6 * tail) + (split > 1 ? cols * (16.0 + 16.0 * split) + 3000 : 0);
       if (t < best) best = t, which = id, parts = split;
     }
   };
