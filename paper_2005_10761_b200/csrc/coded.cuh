@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(256) k_codes_transpose(const int8_t* codes, in
 // A linear layer for a few tokens: reading the codes of W once is all the work, so one launch does everything.  Each block
 // codes the tokens for itself (they are small, and come from L2), then each warp takes two output channels at a time: 16 codes
 // of W a thread, four-way integer dot products with the tokens' codes in shared memory.  One token through 1500 -> 6000: 5.5 us, which is the
-// call itself; through 8192 -> 8192 16.8 us (4.0 TB/s; the tokens' coding comes before the first codes of W).
+// call itself; through 8192 -> 8192 16.9 us (4.0 TB/s; the tokens' coding comes before the first codes of W).
 constexpr int kFewThreads = 256;
 constexpr int kFewBytes = 47 * 1024;       // codes of all tokens in shared memory, at most (48 KB with the rest)
 __host__ __device__ constexpr int few_row(int n_in) { return (n_in + 511) / 512 * 512; }
@@ -423,7 +423,7 @@ k_product_few(const T* x, int64_t ld_x, int vec, const int8_t* codes, int64_t ld
 // tokens x 32 codes) straight from registers.  Reading W is what takes the time here, so nothing of it goes through shared
 // memory: a thread's 16 consecutive codes of a channel are two instructions' operands, in an order of the contraction index that
 // the tokens' codes follow.  The warps' sums meet in shared memory.  Eight tokens through 8192 -> 8192:
-// 17.3 us with the coding launch (3.9 TB/s of codes), through 4096 -> 4096 7.4 us (dot products: 16.0).
+// 17.5 us with the coding launch (3.8 TB/s of codes), through 4096 -> 4096 7.4 us (dot products: 16.0).
 constexpr int kTokThreads = 256, kTokChannels = 32;
 
 __device__ __forceinline__ void mma_codes(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {

@@ -280,7 +280,7 @@ int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, i
   Carve c{ctx->scratch};
   OrthScratch w(c, batch, s, l);
   if (c.at > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
-  // one launch: 2.7 times as fast as a chain at 128 x 128, 1.3 times at 128 x 2048; beyond, X does not fit a cluster
+  // one launch: 2.4 times as fast as a chain at 128 x 128, 1.2 times at 128 x 2048; beyond, X does not fit a cluster
   if ((s <= kSmall && l <= kSmallLong) || (s <= kMid && l <= kMidLong)) return orthogonal_small(ctx, src, to, batch, m, n, steps, coef, st);
   src.m = (int)m, src.n = (int)n;
   src.part = w.part;
@@ -380,7 +380,7 @@ template <class T>
 int product(rtopk_matrix* ctx, const T* x, int64_t ld_x, const int8_t* codes, int64_t ld_codes, const float* scales, int64_t tokens, int64_t n_out, int64_t n_in,
             T* out, int64_t ld_out, cudaStream_t st) {
   // One launch saves 2 us over two, but its dot products take longer than reading W once there are many: 4 tokens through
-  // 1500 -> 6000 6.9 us against 7.5, through 4096 -> 4096 9.2 against 7.4; 8 tokens through 8192 -> 8192 19 against 17.
+  // 1500 -> 6000 6.9 us against 7.5, through 4096 -> 4096 9.2 against 7.4, through 8192 -> 8192 29.7 against 17.5.
   const int64_t few = tokens <= 1 ? 1 : tokens <= 2 ? 2 : 4;
   if (tokens <= 4 && few * few_row((int)n_in) <= kFewBytes && (tokens == 1 || tokens * n_in * n_out <= 40000000)) {
     if (few == 1) return product_few<T, 1>(ctx, x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, out, ld_out, st);
@@ -390,7 +390,9 @@ int product(rtopk_matrix* ctx, const T* x, int64_t ld_x, const int8_t* codes, in
   Carve c{ctx->scratch};
   CodedScratch w(c, tokens, n_out, n_in);
   MAT_TRY(code_rows(ctx, x, ld_x, tokens, n_in, nullptr, w.x_rows, w.ld_in, w.x_row_s, st, w.ld_in));
-  if (tokens <= 8)      // above, the product kernel is as fast or faster: 16 tokens through 8192 -> 8192 18.7 us against 19.9
+  // 8 tokens through 4096 -> 4096 7.4 us, the product kernel 9.2 (both 17.5 through 8192 -> 8192); with 16 tokens the product
+  // kernel is the faster one, 17.5 against 19.9.
+  if (tokens <= 8)
     return launch(ctx, k_product_tokens<T>, dim3((unsigned)ceil_div(n_out, kTokChannels)), kTokThreads, 0, st, w.x_rows, w.ld_in, w.x_row_s, codes, ld_codes, scales, tokens, n_out,
                   n_in, out, ld_out);
   return coded_gemm(ctx, true, false, codes, ld_codes, scales, n_out, w.x_rows, w.ld_in, w.x_row_s, tokens, n_in, out, sizeof(T) == 2, ld_out, st);
