@@ -498,6 +498,14 @@ typedef struct rtopk_matrix rtopk_matrix;
 
 int rtopk_matrix_create(rtopk_matrix** out, int device, void* scratch, int64_t scratch_bytes, void* stream);
 int rtopk_matrix_destroy(rtopk_matrix* ctx);
+/* rtopk_matrix_set_option keys */
+enum {
+  RTOPK_MATRIX_OPT_TEST_GIVEUP = 0 /* for tests of the give-up path only: 1 = the blocks of every tensor-core kernel behave
+                                as if a wait had run out.  The call still returns, copies and products in flight are
+                                waited for, nothing outside the caller's buffers is written, what is written in them is
+                                meaningless, and rtopk_matrix_poll_status reports RTOPK_ERR_INTERNAL.  0 = off */
+};
+int rtopk_matrix_set_option(rtopk_matrix* ctx, int option, int64_t value);
 /* As rtopk_last_cuda_error, rtopk_get_launch_count and rtopk_poll_status, for this context. */
 int rtopk_matrix_last_cuda_error(const rtopk_matrix* ctx);
 int rtopk_matrix_get_launch_count(const rtopk_matrix* ctx, uint64_t* out);

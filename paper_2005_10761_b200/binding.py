@@ -72,6 +72,7 @@ EXPORTS = {
     "rtopk_get_launch_count": (_int, [_vp, _vp]),
     "rtopk_matrix_create": (_int, [C.POINTER(_vp), _int, _vp, _i64, _vp]),
     "rtopk_matrix_destroy": (_int, [_vp]),
+    "rtopk_matrix_set_option": (_int, [_vp, _int, _i64]),
     "rtopk_matrix_last_cuda_error": (_int, [_vp]),
     "rtopk_matrix_get_launch_count": (_int, [_vp, _vp]),
     "rtopk_matrix_poll_status": (_int, [_vp, _vp]),

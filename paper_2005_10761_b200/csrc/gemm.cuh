@@ -61,6 +61,7 @@ struct Gemm {
   int split;                 // parts of the contraction, 1: whole
   uint32_t* parts;           // split: partial sums, [unit][col][lane]
   uint32_t* arrived;         // split: blocks that have left their part, per tile and block of a pair; zero between launches
+  int test_giveup;           // tests only: the first wait for a stage counts as run out
   uint32_t* error;
   // epilogue operands
   const __half* o;           // POLY: A off the diagonal; OUT / UPDATE: X
@@ -342,6 +343,9 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       tma_load<kPair>(dst, &map_p, kb * kDepth, row, q.z, bar);
     }
   };
+  auto tell_pair = [&]() {      // the other block's roles look at its own word
+    if (kPair) cluster_store(at_rank(smem_addr((const void*)(words + 1)), rank ^ 1), 1u);
+  };
   uint32_t early = 0;      // stages whose P is under way
   if (g.p_early && warp == 0 && first < total) {
     const Tile q = tile_at<kCols, S::kTileLanes>(g, first);
@@ -371,6 +375,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       }
     }
     if (!ok && lane == 0) {
+      tell_pair();
       if (rank == 0) {
         for (uint32_t k = it > (uint32_t)kStages ? it - kStages : 0; k < it; ++k) bar_drain(full + 8 * (k % kStages), (k / kStages) & 1);
       } else {      // this block's copies report to the other one: give them time
@@ -383,7 +388,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     if (rank == 0) {
       constexpr uint32_t kDesc = instr_desc(kInt8, kMnMajor, S::kTileLanes, kCols);
       uint32_t it = 0, n = 0;
-      bool ok = true;
+      bool ok = !g.test_giveup || give_up(give);
       for (int u = first; u < total && ok; u += step, ++n) {
         const Tile q = tile_at<kCols, S::kTileLanes>(g, u);
         const int k0 = q.part * part_k, k1 = min(all_k, k0 + part_k);
@@ -411,6 +416,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       }
       if (!ok) {
         if (elect_one()) {
+          tell_pair();
           tc_commit<kPair>(drain);
           bar_drain(drain, 0);
         }

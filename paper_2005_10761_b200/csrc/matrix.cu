@@ -29,6 +29,7 @@ struct rtopk_matrix {
   uint32_t* parts = nullptr;        // partial sums of split products, at the scratch's start
   EncodeTiled encode = nullptr;
   uint64_t launches = 0;
+  int test_giveup = 0;              // RTOPK_MATRIX_OPT_TEST_GIVEUP
 };
 
 namespace {
@@ -187,6 +188,7 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
   g.tiles_l = (int)ceil_div(g.lanes, S::kTileLanes), g.tiles_c = (int)ceil_div(g.cols, kCols);
   g.tiles = (int)gemm_tiles<kCols, kPair>(g);
   g.split = split;
+  g.test_giveup = ctx->test_giveup;
   if (split > 1) g.free_start = 0;      // the parts' room is the context's
   g.parts = ctx->parts, g.arrived = ctx->arrived, g.error = ctx->error;
   CUtensorMap mp, mq;
@@ -262,6 +264,7 @@ int orthogonal_small(rtopk_matrix* ctx, Source src, const Target& to, int64_t ba
   src.m = (int)m, src.n = (int)n;
   SmallOut o = {};
   o.w = to.epi == EPI_UPDATE ? (float*)to.out : nullptr;
+  o.test_giveup = ctx->test_giveup;
   o.out = to.out, o.bf16 = to.bf16, o.ld = to.ld, o.stride = to.stride, o.keep = to.keep, o.rate = to.rate, o.steps = steps;
   for (int i = 0; i < 3 * steps; ++i) o.coef[i] = coef ? coef[i] : kQuintic[i % 3];
   const int64_t s = std::min(m, n), l = std::max(m, n);
@@ -471,6 +474,12 @@ int rtopk_matrix_destroy(rtopk_matrix* ctx) {
   if (ctx->owns_scratch) cudaFree(ctx->scratch);
   if (ctx->error) cudaFree(ctx->error);
   delete ctx;
+  return RTOPK_OK;
+}
+
+int rtopk_matrix_set_option(rtopk_matrix* ctx, int option, int64_t value) {
+  if (!ctx || option != RTOPK_MATRIX_OPT_TEST_GIVEUP || (value != 0 && value != 1)) return RTOPK_ERR_INVALID_ARG;
+  ctx->test_giveup = (int)value;
   return RTOPK_OK;
 }
 

@@ -190,6 +190,7 @@ struct SmallOut {
   float keep, rate;
   float coef[3 * 64];
   int steps;
+  int test_giveup;         // tests only: every wait for a product counts as run out
 };
 
 __host__ __device__ constexpr int small_chunks(int nl) { return (nl + kSmall - 1) / kSmall; }
@@ -236,7 +237,7 @@ __device__ __forceinline__ void small_product(uint32_t d, uint32_t p_hi, uint32_
 __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_constant__ Source s, const __grid_constant__ SmallOut to, int transpose, uint32_t* error) {
   extern __shared__ char small_smem[];
   __shared__ double part[kSmallThreads / 32];
-  __shared__ __align__(8) uint64_t done;
+  __shared__ __align__(8) uint64_t done, drain;
   __shared__ volatile uint32_t words[2];      // tensor-memory address, give-up word
   const int z = blockIdx.x, t = threadIdx.x, lane = t & 31, warp = __shfl_sync(0xFFFFFFFFu, t >> 5, 0);
   const int nl = transpose ? s.m : s.n;
@@ -249,6 +250,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
   const GiveUp give{words + 1, error};
   if (t == 0) {
     bar_init(bar, 1);
+    bar_init(smem_addr(&drain), 1);
     words[1] = 0u;
     bar_init_fence();
   }
@@ -326,7 +328,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
   };
   auto wait = [&]() {
     if (works) {
-      if (!__all_sync(0xFFFFFFFFu, bar_wait(bar, phase, give))) failed = true;
+      if (!__all_sync(0xFFFFFFFFu, to.test_giveup ? give_up(give) : bar_wait(bar, phase, give))) failed = true;
       tc_fence_after();
     }
     phase ^= 1;
@@ -384,7 +386,10 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
     if (failed) break;
   }
   if (failed) {
-    if (t == 0) bar_drain(bar, phase ^ 1);
+    if (warp == 0 && elect_one()) {
+      tc_commit<false>(smem_addr(&drain));
+      bar_drain(smem_addr(&drain), 0);
+    }
     __syncthreads();
   }
   if (warp == 0) tmem_free<false>(tmem, tmem_cols);
@@ -432,7 +437,7 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
   __shared__ double warp_sum[kMidThreads / 32], norms[kMidCluster];
   __shared__ __align__(16) float gram_d[kMid];
   __shared__ float poly_d[kMid], row_part[4][kMid], row_sums[kMidCluster][kMid];
-  __shared__ __align__(8) uint64_t done;
+  __shared__ __align__(8) uint64_t done, drain;
   __shared__ volatile uint32_t words[2];      // tensor-memory address, give-up word
   uint32_t blocks;
   asm volatile("mov.u32 %0, %cluster_nctaid.x;" : "=r"(blocks));
@@ -447,6 +452,7 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
   const GiveUp give{words + 1, error};
   if (t == 0) {
     bar_init(bar, 1);
+    bar_init(smem_addr(&drain), 1);
     words[1] = 0u;
     bar_init_fence();
   }
@@ -525,6 +531,7 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
   uint32_t phase = 0;
   auto wait = [&]() {      // a block that gives up goes on, so that the others' barriers are met; its results mean nothing
     __syncwarp();
+    if (to.test_giveup) give_up(give);
     bar_wait(bar, phase, give);
     phase ^= 1;
     __syncwarp();
@@ -681,7 +688,11 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
       for (int i = 0; i < 16; ++i) x[c][i] = d * x[c][i] + __uint_as_float(acc[i]) * (1.f / kAScale);
     }
   }
-  if (words[1] && t == 0) bar_drain(bar, phase ^ 1);
+  __syncwarp();
+  if (words[1] && warp == 0 && elect_one()) {
+    tc_commit<false>(smem_addr(&drain));
+    bar_drain(smem_addr(&drain), 0);
+  }
   tc_fence_before();
   cluster_sync();
   tc_fence_after();

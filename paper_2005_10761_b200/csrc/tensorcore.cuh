@@ -56,6 +56,7 @@ __device__ __forceinline__ float4 cluster_load4(uint32_t addr) {
 }
 __device__ __forceinline__ void cluster_store(uint32_t addr, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
 __device__ __forceinline__ void cluster_store(uint32_t addr, double v) { asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory"); }
+__device__ __forceinline__ void cluster_store(uint32_t addr, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ void cluster_store(uint32_t addr, uint2 v) {
   asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory");
 }
@@ -93,6 +94,12 @@ struct GiveUp {
   uint32_t* error;           // in the context
 };
 
+// What a wait that has run out does; for tests, at a wait that has not.
+__device__ __forceinline__ bool give_up(const GiveUp& g) {
+  *g.word = 1u;
+  atomicOr(g.error, MAT_ERR_WAIT);
+  return false;
+}
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const GiveUp& g) {
   if (bar_try(bar, parity)) return true;
   const uint64_t t0 = now_ns();
@@ -100,11 +107,7 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const Gi
     if (bar_try(bar, parity)) return true;
     if ((n & 63u) == 0) {
       if (*g.word) return false;
-      if (now_ns() - t0 > kWaitNs) {
-        *g.word = 1u;
-        atomicOr(g.error, MAT_ERR_WAIT);
-        return false;
-      }
+      if (now_ns() - t0 > kWaitNs) return give_up(g);
     }
   }
 }

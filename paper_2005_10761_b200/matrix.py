@@ -202,6 +202,9 @@ class MatrixContext:
                                              coded.n_in, pdx, lddx, pdw, wt, lddw, self._stream())
         self._check(rc, "rtopk_coded_gradients")
 
+    def set_option(self, option: int, value: int) -> None:
+        self._check(self._lib.rtopk_matrix_set_option(self._h, option, value), "rtopk_matrix_set_option")
+
     def poll_status(self) -> None:
         self._check(self._lib.rtopk_matrix_poll_status(self._h, self._stream()), "rtopk_matrix_poll_status")
 

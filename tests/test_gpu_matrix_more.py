@@ -137,3 +137,53 @@ def test_the_round_of_the_example_learns():
     assert losses[-1] < 0.35 * losses[0], (losses[0], losses[-1])
     again = coded_round.train(rounds=5)
     assert again == losses[:5]                     # every kernel gives the same bits every time
+
+
+def test_blocks_that_give_up_say_so_and_leave_everything_in_order(rt):  # noqa: F811
+    """Every kernel with waits: one block, a cluster, the chain, products whole and in parts.  What lies around the results stays,
+    the status says INTERNAL once, and the next call on the same context is right."""
+    shapes = [(60, 60), (100, 900), (200, 1500)]
+    t, k, n = 300, 500, 400
+    ctx = rt.MatrixContext(max([rt.orthogonalize_scratch(1, a, b) for a, b in shapes] + [rt.coded_scratch(t, n, k)]))
+    coded = rt.CodedWeights(n, k)
+    w, x = tokens_of(n, k, 1, torch.float32), tokens_of(t, k, 2, torch.float32)
+    ctx.code_weights(w, coded)
+    for on in (1, 0):
+        ctx.set_option(0, on)
+        for a, b in shapes:
+            u = matrices("gauss", 1, a, b)[0]
+            out = torch.full((a + 2, b + 6), 9.0, device="cuda")
+            ctx.orthogonalize(u, out[1:1 + a, 3:3 + b])
+            got = out[1:1 + a, 3:3 + b].clone()
+            out[1:1 + a, 3:3 + b] = 9.0
+            assert bool((out == 9.0).all())
+            if on:
+                with pytest.raises(rt.RTopKError) as e:
+                    ctx.poll_status()
+                assert e.value.status == 5
+            else:
+                ctx.poll_status()
+                assert rel(got, orth64(u)) <= 4 * U16
+        y = torch.full((t + 2, n + 6), 9.0, device="cuda")
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        ctx.coded_product(x, coded, y[1:1 + t, 3:3 + n])
+        got = y[1:1 + t, 3:3 + n].clone()
+        y[1:1 + t, 3:3 + n] = 9.0
+        assert bool((y == 9.0).all())
+        ctx.coded_gradients(got, x, coded, dx, dw)
+        if on:
+            with pytest.raises(rt.RTopKError) as e:
+                ctx.poll_status()
+            assert e.value.status == 5
+            ctx.poll_status()
+        else:
+            ctx.poll_status()
+            qx, sx = code64(x, 1)
+            qw, sw = code64(w, 1)
+            near(got, (qx @ qw.t()) * sx * sw.t(), torch.float32)
+            qy, sy = code64(got, 0)
+            qx, sx = code64(x, 0)
+            near(dw, (qy.t() @ qx) * sy.t() * sx, torch.float32)
+    with pytest.raises(rt.RTopKError):
+        ctx.set_option(0, 2)
+    ctx.close()
