@@ -465,69 +465,65 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       if (!__all_sync(0xFFFFFFFFu, bar_wait(tm_full + 8 * b, (n / 2) & 1, give))) break;
       tc_fence_after();
       const uint32_t from = tmem + b * kCols + ((uint32_t)(quarter * 32) << 16);
-      if (g.split == 1) {
-#pragma unroll 1
-        for (int c = chunk0; c < cols; c += kNext) {
-          uint32_t acc[32];
-          tmem_load32(from + c, acc);
-          Ahead<kEpi> next;
-          read(c + kNext, next);
-          finish(c, ahead, acc);
-          ahead = next;
-        }
+      auto leave_tile = [&]() {      // its room in tensor memory may be filled again
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
           if (kPair) bar_arrive_cluster(first_of_pair(tm_empty + 8 * b));
           else bar_arrive(tm_empty + 8 * b);
         }
-        continue;
-      }
+      };
       const int64_t part_words = (int64_t)kCols * S::kTileLanes;
-      uint32_t* mine = g.parts + u * part_words + rank * kLanes + in_tile;
-#pragma unroll 1
-      for (int c = chunk0; c < cols; c += kNext) {
-        uint32_t acc[32];
-        tmem_load32(from + c, acc);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) mine[(c + i) * S::kTileLanes] = acc[i];
-      }
-      tc_fence_before();
-      __threadfence();
-      if (!together()) break;
-      if (warp == 2 && lane == 0) {
-        uint32_t* seen = g.arrived + (u / g.split) * kBlocks + rank;
-        const uint32_t before = atomicAdd(seen, 1u);
-        if (before + 1 == (uint32_t)g.split) *seen = 0u;
-        words[2] = before + 1 == (uint32_t)g.split;
-      }
-      if (!together()) break;
-      const bool last = words[2] != 0u;
-      if (lane == 0) {
-        if (kPair) bar_arrive_cluster(first_of_pair(tm_empty + 8 * b));
-        else bar_arrive(tm_empty + 8 * b);
-      }
-      if (!together()) break;      // words[2] may change from here on
-      if (!last) continue;
-      __threadfence();
       const uint32_t* parts = g.parts + (u - q.part) * part_words + rank * kLanes + in_tile;
+      if (g.split > 1) {
+        uint32_t* mine = g.parts + u * part_words + rank * kLanes + in_tile;
+#pragma unroll 1
+        for (int c = chunk0; c < cols; c += kNext) {
+          uint32_t acc[32];
+          tmem_load32(from + c, acc);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) mine[(c + i) * S::kTileLanes] = acc[i];
+        }
+        leave_tile();
+        __threadfence();
+        if (!together()) break;
+        if (warp == 2 && lane == 0) {
+          uint32_t* seen = g.arrived + (u / g.split) * kBlocks + rank;
+          const uint32_t before = atomicAdd(seen, 1u);
+          if (before + 1 == (uint32_t)g.split) *seen = 0u;
+          words[2] = before + 1 == (uint32_t)g.split;
+        }
+        if (!together()) break;
+        const bool last = words[2] != 0u;
+        if (!together()) break;      // words[2] may change from here on
+        if (!last) continue;
+        __threadfence();
+      }
 #pragma unroll 1
       for (int c = chunk0; c < cols; c += kNext) {
         uint32_t acc[32];
+        if (g.split == 1) {
+          tmem_load32(from + c, acc);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) acc[i] = __ldcg(parts + (c + i) * S::kTileLanes);
-        for (int k = 1; k < g.split; ++k) {
-          const uint32_t* next = parts + k * part_words;
-          uint32_t w[32];
+          for (int i = 0; i < 32; ++i) acc[i] = __ldcg(parts + (c + i) * S::kTileLanes);
+#pragma unroll 1
+          for (int k = 1; k < g.split; ++k) {
+            const uint32_t* next = parts + k * part_words;
+            uint32_t w[32];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) w[i] = __ldcg(next + (c + i) * S::kTileLanes);
+            for (int i = 0; i < 32; ++i) w[i] = __ldcg(next + (c + i) * S::kTileLanes);
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            acc[i] = kInt8 ? acc[i] + w[i] : __float_as_uint(__uint_as_float(acc[i]) + __uint_as_float(w[i]));
+            for (int i = 0; i < 32; ++i)
+              acc[i] = kInt8 ? acc[i] + w[i] : __float_as_uint(__uint_as_float(acc[i]) + __uint_as_float(w[i]));
+          }
         }
-        if (c > chunk0) read(c, ahead);
+        Ahead<kEpi> next;
+        read(c + kNext, next);
         finish(c, ahead, acc);
+        ahead = next;
       }
+      if (g.split == 1) leave_tile();
     }
     __syncwarp();
   }
