@@ -335,6 +335,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
   auto load_p = [&](uint32_t s, const Tile& q, int kb) {
     const uint32_t dst = base + s * S::kStageBytes, bar = kPair ? first_of_pair(full + 8 * s) : full + 8 * s;
     const int row = q.l * S::kTileLanes + rank * kLanes;
+    if (rank == 0) bar_expect(full + 8 * s, kBlocks * S::kStageBytes);
     if (kMnMajor) {
       tma_load<kPair>(dst, &map_p, row, kb * kDepth, q.z, bar);
       tma_load<kPair>(dst + S::kPBytes / 2, &map_p, row + 64, kb * kDepth, q.z, bar);
@@ -350,10 +351,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     const Tile q = tile_at<kCols, S::kTileLanes>(g, first);
     const int k0 = q.part * part_k, n = min(kStages, min(all_k, k0 + part_k) - k0);
     for (; early < (uint32_t)n; ++early)
-      if (elect_one()) {
-        if (rank == 0) bar_expect(full + 8 * early, kBlocks * S::kStageBytes);
-        load_p(early, q, k0 + early);
-      }
+      if (elect_one()) load_p(early, q, k0 + early);
   }
   // Each role waits for the kernel before this one only where it first needs to: what leads there, and the instructions it
   // takes, are behind it by then.
@@ -367,12 +365,11 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     for (int u = first; u < total && ok; u += step) {
       const Tile q = tile_at<kCols, S::kTileLanes>(g, u);
       const int k1 = min(all_k, (q.part + 1) * part_k);
+      if (it == 0 && !g.free_start) follow();
 #pragma unroll 1
       for (int kb = q.part * part_k; kb < k1; ++kb, ++it) {
         const uint32_t s = it % kStages;
         if (it >= (uint32_t)kStages && !(ok = __all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * s, (it / kStages - 1) & 1, give)))) break;
-        if (rank == 0 && it >= early && elect_one()) bar_expect(full + 8 * s, kBlocks * S::kStageBytes);
-        if (it == 0 && !g.free_start) follow();
         if (elect_one()) {
           if (it >= early) load_p(s, q, kb);
           tma_load<kPair>(base + s * S::kStageBytes + S::kPBytes, &map_q, kb * kDepth, q.c * kCols + rank * S::kQRows, q.z, kPair ? first_of_pair(full + 8 * s) : full + 8 * s);
@@ -416,10 +413,10 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
             tc_commit<kPair>(empty + 8 * s);
           }
           __syncwarp();
-          if (it == 0 && !g.free_start) follow();
         }
         if (ok && elect_one()) tc_commit<kPair>(tm_full + 8 * b);
         __syncwarp();
+        if (n == 0 && !g.free_start) follow();
       }
       if (!ok) {
         if (elect_one()) {
