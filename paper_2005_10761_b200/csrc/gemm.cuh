@@ -13,8 +13,10 @@
 // the feeding and the issuing warp to keep their addresses in uniform registers; run by one thread they took 0.31 and 0.41 us.
 //
 // What bounds it: large products the tensor cores, and under load the card's power (codes 8192 x 4096 by 4096 x 8192 0.19 ms, 2.9
-// Pop/s, where a short burst does 3.6); products of one or two waves the first bytes (1.2 us), the results behind the last
-// products (256 columns of X 6 to 8 us: 10 bytes an entry, from and to L2, all SMs at once) and tiles that do not fill the SMs.
+// Pop/s, where a short burst does 3.6); products of one or two waves the boundary between launches (1.4 us), the first bytes
+// (0.6 us), the results behind the last products (256 columns of X 6 to 8 us: 10 bytes an entry, from and to L2, all SMs at once)
+// and tiles that do not fill the SMs.  In the smallest, fetching instructions for the first time counts: one copy of the results'
+// code for whole and split tiles, and waiting for the launch before only where a role first has to, took 256 x 256 from 84 to 70 us.
 //
 // Small products leave SMs idle with one tile per block; there the contraction is cut into g.split parts, each block leaves its
 // partial sums in scratch, and the block that comes last to a tile adds the parts in their order and goes on as usual (Gram

@@ -283,7 +283,8 @@ int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, i
   Carve c{ctx->scratch};
   OrthScratch w(c, batch, s, l);
   if (c.at > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
-  // one launch: 2.4 times as fast as a chain at 128 x 128, 1.2 times at 128 x 2048; beyond, X does not fit a cluster
+  // one launch: 1.6 times as fast as a chain at 128 x 256, 1.05 times at 128 x 1000 and 2048 (1.7 times for thirty of them);
+  // beyond, X does not fit a cluster
   if ((s <= kSmall && l <= kSmallLong) || (s <= kMid && l <= kMidLong)) return orthogonal_small(ctx, src, to, batch, m, n, steps, coef, st);
   src.m = (int)m, src.n = (int)n;
   src.part = w.part;

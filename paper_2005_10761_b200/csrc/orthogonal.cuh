@@ -173,7 +173,7 @@ k_split(const __grid_constant__ Source s, float* x, __half* h, int64_t ld, int64
 // operand (its rows along the contraction index) and as an MN-major one (its rows are the contraction index).  The tensor core's 128
 // lanes reach 64 rows past a tile; what they make of those is not read.
 //
-// Measured: 64 x 64 17.6 us, 64 x 256 38 us (a chain of launches: 65 and 71).  One product takes about 2000 cycles: 740 for twelve
+// Measured: 64 x 64 17.7 us, 64 x 256 38 us (a chain of launches: 60 and 62).  One product takes about 2000 cycles: 740 for twelve
 // matrix instructions, 190 to read tensor memory, 800 to split and store (half of the warps: lanes 64 to 127 hold nothing), 200 for
 // the barrier.  mma.sync on the same halves takes 32 cycles an instruction and scheduler: 23 us at 64 x 64.
 constexpr int kSmall = 64, kSmallLong = 256, kSmallThreads = 512;
@@ -424,8 +424,8 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
 // block adds up its part of the entries in the blocks' order and hands the sum to all.  The arithmetic is that of the
 // product kernel: 16-bit operands, X and the diagonals in 32 bits.
 //
-// Measured, against a chain of launches: 128 x 128 28 us against 68, 128 x 256 39 / 71, 128 x 1000 67 / 79, 128 x 2048 78 / 91, thirty of
-// 128 x 1000 73 / 128.  A step is about 5800 cycles in one block; in a cluster 18700, 9200 of them the exchange of 96 KB a
+// Measured, against a chain of launches, us: 128 x 128 29 / 61, 128 x 256 40 / 63, 128 x 1000 68 / 71, 128 x 2048 76 / 80, thirty of
+// 128 x 1000 73 / 122.  A step is about 5800 cycles in one block; in a cluster 18700, 9200 of them the exchange of 96 KB a
 // block through distributed shared memory at about 16 bytes a cycle.
 constexpr int kMid = 128, kMidThreads = 512, kMidChunks = 4, kMidCluster = 8, kMidLong = kMidCluster * kMidChunks * kSmall;
 constexpr int kMidTile = kMid * kDepthBytes;                          // 128 rows of 64 16-bit numbers
