@@ -518,7 +518,7 @@ int rtopk_matrix_poll_status(rtopk_matrix* ctx, void* stream);
  * singular vectors.
  *   src  [in]   batch x m x n of src_dtype;   out [out]  the same shape, out_dtype; may be src itself
  *               when the two views are the same.
- *   steps       1 .. 64;   coef  HOST array of steps triples (a, b, c), or null for
+ *   batch, m, n >= 1;   steps  1 .. 64;   coef  HOST array of steps triples (a, b, c), or null for
  *               (3.4445, -4.7750, 2.0315) in every step.  Singular values must stay below 2 from step
  *               to step (they do, below 1.3, with the default), else 16-bit operands may overflow.
  *   eps         >= 0.  A zero matrix gives zeros; one with a NaN or an infinity gives NaN.

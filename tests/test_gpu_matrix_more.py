@@ -187,3 +187,61 @@ def test_blocks_that_give_up_say_so_and_leave_everything_in_order(rt):  # noqa: 
     with pytest.raises(rt.RTopKError):
         ctx.set_option(0, 2)
     ctx.close()
+
+
+def test_each_call_alone_in_a_graph(rt):  # noqa: F811
+    """Calls that begin with a memory set, with a kernel, with another call's kernels just before: captured and replayed."""
+    t, k, n = 150, 260, 190
+    ctx = rt.MatrixContext(max(rt.coded_scratch(t, n, k), rt.orthogonalize_scratch(1, 100, 900)))
+    coded = rt.CodedWeights(n, k)
+    w, x, dy = tokens_of(n, k, 1, torch.float32), tokens_of(t, k, 2, torch.float32), tokens_of(t, n, 3, torch.float32)
+    u = matrices("gauss", 1, 100, 900)[0]
+    ctx.code_weights(w, coded)
+    calls = {"dw": lambda o: ctx.coded_gradients(dy, x, coded, dw=o), "dx": lambda o: ctx.coded_gradients(dy, None, coded, dx=o),
+             "y": lambda o: ctx.coded_product(x, coded, o), "few": lambda o: ctx.coded_product(x[:2], coded, o), "orth": lambda o: ctx.orthogonalize(u, o)}
+    shapes = {"dw": (n, k), "dx": (t, k), "y": (t, n), "few": (2, n), "orth": (100, 900)}
+    for name, call in calls.items():
+        want, got = torch.zeros(shapes[name], device="cuda"), torch.zeros(shapes[name], device="cuda")
+        call(want)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(got)
+        for _ in range(2):
+            got.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(got, want), name
+    ctx.poll_status()
+    ctx.close()
+
+
+def test_calls_that_share_tensors_one_after_another(rt):  # noqa: F811
+    """Launches may start while their predecessors end: results that the next call reads, and inputs that it overwrites."""
+    m, n, t = 384, 640, 200
+    ctx = rt.MatrixContext(max(rt.orthogonalize_scratch(1, m, n), rt.coded_scratch(t, m, n)))
+    coded = rt.CodedWeights(m, n)
+    x = tokens_of(t, n, 2, torch.float32)
+    w0 = matrices("gauss", 1, m, n)[0] * 0.05
+
+    def chain(sync):
+        w, v, g = w0.clone(), torch.zeros_like(w0), torch.zeros_like(w0)
+        y, dx = torch.zeros((t, m), device="cuda"), torch.zeros_like(x)
+        for _ in range(8):
+            ctx.code_weights(w, coded)
+            if sync:
+                torch.cuda.synchronize()
+            ctx.coded_product(x, coded, y)
+            if sync:
+                torch.cuda.synchronize()
+            ctx.coded_gradients(y, x, coded, dx, g)
+            if sync:
+                torch.cuda.synchronize()
+            ctx.orthogonal_update(g, v, w, 0.02, 0.9)
+            if sync:
+                torch.cuda.synchronize()
+        return w, v, y, dx
+    want = chain(True)
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(chain(False), want))
+    ctx.close()
