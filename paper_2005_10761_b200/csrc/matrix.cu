@@ -50,11 +50,14 @@ int fail(rtopk_matrix* ctx, cudaError_t e) {
   } while (0)
 
 struct OnDevice {
-  int prev = -1;
+  int prev = -1;      // the device to go back to, if it is another one
   bool ok = true;
   explicit OnDevice(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+    int now = -1;
+    if (cudaGetDevice(&now) != cudaSuccess) { ok = false; return; }
+    if (now == dev) return;
+    prev = now;
+    ok = cudaSetDevice(dev) == cudaSuccess;
   }
   ~OnDevice() { if (prev >= 0) cudaSetDevice(prev); }
 };
