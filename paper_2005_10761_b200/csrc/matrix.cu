@@ -314,9 +314,9 @@ int orthogonal(rtopk_matrix* ctx, Source src, const Target& to, int64_t batch, i
     MAT_TRY(gemm<EPI_POLY>(ctx, gram, gram, g, st));
     g.lanes = (int)l, g.tri = 0;
     g.p_early = 1;      // the launch before wrote the polynomial, X is older
-    g.x = w.x, g.o = w.hi[cur], g.ld = w.ld_x, g.stride = w.stride_x, g.d_in = w.poly_d;
+    g.x = w.x, g.ld = w.ld_x, g.stride = w.stride_x, g.d_in = w.poly_d;
     if (i + 1 < steps) {
-      g.h = w.hi[cur ^ 1], g.keep_x = i + 2 < steps;
+      g.h = w.hi[cur ^ 1];
       MAT_TRY(gemm<EPI_APPLY>(ctx, x, poly, g, st));
       cur ^= 1;
     } else {
