@@ -63,7 +63,7 @@ struct Gemm {
   int split;                 // parts of the contraction, 1: whole
   uint32_t* parts;           // split: partial sums, [unit][col][lane]
   uint32_t* arrived;         // split: blocks that have left their part, per tile and block of a pair; zero between launches
-  int test_giveup;           // tests only: the first wait for a stage counts as run out
+  int test_giveup;           // tests only: the first wait for a stage counts as run out, and one block of each pair stops feeding early
   uint32_t* error;
   // epilogue operands
   const __half* o;           // POLY: A off the diagonal
@@ -311,7 +311,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
   const uint32_t full = base + kStages * S::kStageBytes, empty = full + 8 * kStages, tm_full = empty + 8 * kStages, tm_empty = tm_full + 16, drain = tm_empty + 16, meet = drain + 8;
   char* gen = smem_raw + (base - smem_addr(smem_raw)) + kStages * S::kStageBytes;
-  // [0] tensor-memory address, [1] give-up word, [2] whether this block came last to a split tile
+  // [0] tensor-memory address, [1] give-up word, [2] whether this block came last to a split tile, [3] stages it has asked for
   volatile uint32_t* words = (volatile uint32_t*)(gen + 16 * kStages + 64);
   const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // the same for all of a warp, and known to be
   const uint32_t rank = kPair ? rank_in_cluster() : 0;
@@ -348,9 +348,6 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       tma_load<kPair>(dst, &map_p, kb * kDepth, row, q.z, bar);
     }
   };
-  auto tell_pair = [&]() {      // the other block's roles look at its own word
-    if (kPair) cluster_store(at_rank(smem_addr((const void*)(words + 1)), rank ^ 1), 1u);
-  };
   uint32_t early = 0;      // stages whose P is under way
   if (g.p_early && warp == 0 && first < total) {
     const Tile q = tile_at<kCols, S::kTileLanes>(g, first);
@@ -366,6 +363,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
   };
   if (warp == 0) {
     uint32_t it = 0;
+    const uint32_t feed = kPair && g.test_giveup && ((first ^ rank) & 1) ? max(1u, early) : ~0u;
     bool ok = true;
     for (int u = first; u < total && ok; u += step) {
       const Tile q = tile_at<kCols, S::kTileLanes>(g, u);
@@ -375,6 +373,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
       for (int kb = q.part * part_k; kb < k1; ++kb, ++it) {
         const uint32_t s = it % kStages;
         if (it >= (uint32_t)kStages && !(ok = __all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * s, (it / kStages - 1) & 1, give)))) break;
+        if (!(ok = it < feed)) break;
         if (elect_one()) {
           if (it >= early) load_p(s, q, kb);
           tma_load<kPair>(base + s * S::kStageBytes + S::kPBytes, &map_q, kb * kDepth, q.c * kCols + rank * S::kQRows, q.z, kPair ? first_of_pair(full + 8 * s) : full + 8 * s);
@@ -382,15 +381,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
         __syncwarp();
       }
     }
-    if (!ok && lane == 0) {
-      tell_pair();
-      if (rank == 0) {
-        for (uint32_t k = it > (uint32_t)kStages ? it - kStages : 0; k < it; ++k) bar_drain(full + 8 * (k % kStages), (k / kStages) & 1);
-      } else {      // this block's copies report to the other one: give them time
-        const uint64_t t0 = now_ns();
-        while (now_ns() - t0 < 1000000ull) {}
-      }
-    }
+    if (lane == 0) words[3] = it;
     __syncwarp();
   } else if (warp == 1) {
     if (rank == 0) {
@@ -422,13 +413,6 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
         if (ok && elect_one()) tc_commit<kPair>(tm_full + 8 * b);
         __syncwarp();
         if (n == 0 && !g.free_start) follow();
-      }
-      if (!ok) {
-        if (elect_one()) {
-          tell_pair();
-          tc_commit<kPair>(drain);
-          bar_drain(drain, 0);
-        }
       }
     } else if (!g.free_start) {
       follow();
@@ -539,11 +523,35 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     }
     __syncwarp();
   }
+  // The other block's roles look at its own word.
+  if (kPair && lane == 0 && words[1]) cluster_store(at_rank(smem_addr((const void*)(words + 1)), rank ^ 1), 1u);
   if (g.free_start) follow();
-  tc_fence_before();
-  if (kPair) cluster_sync();
-  else __syncthreads();
-  tc_fence_after();
+  auto all = [&]() {
+    tc_fence_before();
+    if (kPair) cluster_sync();
+    else __syncthreads();
+    tc_fence_after();
+  };
+  all();
+  if (words[1]) {      // the same in both blocks of a pair by now: nothing may be on its way to their memory when they leave
+    if (rank == 0 && lane == 0 && warp == 0) {
+      const uint64_t t0 = now_ns();
+      // Both blocks' copies report to this one's barriers.  Where one has asked for a stage and the other has not, the barrier is
+      // told what to expect.
+      const uint32_t mine = words[3], other = kPair ? cluster_load(at_rank(smem_addr((const void*)(words + 3)), 1)) : mine, most = max(mine, other);
+      for (uint32_t k = most > (uint32_t)kStages ? most - kStages : 0; k < most; ++k) {
+        const uint32_t bar = full + 8 * (k % kStages);
+        if (k >= mine) bar_expect(bar, S::kStageBytes);
+        else if (k >= other) bar_complete(bar, S::kStageBytes);
+        bar_drain(bar, (k / kStages) & 1, t0);
+      }
+    }
+    if (rank == 0 && warp == 1 && elect_one()) {
+      tc_commit<kPair>(drain);
+      bar_drain(drain, 0, now_ns());
+    }
+    all();
+  }
   if (warp == 1) tmem_free<kPair>(tmem, kTmemCols);
 }
 

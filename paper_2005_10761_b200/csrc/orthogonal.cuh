@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
   if (failed) {
     if (warp == 0 && elect_one()) {
       tc_commit<false>(smem_addr(&drain));
-      bar_drain(smem_addr(&drain), 0);
+      bar_drain(smem_addr(&drain), 0, now_ns());
     }
     __syncthreads();
   }
@@ -691,7 +691,7 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
   __syncwarp();
   if (words[1] && warp == 0 && elect_one()) {
     tc_commit<false>(smem_addr(&drain));
-    bar_drain(smem_addr(&drain), 0);
+    bar_drain(smem_addr(&drain), 0, now_ns());
   }
   tc_fence_before();
   cluster_sync();

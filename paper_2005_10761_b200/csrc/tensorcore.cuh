@@ -34,6 +34,10 @@ __device__ __forceinline__ void bar_init_fence() { asm volatile("fence.mbarrier_
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// Stands in for the bytes of a copy that was expected and never issued.
+__device__ __forceinline__ void bar_complete(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -52,6 +56,11 @@ __device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ float4 cluster_load4(uint32_t addr) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t cluster_load(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
 }
 __device__ __forceinline__ void cluster_store(uint32_t addr, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
@@ -111,9 +120,8 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const Gi
     }
   }
 }
-// For a block that gives up: waits for its own copies and products in flight, again with a limit.
-__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
-  const uint64_t t0 = now_ns();
+// For a block that gives up: waits for its own copies or products in flight, again with a limit, which counts from t0.
+__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity, uint64_t t0) {
   while (!bar_try(bar, parity) && now_ns() - t0 < kWaitNs) {}
 }
 

@@ -42,3 +42,52 @@ def test_x_stays_in_32_bits_to_the_result(rt, m, n):  # noqa: F811
     ctx.orthogonal_update(g, v, w, 1.0, 0.5, scale=-1.0)
     assert rel(w, orth64(g + 0.5 * g)) <= ORTHOGONAL_ROWS
     ctx.close()
+
+
+def test_products_that_give_up_leave_no_copy_behind(rt):  # noqa: F811
+    """Blocks and pairs of blocks of the product kernel, with few steps (all copies issued, none waited for by the feeding warp) and
+    with many, the pair's blocks at different steps when they stop.  Every call reports for itself; it ends long before the
+    limit of a wait (2 s), so the copies in flight were waited for and not timed out; what runs right behind it is right."""
+    import time
+    shapes = [(200, 1500), (300, 300), (1300, 1400), (2100, 700)]
+    layers = [(300, 500, 400), (64, 600, 300), (1100, 4100, 2000), (2000, 200, 1500)]
+    ctx = rt.MatrixContext(max([rt.orthogonalize_scratch(1, a, b) for a, b in shapes] + [rt.coded_scratch(t, n, k) for t, k, n in layers]))
+
+    def calls():
+        for a, b in shapes:
+            u, out = torch.randn((a, b), generator=gen(a), device="cuda"), torch.empty((a, b), device="cuda")
+            yield lambda: ctx.orthogonalize(u, out), out
+            v, w = torch.zeros_like(u), torch.zeros_like(u)
+            yield lambda: (v.zero_(), w.zero_(), ctx.orthogonal_update(u, v, w, 0.1, 0.9)), w
+        for t, k, n in layers:
+            coded = rt.CodedWeights(n, k)
+            w, x, dy = (torch.randn(s, generator=gen(t), device="cuda") for s in ((n, k), (t, k), (t, n)))
+            ctx.code_weights(w, coded)
+            y, dx, dw = torch.empty((t, n), device="cuda"), torch.empty((t, k), device="cuda"), torch.empty((n, k), device="cuda")
+            yield lambda: ctx.coded_product(x, coded, y), y
+            yield lambda: ctx.coded_gradients(dy, None, coded, dx=dx), dx
+            yield lambda: ctx.coded_gradients(dy, x, coded, dw=dw), dw
+            both = torch.empty((t * k + n * k,), device="cuda")
+            yield lambda: ctx.coded_gradients(dy, x, coded, both[:t * k].view(t, k), both[t * k:].view(n, k)), both
+
+    for call, out in calls():
+        call()
+        want = out.clone()
+        torch.cuda.synchronize()
+        ctx.set_option(0, 1)
+        t0 = time.monotonic()
+        call()
+        with pytest.raises(rt.RTopKError) as e:
+            ctx.poll_status()
+        assert e.value.status == 5
+        assert time.monotonic() - t0 < 1.0
+        call()
+        ctx.set_option(0, 0)
+        with pytest.raises(rt.RTopKError):      # clears the counters of parts that were never added up
+            ctx.poll_status()
+        for _ in range(2):
+            out.fill_(9.0)
+            call()
+            assert torch.equal(out, want)
+        ctx.poll_status()
+    ctx.close()
