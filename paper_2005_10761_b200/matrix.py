@@ -40,18 +40,46 @@ def _dtype(t: torch.Tensor, what: str) -> int:
 class CodedWeights:
     """The 8-bit codes of an (n_out, n_in) weight matrix and one scale for each output channel: what a master broadcasts.
     ``codes`` is int8 [n_out, ld], ``codes_t`` the same codes transposed (None with ``transposed=False``, for layers that
-    take no gradient with respect to their input), ``scales`` float32 [n_out]."""
+    take no gradient with respect to their input), ``scales`` float32 [n_out].  Each may be replaced by another tensor of that form, with
+    rows of at least the codes' number, contiguous, a multiple of 16 bytes apart; calls use the tensors that are there when they
+    are made."""
 
     def __init__(self, n_out: int, n_in: int, transposed: bool = True, device=None):
         device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
-        self.n_out, self.n_in = n_out, n_in
+        self._n_out, self._n_in = n_out, n_in
         self.codes = torch.zeros((n_out, -(-n_in // 128) * 128), dtype=torch.int8, device=device)
         self.codes_t = torch.zeros((n_in, -(-n_out // 128) * 128), dtype=torch.int8, device=device) if transposed else None
         self.scales = torch.zeros(n_out, dtype=torch.float32, device=device)
-        # (pointer, row stride) of both arrays and the scales' pointer, as the calls take them
-        self._codes = (self.codes.data_ptr(), self.codes.stride(0))
-        self._codes_t = (self.codes_t.data_ptr(), self.codes_t.stride(0)) if transposed else (None, 0)
-        self._scales = self.scales.data_ptr()
+
+    n_out = property(lambda self: self._n_out)
+    n_in = property(lambda self: self._n_in)
+    codes = property(lambda self: self._codes)
+    codes_t = property(lambda self: self._codes_t)
+    scales = property(lambda self: self._scales)
+
+    @codes.setter
+    def codes(self, t):
+        self._codes = self._checked(t, "codes", self._n_out, self._n_in)
+
+    @codes_t.setter
+    def codes_t(self, t):
+        self._codes_t = None if t is None else self._checked(t, "codes_t", self._n_in, self._n_out)
+
+    @scales.setter
+    def scales(self, t):
+        if t.dtype != torch.float32:
+            raise TypeError("scales must be float32")
+        if t.shape != (self._n_out,) or not t.is_contiguous():
+            raise ValueError(f"scales must be contiguous and of shape {(self._n_out,)}")
+        self._scales = t
+
+    @staticmethod
+    def _checked(t, what, rows, cols):
+        if t.dtype != torch.int8:
+            raise TypeError(f"{what} must be int8")
+        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < cols or (t.stride(1) != 1 and t.shape[1] > 1):
+            raise ValueError(f"{what} must have {rows} contiguous rows of at least {cols} codes")
+        return t
 
     def dense(self) -> torch.Tensor:
         """The values that the codes stand for."""
@@ -125,6 +153,11 @@ class MatrixContext:
         return p, ld, (t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else 0)
 
     @staticmethod
+    def _codes(t: Optional[torch.Tensor]):
+        """(pointer, row stride) of an array of codes."""
+        return (None, 0) if t is None else (t.data_ptr(), t.stride(0))
+
+    @staticmethod
     def _sizes(t: torch.Tensor):
         return (t.shape[0] if t.dim() == 3 else 1), t.shape[-2], t.shape[-1]
 
@@ -162,20 +195,20 @@ class MatrixContext:
     def code_weights(self, weights, coded: CodedWeights) -> None:
         """coded <- the codes of weights ([n_out, n_in], float32 or bfloat16), one scale for each row."""
         p, ld = self._rows(weights, "weights", (coded.n_out, coded.n_in))
-        rc = self._lib.rtopk_code_weights(self._h, p, _dtype(weights, "weights"), ld, coded.n_out, coded.n_in, *coded._codes,
-                                          *coded._codes_t, coded._scales, self._stream())
+        rc = self._lib.rtopk_code_weights(self._h, p, _dtype(weights, "weights"), ld, coded.n_out, coded.n_in,
+                                          *self._codes(coded._codes), *self._codes(coded._codes_t), coded._scales.data_ptr(),
+                                          self._stream())
         self._check(rc, "rtopk_code_weights")
 
     def coded_product(self, x, coded: CodedWeights, out) -> None:
         """out[t, n] <- x W^T with W as codes and x ([tokens, n_in], float32 or bfloat16) coded for each token."""
-        tokens, n_in, n_out = x.shape[0], coded.n_in, coded.n_out
+        tokens, n_in, n_out, codes = x.shape[0], coded._n_in, coded._n_out, coded._codes
         p, ld = self._rows(x, "x", (tokens, n_in))
         po, ldo = self._rows(out, "out", (tokens, n_out))
         if out.dtype != x.dtype:
             raise TypeError("out must have the type of x")
-        codes, ld_codes = coded._codes
-        rc = self._lib.rtopk_coded_product(self._h, p, _dtype(x, "x"), ld, codes, ld_codes, coded._scales, tokens, n_out, n_in,
-                                           po, ldo, self._stream())
+        rc = self._lib.rtopk_coded_product(self._h, p, _dtype(x, "x"), ld, codes.data_ptr(), codes.stride(0),
+                                           coded._scales.data_ptr(), tokens, n_out, n_in, po, ldo, self._stream())
         self._check(rc, "rtopk_coded_product")
 
     def coded_gradients(self, dy, x, coded: CodedWeights, dx=None, dw=None) -> None:
@@ -196,10 +229,10 @@ class MatrixContext:
             pdx, lddx = self._rows(dx, "dx", (tokens, coded.n_in))
             if dx.dtype != dy.dtype:
                 raise TypeError("dx must have the type of dy")
-            if coded.codes_t is None:
+            if coded._codes_t is None:
                 raise ValueError("these weights were made without their transposed codes")
-        rc = self._lib.rtopk_coded_gradients(self._h, py, ldy, px, ldx, dt, *coded._codes_t, coded._scales, tokens, coded.n_out,
-                                             coded.n_in, pdx, lddx, pdw, wt, lddw, self._stream())
+        rc = self._lib.rtopk_coded_gradients(self._h, py, ldy, px, ldx, dt, *self._codes(coded._codes_t), coded._scales.data_ptr(),
+                                             tokens, coded.n_out, coded.n_in, pdx, lddx, pdw, wt, lddw, self._stream())
         self._check(rc, "rtopk_coded_gradients")
 
     def set_option(self, option: int, value: int) -> None:

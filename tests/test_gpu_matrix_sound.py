@@ -91,3 +91,32 @@ def test_products_that_give_up_leave_no_copy_behind(rt):  # noqa: F811
             assert torch.equal(out, want)
         ctx.poll_status()
     ctx.close()
+
+
+def test_coded_weights_received_copied_and_moved(rt):  # noqa: F811
+    """The calls read and write the tensors that the object holds at the time."""
+    import copy
+    t, k, n = 5, 200, 96
+    ctx = rt.MatrixContext(rt.coded_scratch(t, n, k))
+    a, b = rt.CodedWeights(n, k), rt.CodedWeights(n, k)
+    wa, wb, x = (torch.randn(s, generator=gen(i), device="cuda") for i, s in enumerate(((n, k), (n, k), (t, k))))
+    ctx.code_weights(wa, a)
+    ctx.code_weights(wb, b)
+
+    def product(c):
+        y, dx = torch.empty((t, n), device="cuda"), torch.empty((t, k), device="cuda")
+        ctx.coded_product(x, c, y)
+        ctx.coded_gradients(y, None, c, dx=dx)
+        return y, dx
+
+    def same(p, q):
+        return all(torch.equal(u, v) for u, v in zip(p, q))
+    of_a, of_b = product(a), product(b)
+    assert not same(of_a, of_b)
+    received = rt.CodedWeights(n, k)
+    received.codes, received.codes_t, received.scales = (v.clone() for v in (b.codes, b.codes_t, b.scales))
+    assert same(product(received), of_b)
+    copied = copy.deepcopy(a)
+    ctx.code_weights(wb, copied)                    # the original keeps its codes
+    assert same(product(copied), of_b) and same(product(a), of_a)
+    ctx.close()
