@@ -134,28 +134,31 @@ class MatrixContext:
                 detail += f", cudaError {self._lib.rtopk_matrix_last_cuda_error(self._h)}"
             raise RTopKError(rc, what, detail)
 
-    @staticmethod
-    def _rows(t: torch.Tensor, what: str, shape=None):
+    def _on_device(self, t: torch.Tensor, what: str) -> int:
+        """The tensor's address; another device's means nothing to the kernels."""
+        if t.get_device() != self.device:
+            raise ValueError(f"{what} must be on device {self.device}")
+        return t.data_ptr()
+
+    def _rows(self, t: torch.Tensor, what: str, shape=None):
         """(pointer, row stride) of a matrix with contiguous rows."""
         sizes, strides = t.shape, t.stride()
         if shape is not None and sizes != shape:
             raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(sizes)}")
         if strides[-1] != 1 and sizes[-1] > 1:
             raise ValueError(f"the rows of {what} must be contiguous")
-        return t.data_ptr(), (strides[-2] if sizes[-2] > 1 else sizes[-1])
+        return self._on_device(t, what), (strides[-2] if sizes[-2] > 1 else sizes[-1])
 
-    @classmethod
-    def _batch(cls, t: torch.Tensor, what: str, shape=None):
+    def _batch(self, t: torch.Tensor, what: str, shape=None):
         """(pointer, row stride, matrix stride) of a matrix or a batch of them."""
         if t.dim() not in (2, 3):
             raise ValueError(f"{what} must be a matrix or a batch of matrices")
-        p, ld = cls._rows(t, what, shape)
+        p, ld = self._rows(t, what, shape)
         return p, ld, (t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else 0)
 
-    @staticmethod
-    def _codes(t: Optional[torch.Tensor]):
+    def _codes(self, t: Optional[torch.Tensor]):
         """(pointer, row stride) of an array of codes."""
-        return (None, 0) if t is None else (t.data_ptr(), t.stride(0))
+        return (None, 0) if t is None else (self._on_device(t, "the codes"), t.stride(0))
 
     @staticmethod
     def _sizes(t: torch.Tensor):
@@ -196,8 +199,8 @@ class MatrixContext:
         """coded <- the codes of weights ([n_out, n_in], float32 or bfloat16), one scale for each row."""
         p, ld = self._rows(weights, "weights", (coded.n_out, coded.n_in))
         rc = self._lib.rtopk_code_weights(self._h, p, _dtype(weights, "weights"), ld, coded.n_out, coded.n_in,
-                                          *self._codes(coded._codes), *self._codes(coded._codes_t), coded._scales.data_ptr(),
-                                          self._stream())
+                                          *self._codes(coded._codes), *self._codes(coded._codes_t),
+                                          self._on_device(coded._scales, "scales"), self._stream())
         self._check(rc, "rtopk_code_weights")
 
     def coded_product(self, x, coded: CodedWeights, out) -> None:
@@ -207,8 +210,8 @@ class MatrixContext:
         po, ldo = self._rows(out, "out", (tokens, n_out))
         if out.dtype != x.dtype:
             raise TypeError("out must have the type of x")
-        rc = self._lib.rtopk_coded_product(self._h, p, _dtype(x, "x"), ld, codes.data_ptr(), codes.stride(0),
-                                           coded._scales.data_ptr(), tokens, n_out, n_in, po, ldo, self._stream())
+        rc = self._lib.rtopk_coded_product(self._h, p, _dtype(x, "x"), ld, self._on_device(codes, "codes"), codes.stride(0),
+                                           self._on_device(coded._scales, "scales"), tokens, n_out, n_in, po, ldo, self._stream())
         self._check(rc, "rtopk_coded_product")
 
     def coded_gradients(self, dy, x, coded: CodedWeights, dx=None, dw=None) -> None:
@@ -231,8 +234,9 @@ class MatrixContext:
                 raise TypeError("dx must have the type of dy")
             if coded._codes_t is None:
                 raise ValueError("these weights were made without their transposed codes")
-        rc = self._lib.rtopk_coded_gradients(self._h, py, ldy, px, ldx, dt, *self._codes(coded._codes_t), coded._scales.data_ptr(),
-                                             tokens, coded.n_out, coded.n_in, pdx, lddx, pdw, wt, lddw, self._stream())
+        rc = self._lib.rtopk_coded_gradients(self._h, py, ldy, px, ldx, dt, *self._codes(coded._codes_t),
+                                             self._on_device(coded._scales, "scales"), tokens, coded.n_out, coded.n_in, pdx, lddx,
+                                             pdw, wt, lddw, self._stream())
         self._check(rc, "rtopk_coded_gradients")
 
     def set_option(self, option: int, value: int) -> None:

@@ -78,3 +78,32 @@ def test_coded_weights_that_do_not_fit_are_refused():
     coded = rt.CodedWeights(40, 30, device="cpu")
     with pytest.raises(AttributeError):
         coded.n_out = 41
+
+
+def test_tensors_of_another_device_are_refused_before_the_library_sees_them():
+    """A context of device 0 and tensors of the CPU: their addresses mean nothing there."""
+    ctx, f = context(device=0), torch.zeros
+    coded = rt.CodedWeights(40, 30, device="cpu")
+    for call in (lambda: ctx.orthogonalize(f(4, 5), f(4, 5)), lambda: ctx.orthogonal_update(f(4, 5), f(4, 5), f(4, 5), 0.1, 0.9),
+                 lambda: ctx.code_weights(f(40, 30), coded), lambda: ctx.coded_product(f(3, 30), coded, f(3, 40)),
+                 lambda: ctx.coded_gradients(f(3, 40), f(3, 30), coded, f(3, 30), f(40, 30))):
+        with pytest.raises(ValueError):
+            call()
+    assert not ctx._lib.calls
+
+
+def test_codes_of_another_device_are_refused(monkeypatch):
+    ctx, f = context(device=0), torch.zeros
+    for name in ("codes", "codes_t", "scales"):
+        coded = rt.CodedWeights(40, 30, device="cpu")
+        away = getattr(coded, name)
+        monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 1 if t is away else 0)
+        calls = [lambda: ctx.code_weights(f(40, 30), coded)]
+        if name != "codes":
+            calls.append(lambda: ctx.coded_gradients(f(3, 40), None, coded, f(3, 30)))
+        if name != "codes_t":
+            calls.append(lambda: ctx.coded_product(f(3, 30), coded, f(3, 40)))
+        for call in calls:
+            with pytest.raises(ValueError):
+                call()
+    assert not ctx._lib.calls
