@@ -223,6 +223,8 @@ class MatrixContext:
         px = ldx = pdx = lddx = pdw = lddw = 0
         wt = GRAD_F32
         if dw is not None:
+            if x is None:
+                raise ValueError("dw needs x")
             px, ldx = self._rows(x, "x", (tokens, coded.n_in))
             if x.dtype != dy.dtype:
                 raise TypeError("x must have the type of dy")

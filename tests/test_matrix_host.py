@@ -107,3 +107,10 @@ def test_codes_of_another_device_are_refused(monkeypatch):
             with pytest.raises(ValueError):
                 call()
     assert not ctx._lib.calls
+
+
+def test_gradients_without_x_name_what_is_missing():
+    ctx, coded = context(), rt.CodedWeights(40, 30, device="cpu")
+    with pytest.raises(ValueError, match="x"):
+        ctx.coded_gradients(torch.zeros(3, 40), None, coded, dw=torch.zeros(40, 30))
+    assert not ctx._lib.calls
