@@ -147,7 +147,9 @@ class MatrixContext:
             raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(sizes)}")
         if strides[-1] != 1 and sizes[-1] > 1:
             raise ValueError(f"the rows of {what} must be contiguous")
-        return self._on_device(t, what), (strides[-2] if sizes[-2] > 1 else sizes[-1])
+        if t.get_device() != self.device:
+            raise ValueError(f"{what} must be on device {self.device}")
+        return t.data_ptr(), (strides[-2] if sizes[-2] > 1 else sizes[-1])
 
     def _batch(self, t: torch.Tensor, what: str, shape=None):
         """(pointer, row stride, matrix stride) of a matrix or a batch of them."""
@@ -158,7 +160,7 @@ class MatrixContext:
 
     def _codes(self, t: Optional[torch.Tensor]):
         """(pointer, row stride) of an array of codes."""
-        return (None, 0) if t is None else (self._on_device(t, "the codes"), t.stride(0))
+        return (None, 0) if t is None else (self._on_device(t, "the codes"), t.stride()[0])
 
     @staticmethod
     def _sizes(t: torch.Tensor):
@@ -208,11 +210,13 @@ class MatrixContext:
         tokens, n_in, n_out, codes = x.shape[0], coded._n_in, coded._n_out, coded._codes
         p, ld = self._rows(x, "x", (tokens, n_in))
         po, ldo = self._rows(out, "out", (tokens, n_out))
-        if out.dtype != x.dtype:
-            raise TypeError("out must have the type of x")
-        rc = self._lib.rtopk_coded_product(self._h, p, _dtype(x, "x"), ld, self._on_device(codes, "codes"), codes.stride(0),
+        dtype = _DTYPES.get(x.dtype)
+        if dtype is None or out.dtype != x.dtype:
+            raise TypeError("x must be float32 or bfloat16, and out have its type")
+        rc = self._lib.rtopk_coded_product(self._h, p, dtype, ld, self._on_device(codes, "codes"), codes.stride()[0],
                                            self._on_device(coded._scales, "scales"), tokens, n_out, n_in, po, ldo, self._stream())
-        self._check(rc, "rtopk_coded_product")
+        if rc:
+            self._check(rc, "rtopk_coded_product")
 
     def coded_gradients(self, dy, x, coded: CodedWeights, dx=None, dw=None) -> None:
         """The gradients of :meth:`coded_product` for dy ([tokens, n_out]): dx like x, dw ([n_out, n_in], float32 or bfloat16).
