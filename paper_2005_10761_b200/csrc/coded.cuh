@@ -133,7 +133,7 @@ __device__ __forceinline__ void store8(uint2 w, int left, int8_t* out) {
 template <class T, int kWarps, bool kMul>
 __global__ void __launch_bounds__(256)
 k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* mul, int mul_vec, int8_t* codes, int64_t ld_codes, int padded, float* scales,
-            uint32_t* clear, int clear_words) {
+            uint32_t* clear, int64_t clear_words) {
   constexpr int kKeep = 16 / sizeof(T), kSpan = kWarps * 32 * 8;
   __shared__ uint32_t part[8];
   const int group = threadIdx.x / (32 * kWarps), t = threadIdx.x % (32 * kWarps);
@@ -141,7 +141,7 @@ k_code_rows(const T* src, int64_t ld, int rows, int cols, int vec, const float* 
   const bool in = row < rows;
   launch_wait();
   launch_next();
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < clear_words; i += gridDim.x * 256) clear[i] = 0u;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < clear_words; i += (int64_t)gridDim.x * 256) clear[i] = 0u;      // blocks x 256 may pass 32 bits
   const T* p = src + (int64_t)(in ? row : 0) * ld;
   auto values = [&](const Eight<T>& e, int c, float (&v)[8]) {
     e.widen_to(v);

@@ -3,7 +3,7 @@ here as in test_gpu_matrix.py."""
 import pytest
 import torch
 
-from test_gpu_matrix import U16, gen, mu_exact, orth64, rel, rt  # noqa: F401
+from test_gpu_matrix import U16, code64, gen, matrices, near, orth64, rel, rt  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -119,4 +119,30 @@ def test_coded_weights_received_copied_and_moved(rt):  # noqa: F811
     copied = copy.deepcopy(a)
     ctx.code_weights(wb, copied)                    # the original keeps its codes
     assert same(product(copied), of_b) and same(product(a), of_a)
+    ctx.close()
+
+
+def test_more_rows_than_32_bits_of_threads(rt):  # noqa: F811
+    """Eight rows a block of 256 threads: past 2^26 rows a thread's number in the launch no longer fits 31 bits.  Rows are compared at
+    both ends and around that one."""
+    n, k, m = (1 << 26) + 41, 8, 3
+    at = torch.cat([torch.arange(64), torch.arange((1 << 26) - 32, (1 << 26) + 41)]).cuda()
+    x = torch.empty((n, k), dtype=torch.bfloat16, device="cuda").normal_(generator=gen(1))
+    coded = rt.CodedWeights(n, k, transposed=False)
+    ctx = rt.MatrixContext(0)
+    ctx.code_weights(x, coded)
+    q, s = code64(x[at], 1)
+    assert torch.equal(coded.codes[at][:, :k].double(), q) and torch.equal(coded.scales[at].double(), s.flatten())
+    assert bool((coded.scales > 0).all())
+    ctx.close()
+    del coded
+    w = torch.randn((m, k), generator=gen(2), device="cuda")
+    ctx, coded = rt.MatrixContext(rt.coded_scratch(n, m, k)), rt.CodedWeights(m, k)
+    ctx.code_weights(w, coded)
+    out = torch.full((n, m), float("nan"), dtype=torch.bfloat16, device="cuda")
+    ctx.coded_product(x, coded, out)
+    ctx.poll_status()
+    qw, sw = code64(w, 1)
+    near(out[at], (q @ qw.t()) * s * sw.t(), torch.bfloat16)
+    assert not bool(out.isnan().any())             # every row was written
     ctx.close()
