@@ -384,6 +384,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     if (lane == 0) words[3] = it;
     __syncwarp();
   } else if (warp == 1) {
+    if (!g.free_start) follow();      // before the first wait with a limit, which is not to count what is left of that kernel
     if (rank == 0) {
       constexpr uint32_t kDesc = instr_desc(kInt8, kMnMajor, S::kTileLanes, kCols);
       uint32_t it = 0, n = 0;
@@ -412,10 +413,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
         }
         if (ok && elect_one()) tc_commit<kPair>(tm_full + 8 * b);
         __syncwarp();
-        if (n == 0 && !g.free_start) follow();
       }
-    } else if (!g.free_start) {
-      follow();
     }
     __syncwarp();
   } else {
