@@ -47,6 +47,19 @@ __device__ __forceinline__ float4 source4(const Source& s, int64_t i, int left) 
   return s.bf16 ? load4((const __nv_bfloat16*)s.src + i, left, s.vec) : load4((const float*)s.src + i, left, s.vec);
 }
 
+// X = (u up) by.  One binary32 factor would be infinite for norms below 1e-37, which eps = 0 allows, and subnormal for norms above
+// 3e39; up is 1 in between.
+struct Factor {
+  float up, by;
+  __device__ __forceinline__ float operator()(float u) const { return u * up * by; }
+};
+__device__ __forceinline__ Factor factor_of(double sum_of_squares, float eps, float scale) {
+  if (sum_of_squares == 0.0) return {1.f, 0.f};
+  const double f = (double)scale / (sqrt(sum_of_squares) + (double)eps);
+  const double up = f > 0x1p120 ? 0x1p64 : f < 0x1p-120 ? 0x1p-64 : 1.0;
+  return {(float)up, (float)(f / up)};
+}
+
 // Sums of squares, in binary64 so that neither large nor small gradients leave the range; one partial sum per block, added
 // up in a fixed order by the readers.  A warp takes 1024 neighbours of a row at a time, all loads under way before the first is
 // used: bound by memory, four updates of 6000 x 1500 (432 MB) 44 us where part of them is still in L2.
@@ -108,7 +121,7 @@ __global__ void __launch_bounds__(256) k_norm(const __grid_constant__ Source s) 
 __global__ void __launch_bounds__(256)
 k_split(const __grid_constant__ Source s, float* x, __half* h, int64_t ld, int64_t stride, float* row_sums, int slots, int64_t d_stride, int transpose) {
   __shared__ float tile[64][65];
-  __shared__ float inv_s;
+  __shared__ Factor factor_s;
   const int z = blockIdx.z, c0 = blockIdx.x * 64, r0 = blockIdx.y * 64;
   launch_wait();
   launch_next();
@@ -116,7 +129,7 @@ k_split(const __grid_constant__ Source s, float* x, __half* h, int64_t ld, int64
     double sum = 0.0;
     for (int i = threadIdx.x; i < s.parts; i += 32) sum += s.part[z * kNormBlocks + i];
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-    if (threadIdx.x == 0) inv_s = sum == 0.0 ? 0.f : (float)((double)kXScale / (sqrt(sum) + (double)s.eps));
+    if (threadIdx.x == 0) factor_s = factor_of(sum, s.eps, kXScale);
   }
   {
     const int c = (threadIdx.x & 15) * 4, left = s.n - c0 - c;
@@ -136,7 +149,7 @@ k_split(const __grid_constant__ Source s, float* x, __half* h, int64_t ld, int64
     }
   }
   __syncthreads();
-  const float inv = inv_s;
+  const Factor scaled = factor_s;
   x += z * stride, h += z * stride, row_sums += (int64_t)z * slots * d_stride;
   const int ns = transpose ? s.n : s.m, nl = transpose ? s.m : s.n;
   const int a0 = transpose ? c0 : r0, b0 = transpose ? r0 : c0;      // of X: rows and columns
@@ -146,7 +159,7 @@ k_split(const __grid_constant__ Source s, float* x, __half* h, int64_t ld, int64
     float u[8], sum = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      u[j] = (transpose ? tile[b + j][a] : tile[a][b + j]) * inv;
+      u[j] = scaled(transpose ? tile[b + j][a] : tile[a][b + j]);
       sum = fmaf(u[j], u[j], sum);
     }
     sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
@@ -299,14 +312,14 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
   const uint32_t tmem = words[0];
   sum = 0.0;
   for (int i = 0; i < kSmallThreads / 32; ++i) sum += part[i];
-  const float inv = sum == 0.0 ? 0.f : (float)((double)kSmallScale / (sqrt(sum) + (double)s.eps));
+  const Factor scaled = factor_of(sum, s.eps, kSmallScale);
 #pragma unroll
   for (int i = 0; i < kSmallKeep; ++i) {
     if (i >= turns) break;
     int r, c;
     if (!entry(i, r, c)) continue;
     const int row = transpose ? c : r, col = transpose ? r : c, at = col / kSmall * kTileBytes + tile_byte(row, col & (kSmall - 1));
-    const float v = u[i] * inv;
+    const float v = scaled(u[i]);
     const __half h = to_half(v);
     *(__half*)(x_hi + at) = h;
     *(__half*)(x_lo + at) = to_half(v - __half2float(h));
@@ -509,12 +522,12 @@ __global__ void __launch_bounds__(kMidThreads, 1) k_orth_cluster(const __grid_co
   cluster_sync();
   sum = 0.0;
   for (uint32_t i = 0; i < blocks; ++i) sum += norms[i];
-  const float inv = sum == 0.0 ? 0.f : (float)((double)kXScale / (sqrt(sum) + (double)s.eps));
+  const Factor scaled = factor_of(sum, s.eps, kXScale);
   float x[kMidChunks][16];
 #pragma unroll
   for (int c = 0; c < kMidChunks; ++c)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[c][i] = c < chunks ? stage[(c * kMid + row) * kMidPitch + group * 16 + i] * inv : 0.f;
+    for (int i = 0; i < 16; ++i) x[c][i] = c < chunks ? scaled(stage[(c * kMid + row) * kMidPitch + group * 16 + i]) : 0.f;
   __syncthreads();
 
   // Sixteen neighbours of a row of a tile.

@@ -146,3 +146,26 @@ def test_more_rows_than_32_bits_of_threads(rt):  # noqa: F811
     near(out[at], (q @ qw.t()) * s * sw.t(), torch.bfloat16)
     assert not bool(out.isnan().any())             # every row was written
     ctx.close()
+
+
+@pytest.mark.parametrize("m,n", [(40, 96), (96, 40), (100, 700), (200, 300), (300, 200)])
+def test_norms_at_both_ends_of_the_range(rt, m, n):  # noqa: F811
+    """The whole range of binary32: with eps = 0 entries down to single steps of the subnormal numbers, where 1 / norm is past the range,
+    and entries near the largest number, where it is subnormal."""
+    u = matrices("gauss", 1, m, n, 6)
+    for scale in (1e-36, 1e-38, 1e-39, 1e-41, 1e-44):
+        v = u * scale
+        want = orth64(v, eps=0.0)
+        assert rel(orthogonalize(rt, v, eps=0.0), want) <= 4 * U16, scale
+        zeros = v.clone()
+        zeros[:, 0] = 0.0                           # zero times an infinite factor would be NaN
+        assert rel(orthogonalize(rt, zeros, eps=0.0), orth64(zeros, eps=0.0)) <= 4 * U16, scale
+        g, mom, w = v.clone(), torch.zeros_like(v), torch.zeros_like(v)
+        ctx = rt.MatrixContext(rt.orthogonalize_scratch(1, m, n))
+        ctx.orthogonal_update(g, mom, w, 1.0, 0.0, scale=-1.0, eps=0.0)
+        assert torch.equal(mom, v) and rel(w, want) <= 4 * U16, scale
+        ctx.close()
+    big = u / u.abs().max() * 3.4e38
+    assert rel(orthogonalize(rt, big), orth64(big)) <= 4 * U16
+    full = torch.full_like(u, 3.4e38) * torch.sign(u)
+    assert rel(orthogonalize(rt, full), orth64(full)) <= 4 * U16
