@@ -525,7 +525,7 @@ int rtopk_matrix_poll_status(rtopk_matrix* ctx, void* stream);
  * The products take 16-bit floating-point operands and 32-bit sums.  X itself and the diagonals of X X^T
  * and of its polynomial are kept in 32 bits beside them: the result is within about 1e-3 of the
  * exact iteration (2-norm of the difference over 2-norm of the result).
- * Errors: INVALID_ARG, UNSUPPORTED (batch above 65535, m above 4194240), CUDA.
+ * Errors: INVALID_ARG, UNSUPPORTED (batch above 65535, m above 4194240, more scratch than 64 bits count), CUDA.
  */
 int rtopk_orthogonalize_scratch(int64_t batch, int64_t m, int64_t n, int64_t* bytes);
 int rtopk_orthogonalize(rtopk_matrix* ctx, const void* src, int src_dtype, int64_t ld_src, int64_t stride_src, void* out,

@@ -110,6 +110,9 @@ struct OrthScratch {
   }
 };
 
+// Sizes whose scratch would not fit 64 bits of bytes (nor any memory).
+bool orth_too_large(int64_t batch, int64_t m, int64_t n) { return (double)batch * (double)std::min(m, n) * (double)up(std::max(m, n), 64) > 0x1p56; }
+
 struct CodedScratch {
   int8_t *x_rows, *dy_rows, *x_cols, *dy_cols;
   float *x_row_s, *dy_row_s, *x_col_s, *dy_col_s;
@@ -335,7 +338,7 @@ int check_orth(const rtopk_matrix* ctx, int64_t batch, int64_t m, int64_t n, int
   if (coef)
     for (int i = 0; i < 3 * steps; ++i)
       if (!std::isfinite(coef[i])) return RTOPK_ERR_INVALID_ARG;
-  if (batch > kBatchMax || m > 64 * kBatchMax) return RTOPK_ERR_UNSUPPORTED;
+  if (batch > kBatchMax || m > 64 * kBatchMax || orth_too_large(batch, m, n)) return RTOPK_ERR_UNSUPPORTED;
   return RTOPK_OK;
 }
 
@@ -511,6 +514,7 @@ int rtopk_matrix_poll_status(rtopk_matrix* ctx, void* stream) {
 
 int rtopk_orthogonalize_scratch(int64_t batch, int64_t m, int64_t n, int64_t* bytes) {
   if (!bytes || batch < 1 || m < 1 || n < 1 || batch > kBatchMax || m > kDimMax || n > kDimMax) return RTOPK_ERR_INVALID_ARG;
+  if (orth_too_large(batch, m, n)) return RTOPK_ERR_UNSUPPORTED;
   Carve c{nullptr};
   OrthScratch w(c, batch, std::min(m, n), std::max(m, n));
   *bytes = c.at;

@@ -16,7 +16,7 @@ def _scratch(what: str, *sizes: int) -> int:
     n = _i64(0)
     rc = getattr(load_library(), what)(*sizes, C.byref(n))
     if rc != 0:
-        raise RTopKError(rc, what, "invalid argument")
+        raise RTopKError(rc, what, load_library().rtopk_status_string(rc).decode())
     return int(n.value)
 
 

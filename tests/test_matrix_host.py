@@ -114,3 +114,17 @@ def test_gradients_without_x_name_what_is_missing():
     with pytest.raises(ValueError, match="x"):
         ctx.coded_gradients(torch.zeros(3, 40), None, coded, dw=torch.zeros(40, 30))
     assert not ctx._lib.calls
+
+
+def test_scratch_sizes_are_sizes_or_refusals():
+    """Either at least the bytes of X in its three forms, or UNSUPPORTED; never a wrapped number."""
+    import itertools
+    for batch, m, n in itertools.product((1, 3, 65535), (1, 1000, 1 << 20, 1 << 30), (1, 1500, 1 << 24, 1 << 30)):
+        try:
+            assert rt.orthogonalize_scratch(batch, m, n) >= 8 * batch * m * n
+        except rt.RTopKError as e:
+            assert e.status == 4 and batch * m * n >= 1 << 50, (batch, m, n)
+    with pytest.raises(rt.RTopKError):
+        rt.orthogonalize_scratch(1, 1 << 30, 1 << 30)
+    for tokens, n_out, n_in in itertools.product((0, 1, 1 << 30), (1, 1 << 30), (1, 1 << 30)):
+        assert rt.coded_scratch(tokens, n_out, n_in) >= tokens * (n_in + n_out) + (n_in + n_out) * max(tokens, 128)
