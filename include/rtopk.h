@@ -567,7 +567,7 @@ int rtopk_coded_scratch(int64_t tokens, int64_t n_out, int64_t n_in, int64_t* by
 /*
  * A linear layer on codes: x (tokens x n_in of dtype) is coded for each token, and
  *     out[t][n] = s_t s_n sum_k q_x[t][k] q_w[n][k]        (tokens x n_out of dtype)
- * The integer sums are exact.  tokens = 0 does nothing.
+ * The integer sums are exact.  tokens = 0 does nothing and needs no scratch.
  * Errors: INVALID_ARG, UNSUPPORTED (n_in above 131072, where a sum could leave 32 bits), CUDA.
  */
 int rtopk_coded_product(rtopk_matrix* ctx, const void* x, int dtype, int64_t ld_x, const int8_t* codes, int64_t ld_codes,
@@ -580,7 +580,7 @@ int rtopk_coded_product(rtopk_matrix* ctx, const void* x, int dtype, int64_t ld_
  *     dw[n][k] = s_n s_k sum_t q(dy)[t][n] q(x)[t][k]      both coded for each channel, over the tokens.
  *   dx  tokens x n_in of dtype, may be null (codes_t and scales are read for dx alone);
  *   dw  n_out x n_in of dw_dtype, overwritten, may be null (x is read for dw alone): a worker's gradient as
- *       rtopk_sparsify takes it.  With tokens = 0 it is zero.
+ *       rtopk_sparsify takes it.  With tokens = 0 it is zero, and no scratch is needed.
  * Errors: INVALID_ARG, UNSUPPORTED (n_out for dx, tokens for dw above 131072), CUDA.
  */
 int rtopk_coded_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int dtype,

@@ -584,10 +584,10 @@ int rtopk_coded_product(rtopk_matrix* ctx, const void* x, int dtype, int64_t ld_
   if (bad_dtype(dtype) || bad_codes(codes, ld_codes, n_in) || !scales || !aligned_to(scales, 4)) return RTOPK_ERR_INVALID_ARG;
   if (tokens && (bad_view(x, elem(dtype), 1, tokens, n_in, ld_x, 0) || bad_view(out, elem(dtype), 1, tokens, n_out, ld_out, 0))) return RTOPK_ERR_INVALID_ARG;
   if (n_in > kDepthMax) return RTOPK_ERR_UNSUPPORTED;
+  if (!tokens) return RTOPK_OK;
   int64_t need = 0;
   rtopk_coded_scratch(tokens, n_out, n_in, &need);
   if (need > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
-  if (!tokens) return RTOPK_OK;
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
   if (dtype == RTOPK_F32) return product(ctx, (const float*)x, ld_x, codes, ld_codes, scales, tokens, n_out, n_in, (float*)out, ld_out, (cudaStream_t)stream);
@@ -605,7 +605,7 @@ int rtopk_coded_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy, cons
   if ((dx && n_out > kDepthMax) || (dw && tokens > kDepthMax)) return RTOPK_ERR_UNSUPPORTED;
   int64_t need = 0;
   rtopk_coded_scratch(tokens, n_out, n_in, &need);
-  if (need > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
+  if (tokens && need > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
   cudaStream_t st = (cudaStream_t)stream;

@@ -169,3 +169,16 @@ def test_norms_at_both_ends_of_the_range(rt, m, n):  # noqa: F811
     assert rel(orthogonalize(rt, big), orth64(big)) <= 4 * U16
     full = torch.full_like(u, 3.4e38) * torch.sign(u)
     assert rel(orthogonalize(rt, full), orth64(full)) <= 4 * U16
+
+
+def test_no_tokens_need_no_scratch(rt):  # noqa: F811
+    ctx, coded = rt.MatrixContext(0), rt.CodedWeights(40, 30)
+    f = lambda *s: torch.full(s, 2.0, device="cuda")       # noqa: E731
+    dw = f(40, 33)
+    ctx.coded_product(f(0, 30), coded, f(0, 40))
+    ctx.coded_gradients(f(0, 40), f(0, 30), coded, f(0, 30), dw[:, :30])
+    ctx.poll_status()
+    assert bool((dw[:, :30] == 0).all()) and bool((dw[:, 30:] == 2.0).all())
+    with pytest.raises(rt.RTopKError):                      # arguments are looked at all the same
+        ctx.coded_gradients(f(0, 40), f(0, 30), coded)
+    ctx.close()
