@@ -479,19 +479,19 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
           for (int i = 0; i < 32; ++i) mine[(c + i) * S::kTileLanes] = acc[i];
         }
         leave_tile();
-        __threadfence();
         if (!together()) break;
         if (warp == 2 && lane == 0) {
           uint32_t* seen = g.arrived + (u / g.split) * kBlocks + rank;
+          __threadfence();      // stands between the block's parts, which this thread has seen to be written, and its count,
           const uint32_t before = atomicAdd(seen, 1u);
           if (before + 1 == (uint32_t)g.split) *seen = 0u;
+          __threadfence();      // and between the others' counts and the block's reading of their parts
           words[2] = before + 1 == (uint32_t)g.split;
         }
         if (!together()) break;
         const bool last = words[2] != 0u;
         if (!together()) break;      // words[2] may change from here on
         if (!last) continue;
-        __threadfence();
       }
 #pragma unroll 1
       for (int c = chunk0; c < cols; c += kNext) {
