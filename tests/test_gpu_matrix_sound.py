@@ -182,3 +182,11 @@ def test_no_tokens_need_no_scratch(rt):  # noqa: F811
     with pytest.raises(rt.RTopKError):                      # arguments are looked at all the same
         ctx.coded_gradients(f(0, 40), f(0, 30), coded)
     ctx.close()
+
+
+@pytest.mark.parametrize("n", [1 << 16, (1 << 22) + 8, 1 << 25])
+def test_long_rows_of_equal_squares(rt, n):  # noqa: F811
+    """Equal terms make every rounding of a chain of sums fall the same way.  One row has no products, only its sum of squares: the bound is
+    that of orthogonal rows."""
+    for u in (torch.ones((1, 1, n), device="cuda"), torch.full((1, n, 1), -0.3, device="cuda")):
+        assert rel(orthogonalize(rt, u), orth64(u)) <= ORTHOGONAL_ROWS
