@@ -209,6 +209,12 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
 // the results of a tile take so many cycles a column after the last products, six tenths of that beside the next tile's; parts
 // are written and read again.  Where the choice is close: the product with X of 2048 x 2048 as two 128-column tiles a pair or one
 // of 256, 234 and 241 us the whole operator; of four 1500 x 6000, eight tiles of 256 or sixteen of 128, 1372 and 1495 us.
+//
+// Contractions beyond kStepsMax steps are cut further, as far as their parts fit the scratch, in several waves if need be: the tensor core
+// drops what falls below its accumulator's last bit, which in 4096 instructions takes up to 2.5e-4 of a sum of equal terms; the
+// parts are added with rounding.  One step of two nearly equal rows of 2^24 numbers: error 6.7e-3 in eight parts, 5.4e-4 in 256, as
+// for short rows.
+constexpr int64_t kStepsMax = 1024;
 template <int kEpi>
 int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, cudaStream_t st) {
   constexpr double kColumn = kEpi == EPI_CODED ? 35 : kEpi == EPI_GRAM || kEpi == EPI_OUT ? 45 : 75;
@@ -217,8 +223,9 @@ int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, c
   int which = 0, parts = 1;
   auto consider = [&](int id, int64_t tiles, int cols, int blocks, int stage_bytes) {
     const int64_t sms = std::min(ctx->sms, kPartBlocks) / blocks, all = tiles * g.batch;
-    for (int split = 1; split <= 8; ++split) {
-      if (split > 1 && (all * split > sms || steps < 4 * split || all > kSplitTiles)) break;
+    const int64_t room = kPartsBytes / ((int64_t)cols * kLanes * blocks * 4), least = std::min(ceil_div(steps, kStepsMax), std::max<int64_t>(1, room / all));
+    for (int split = (int)least; split <= std::max<int64_t>(8, least); ++split) {
+      if (split > 1 && ((split > least && all * split > sms) || steps < 4 * split || all > kSplitTiles)) break;
       if ((split - 1) * ceil_div(steps, split) >= steps) continue;      // a part without any step
       const double main = (double)ceil_div(steps, split) * std::max(stage_bytes / 64.0, cols * 2.0) + 500, tail = cols * kColumn;
       const double t = main + tail + (ceil_div(all * split, sms) - 1) * std::max(main, 0.6 * tail) + (split > 1 ? cols * (16.0 + 16.0 * split) + 3000 : 0);

@@ -190,3 +190,17 @@ def test_long_rows_of_equal_squares(rt, n):  # noqa: F811
     that of orthogonal rows."""
     for u in (torch.ones((1, 1, n), device="cuda"), torch.full((1, min(n, 64 * 65535), 1), -0.3, device="cuda")):      # as many rows as are taken
         assert rel(orthogonalize(rt, u), orth64(u)) <= ORTHOGONAL_ROWS
+
+
+@pytest.mark.parametrize("n", [1 << 12, 1 << 17, (1 << 20) + 24, 1 << 22, 1 << 24])
+def test_long_rows_that_nearly_depend_on_each_other(rt, n):  # noqa: F811
+    """What the tensor core adds up in one accumulator loses a little at every step, always downwards; the products of nearly equal rows
+    show it most.  One step of two rows has one entry off each diagonal, about 0.5 of a Gram matrix with an eigenvalue near 1 and
+    a + b + c = 0.70 times X as the result.  Rounding that entry to 16 bits (u = 2^-11 of it) moves the result by |b + 2 c| 0.5 u = 0.36 u;
+    the polynomial's, (b + c) 0.5 = -1.37, by 1.37 u: 2.5 u of 0.70 together.  3 u taken, whatever the length."""
+    u = matrices("gauss", 1, 2, n)
+    u[0, 1] = u[0, 0] + 0.1 * u[0, 1]
+    t = torch.ones((1, 2, n), device="cuda")
+    t[0, 1, ::2] = 0.5
+    for v in (u, t, t[:, :, :min(n, 64 * 65535)].mT.contiguous()):
+        assert rel(orthogonalize(rt, v, steps=1), orth64(v, 1)) <= 3 * U16
