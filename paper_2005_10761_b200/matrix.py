@@ -88,7 +88,9 @@ class CodedWeights:
 
 class MatrixContext:
     """A context of the matrix operators on one device, with its scratch.  Tensors must live on that device; rows must be
-    contiguous (last stride 1), everything else is passed as strides."""
+    contiguous (last stride 1), everything else is passed as strides.  Calls go to the current stream; those that share a
+    context share its scratch and must follow one another, on one stream or ordered by events.  A graph that captured calls needs
+    the context until its last replay."""
 
     def __init__(self, scratch_bytes: int, device: Optional[int] = None):
         if not torch.cuda.is_available():
@@ -97,7 +99,8 @@ class MatrixContext:
         self._h = None
         self.device = torch.cuda.current_device() if device is None else int(device)
         self._raw_stream = torch._C._cuda_getCurrentRawStream      # the handle alone: a Stream object takes microseconds
-        # from torch's allocator, which knows the stream that the scratch was made on; others are made known to it as they come
+        # From torch's allocator, which knows the stream that the scratch was made on; others are made known to it as they come.  That
+        # stream may still be using the memory for what it held before, and it clears the library's counters: others wait for it.
         self._scratch = torch.empty(scratch_bytes, dtype=torch.uint8, device=f"cuda:{self.device}") if scratch_bytes > 0 else None
         self._streams = {self._raw_stream(self.device)}
         h = _vp()
@@ -106,13 +109,19 @@ class MatrixContext:
         if rc != 0:
             raise RTopKError(rc, "rtopk_matrix_create", self._lib.rtopk_status_string(rc).decode())
         self._h = h
+        self._made = torch.cuda.current_stream(self.device).record_event()
 
     def _stream(self) -> int:
         s = self._raw_stream(self.device)
         if s not in self._streams:
-            self._streams.add(s)
+            stream = torch.cuda.current_stream(self.device)
             if self._scratch is not None:
-                self._scratch.record_stream(torch.cuda.current_stream(self.device))
+                self._scratch.record_stream(stream)
+            with torch.cuda.device(self.device):
+                capturing = torch.cuda.is_current_stream_capturing()
+            if not capturing:       # a capture cannot wait for what is outside it; torch.cuda.graph synchronises before
+                stream.wait_event(self._made)
+                self._streams.add(s)
         return s
 
     def close(self) -> None:

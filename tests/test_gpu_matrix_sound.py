@@ -216,3 +216,45 @@ def test_many_steps(rt, m, n):  # noqa: F811
         assert rel(orthogonalize(rt, u, steps=steps), orth64(u, steps)) <= most, steps
         cubic = [(1.5, -0.5, 0.0)] * steps
         assert rel(orthogonalize(rt, u, steps=steps, coef=cubic), orth64(u, steps, coef=cubic)) <= 4 * U16, steps
+
+
+def test_a_context_used_on_another_stream_than_it_was_made_on(rt):  # noqa: F811
+    """Its scratch comes from torch's allocator, which hands out memory that the making stream may still be using; a call on another stream
+    must not write there before that stream is done with it."""
+    t, k, n = 200, 300, 1200
+    size = rt.coded_scratch(t, n, k)
+    coded, x, y = rt.CodedWeights(n, k), torch.randn((t, k), generator=gen(1), device="cuda"), torch.empty((t, n), device="cuda")
+    ctx = rt.MatrixContext(size)
+    ctx.code_weights(torch.randn((n, k), generator=gen(2), device="cuda"), coded)
+    ctx.coded_product(x, coded, y)
+    want = y.clone()
+    ctx.close()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    old = torch.ones(size, dtype=torch.uint8, device="cuda")
+    at = old.data_ptr()
+    assert int(old.sum()) == size                   # its kernel is loaded from here on
+    torch.cuda.synchronize()
+    torch.cuda._sleep(300_000_000)                  # 0.15 s, no more than one block
+    total = old.sum()
+    del old
+    ctx = rt.MatrixContext(size)
+    assert ctx._scratch.data_ptr() == at            # the case in question
+    with torch.cuda.stream(side):
+        y.zero_()
+        ctx.coded_product(x, coded, y)
+    torch.cuda.synchronize()
+    assert int(total) == size
+    assert torch.equal(y, want)
+    # and captured on a stream of its own
+    graph = torch.cuda.CUDAGraph()
+    ctx = rt.MatrixContext(size)
+    with torch.cuda.graph(graph):
+        ctx.coded_product(x, coded, y)
+    y.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
+    ctx.poll_status()
+    ctx.close()
