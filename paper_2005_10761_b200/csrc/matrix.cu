@@ -217,7 +217,7 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
 constexpr int64_t kStepsMax = 1024;
 template <int kEpi>
 int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, cudaStream_t st) {
-  constexpr double kColumn = kEpi == EPI_CODED ? 35 : kEpi == EPI_GRAM || kEpi == EPI_OUT ? 45 : 75;
+  constexpr double kColumn = kEpi == EPI_CODED ? 35 : kEpi == EPI_GRAM ? 45 : 75;
   const int64_t steps = ceil_div((int64_t)g.depth * (kEpi == EPI_CODED ? 1 : 2), kDepthBytes);
   double best = 1e300;
   int which = 0, parts = 1;
