@@ -526,7 +526,7 @@ int rtopk_matrix_poll_status(rtopk_matrix* ctx, void* stream);
  * polynomial are kept in 32 bits beside them.  Up to 64 x 256 the operands are pairs of 16-bit numbers.  With the default
  * coefficients and five steps the result is within about 1e-3 of the exact iteration (2-norm of the difference over
  * 2-norm of the result): 3e-4 to 7e-4 for a full spectrum or one with 10 % noise, 1e-3 to 3e-3 where a low rank stands over 1 % noise
- * and less, 2e-5 up to 64 x 256.  These coefficients do not contract around 1, so that more steps let the difference grow: 300 x 700
+ * and less and for two or three long rows, whose few roundings do not average out; 3e-5 up to 64 x 256.  These coefficients do not contract around 1, so that more steps let the difference grow: 300 x 700
  * 6e-4 after five, 1.2e-3 after 8, 2.3e-3 after 16, 6e-3 after 24, 9e-3 after 64.  Steps that do contract, such as
  * (1.5, -0.5, 0), keep it at 1e-4.
  * Errors: INVALID_ARG, UNSUPPORTED (batch above 65535, m above 4194240, more scratch than 64 bits count), CUDA.
