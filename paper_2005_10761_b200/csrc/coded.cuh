@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(256) k_codes_transpose(const int8_t* codes, in
 
 // A linear layer for a few tokens: reading the codes of W once is all the work, so one launch does everything.  Each block
 // codes the tokens for itself (they are small, and come from L2), then each warp takes two output channels at a time: 16 codes
-// of W a thread, four-way integer dot products with the tokens' codes in shared memory.  One token through 1500 -> 6000: 5.5 us, which is the
+// of W a thread, four-way integer dot products with the tokens' codes in shared memory.  One token through 1500 -> 6000: 6.2 us, which is the
 // call itself; through 8192 -> 8192 16.9 us (4.0 TB/s; the tokens' coding comes before the first codes of W).
 constexpr int kFewThreads = 256;
 constexpr int kFewBytes = 47 * 1024;       // codes of all tokens in shared memory, at most (48 KB with the rest)

@@ -207,8 +207,8 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
 // Which tile, and in how many parts: the one for which this estimate of the time, in cycles, is least.  A step of 128 bytes of
 // the contraction index takes the tensor core's time or what its stage needs from L2 (64 bytes a cycle and SM, measured);
 // the results of a tile take so many cycles a column after the last products, six tenths of that beside the next tile's; parts
-// are written and read again.  Where the choice is close: the product with X of 2048 x 2048 as two 128-column tiles a pair or one
-// of 256, 234 and 241 us the whole operator; of four 1500 x 6000, eight tiles of 256 or sixteen of 128, 1372 and 1495 us.
+// are written and read again.  Where the choice is close: the products with X of 2048 x 2048 as two 128-column tiles a pair or one
+// of 256, 257 and 258 us the whole operator; of four 1500 x 6000, eight tiles of 256 or sixteen of 128, 1350 and 1420 us.
 //
 // Contractions beyond kStepsMax steps are cut further, as far as their parts fit the scratch, in several waves if need be: the tensor core
 // drops what falls below its accumulator's last bit, which in 4096 instructions takes up to 2.5e-4 of a sum of equal terms; the

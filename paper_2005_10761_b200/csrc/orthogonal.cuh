@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_orth_small(const __grid_const
 //
 // Measured, against a chain of launches, us: 128 x 128 29 / 61, 128 x 256 40 / 63, 128 x 1000 68 / 71, 128 x 2048 76 / 80, thirty of
 // 128 x 1000 73 / 122.  A step is about 5800 cycles in one block; in a cluster 18700, 9200 of them the exchange of 96 KB a
-// block through distributed shared memory at about 16 bytes a cycle.
+// block through distributed shared memory at about 16 bytes a cycle.  512 threads leave 128 registers for each; 124 bytes a thread spill.
 constexpr int kMid = 128, kMidThreads = 512, kMidChunks = 4, kMidCluster = 8, kMidLong = kMidCluster * kMidChunks * kSmall;
 constexpr int kMidTile = kMid * kDepthBytes;                          // 128 rows of 64 16-bit numbers
 constexpr int kMidPart = kMid * kMid * 4, kMidPitch = kSmall + 1;
