@@ -591,6 +591,112 @@ int rtopk_coded_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy, cons
                           const int8_t* codes_t, int64_t ld_t, const float* scales, int64_t tokens, int64_t n_out,
                           int64_t n_in, void* dx, int64_t ld_dx, void* dw, int dw_dtype, int64_t ld_dw, void* stream);
 
+/*
+ * Linear layers on 4-bit codes: half the bytes of the 8-bit ones and twice the tensor cores' rate, for values that bear a step of 17 to
+ * 33 %.  A block of 32 values along the contraction (a row's last may be shorter) has the scale 2^e with the least e >= -127 that
+ * leaves no magnitude above 6 2^e, and codes
+ *     q = v / 2^e rounded to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, ties to the even code.
+ * A code is four bits, sign, exponent (2), mantissa (1), two in a byte, the first of a row in its low half; a scale is the byte
+ * e + 127.  A block with an infinity or a NaN has the scale 255 and zeros for codes: everything that it takes part in is NaN.
+ *
+ * A code array of `rows` rows and `cols` codes: rows of ld bytes, ld a multiple of 16; scales in pieces of 512 bytes for 128 rows and 128
+ * codes.  Row r's scale for its codes 32 b .. 32 b + 31 is the byte
+ *     ((r / 128) P + b / 4) 512 + (r mod 32) 16 + (r mod 128) / 32 * 4 + b mod 4,      P = 2 ceil(cols / 256),
+ * and the scales of codes past a row's end, where there are any, are no NaN.  Codes past a row's end are zero up to a whole number of blocks.
+ * Both bases 16-byte aligned.  rtopk_micro_layout (host only, no GPU work) gives the least ld and the scales' bytes; either may be null.
+ */
+int rtopk_micro_layout(int64_t rows, int64_t cols, int64_t* ld, int64_t* scale_bytes);
+
+/*
+ * W (n_out x n_in of dtype) -> codes along n_in, and with codes_t, which may be null, the same codes transposed (n_in rows along n_out) for the
+ * gradient with respect to x.
+ *   tile   32: one scale for every 32 x 32 weights, so that W^T has the same codes;   1: for every 32 weights of a row
+ *          (nearer to W; codes_t is null).
+ * Needs no scratch.  Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 1 pieces of 128 x 128), CUDA.
+ */
+int rtopk_micro_weights(rtopk_matrix* ctx, const void* weights, int dtype, int64_t ld_w, int64_t n_out, int64_t n_in, int tile,
+                        uint8_t* codes, int64_t ld_codes, uint8_t* scales, uint8_t* codes_t, int64_t ld_t, uint8_t* scales_t,
+                        void* stream);
+
+/* Scratch of the two calls below for up to `tokens` tokens. */
+int rtopk_micro_scratch(int64_t tokens, int64_t n_out, int64_t n_in, int64_t* bytes);
+
+/*
+ * A linear layer on them: x (tokens x n_in of dtype) is coded along n_in, and
+ *     out[t][n] = sum_k 2^(e_x + e_w) q_x[t][k] q_w[n][k]        (tokens x n_out of dtype)
+ * with exact products and 32-bit sums.  tokens = 0 does nothing and needs no scratch.
+ * Errors: INVALID_ARG, UNSUPPORTED (as above, for x), CUDA.
+ */
+int rtopk_micro_product(rtopk_matrix* ctx, const void* x, int dtype, int64_t ld_x, const uint8_t* codes, int64_t ld_codes,
+                        const uint8_t* scales, int64_t tokens, int64_t n_out, int64_t n_in, void* out, int64_t ld_out, void* stream);
+
+/*
+ * The gradients of that layer for dy (tokens x n_out of dtype), the rounding to codes taken as the identity:
+ *     dx[t][k] = sum_n 2^(e_dy + e_w) q_dy[t][n] q_w[n][k]        dy coded along n_out, W's codes those of the forward pass;
+ *     dw[n][k] = sum_t 2^(e_dy + e_x) q_dy[t][n] q_x[t][k]        both coded along the tokens.
+ *   dx  tokens x n_in of dtype, may be null (codes_t and scales_t are read for dx alone);
+ *   dw  n_out x n_in of dw_dtype, overwritten, may be null (x is read for dw alone).  With tokens = 0 it is zero, and no scratch is needed.
+ * Errors: INVALID_ARG, UNSUPPORTED (as above, for x and dy), CUDA.
+ */
+int rtopk_micro_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int dtype,
+                          const uint8_t* codes_t, int64_t ld_t, const uint8_t* scales_t, int64_t tokens, int64_t n_out, int64_t n_in,
+                          void* dx, int64_t ld_dx, void* dw, int dw_dtype, int64_t ld_dw, void* stream);
+
+/*
+ * Dropout whose mask is never stored.  Element (i, j) of the rows x cols elements has a 16-bit number: of
+ *     Philox4x32-10(counter = (j / 8, i, 2^31 + 2^16 site + worker, step), key = (seed low word, seed high word))
+ * the half of the four words, lowest first, at j mod 8.  With T = min(rint(65536 p), 65535) an element whose number is below T is
+ * dropped; the others are multiplied by 65536 / (65536 - T), rounded to binary32.  No counter is one of the sampler's.
+ * The struct is HOST memory, read before the call returns.
+ *   p         0 <= p < 1;   worker  < 65536;   site  < 32768, which of a network's masks;
+ *   step_ptr  DEVICE word added to `step` when the call's kernels run, or null: a captured graph's round.
+ */
+typedef struct {
+  double p;
+  uint64_t seed;
+  const uint32_t* step_ptr;
+  uint32_t step, worker, site;
+} rtopk_mask;
+
+/*
+ * out = D(x), D the dropout of `mask`; x, out rows x cols of dtype, out may be x.  Its gradient is the same call on the gradient of out.
+ * What is dropped is 0 whatever it was.  Needs no scratch.  Errors: INVALID_ARG, UNSUPPORTED (2^46 elements and more), CUDA.
+ */
+int rtopk_dropout(rtopk_matrix* ctx, const void* x, int dtype, int64_t ld_x, int64_t rows, int64_t cols, const rtopk_mask* mask,
+                  void* out, int64_t ld_out, void* stream);
+
+/*
+ * Layer normalisation of every row, behind dropout and the residual sum:
+ *     t = residual + D(x);   mean = sum t / cols;   rstd = 1 / sqrt(sum (t - mean)^2 / cols + eps);
+ *     out = gamma (t - mean) rstd + beta
+ *   residual   may be null (t = D(x));   mask  may be null (t = residual + x);
+ *   gamma, beta  cols binary32 each, may be null (1 and 0);
+ *   total [out]  t rounded to dtype, may be null;   mean, rstd [out]  rows binary32 each, may be null.  Both are of t before it is rounded.
+ * x, residual, out, total rows x cols of dtype; out and total may each be x or residual itself, with its row stride.  eps finite, >= 0.
+ * A row with a NaN or an infinity gives NaN.  Needs no scratch.  Errors: INVALID_ARG, CUDA.
+ */
+int rtopk_layer_norm(rtopk_matrix* ctx, const void* x, int64_t ld_x, const void* residual, int64_t ld_r, int dtype, int64_t rows,
+                     int64_t cols, const float* gamma, const float* beta, float eps, const rtopk_mask* mask, void* out, int64_t ld_out,
+                     void* total, int64_t ld_t, float* mean, float* rstd, void* stream);
+
+/* Scratch of the call below for dgamma or dbeta. */
+int rtopk_layer_norm_scratch(int64_t rows, int64_t cols, int64_t* bytes);
+
+/*
+ * Its gradients for dy (that of out) and dtotal (what reaches t on its other way; may be null), with h = (total - mean) rstd and g = gamma dy:
+ *     dresidual = rstd (g - sum g / cols - h sum (g h) / cols) + dtotal;      dx = D(dresidual)
+ *     dgamma = sum over the rows of dy h;   dbeta = sum over the rows of dy
+ *   total, mean, rstd [in]  of the forward call (without residual and mask, total is its x);   gamma  may be null (1);
+ *   mask       the forward call's, or null;   dx  given if and only if mask is (without one it is dresidual);
+ *   dresidual  may be null; it, or dx, may be dy or dtotal itself, with its row stride;
+ *   dgamma, dbeta  cols binary32 each, overwritten, may be null.  With rows = 0 they are zero, and no scratch is needed.
+ * At least one of the four results is asked for.  The same bits every time.  Errors: INVALID_ARG, CUDA.
+ */
+int rtopk_layer_norm_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy, const void* total, int64_t ld_t, const void* dtotal,
+                               int64_t ld_dt, int dtype, int64_t rows, int64_t cols, const float* mean, const float* rstd,
+                               const float* gamma, const rtopk_mask* mask, void* dresidual, int64_t ld_dr, void* dx, int64_t ld_dx,
+                               float* dgamma, float* dbeta, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

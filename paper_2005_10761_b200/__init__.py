@@ -7,8 +7,9 @@ fallback: using the binding without the built library or without a CUDA device r
 from .workloads import Workload, configs, gradient, zero_residual  # noqa: F401
 from .binding import (RTopK, RTopKError, library_path, load_library, packed_layout, tiled_layout, warmup_sizes, GRAD_F32, GRAD_BF16,  # noqa: F401
                       SCALE_MEAN, SCALE_SUM, SCALE_UNBIASED, SCALE_COUNT, EXPORTS)
-from .matrix import CodedWeights, MatrixContext, coded_scratch, orthogonalize_scratch  # noqa: F401
+from .matrix import (CodedWeights, Mask, MatrixContext, MicroWeights, coded_scratch, layer_norm_scratch, micro_layout, micro_scratch,  # noqa: F401
+                     orthogonalize_scratch)
 
 __all__ = ["RTopK", "RTopKError", "library_path", "load_library", "packed_layout", "tiled_layout", "warmup_sizes", "Workload", "configs", "gradient",
            "zero_residual", "GRAD_F32", "GRAD_BF16", "SCALE_MEAN", "SCALE_SUM", "SCALE_UNBIASED", "SCALE_COUNT", "EXPORTS",
-           "MatrixContext", "CodedWeights", "orthogonalize_scratch", "coded_scratch"]
+           "MatrixContext", "CodedWeights", "orthogonalize_scratch", "coded_scratch", "MicroWeights", "Mask", "micro_layout", "micro_scratch", "layer_norm_scratch"]

@@ -86,6 +86,18 @@ EXPORTS = {
     "rtopk_coded_product": (_int, [_vp, _vp, _int, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp]),
     "rtopk_coded_gradients": (_int, [_vp, _vp, _i64, _vp, _i64, _int, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _int,
                                      _i64, _vp]),
+    "rtopk_micro_layout": (_int, [_i64, _i64, C.POINTER(_i64), C.POINTER(_i64)]),
+    "rtopk_micro_weights": (_int, [_vp, _vp, _int, _i64, _i64, _i64, _int, _vp, _i64, _vp, _vp, _i64, _vp, _vp]),
+    "rtopk_micro_scratch": (_int, [_i64, _i64, _i64, C.POINTER(_i64)]),
+    "rtopk_micro_product": (_int, [_vp, _vp, _int, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp]),
+    "rtopk_micro_gradients": (_int, [_vp, _vp, _i64, _vp, _i64, _int, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _int,
+                                     _i64, _vp]),
+    "rtopk_dropout": (_int, [_vp, _vp, _int, _i64, _i64, _i64, _vp, _vp, _i64, _vp]),
+    "rtopk_layer_norm": (_int, [_vp, _vp, _i64, _vp, _i64, _int, _i64, _i64, _vp, _vp, C.c_float, _vp, _vp, _i64, _vp, _i64, _vp,
+                                _vp, _vp]),
+    "rtopk_layer_norm_scratch": (_int, [_i64, _i64, C.POINTER(_i64)]),
+    "rtopk_layer_norm_gradients": (_int, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _int, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i64,
+                                          _vp, _i64, _vp, _vp, _vp]),
 }
 
 _lib: Optional[C.CDLL] = None

@@ -51,7 +51,8 @@ enum Epi : int {
   EPI_APPLY = 2,   // X <- (that) X, in 32 bits and in 16
   EPI_OUT = 3,     // the last X, into the caller's matrix
   EPI_UPDATE = 4,  // the last X, into the caller's weights
-  EPI_CODED = 5    // 8-bit codes: times the two scales
+  EPI_CODED = 5,   // 8-bit codes: times the two scales
+  EPI_MICRO = 6    // 4-bit codes with a power of two for every 32 along the contraction, which the tensor core multiplies in
 };
 
 struct Gemm {
@@ -183,7 +184,7 @@ __device__ __forceinline__ void read_ahead(const Gemm& g, int z, int lane, int c
     load_strip<kFull>((const float*)g.x + z * g.stride + col0 * g.ld + safe, n, g.ld, ahead.at);
   }
   if constexpr (kEpi == EPI_CODED) ahead.col = g.scale_col[my_col];
-  else if constexpr (kEpi != EPI_GRAM) ahead.col = g.d_in[z * g.d_stride + my_col];
+  else if constexpr (kEpi != EPI_GRAM && kEpi != EPI_MICRO) ahead.col = g.d_in[z * g.d_stride + my_col];
 }
 
 // 32 columns (col0 ..) of lane `lane` of one tile; all 32 threads of the warp come here, each with its lane.  kFull: the
@@ -193,8 +194,8 @@ template <int kEpi, bool kFull>
 __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col0, int n, float of_lane, float* cols, const Ahead<kEpi>& ahead, const uint32_t (&acc)[32]) {
   const int me = threadIdx.x & 31;
   bool in = kFull || lane < g.lanes;
-  float of_col[kEpi == EPI_GRAM ? 1 : 32];      // every column's number in every thread: by way of the warp's place in shared memory
-  if constexpr (kEpi != EPI_GRAM) {
+  float of_col[kEpi == EPI_GRAM || kEpi == EPI_MICRO ? 1 : 32];      // every column's number in every thread: by way of the warp's place in shared memory
+  if constexpr (kEpi != EPI_GRAM && kEpi != EPI_MICRO) {
     cols[me] = ahead.col;
     __syncwarp();
 #pragma unroll
@@ -233,9 +234,12 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
     for (int c = 0; c < 32; c += 8)
       if (kFull || c < n) store_half8(row + c, v + c);
     if (cb > lb) store_strip<kFull>(g.h + z * g.stride + col0 * g.ld + lane, n, g.ld, [&](int c) { return to_half(v[c]); });
-  } else if constexpr (kEpi == EPI_CODED) {
+  } else if constexpr (kEpi == EPI_CODED || kEpi == EPI_MICRO) {
 #pragma unroll
-    for (int c = 0; c < 32; ++c) v[c] = (float)(int)acc[c] * of_col[c] * of_lane;
+    for (int c = 0; c < 32; ++c) {
+      if constexpr (kEpi == EPI_MICRO) v[c] = __uint_as_float(acc[c]);
+      else v[c] = (float)(int)acc[c] * of_col[c] * of_lane;
+    }
     if (!in) return;
     const int64_t at = lane + col0 * g.out_col;
     if (g.out_bf16) store_strip<kFull>((__nv_bfloat16*)g.out + at, n, g.out_col, [&](int c) { return __float2bfloat16_rn(v[c]); });
@@ -296,26 +300,37 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
   }
 }
 
-template <int kCols, bool kPair>
+template <int kCols, bool kPair, bool kMicro = false>
 struct GemmShape {
   static constexpr int kTileLanes = kPair ? 2 * kLanes : kLanes;
   static constexpr int kQRows = kPair ? kCols / 2 : kCols;             // rows of Q in one block's stage
-  static constexpr int kPBytes = kLanes * kDepthBytes, kQBytes = kQRows * kDepthBytes, kStageBytes = kPBytes + kQBytes;
-  static constexpr int kFit = (kSmemLimit - kSmemMisc) / kStageBytes;
-  static constexpr int kStages = kFit > 8 ? 8 : kFit;
+  static constexpr int kPBytes = kLanes * kDepthBytes, kQBytes = kQRows * kDepthBytes;
+  // scales of 4-bit codes: eight for each row of a stage, 1024 bytes for 128 rows; a block multiplies all of the tile's columns, so it has
+  // all of their scales.  In tensor memory each stage has its own columns for them: they are filled when the stage's products before are done.
+  static constexpr int kQAtoms = kMicro ? (kCols + 127) / 128 : 0, kScaleBytes = kMicro ? 1024 * (1 + kQAtoms) : 0, kScaleCols = kMicro ? 8 * (1 + kQAtoms) : 0;
+  static constexpr int kStageBytes = kPBytes + kQBytes + kScaleBytes;
+  static constexpr int kFit = (kSmemLimit - kSmemMisc) / kStageBytes, kRoom = kMicro ? (512 - 2 * kCols) / kScaleCols : 8;
+  static constexpr int kMost = kRoom < 8 ? kRoom : 8, kStages = kFit > kMost ? kMost : kFit;
+  static constexpr int kTmemUsed = 2 * kCols + (kMicro ? kStages * kScaleCols : 0), kTmemCols = kTmemUsed <= 128 ? 128 : kTmemUsed <= 256 ? 256 : 512;
   static constexpr int kSmem = kStages * kStageBytes + 2048;      // the rest is static
 };
 
+// The scales' maps, for products that have them: words of 32 bits, [128 rows][step of the contraction index][256].
+template <int kEpi>
+struct Scales {};
+template <>
+struct Scales<EPI_MICRO> { CUtensorMap p, q; };
+
 template <int kCols, bool kPair, int kEpi>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ Gemm g) {
-  using S = GemmShape<kCols, kPair>;
-  constexpr bool kInt8 = kEpi == EPI_CODED;
+k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ Scales<kEpi> scales, const __grid_constant__ Gemm g) {
+  constexpr bool kInt8 = kEpi == EPI_CODED, kMicro = kEpi == EPI_MICRO;
+  using S = GemmShape<kCols, kPair, kMicro>;
   constexpr bool kMnMajor = kEpi == EPI_APPLY || kEpi == EPI_OUT || kEpi == EPI_UPDATE;   // P is stored with its lanes contiguous
   constexpr int kStages = S::kStages;
-  constexpr int kDepth = kInt8 ? kDepthBytes : kDepthBytes / 2;      // elements of the contraction index per stage
+  constexpr int kDepth = kInt8 || kMicro ? kDepthBytes : kDepthBytes / 2;      // of the contraction index per stage, in elements of the map
   constexpr int kBlocks = kPair ? 2 : 1;
-  constexpr uint32_t kTmemCols = 2 * kCols;
+  constexpr uint32_t kTmemCols = S::kTmemCols;
 
   extern __shared__ char smem_raw[];
   __shared__ __align__(16) float epi_cols[kEpiWarps][32];
@@ -337,6 +352,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     bar_init_fence();
     tma_prefetch(&map_p);
     tma_prefetch(&map_q);
+    if constexpr (kMicro) tma_prefetch(&scales.p), tma_prefetch(&scales.q);
   }
   if (warp == 1) tmem_alloc<kPair>(smem_addr((const void*)words), kTmemCols);
   tc_fence_before();
@@ -358,6 +374,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
     } else {
       tma_load<kPair>(dst, &map_p, kb * kDepth, row, q.z, bar);
     }
+    if constexpr (kMicro) tma_load<kPair>(dst + S::kPBytes + S::kQBytes, &scales.p, 0, kb, row / kLanes, bar);
   };
   uint32_t early = 0;      // stages whose P is under way
   if (g.p_early && warp == 0 && first < total) {
@@ -387,7 +404,12 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
         if (!(ok = it < feed)) break;
         if (elect_one()) {
           if (it >= early) load_p(s, q, kb);
-          tma_load<kPair>(base + s * S::kStageBytes + S::kPBytes, &map_q, kb * kDepth, q.c * kCols + rank * S::kQRows, q.z, kPair ? first_of_pair(full + 8 * s) : full + 8 * s);
+          const uint32_t dst = base + s * S::kStageBytes + S::kPBytes, bar = kPair ? first_of_pair(full + 8 * s) : full + 8 * s;
+          tma_load<kPair>(dst, &map_q, kb * kDepth, q.c * kCols + rank * S::kQRows, q.z, bar);
+          if constexpr (kMicro) {
+#pragma unroll
+            for (int a = 0; a < S::kQAtoms; ++a) tma_load<kPair>(dst + S::kQBytes + 1024 * (1 + a), &scales.q, 0, kb, q.c * kCols / kLanes + a, bar);
+          }
         }
         __syncwarp();
       }
@@ -415,9 +437,24 @@ k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtens
           // one instruction takes 32 bytes of the contraction index: 16 steps of an MN-major tile are 2048 bytes on
           const uint64_t dp = smem_desc(src, kMnMajor ? S::kPBytes / 2 : 16), dq = smem_desc(src + S::kPBytes, 16);
           if (elect_one()) {
+            if constexpr (kMicro) {
+              // Of P's scales, then of Q's: 128 codes are four columns for each 128 rows.  A tile of Q that begins in the middle of 128 rows
+              // finds its scales two columns on.
+              const uint32_t to = tmem + 2 * kCols + s * S::kScaleCols, from = src + S::kPBytes + S::kQBytes, shift = q.c * kCols % kLanes / 32;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              tc_mma<kPair, kInt8>(tmem + b * kCols, dp + (kMnMajor ? k * (2048 >> 4) : k * 2), dq + k * 2, kDesc, kb > k0 || k);
+              for (int j = 0; j < 2; ++j) {
+                tc_copy_scales<kPair>(to + 4 * j, scale_desc(from + 512 * j));
+#pragma unroll
+                for (int a = 0; a < S::kQAtoms; ++a) tc_copy_scales<kPair>(to + 8 + 4 * (S::kQAtoms * j + a), scale_desc(from + 1024 * (1 + a) + 512 * j));
+              }
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                tc_mma_micro<kPair>(tmem + b * kCols, dp + k * 2, dq + k * 2, micro_desc(S::kTileLanes, kCols, k & 1), to + 4 * (k / 2), to + 8 + 4 * S::kQAtoms * (k / 2) + shift, kb > k0 || k);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                tc_mma<kPair, kInt8>(tmem + b * kCols, dp + (kMnMajor ? k * (2048 >> 4) : k * 2), dq + k * 2, kDesc, kb > k0 || k);
+            }
             tc_commit<kPair>(empty + 8 * s);
           }
           __syncwarp();

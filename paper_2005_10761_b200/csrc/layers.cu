@@ -1,0 +1,330 @@
+// Host side of a worker's layers: linear layers on 4-bit codes, dropout and layer normalisation.
+#include "matrix_host.cuh"
+
+#include <cmath>
+
+#include "micro.cuh"
+#include "norm.cuh"
+
+using namespace rtopk::mat;
+
+namespace {
+
+// ----------------------------------------------------------------------------- 4-bit codes
+int64_t micro_ld(int64_t cols) { return up(ceil_div(cols, 2), 16); }                                  // bytes of a row of codes, at least
+int64_t micro_scale_bytes(int64_t rows, int64_t cols) { return ceil_div(rows, 128) * ceil_div(cols, 256) * 1024; }
+
+struct MicroScratch {
+  MicroOut x_rows, dy_rows, x_cols, dy_cols;
+  MicroScratch(Carve& c, int64_t tokens, int64_t n_out, int64_t n_in) {
+    c.take<char>(kPartsBytes);
+    auto codes = [&](int64_t rows, int64_t cols) {
+      MicroOut o;
+      o.ld = up(ceil_div(cols, 2), 128);
+      o.codes = c.take<uint8_t>(rows * o.ld);
+      o.scales = c.take<uint8_t>(micro_scale_bytes(rows, cols));
+      return o;
+    };
+    tokens = std::max<int64_t>(tokens, 1);
+    x_rows = codes(tokens, n_in);
+    dy_rows = codes(tokens, n_out);
+    x_cols = codes(n_in, tokens);
+    dy_cols = codes(n_out, tokens);
+  }
+};
+
+template <class T, bool kRows, bool kColumns, bool kTile>
+int micro_code(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, const MicroOut& by_row, const MicroOut& by_col, cudaStream_t st) {
+  const int64_t tiles_c = ceil_div(cols, 128), tiles = tiles_c * ceil_div(rows, 128);
+  return launch(ctx, k_micro_code<T, kRows, kColumns, kTile>, dim3((unsigned)tiles), 256, 0, st, src, ld, rows, cols, rows_aligned(src, sizeof(T), 1, ld, 0, 16) ? 1 : 0, tiles_c, by_row,
+                by_col);
+}
+
+// lanes, cols: the rows of the two code arrays; depth: codes along the contraction
+int micro_gemm(rtopk_matrix* ctx, bool lanes_early, bool free_start, const MicroOut& lane, int64_t lanes, const MicroOut& col, int64_t cols, int64_t depth, void* out, int bf16,
+               int64_t ld_out, cudaStream_t st) {
+  Gemm g = {};
+  const int64_t bytes = ceil_div(depth, 2);
+  g.lanes = (int)lanes, g.cols = (int)cols, g.depth = (int)bytes, g.batch = 1;
+  g.out = out, g.out_bf16 = bf16, g.out_col = ld_out, g.out_lane = 1;
+  g.p_early = lanes_early, g.free_start = free_start;
+  return gemm<EPI_MICRO>(ctx, {lane.codes, bytes, lanes, lane.ld, 0, lane.scales}, {col.codes, bytes, cols, col.ld, 0, col.scales}, g, st);
+}
+
+bool bad_micro(const void* codes, int64_t ld, const void* scales, int64_t cols) {
+  return !codes || !scales || !aligned_to(codes, 16) || !aligned_to(scales, 16) || ld < micro_ld(cols) || ld % 16;
+}
+MicroOut as_micro(const uint8_t* codes, int64_t ld, const uint8_t* scales) { return {const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), ld}; }
+
+int check_micro(const rtopk_matrix* ctx, int64_t tokens, int64_t n_out, int64_t n_in) {
+  if (!ctx || tokens < 0 || n_out < 1 || n_in < 1 || tokens > kDimMax || n_out > kDimMax || n_in > kDimMax) return RTOPK_ERR_INVALID_ARG;
+  return RTOPK_OK;
+}
+// Blocks of a coding launch are counted in 31 bits.
+bool micro_too_large(int64_t rows, int64_t cols) { return ceil_div(rows, 128) * ceil_div(cols, 128) > INT32_MAX; }
+
+template <class T>
+int micro_weights(rtopk_matrix* ctx, const T* w, int64_t ld, int64_t n_out, int64_t n_in, int tile, const MicroOut& rows, const MicroOut& cols, cudaStream_t st) {
+  if (tile == 1) return micro_code<T, true, false, false>(ctx, w, ld, n_out, n_in, rows, cols, st);
+  if (!cols.codes) return micro_code<T, true, false, true>(ctx, w, ld, n_out, n_in, rows, cols, st);
+  return micro_code<T, true, true, true>(ctx, w, ld, n_out, n_in, rows, cols, st);
+}
+
+template <class T>
+int micro_product(rtopk_matrix* ctx, const T* x, int64_t ld_x, const MicroOut& w, int64_t tokens, int64_t n_out, int64_t n_in, T* out, int64_t ld_out, cudaStream_t st) {
+  Carve c{ctx->scratch};
+  MicroScratch s(c, tokens, n_out, n_in);
+  MAT_TRY((micro_code<T, true, false, false>(ctx, x, ld_x, tokens, n_in, s.x_rows, s.x_rows, st)));
+  return micro_gemm(ctx, true, false, w, n_out, s.x_rows, tokens, n_in, out, sizeof(T) == 2, ld_out, st);
+}
+
+template <class T>
+int micro_gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, const MicroOut& w_t, int64_t tokens, int64_t n_out, int64_t n_in, T* dx, int64_t ld_dx,
+                    void* dw, int dw_bf16, int64_t ld_dw, cudaStream_t st) {
+  Carve c{ctx->scratch};
+  MicroScratch s(c, tokens, n_out, n_in);
+  if (dw) MAT_TRY((micro_code<T, false, true, false>(ctx, x, ld_x, tokens, n_in, s.x_cols, s.x_cols, st)));
+  if (dx && dw) MAT_TRY((micro_code<T, true, true, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
+  else if (dx) MAT_TRY((micro_code<T, true, false, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
+  else MAT_TRY((micro_code<T, false, true, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
+  if (dx) MAT_TRY(micro_gemm(ctx, true, false, w_t, n_in, s.dy_rows, tokens, n_out, dx, sizeof(T) == 2, ld_dx, st));
+  // The second product does not depend on the first and starts as SMs fall free.
+  if (dw) MAT_TRY(micro_gemm(ctx, false, dx != nullptr, s.x_cols, n_in, s.dy_cols, n_out, tokens, dw, dw_bf16, ld_dw, st));
+  return RTOPK_OK;
+}
+
+// ----------------------------------------------------------------------------- dropout and layer normalisation
+// false: not a mask
+bool as_mask(const rtopk_mask* m, Mask* out) {
+  *out = {};
+  if (!m) return true;
+  if (!(m->p >= 0.0 && m->p < 1.0) || m->worker > 65535u || m->site > 32767u || !aligned_to(m->step_ptr, 4)) return false;
+  const double limit = std::min(std::nearbyint(m->p * 65536.0), 65535.0);
+  out->limit = (uint32_t)limit;
+  out->factor = (float)(65536.0 / (65536.0 - limit));
+  out->key0 = (uint32_t)m->seed, out->key1 = (uint32_t)(m->seed >> 32);
+  out->tag = 0x80000000u | m->site << 16 | m->worker;
+  out->step = m->step, out->step_ptr = m->step_ptr;
+  return true;
+}
+
+int check_rows(const rtopk_matrix* ctx, int64_t rows, int64_t cols, int dtype) {
+  return !ctx || rows < 0 || cols < 1 || rows > kDimMax || cols > kDimMax || bad_dtype(dtype) ? RTOPK_ERR_INVALID_ARG : RTOPK_OK;
+}
+
+template <class T>
+int dropout(rtopk_matrix* ctx, const T* x, int64_t ld_x, int64_t rows, int64_t cols, const Mask& mask, T* out, int64_t ld_out, cudaStream_t st) {
+  const bool vec = rows_aligned(x, sizeof(T), 1, ld_x, 0, 16) && rows_aligned(out, sizeof(T), 1, ld_out, 0, 16);
+  const int64_t units = ceil_div(cols, vec ? 8 : kWarpCols);      // of a row: threads or warps
+  const int64_t per = vec ? 256 * 4 : 8 * 4;                      // of a block
+  const int64_t band = std::max<int64_t>(1, std::min(rows, (int64_t(1) << 31) / units - 1));      // rows whose units 31 bits count
+  if (ceil_div(rows, band) > 65535) return RTOPK_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)ceil_div(band * units, per), (unsigned)ceil_div(rows, band));
+  if (vec) return launch(ctx, k_dropout<T, true>, grid, 256, 0, st, x, ld_x, rows, cols, band, mask, out, ld_out);
+  return launch(ctx, k_dropout<T, false>, grid, 256, 0, st, x, ld_x, rows, cols, band, mask, out, ld_out);
+}
+
+// The row kernels by the number of warps of a row: as many as hold it in their registers (1024 columns each), more where there are
+// too few rows to fill the SMs.
+template <class F>
+int by_warps(const rtopk_matrix* ctx, int64_t rows, int64_t cols, F go) {
+  const int64_t warps = rows <= 4 * ctx->sms ? ceil_div(cols, 256) : ceil_div(cols, 1024);
+  if (warps <= 1) return go(std::integral_constant<int, 1>{});
+  if (warps <= 2) return go(std::integral_constant<int, 2>{});
+  if (warps <= 4) return go(std::integral_constant<int, 4>{});
+  if (warps <= 8) return go(std::integral_constant<int, 8>{});
+  return go(std::integral_constant<int, 16>{});
+}
+
+template <class T>
+int layer_norm(rtopk_matrix* ctx, const NormArgs<T>& a, bool vec, cudaStream_t st) {
+  return by_warps(ctx, a.rows, a.cols, [&](auto w) {
+    constexpr int kWarps = decltype(w)::value;
+    using S = RowShape<kWarps>;
+    return launch(ctx, vec ? k_layer_norm<T, kWarps, true> : k_layer_norm<T, kWarps, false>, dim3((unsigned)ceil_div(a.rows, S::kRowsPer)), S::kThreads, 0, st, a);
+  });
+}
+
+// Ranges of rows whose column sums are formed apart: four blocks for each of 148 SMs, but no fewer than 32 rows each.
+int64_t norm_parts(int64_t rows, int64_t cols) { return std::max<int64_t>(1, std::min(ceil_div(rows, 32), 592 / ceil_div(cols, kWarpCols))); }
+
+struct NormScratch {
+  float* parts;
+  int64_t count;
+  NormScratch(Carve& c, int64_t rows, int64_t cols) {
+    count = norm_parts(rows, cols);
+    parts = c.take<float>(count * 2 * cols);
+  }
+};
+
+template <class T>
+int layer_norm_gradients(rtopk_matrix* ctx, const NormBackArgs<T>& a, float* dgamma, float* dbeta, bool vec, cudaStream_t st) {
+  if (dgamma || dbeta) {      // first: the gradients may be written over what they are made of
+    Carve c{ctx->scratch};
+    NormScratch s(c, a.rows, a.cols);
+    const int per = (int)ceil_div(a.rows, s.count);
+    const int64_t count = ceil_div(a.rows, per);
+    MAT_TRY(launch(ctx, vec ? k_norm_columns<T, true> : k_norm_columns<T, false>, dim3((unsigned)ceil_div(a.cols, kWarpCols), (unsigned)count), 256, 0, st, a.dy, a.ld_dy, a.total, a.ld_t,
+                   a.mean, a.rstd, a.rows, a.cols, per, s.parts));
+    MAT_TRY(launch(ctx, k_norm_join, dim3((unsigned)ceil_div(2 * (int64_t)a.cols, 256)), 256, 0, st, s.parts, count, a.cols, dgamma, dbeta));
+  }
+  if (!a.dresidual && !a.dx) return RTOPK_OK;
+  return by_warps(ctx, a.rows, a.cols, [&](auto w) {
+    constexpr int kWarps = decltype(w)::value;
+    using S = RowShape<kWarps>;
+    return launch(ctx, vec ? k_layer_norm_back<T, kWarps, true> : k_layer_norm_back<T, kWarps, false>, dim3((unsigned)ceil_div(a.rows, S::kRowsPer)), S::kThreads, 0, st, a);
+  });
+}
+
+}  // namespace
+
+cudaError_t rtopk::mat::allow_layers() { return allow_smem<EPI_MICRO>(); }
+
+extern "C" {
+
+int rtopk_micro_layout(int64_t rows, int64_t cols, int64_t* ld, int64_t* scale_bytes) {
+  if (rows < 1 || cols < 1 || rows > kDimMax || cols > kDimMax) return RTOPK_ERR_INVALID_ARG;
+  if (ld) *ld = micro_ld(cols);
+  if (scale_bytes) *scale_bytes = micro_scale_bytes(rows, cols);
+  return RTOPK_OK;
+}
+
+int rtopk_micro_weights(rtopk_matrix* ctx, const void* weights, int dtype, int64_t ld_w, int64_t n_out, int64_t n_in, int tile, uint8_t* codes, int64_t ld_codes, uint8_t* scales,
+                        uint8_t* codes_t, int64_t ld_t, uint8_t* scales_t, void* stream) {
+  MAT_TRY(check_micro(ctx, 0, n_out, n_in));
+  if (bad_dtype(dtype) || bad_view(weights, elem(dtype), 1, n_out, n_in, ld_w, 0) || bad_micro(codes, ld_codes, scales, n_in) || (tile != 1 && tile != 32) ||
+      (codes_t && (tile != 32 || bad_micro(codes_t, ld_t, scales_t, n_out))))
+    return RTOPK_ERR_INVALID_ARG;
+  if (micro_too_large(n_out, n_in)) return RTOPK_ERR_UNSUPPORTED;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  const MicroOut rows = as_micro(codes, ld_codes, scales), cols = as_micro(codes_t, ld_t, scales_t);
+  if (dtype == RTOPK_F32) return micro_weights(ctx, (const float*)weights, ld_w, n_out, n_in, tile, rows, cols, (cudaStream_t)stream);
+  return micro_weights(ctx, (const __nv_bfloat16*)weights, ld_w, n_out, n_in, tile, rows, cols, (cudaStream_t)stream);
+}
+
+int rtopk_micro_scratch(int64_t tokens, int64_t n_out, int64_t n_in, int64_t* bytes) {
+  if (!bytes || tokens < 0 || n_out < 1 || n_in < 1 || tokens > kDimMax || n_out > kDimMax || n_in > kDimMax) return RTOPK_ERR_INVALID_ARG;
+  Carve c{nullptr};
+  MicroScratch s(c, tokens, n_out, n_in);
+  *bytes = c.at;
+  return RTOPK_OK;
+}
+
+int rtopk_micro_product(rtopk_matrix* ctx, const void* x, int dtype, int64_t ld_x, const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t tokens, int64_t n_out,
+                        int64_t n_in, void* out, int64_t ld_out, void* stream) {
+  MAT_TRY(check_micro(ctx, tokens, n_out, n_in));
+  if (bad_dtype(dtype) || bad_micro(codes, ld_codes, scales, n_in)) return RTOPK_ERR_INVALID_ARG;
+  if (tokens && (bad_view(x, elem(dtype), 1, tokens, n_in, ld_x, 0) || bad_view(out, elem(dtype), 1, tokens, n_out, ld_out, 0))) return RTOPK_ERR_INVALID_ARG;
+  if (!tokens) return RTOPK_OK;
+  if (micro_too_large(tokens, n_in)) return RTOPK_ERR_UNSUPPORTED;
+  int64_t need = 0;
+  rtopk_micro_scratch(tokens, n_out, n_in, &need);
+  if (need > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  const MicroOut w = as_micro(codes, ld_codes, scales);
+  if (dtype == RTOPK_F32) return micro_product(ctx, (const float*)x, ld_x, w, tokens, n_out, n_in, (float*)out, ld_out, (cudaStream_t)stream);
+  return micro_product(ctx, (const __nv_bfloat16*)x, ld_x, w, tokens, n_out, n_in, (__nv_bfloat16*)out, ld_out, (cudaStream_t)stream);
+}
+
+int rtopk_micro_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int dtype, const uint8_t* codes_t, int64_t ld_t, const uint8_t* scales_t,
+                          int64_t tokens, int64_t n_out, int64_t n_in, void* dx, int64_t ld_dx, void* dw, int dw_dtype, int64_t ld_dw, void* stream) {
+  MAT_TRY(check_micro(ctx, tokens, n_out, n_in));
+  if (bad_dtype(dtype) || (!dx && !dw) || (tokens && bad_view(dy, elem(dtype), 1, tokens, n_out, ld_dy, 0))) return RTOPK_ERR_INVALID_ARG;
+  if (dx && ((tokens && bad_view(dx, elem(dtype), 1, tokens, n_in, ld_dx, 0)) || bad_micro(codes_t, ld_t, scales_t, n_out))) return RTOPK_ERR_INVALID_ARG;
+  if (dw && (bad_dtype(dw_dtype) || bad_view(dw, elem(dw_dtype), 1, n_out, n_in, ld_dw, 0) || (tokens && bad_view(x, elem(dtype), 1, tokens, n_in, ld_x, 0))))
+    return RTOPK_ERR_INVALID_ARG;
+  if (micro_too_large(tokens, std::max(n_in, n_out))) return RTOPK_ERR_UNSUPPORTED;
+  int64_t need = 0;
+  rtopk_micro_scratch(tokens, n_out, n_in, &need);
+  if (tokens && need > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (!tokens) {      // an empty sum
+    if (dw) MAT_CUDA(cudaMemset2DAsync(dw, ld_dw * elem(dw_dtype), 0, n_in * elem(dw_dtype), n_out, st));
+    return RTOPK_OK;
+  }
+  const MicroOut w_t = as_micro(codes_t, ld_t, scales_t);
+  if (dtype == RTOPK_F32)
+    return micro_gradients(ctx, (const float*)dy, ld_dy, (const float*)x, ld_x, w_t, tokens, n_out, n_in, (float*)dx, ld_dx, dw, dw_dtype == RTOPK_BF16, ld_dw, st);
+  return micro_gradients(ctx, (const __nv_bfloat16*)dy, ld_dy, (const __nv_bfloat16*)x, ld_x, w_t, tokens, n_out, n_in, (__nv_bfloat16*)dx, ld_dx, dw, dw_dtype == RTOPK_BF16, ld_dw, st);
+}
+
+int rtopk_dropout(rtopk_matrix* ctx, const void* x, int dtype, int64_t ld_x, int64_t rows, int64_t cols, const rtopk_mask* mask, void* out, int64_t ld_out, void* stream) {
+  MAT_TRY(check_rows(ctx, rows, cols, dtype));
+  Mask m;
+  if (!mask || !as_mask(mask, &m)) return RTOPK_ERR_INVALID_ARG;
+  if (!rows) return RTOPK_OK;
+  if (bad_view(x, elem(dtype), 1, rows, cols, ld_x, 0) || bad_view(out, elem(dtype), 1, rows, cols, ld_out, 0)) return RTOPK_ERR_INVALID_ARG;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  if (dtype == RTOPK_F32) return dropout(ctx, (const float*)x, ld_x, rows, cols, m, (float*)out, ld_out, (cudaStream_t)stream);
+  return dropout(ctx, (const __nv_bfloat16*)x, ld_x, rows, cols, m, (__nv_bfloat16*)out, ld_out, (cudaStream_t)stream);
+}
+
+int rtopk_layer_norm(rtopk_matrix* ctx, const void* x, int64_t ld_x, const void* residual, int64_t ld_r, int dtype, int64_t rows, int64_t cols, const float* gamma, const float* beta,
+                     float eps, const rtopk_mask* mask, void* out, int64_t ld_out, void* total, int64_t ld_t, float* mean, float* rstd, void* stream) {
+  MAT_TRY(check_rows(ctx, rows, cols, dtype));
+  Mask m;
+  if (!as_mask(mask, &m) || !(eps >= 0.f) || !std::isfinite(eps) || !aligned_to(gamma, 4) || !aligned_to(beta, 4) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
+    return RTOPK_ERR_INVALID_ARG;
+  if (!rows) return RTOPK_OK;
+  const size_t e = elem(dtype);
+  if (bad_view(x, e, 1, rows, cols, ld_x, 0) || bad_view(out, e, 1, rows, cols, ld_out, 0) || (residual && bad_view(residual, e, 1, rows, cols, ld_r, 0)) ||
+      (total && bad_view(total, e, 1, rows, cols, ld_t, 0)))
+    return RTOPK_ERR_INVALID_ARG;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  const bool vec = rows_aligned(x, e, 1, ld_x, 0, 16) && rows_aligned(out, e, 1, ld_out, 0, 16) && (!residual || rows_aligned(residual, e, 1, ld_r, 0, 16)) &&
+                   (!total || rows_aligned(total, e, 1, ld_t, 0, 16)) && aligned_to(gamma, 16) && aligned_to(beta, 16);
+  auto go = [&](auto t) {
+    using T = decltype(t);
+    const NormArgs<T> a = {(const T*)x, (const T*)residual, (T*)out, (T*)total, ld_x, ld_r, ld_out, ld_t, gamma, beta, mean, rstd, (int)rows, (int)cols, eps, m};
+    return layer_norm(ctx, a, vec, (cudaStream_t)stream);
+  };
+  return dtype == RTOPK_F32 ? go(float{}) : go(__nv_bfloat16{});
+}
+
+int rtopk_layer_norm_scratch(int64_t rows, int64_t cols, int64_t* bytes) {
+  if (!bytes || rows < 0 || cols < 1 || rows > kDimMax || cols > kDimMax) return RTOPK_ERR_INVALID_ARG;
+  Carve c{nullptr};
+  NormScratch s(c, rows, cols);
+  *bytes = c.at;
+  return RTOPK_OK;
+}
+
+int rtopk_layer_norm_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy, const void* total, int64_t ld_t, const void* dtotal, int64_t ld_dt, int dtype, int64_t rows, int64_t cols,
+                               const float* mean, const float* rstd, const float* gamma, const rtopk_mask* mask, void* dresidual, int64_t ld_dr, void* dx, int64_t ld_dx, float* dgamma,
+                               float* dbeta, void* stream) {
+  MAT_TRY(check_rows(ctx, rows, cols, dtype));
+  Mask m;
+  if (!as_mask(mask, &m) || (dx != nullptr) != (mask != nullptr) || (!dresidual && !dx && !dgamma && !dbeta) || !aligned_to(gamma, 4) || !aligned_to(dgamma, 4) || !aligned_to(dbeta, 4))
+    return RTOPK_ERR_INVALID_ARG;
+  const size_t e = elem(dtype);
+  if (rows && (bad_view(dy, e, 1, rows, cols, ld_dy, 0) || bad_view(total, e, 1, rows, cols, ld_t, 0) || (dtotal && bad_view(dtotal, e, 1, rows, cols, ld_dt, 0)) || !mean || !rstd ||
+               !aligned_to(mean, 4) || !aligned_to(rstd, 4) || (dresidual && bad_view(dresidual, e, 1, rows, cols, ld_dr, 0)) || (dx && bad_view(dx, e, 1, rows, cols, ld_dx, 0))))
+    return RTOPK_ERR_INVALID_ARG;
+  int64_t need = 0;
+  rtopk_layer_norm_scratch(rows, cols, &need);
+  if (rows && (dgamma || dbeta) && need > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
+  OnDevice on(ctx->device);
+  if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (!rows) {      // empty sums
+    if (dgamma) MAT_CUDA(cudaMemsetAsync(dgamma, 0, cols * sizeof(float), st));
+    if (dbeta) MAT_CUDA(cudaMemsetAsync(dbeta, 0, cols * sizeof(float), st));
+    return RTOPK_OK;
+  }
+  auto aligned = [&](const void* p, int64_t ld) { return !p || rows_aligned(p, e, 1, ld, 0, 16); };
+  const bool vec = aligned(dy, ld_dy) && aligned(total, ld_t) && aligned(dtotal, ld_dt) && aligned(dresidual, ld_dr) && aligned(dx, ld_dx) && aligned_to(gamma, 16);
+  auto go = [&](auto t) {
+    using T = decltype(t);
+    const NormBackArgs<T> a = {(const T*)dy, (const T*)total, (const T*)dtotal, (T*)dresidual, (T*)dx, ld_dy, ld_t, ld_dt, ld_dr, ld_dx, gamma, mean, rstd, (int)rows, (int)cols, m};
+    return layer_norm_gradients(ctx, a, dgamma, dbeta, vec, st);
+  };
+  return dtype == RTOPK_F32 ? go(float{}) : go(__nv_bfloat16{});
+}
+
+}  // extern "C"

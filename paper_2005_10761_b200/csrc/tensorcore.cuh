@@ -176,6 +176,26 @@ __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint3
   else TC_MMA("1", "f16");
 }
 #undef TC_MMA
+// 4-bit floating-point codes (64 of the contraction index) with a power of two for every 32 of them and row: the scales lie in
+// tensor memory, byte pairs of a column's words, row r of 32 in lane r, the next 32 rows in the next column.
+#define TC_MMA_MICRO(group)                                                                                             \
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"                                                          \
+               "tcgen05.mma.cta_group::" group ".kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n\t}" ::"r"(d), \
+               "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(scale_a), "r"(scale_b)                                  \
+               : "memory")
+template <bool kPair>
+__device__ __forceinline__ void tc_mma_micro(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, uint32_t accumulate) {
+  if (kPair) TC_MMA_MICRO("2");
+  else TC_MMA_MICRO("1");
+}
+#undef TC_MMA_MICRO
+// 512 bytes, 16 for each of 32 rows, into four columns of tensor memory, the same for each quarter of the lanes; in a pair each block's
+// own bytes into its own columns.  Products issued after it by the same thread see them.
+template <bool kPair>
+__device__ __forceinline__ void tc_copy_scales(uint32_t dst, uint64_t src) {
+  if (kPair) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(dst), "l"(src) : "memory");
+}
 // The barrier (in a pair: both blocks') completes when all products issued before by this thread are done.
 template <bool kPair>
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
@@ -224,6 +244,13 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t slab_bytes
 // Instruction descriptor: f16 x f16 -> f32 or s8 x s8 -> s32, m x n.
 __host__ __device__ constexpr uint32_t instr_desc(bool int8, bool a_mn_major, uint32_t m, uint32_t n, bool b_mn_major = false) {
   return (int8 ? (2u << 4) | (1u << 7) | (1u << 10) : (1u << 4)) | (a_mn_major ? 1u << 15 : 0u) | (b_mn_major ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
+}
+
+// Of the scales' bytes: no swizzle, groups of eight 16-byte rows 128 bytes apart.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) { return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(128u >> 4) << 32) | (1ull << 46); }
+// 4-bit codes with a scale in 8 exponent bits for every 32; `pair`: which two of a word's four scales.
+__host__ __device__ constexpr uint32_t micro_desc(uint32_t m, uint32_t n, uint32_t pair) {
+  return (2 * pair << 4) | (1u << 7) | (1u << 10) | ((n >> 3) << 17) | (1u << 23) | ((m >> 4) << 24) | (2 * pair << 29);
 }
 
 // ----------------------------------------------------------------------------- launch order

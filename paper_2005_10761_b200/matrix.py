@@ -1,5 +1,6 @@
 """ctypes binding of the matrix operators in include/rtopk.h: the orthogonal factor of an update, the master update with
-it, and linear layers on 8-bit codes.  Argument marshalling only, as in binding.py."""
+it, linear layers on 8-bit and on 4-bit codes, and what stands between them: dropout and layer normalisation.  Argument
+marshalling only, as in binding.py."""
 from __future__ import annotations
 
 import ctypes as C
@@ -28,6 +29,25 @@ def orthogonalize_scratch(batch: int, m: int, n: int) -> int:
 def coded_scratch(tokens: int, n_out: int, n_in: int) -> int:
     """Scratch bytes of :meth:`MatrixContext.coded_product` and :meth:`MatrixContext.coded_gradients` for up to `tokens` tokens."""
     return _scratch("rtopk_coded_scratch", tokens, n_out, n_in)
+
+
+def micro_scratch(tokens: int, n_out: int, n_in: int) -> int:
+    """Scratch bytes of :meth:`MatrixContext.micro_product` and :meth:`MatrixContext.micro_gradients` for up to `tokens` tokens."""
+    return _scratch("rtopk_micro_scratch", tokens, n_out, n_in)
+
+
+def micro_layout(rows: int, cols: int):
+    """(least bytes of a row of 4-bit codes, bytes of the scales) of an array of `rows` rows of `cols` codes."""
+    ld, scales = _i64(0), _i64(0)
+    rc = load_library().rtopk_micro_layout(rows, cols, C.byref(ld), C.byref(scales))
+    if rc != 0:
+        raise RTopKError(rc, "rtopk_micro_layout", "invalid argument")
+    return int(ld.value), int(scales.value)
+
+
+def layer_norm_scratch(rows: int, cols: int) -> int:
+    """Scratch bytes of :meth:`MatrixContext.layer_norm_gradients` with dgamma or dbeta."""
+    return _scratch("rtopk_layer_norm_scratch", rows, cols)
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:
@@ -84,6 +104,119 @@ class CodedWeights:
     def dense(self) -> torch.Tensor:
         """The values that the codes stand for."""
         return self.codes[:, :self.n_in].float() * self.scales[:, None]
+
+
+class MicroWeights:
+    """The 4-bit codes of an (n_out, n_in) weight matrix with a power of two for each `tile` x 32 of them (`tile` 32, or 1 without the
+    transposed codes).  ``codes`` is uint8 [n_out, ld], two codes a byte, ``scales`` uint8 [scale bytes], ``codes_t`` and ``scales_t`` the
+    same transposed (None with ``transposed=False``).  Each may be replaced by another tensor of that form; calls use the tensors
+    that are there when they are made."""
+
+    def __init__(self, n_out: int, n_in: int, transposed: bool = True, tile: int = 32, device=None):
+        if tile not in (1, 32) or (transposed and tile != 32):
+            raise ValueError("tile must be 32, or 1 for weights without transposed codes")
+        device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+        self._n_out, self._n_in, self._tile = n_out, n_in, tile
+
+        def arrays(rows, cols):
+            ld, scale_bytes = micro_layout(rows, cols)
+            return (torch.zeros((rows, -(-ld // 128) * 128), dtype=torch.uint8, device=device),
+                    torch.zeros(scale_bytes, dtype=torch.uint8, device=device))
+        self.codes, self.scales = arrays(n_out, n_in)
+        self.codes_t, self.scales_t = arrays(n_in, n_out) if transposed else (None, None)
+
+    n_out = property(lambda self: self._n_out)
+    n_in = property(lambda self: self._n_in)
+    tile = property(lambda self: self._tile)
+    codes = property(lambda self: self._codes)
+    scales = property(lambda self: self._scales)
+    codes_t = property(lambda self: self._codes_t)
+    scales_t = property(lambda self: self._scales_t)
+
+    @codes.setter
+    def codes(self, t):
+        self._codes = self._checked_codes(t, "codes", self._n_out, self._n_in)
+
+    @scales.setter
+    def scales(self, t):
+        self._scales = self._checked_scales(t, "scales", self._n_out, self._n_in)
+
+    @codes_t.setter
+    def codes_t(self, t):
+        self._codes_t = None if t is None else self._checked_codes(t, "codes_t", self._n_in, self._n_out)
+
+    @scales_t.setter
+    def scales_t(self, t):
+        self._scales_t = None if t is None else self._checked_scales(t, "scales_t", self._n_in, self._n_out)
+
+    @staticmethod
+    def _checked_codes(t, what, rows, cols):
+        if t.dtype != torch.uint8:
+            raise TypeError(f"{what} must be uint8")
+        least = micro_layout(rows, cols)[0]
+        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < least or t.stride(1) != 1:
+            raise ValueError(f"{what} must have {rows} contiguous rows of at least {least} bytes")
+        return t
+
+    @staticmethod
+    def _checked_scales(t, what, rows, cols):
+        if t.dtype != torch.uint8:
+            raise TypeError(f"{what} must be uint8")
+        count = micro_layout(rows, cols)[1]
+        if t.shape != (count,) or not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous and of shape {(count,)}")
+        return t
+
+    def dense(self) -> torch.Tensor:
+        """The values that the codes stand for."""
+        byte = self.codes[:, :(self.n_in + 1) // 2].long()
+        code = torch.stack((byte & 15, byte >> 4), 2).flatten(1)[:, :self.n_in]
+        table = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=code.device)
+        value = torch.where(code >= 8, -table[code & 7], table[code & 7])
+        r = torch.arange(self.n_out, device=code.device)[:, None]
+        b = torch.arange(self.n_in, device=code.device)[None, :] // 32
+        pieces = -(-self.n_in // 256) * 2
+        scale = self.scales[((r // 128) * pieces + b // 4) * 512 + r % 32 * 16 + r % 128 // 32 * 4 + b % 4].int()
+        power = torch.where(scale == 0, 1 << 22, scale << 23).int().view(torch.float32)      # 2^(scale - 127) by its bits
+        return torch.where(scale == 255, float("nan"), value * power)
+
+
+class _MaskStruct(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("step_ptr", _vp), ("step", C.c_uint32), ("worker", C.c_uint32), ("site", C.c_uint32)]
+
+
+class Mask:
+    """Which elements dropout drops: a share p of them, by (seed, step, worker, site) and their place in the rows; nothing is stored.  `step`
+    is a number, or a one-element int32 tensor on the context's device that kernels read when they run (for captured graphs);
+    it may be changed from call to call."""
+
+    def __init__(self, p: float, seed: int, step=0, worker: int = 0, site: int = 0):
+        if not 0 <= p < 1:
+            raise ValueError("p must be at least 0 and less than 1")
+        if not 0 <= worker < 65536 or not 0 <= site < 32768:
+            raise ValueError("worker must be below 65536 and site below 32768")
+        if not 0 <= seed < 1 << 64:
+            raise ValueError("seed must be a number of 64 bits")
+        self._struct = _MaskStruct(p, seed, None, 0, worker, site)
+        self.step = step
+
+    p = property(lambda self: self._struct.p)
+    seed = property(lambda self: self._struct.seed)
+    worker = property(lambda self: self._struct.worker)
+    site = property(lambda self: self._struct.site)
+    step = property(lambda self: self._step)
+
+    @step.setter
+    def step(self, step):
+        if isinstance(step, torch.Tensor):
+            if step.dtype != torch.int32 or step.numel() != 1:
+                raise ValueError("step must be a number or one int32")
+            self._struct.step, self._struct.step_ptr = 0, step.data_ptr()
+        else:
+            if not 0 <= step < 1 << 32:
+                raise ValueError("step must be a number of 32 bits")
+            self._struct.step, self._struct.step_ptr = step, None
+        self._step = step
 
 
 class MatrixContext:
@@ -253,6 +386,131 @@ class MatrixContext:
                                              self._on_device(coded._scales, "scales"), tokens, coded.n_out, coded.n_in, pdx, lddx,
                                              pdw, wt, lddw, self._stream())
         self._check(rc, "rtopk_coded_gradients")
+
+    def micro_weights(self, weights, micro: MicroWeights) -> None:
+        """micro <- the 4-bit codes of weights ([n_out, n_in], float32 or bfloat16)."""
+        p, ld = self._rows(weights, "weights", (micro.n_out, micro.n_in))
+        codes_t, scales_t = micro._codes_t, micro._scales_t
+        if (codes_t is None) != (scales_t is None):
+            raise ValueError("codes_t and scales_t go together")
+        rc = self._lib.rtopk_micro_weights(self._h, p, _dtype(weights, "weights"), ld, micro.n_out, micro.n_in, micro._tile,
+                                           *self._codes(micro._codes), self._on_device(micro._scales, "scales"), *self._codes(codes_t),
+                                           None if scales_t is None else self._on_device(scales_t, "scales_t"), self._stream())
+        self._check(rc, "rtopk_micro_weights")
+
+    def micro_product(self, x, micro: MicroWeights, out) -> None:
+        """out[t, n] <- x W^T with W as 4-bit codes and x ([tokens, n_in], float32 or bfloat16) coded in the call."""
+        tokens, n_in, n_out, codes = x.shape[0], micro._n_in, micro._n_out, micro._codes
+        p, ld = self._rows(x, "x", (tokens, n_in))
+        po, ldo = self._rows(out, "out", (tokens, n_out))
+        dtype = _DTYPES.get(x.dtype)
+        if dtype is None or out.dtype != x.dtype:
+            raise TypeError("x must be float32 or bfloat16, and out have its type")
+        rc = self._lib.rtopk_micro_product(self._h, p, dtype, ld, self._on_device(codes, "codes"), codes.stride()[0],
+                                           self._on_device(micro._scales, "scales"), tokens, n_out, n_in, po, ldo, self._stream())
+        if rc:
+            self._check(rc, "rtopk_micro_product")
+
+    def micro_gradients(self, dy, x, micro: MicroWeights, dx=None, dw=None) -> None:
+        """The gradients of :meth:`micro_product` for dy ([tokens, n_out]): dx like x, dw ([n_out, n_in], float32 or bfloat16).
+        Either may be left out; x may be None when dw is."""
+        tokens = dy.shape[0]
+        py, ldy = self._rows(dy, "dy", (tokens, micro.n_out))
+        dt = _dtype(dy, "dy")
+        px = ldx = pdx = lddx = pdw = lddw = 0
+        wt = GRAD_F32
+        codes_t, scales_t = (None, 0), None
+        if dw is not None:
+            if x is None:
+                raise ValueError("dw needs x")
+            px, ldx = self._rows(x, "x", (tokens, micro.n_in))
+            if x.dtype != dy.dtype:
+                raise TypeError("x must have the type of dy")
+            pdw, lddw = self._rows(dw, "dw", (micro.n_out, micro.n_in))
+            wt = _dtype(dw, "dw")
+        if dx is not None:
+            pdx, lddx = self._rows(dx, "dx", (tokens, micro.n_in))
+            if dx.dtype != dy.dtype:
+                raise TypeError("dx must have the type of dy")
+            if micro._codes_t is None or micro._scales_t is None:
+                raise ValueError("these weights were made without their transposed codes")
+            codes_t, scales_t = self._codes(micro._codes_t), self._on_device(micro._scales_t, "scales_t")
+        rc = self._lib.rtopk_micro_gradients(self._h, py, ldy, px, ldx, dt, *codes_t, scales_t, tokens, micro.n_out, micro.n_in, pdx,
+                                             lddx, pdw, wt, lddw, self._stream())
+        self._check(rc, "rtopk_micro_gradients")
+
+    def _mask(self, mask: Optional[Mask]):
+        if mask is None:
+            return None
+        if isinstance(mask._step, torch.Tensor):
+            self._on_device(mask._step, "the mask's step")
+        return C.byref(mask._struct)
+
+    def _like(self, t, what: str, x, shape):
+        """(pointer, row stride) of an optional matrix of x's shape and type."""
+        if t is None:
+            return None, 0
+        if t.dtype != x.dtype:
+            raise TypeError(f"{what} must have the other matrices' type")
+        return self._rows(t, what, shape)
+
+    def _vector(self, t, what: str, n: int):
+        if t is None:
+            return None
+        if t.dtype != torch.float32:
+            raise TypeError(f"{what} must be float32")
+        if t.shape != (n,) or (n > 1 and t.stride()[0] != 1):
+            raise ValueError(f"{what} must be contiguous and of shape {(n,)}")
+        return self._on_device(t, what)
+
+    def dropout(self, x, out, mask: Mask) -> None:
+        """out <- x where the mask keeps an element, times 1 / the share that is kept, else 0 ([rows, cols], float32 or bfloat16; out may be
+        x).  The gradient is the same call on out's gradient."""
+        if x.dim() != 2:
+            raise ValueError("x must be a matrix")
+        p, ld = self._rows(x, "x")
+        po, ldo = self._like(out, "out", x, x.shape)
+        rc = self._lib.rtopk_dropout(self._h, p, _dtype(x, "x"), ld, x.shape[0], x.shape[1], self._mask(mask), po, ldo, self._stream())
+        if rc:
+            self._check(rc, "rtopk_dropout")
+
+    def layer_norm(self, x, gamma, beta, out, residual=None, total=None, mean=None, rstd=None, eps=1e-5, mask: Optional[Mask] = None) -> None:
+        """total <- residual + dropout(x); out <- gamma (total - mean) rstd + beta over each row of [rows, cols] matrices, float32 or bfloat16.
+        residual, mask, gamma, beta (float32 [cols]) may be None; total, mean and rstd (float32 [rows]) are written where given, for
+        :meth:`layer_norm_gradients`."""
+        if x.dim() != 2:
+            raise ValueError("x must be a matrix")
+        rows, cols = shape = x.shape
+        p, ld = self._rows(x, "x")
+        pr, ldr = self._like(residual, "residual", x, shape)
+        po, ldo = self._like(out, "out", x, shape)
+        pt, ldt = self._like(total, "total", x, shape)
+        rc = self._lib.rtopk_layer_norm(self._h, p, ld, pr, ldr, _dtype(x, "x"), rows, cols, self._vector(gamma, "gamma", cols),
+                                        self._vector(beta, "beta", cols), eps, self._mask(mask), po, ldo, pt, ldt,
+                                        self._vector(mean, "mean", rows), self._vector(rstd, "rstd", rows), self._stream())
+        if rc:
+            self._check(rc, "rtopk_layer_norm")
+
+    def layer_norm_gradients(self, dy, total, mean, rstd, gamma, dresidual=None, dgamma=None, dbeta=None, dtotal=None, dx=None,
+                             mask: Optional[Mask] = None) -> None:
+        """The gradients of :meth:`layer_norm` for dy (of out) and dtotal (of total, where it is used elsewhere; may be None): dresidual (without
+        a mask also that of x), dx with a mask, dgamma and dbeta (float32 [cols]).  total, mean and rstd are the forward call's;
+        without residual and mask, total is its x."""
+        if dy.dim() != 2:
+            raise ValueError("dy must be a matrix")
+        if (mask is None) != (dx is None):
+            raise ValueError("dx goes with a mask: without one it is dresidual")
+        rows, cols = shape = dy.shape
+        p, ld = self._rows(dy, "dy")
+        pt, ldt = self._like(total, "total", dy, shape)
+        pa, lda = self._like(dtotal, "dtotal", dy, shape)
+        pr, ldr = self._like(dresidual, "dresidual", dy, shape)
+        px, ldx = self._like(dx, "dx", dy, shape)
+        rc = self._lib.rtopk_layer_norm_gradients(self._h, p, ld, pt, ldt, pa, lda, _dtype(dy, "dy"), rows, cols, self._vector(mean, "mean", rows),
+                                                  self._vector(rstd, "rstd", rows), self._vector(gamma, "gamma", cols), self._mask(mask), pr, ldr,
+                                                  px, ldx, self._vector(dgamma, "dgamma", cols), self._vector(dbeta, "dbeta", cols), self._stream())
+        if rc:
+            self._check(rc, "rtopk_layer_norm_gradients")
 
     def set_option(self, option: int, value: int) -> None:
         self._check(self._lib.rtopk_matrix_set_option(self._h, option, value), "rtopk_matrix_set_option")
