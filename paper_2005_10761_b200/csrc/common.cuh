@@ -234,8 +234,8 @@ __device__ __forceinline__ bool pick_digit(const uint32_t* hist, int nbins, uint
 // Salmon, Moraes, Dror, Shaw, "Parallel Random Numbers: As Easy as 1, 2, 3" (SC'11): ten rounds;
 // each multiplies counter words 0 and 2 by the two round multipliers, XORs the high halves with
 // words 1 and 3 and the round key, and bumps the key by the Weyl constants.
-__device__ __forceinline__ uint4 philox4x32_10(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0,
-                                               uint32_t k1) {
+__device__ __forceinline__ uint2 philox4x32_10_lo(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3,
+                                                  uint32_t k0, uint32_t k1) {
 #pragma unroll
   for (int i = 0; i < 10; ++i) {
     const uint32_t h0 = __umulhi(0xD2511F53u, c0), l0 = 0xD2511F53u * c0;
@@ -244,12 +244,17 @@ __device__ __forceinline__ uint4 philox4x32_10(uint32_t c0, uint32_t c1, uint32_
     c2 = h0 ^ c3 ^ k1; c3 = l0;
     k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
   }
-  return make_uint4(c0, c1, c2, c3);
+  return make_uint2(c0, c1);   // output words 0 and 1
 }
-__device__ __forceinline__ uint2 philox4x32_10_lo(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3,
-                                                  uint32_t k0, uint32_t k1) {
-  const uint4 x = philox4x32_10(c0, c1, c2, c3, k0, k1);
-  return make_uint2(x.x, x.y);   // output words 0 and 1
+// With the rounds' keys written out, two for each.
+__device__ __forceinline__ uint4 philox4x32_10(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, const uint32_t (&keys)[20]) {
+#pragma unroll
+  for (int i = 0; i < 10; ++i) {
+    const unsigned long long p0 = 0xD2511F53ull * c0, p1 = 0xCD9E8D57ull * c2;
+    c0 = (uint32_t)(p1 >> 32) ^ c1 ^ keys[2 * i]; c1 = (uint32_t)p1;
+    c2 = (uint32_t)(p0 >> 32) ^ c3 ^ keys[2 * i + 1]; c3 = (uint32_t)p0;
+  }
+  return make_uint4(c0, c1, c2, c3);
 }
 
 // Floyd iteration j draws uniformly from {0..j}: floor(u64 * (j+1) / 2^64), u64 = (x1 << 32) | x0.

@@ -102,7 +102,7 @@ bool as_mask(const rtopk_mask* m, Mask* out) {
   const double limit = std::min(std::nearbyint(m->p * 65536.0), 65535.0);
   out->limit = (uint32_t)limit;
   out->factor = (float)(65536.0 / (65536.0 - limit));
-  out->key0 = (uint32_t)m->seed, out->key1 = (uint32_t)(m->seed >> 32);
+  for (uint32_t i = 0; i < 10; ++i) out->keys[2 * i] = (uint32_t)m->seed + i * 0x9E3779B9u, out->keys[2 * i + 1] = (uint32_t)(m->seed >> 32) + i * 0xBB67AE85u;
   out->tag = 0x80000000u | m->site << 16 | m->worker;
   out->step = m->step, out->step_ptr = m->step_ptr;
   return true;
@@ -120,29 +120,57 @@ int dropout(rtopk_matrix* ctx, const T* x, int64_t ld_x, int64_t rows, int64_t c
   const int64_t band = std::max<int64_t>(1, std::min(rows, (int64_t(1) << 31) / units - 1));      // rows whose units 31 bits count
   if (ceil_div(rows, band) > 65535) return RTOPK_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)ceil_div(band * units, per), (unsigned)ceil_div(rows, band));
-  if (vec) return launch(ctx, k_dropout<T, true>, grid, 256, 0, st, x, ld_x, rows, cols, band, mask, out, ld_out);
-  return launch(ctx, k_dropout<T, false>, grid, 256, 0, st, x, ld_x, rows, cols, band, mask, out, ld_out);
+  Divisor d = {0, (uint32_t)units, 0};
+  while (units > int64_t(2) << d.shift) ++d.shift;
+  d.m = (uint32_t)((uint64_t(1) << (32 + d.shift)) / units + 1);
+  return launch(ctx, vec ? k_dropout<T, true> : k_dropout<T, false>, grid, 256, 0, st, x, ld_x, rows, cols, band, d, mask, out, ld_out);
 }
 
-// The row kernels by the number of warps of a row: as many as hold it in their registers (1024 columns each), more where there are
-// too few rows to fill the SMs.
-template <class F>
-int by_warps(const rtopk_matrix* ctx, int64_t rows, int64_t cols, F go) {
-  const int64_t warps = rows <= 4 * ctx->sms ? ceil_div(cols, 256) : ceil_div(cols, 1024);
-  if (warps <= 1) return go(std::integral_constant<int, 1>{});
-  if (warps <= 2) return go(std::integral_constant<int, 2>{});
-  if (warps <= 4) return go(std::integral_constant<int, 4>{});
-  if (warps <= 8) return go(std::integral_constant<int, 8>{});
-  return go(std::integral_constant<int, 16>{});
-}
+// How a block takes rows: `warps` warps for each, `keep` pieces of 256 columns a warp, `rows_per` rows at a time, `stages` of them in shared memory.
+// Two pieces, so that what is done once a row is shared by 16 columns of a thread; one where there are too few rows to fill the SMs,
+// four where two do not reach.  Without alignment the next row waits in registers, which four pieces would not leave.
+constexpr int kRowBlocks = 160;
+struct RowSplit {
+  int warps, rows_per, keep, stages, smem;
+  int64_t blocks;
+  bool fits;
+  // most: arrays that a call may have, which decides; arrays: those of this one
+  RowSplit(int sms, int64_t rows, int64_t cols, int elem, int arrays, int most, bool vec) {
+    const int64_t pieces = ceil_div(cols, kWarpCols);
+    fits = pieces <= kRowWarps * (vec ? 4 : 2);
+    if (!fits) return;
+    keep = pieces > 2 * kRowWarps ? 4 : pieces > kRowWarps || rows * pieces > sms * kRowWarps ? 2 : 1;
+    warps = (int)ceil_div(pieces, keep);
+    rows_per = (int)std::min<int64_t>(kRowWarps / warps, ceil_div(rows, sms));
+    const int array = rows_per * warps * kWarpCols * keep * elem, stage = arrays * array;
+    stages = vec ? std::min(4, kRowSmem / stage) : 1;
+    fits = (vec ? 2 : 1) * most * array <= kRowSmem;
+    blocks = std::min<int64_t>(std::min(sms, kRowBlocks), ceil_div(rows, rows_per));
+    smem = std::max(stages * stage, rows_per * 2 * warps * kWarpCols * keep * 4);
+  }
+};
+// Of the kernels for longer rows.
+struct LongSplit {
+  int warps, rows_per;
+  unsigned blocks;
+  LongSplit(int64_t rows, int64_t cols) {
+    warps = (int)std::min<int64_t>(16, ceil_div(cols, 4 * kWarpCols));
+    rows_per = std::max(1, 8 / warps);
+    blocks = (unsigned)ceil_div(rows, rows_per);
+  }
+};
 
 template <class T>
 int layer_norm(rtopk_matrix* ctx, const NormArgs<T>& a, bool vec, cudaStream_t st) {
-  return by_warps(ctx, a.rows, a.cols, [&](auto w) {
-    constexpr int kWarps = decltype(w)::value;
-    using S = RowShape<kWarps>;
-    return launch(ctx, vec ? k_layer_norm<T, kWarps, true> : k_layer_norm<T, kWarps, false>, dim3((unsigned)ceil_div(a.rows, S::kRowsPer)), S::kThreads, 0, st, a);
-  });
+  const RowSplit f(ctx->sms, a.rows, a.cols, sizeof(T), a.residual ? 2 : 1, 2, vec);
+  if (f.fits) {
+    auto go = [&](auto kernel) { return launch(ctx, kernel, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, f.smem, st, a, f.warps, f.rows_per, f.stages); };
+    if (f.keep == 1) return go(vec ? k_layer_norm_rows<T, true, 1> : k_layer_norm_rows<T, false, 1>);
+    if (f.keep == 2) return go(vec ? k_layer_norm_rows<T, true, 2> : k_layer_norm_rows<T, false, 2>);
+    return go(k_layer_norm_rows<T, true, 4>);
+  }
+  const LongSplit s(a.rows, a.cols);
+  return launch(ctx, vec ? k_layer_norm<T, true, 4> : k_layer_norm<T, false, 4>, dim3(s.blocks), 32 * s.warps * s.rows_per, 0, st, a, s.warps, s.rows_per);
 }
 
 // Ranges of rows whose column sums are formed apart: four blocks for each of 148 SMs, but no fewer than 32 rows each.
@@ -150,35 +178,49 @@ int64_t norm_parts(int64_t rows, int64_t cols) { return std::max<int64_t>(1, std
 
 struct NormScratch {
   float* parts;
-  int64_t count;
-  NormScratch(Carve& c, int64_t rows, int64_t cols) {
-    count = norm_parts(rows, cols);
-    parts = c.take<float>(count * 2 * cols);
-  }
+  NormScratch(Carve& c, int64_t rows, int64_t cols) { parts = c.take<float>(std::max(norm_parts(rows, cols), cols <= 4 * kRowWarps * kWarpCols ? std::min<int64_t>(rows, kRowBlocks) : 0) * 2 * cols); }
 };
+
+template <class T, bool kVec, int kKeep>
+cudaError_t allow_rows() {
+  const cudaError_t e = cudaFuncSetAttribute(k_layer_norm_rows<T, kVec, kKeep>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(k_layer_norm_back_rows<T, kVec, kKeep>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem);
+}
 
 template <class T>
 int layer_norm_gradients(rtopk_matrix* ctx, const NormBackArgs<T>& a, float* dgamma, float* dbeta, bool vec, cudaStream_t st) {
-  if (dgamma || dbeta) {      // first: the gradients may be written over what they are made of
-    Carve c{ctx->scratch};
-    NormScratch s(c, a.rows, a.cols);
-    const int per = (int)ceil_div(a.rows, s.count);
+  Carve c{ctx->scratch};
+  float* parts = dgamma || dbeta ? NormScratch(c, a.rows, a.cols).parts : nullptr;
+  auto join = [&](int64_t count) { return launch(ctx, k_norm_join, dim3((unsigned)ceil_div(2 * (int64_t)a.cols, 32)), 256, 0, st, parts, count, a.cols, dgamma, dbeta); };
+  const RowSplit f(ctx->sms, a.rows, a.cols, sizeof(T), a.dtotal ? 3 : 2, 3, vec);
+  if (f.fits) {
+    auto go = [&](auto kernel) { return launch(ctx, kernel, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, f.smem, st, a, f.warps, f.rows_per, f.stages, parts); };
+    if (f.keep == 1) MAT_TRY(go(vec ? k_layer_norm_back_rows<T, true, 1> : k_layer_norm_back_rows<T, false, 1>));
+    else if (f.keep == 2) MAT_TRY(go(vec ? k_layer_norm_back_rows<T, true, 2> : k_layer_norm_back_rows<T, false, 2>));
+    else MAT_TRY(go(k_layer_norm_back_rows<T, true, 4>));
+    return parts ? join(f.blocks) : RTOPK_OK;
+  }
+  if (parts) {      // first: the gradients may be written over what they are made of
+    const int per = (int)ceil_div(a.rows, norm_parts(a.rows, a.cols));
     const int64_t count = ceil_div(a.rows, per);
     MAT_TRY(launch(ctx, vec ? k_norm_columns<T, true> : k_norm_columns<T, false>, dim3((unsigned)ceil_div(a.cols, kWarpCols), (unsigned)count), 256, 0, st, a.dy, a.ld_dy, a.total, a.ld_t,
-                   a.mean, a.rstd, a.rows, a.cols, per, s.parts));
-    MAT_TRY(launch(ctx, k_norm_join, dim3((unsigned)ceil_div(2 * (int64_t)a.cols, 256)), 256, 0, st, s.parts, count, a.cols, dgamma, dbeta));
+                   a.mean, a.rstd, a.rows, a.cols, per, parts));
+    MAT_TRY(join(count));
   }
   if (!a.dresidual && !a.dx) return RTOPK_OK;
-  return by_warps(ctx, a.rows, a.cols, [&](auto w) {
-    constexpr int kWarps = decltype(w)::value;
-    using S = RowShape<kWarps>;
-    return launch(ctx, vec ? k_layer_norm_back<T, kWarps, true> : k_layer_norm_back<T, kWarps, false>, dim3((unsigned)ceil_div(a.rows, S::kRowsPer)), S::kThreads, 0, st, a);
-  });
+  const LongSplit s(a.rows, a.cols);
+  return launch(ctx, vec ? k_layer_norm_back<T, true, 4> : k_layer_norm_back<T, false, 4>, dim3(s.blocks), 32 * s.warps * s.rows_per, 0, st, a, s.warps, s.rows_per);
 }
 
 }  // namespace
 
-cudaError_t rtopk::mat::allow_layers() { return allow_smem<EPI_MICRO>(); }
+cudaError_t rtopk::mat::allow_layers() {
+  using B = __nv_bfloat16;
+  for (const cudaError_t e : {allow_smem<EPI_MICRO>(), allow_rows<float, true, 1>(), allow_rows<float, true, 2>(), allow_rows<float, true, 4>(), allow_rows<float, false, 1>(), allow_rows<float, false, 2>(),
+                              allow_rows<B, true, 1>(), allow_rows<B, true, 2>(), allow_rows<B, true, 4>(), allow_rows<B, false, 1>(), allow_rows<B, false, 2>()})
+    if (e != cudaSuccess) return e;
+  return cudaSuccess;
+}
 
 extern "C" {
 
