@@ -114,63 +114,81 @@ int check_rows(const rtopk_matrix* ctx, int64_t rows, int64_t cols, int dtype) {
 
 template <class T>
 int dropout(rtopk_matrix* ctx, const T* x, int64_t ld_x, int64_t rows, int64_t cols, const Mask& mask, T* out, int64_t ld_out, cudaStream_t st) {
-  const bool vec = rows_aligned(x, sizeof(T), 1, ld_x, 0, 16) && rows_aligned(out, sizeof(T), 1, ld_out, 0, 16);
-  const int64_t units = ceil_div(cols, vec ? 8 : kWarpCols);      // of a row: threads or warps
-  const int64_t per = vec ? 256 * 4 : 8 * 4;                      // of a block
-  const int64_t band = std::max<int64_t>(1, std::min(rows, (int64_t(1) << 31) / units - 1));      // rows whose units 31 bits count
+  const bool vec = cols % 8 == 0 && rows_aligned(x, sizeof(T), 1, ld_x, 0, 16) && rows_aligned(out, sizeof(T), 1, ld_out, 0, 16);
+  const int64_t units = ceil_div(cols, vec ? 8 : kWarpCols), per = vec ? 256 : 8;      // of four rows: threads or warps; of a block
+  const int64_t band = std::min(up(rows, 4), ((int64_t(1) << 31) / units - 256) / 4 * 4);      // rows whose units 31 bits count
   if (ceil_div(rows, band) > 65535) return RTOPK_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)ceil_div(band * units, per), (unsigned)ceil_div(rows, band));
+  const dim3 grid((unsigned)ceil_div(band / 4 * units, per), (unsigned)ceil_div(rows, band));
   Divisor d = {0, (uint32_t)units, 0};
   while (units > int64_t(2) << d.shift) ++d.shift;
   d.m = (uint32_t)((uint64_t(1) << (32 + d.shift)) / units + 1);
   return launch(ctx, vec ? k_dropout<T, true> : k_dropout<T, false>, grid, 256, 0, st, x, ld_x, rows, cols, band, d, mask, out, ld_out);
 }
 
-// How a block takes rows: `warps` warps for each, `keep` pieces of 256 columns a warp, `rows_per` rows at a time, `stages` of them in shared memory.
-// Two pieces, so that what is done once a row is shared by 16 columns of a thread; one where there are too few rows to fill the SMs,
-// four where two do not reach.  Without alignment the next row waits in registers, which four pieces would not leave.
+// How a block takes rows: `warps` warps for each, `keep` pieces of 256 columns a warp, `rows_per` rows at a time.  Two pieces, so that what is
+// done once a row is shared by 16 columns of a thread; one where there are too few rows to fill the SMs, four where two do not
+// reach.  Without alignment the next row waits in registers, which four pieces would not leave.
 constexpr int kRowBlocks = 160;
 struct RowSplit {
-  int warps, rows_per, keep, stages, smem;
+  int warps, rows_per, keep;
   int64_t blocks;
   bool fits;
-  // most: arrays that a call may have, which decides; arrays: those of this one
-  RowSplit(int sms, int64_t rows, int64_t cols, int elem, int arrays, int most, bool vec) {
+  RowSplit(int sms, int64_t rows, int64_t cols, int most, bool vec) {      // most: pieces a warp, at most
     const int64_t pieces = ceil_div(cols, kWarpCols);
-    fits = pieces <= kRowWarps * (vec ? 4 : 2);
+    fits = pieces <= kRowWarps * (vec ? most : 2);
     if (!fits) return;
     keep = pieces > 2 * kRowWarps ? 4 : pieces > kRowWarps || rows * pieces > sms * kRowWarps ? 2 : 1;
     warps = (int)ceil_div(pieces, keep);
     rows_per = (int)std::min<int64_t>(kRowWarps / warps, ceil_div(rows, sms));
-    const int array = rows_per * warps * kWarpCols * keep * elem, stage = arrays * array;
-    stages = vec ? std::min(4, kRowSmem / stage) : 1;
-    fits = (vec ? 2 : 1) * most * array <= kRowSmem;
     blocks = std::min<int64_t>(std::min(sms, kRowBlocks), ceil_div(rows, rows_per));
-    smem = std::max(stages * stage, rows_per * 2 * warps * kWarpCols * keep * 4);
-  }
-};
-// Of the kernels for longer rows.
-struct LongSplit {
-  int warps, rows_per;
-  unsigned blocks;
-  LongSplit(int64_t rows, int64_t cols) {
-    warps = (int)std::min<int64_t>(16, ceil_div(cols, 4 * kWarpCols));
-    rows_per = std::max(1, 8 / warps);
-    blocks = (unsigned)ceil_div(rows, rows_per);
   }
 };
 
+template <class T, bool kVec, int kKeep, bool kResidual>
+int norm_rows(rtopk_matrix* ctx, const NormArgs<T>& a, const RowSplit& f, cudaStream_t st) {
+  return launch(ctx, k_layer_norm_rows<T, kVec, kKeep, kResidual>, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, RowShape<T, kVec, kKeep, kResidual ? 2 : 1>::kSmem, st, a, f.warps,
+                f.rows_per);
+}
+template <class T, bool kResidual>
+int norm_rows(rtopk_matrix* ctx, const NormArgs<T>& a, const RowSplit& f, bool vec, cudaStream_t st) {
+  if (f.keep == 4) return norm_rows<T, true, 4, kResidual>(ctx, a, f, st);
+  if (f.keep == 2) return vec ? norm_rows<T, true, 2, kResidual>(ctx, a, f, st) : norm_rows<T, false, 2, kResidual>(ctx, a, f, st);
+  return vec ? norm_rows<T, true, 1, kResidual>(ctx, a, f, st) : norm_rows<T, false, 1, kResidual>(ctx, a, f, st);
+}
 template <class T>
 int layer_norm(rtopk_matrix* ctx, const NormArgs<T>& a, bool vec, cudaStream_t st) {
-  const RowSplit f(ctx->sms, a.rows, a.cols, sizeof(T), a.residual ? 2 : 1, 2, vec);
-  if (f.fits) {
-    auto go = [&](auto kernel) { return launch(ctx, kernel, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, f.smem, st, a, f.warps, f.rows_per, f.stages); };
-    if (f.keep == 1) return go(vec ? k_layer_norm_rows<T, true, 1> : k_layer_norm_rows<T, false, 1>);
-    if (f.keep == 2) return go(vec ? k_layer_norm_rows<T, true, 2> : k_layer_norm_rows<T, false, 2>);
-    return go(k_layer_norm_rows<T, true, 4>);
-  }
-  const LongSplit s(a.rows, a.cols);
-  return launch(ctx, vec ? k_layer_norm<T, true, 4> : k_layer_norm<T, false, 4>, dim3(s.blocks), 32 * s.warps * s.rows_per, 0, st, a, s.warps, s.rows_per);
+  const RowSplit f(ctx->sms, a.rows, a.cols, 4, vec);
+  if (f.fits) return a.residual ? norm_rows<T, true>(ctx, a, f, vec, st) : norm_rows<T, false>(ctx, a, f, vec, st);
+  return launch(ctx, vec ? k_layer_norm_long<T, true> : k_layer_norm_long<T, false>, dim3((unsigned)a.rows), 32 * kRowWarps, 0, st, a);
+}
+
+// The columns' sums of a block's groups meet in its shared memory.
+template <class T, bool kVec, int kKeep, bool kMore>
+constexpr int kBackSmem = std::max(RowShape<T, kVec, kKeep, kMore ? 3 : 2>::kSmem, 2 * kRowWarps * kWarpCols * kKeep * 4);
+template <class T, bool kVec, int kKeep, bool kMore>
+int back_rows(rtopk_matrix* ctx, const NormBackArgs<T>& a, const RowSplit& f, float* parts, cudaStream_t st) {
+  return launch(ctx, k_layer_norm_back_rows<T, kVec, kKeep, kMore>, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, kBackSmem<T, kVec, kKeep, kMore>, st, a, f.warps, f.rows_per, parts);
+}
+template <class T, bool kMore>
+int back_rows(rtopk_matrix* ctx, const NormBackArgs<T>& a, const RowSplit& f, bool vec, float* parts, cudaStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (f.keep == 4) return back_rows<T, true, 4, kMore>(ctx, a, f, parts, st);
+  if (f.keep == 2) return vec ? back_rows<T, true, 2, kMore>(ctx, a, f, parts, st) : back_rows<T, false, 2, kMore>(ctx, a, f, parts, st);
+  return vec ? back_rows<T, true, 1, kMore>(ctx, a, f, parts, st) : back_rows<T, false, 1, kMore>(ctx, a, f, parts, st);
+}
+
+template <class T, bool kVec, int kKeep, bool kResidual>
+cudaError_t allow_rows() {
+  const cudaError_t e = cudaFuncSetAttribute(k_layer_norm_rows<T, kVec, kKeep, kResidual>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem);
+  if constexpr (sizeof(T) == 4 && kKeep == 4) return e;
+  else return e != cudaSuccess ? e : cudaFuncSetAttribute(k_layer_norm_back_rows<T, kVec, kKeep, kResidual>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem);
+}
+template <class T>
+cudaError_t allow_rows() {
+  for (const cudaError_t e : {allow_rows<T, true, 1, false>(), allow_rows<T, true, 1, true>(), allow_rows<T, true, 2, false>(), allow_rows<T, true, 2, true>(), allow_rows<T, true, 4, false>(),
+                              allow_rows<T, true, 4, true>(), allow_rows<T, false, 1, false>(), allow_rows<T, false, 1, true>(), allow_rows<T, false, 2, false>(), allow_rows<T, false, 2, true>()})
+    if (e != cudaSuccess) return e;
+  return cudaSuccess;
 }
 
 // Ranges of rows whose column sums are formed apart: four blocks for each of 148 SMs, but no fewer than 32 rows each.
@@ -181,23 +199,14 @@ struct NormScratch {
   NormScratch(Carve& c, int64_t rows, int64_t cols) { parts = c.take<float>(std::max(norm_parts(rows, cols), cols <= 4 * kRowWarps * kWarpCols ? std::min<int64_t>(rows, kRowBlocks) : 0) * 2 * cols); }
 };
 
-template <class T, bool kVec, int kKeep>
-cudaError_t allow_rows() {
-  const cudaError_t e = cudaFuncSetAttribute(k_layer_norm_rows<T, kVec, kKeep>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(k_layer_norm_back_rows<T, kVec, kKeep>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem);
-}
-
 template <class T>
 int layer_norm_gradients(rtopk_matrix* ctx, const NormBackArgs<T>& a, float* dgamma, float* dbeta, bool vec, cudaStream_t st) {
   Carve c{ctx->scratch};
   float* parts = dgamma || dbeta ? NormScratch(c, a.rows, a.cols).parts : nullptr;
   auto join = [&](int64_t count) { return launch(ctx, k_norm_join, dim3((unsigned)ceil_div(2 * (int64_t)a.cols, 32)), 256, 0, st, parts, count, a.cols, dgamma, dbeta); };
-  const RowSplit f(ctx->sms, a.rows, a.cols, sizeof(T), a.dtotal ? 3 : 2, 3, vec);
+  const RowSplit f(ctx->sms, a.rows, a.cols, sizeof(T) == 2 ? 4 : 2, vec);
   if (f.fits) {
-    auto go = [&](auto kernel) { return launch(ctx, kernel, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, f.smem, st, a, f.warps, f.rows_per, f.stages, parts); };
-    if (f.keep == 1) MAT_TRY(go(vec ? k_layer_norm_back_rows<T, true, 1> : k_layer_norm_back_rows<T, false, 1>));
-    else if (f.keep == 2) MAT_TRY(go(vec ? k_layer_norm_back_rows<T, true, 2> : k_layer_norm_back_rows<T, false, 2>));
-    else MAT_TRY(go(k_layer_norm_back_rows<T, true, 4>));
+    MAT_TRY((a.dtotal ? back_rows<T, true>(ctx, a, f, vec, parts, st) : back_rows<T, false>(ctx, a, f, vec, parts, st)));
     return parts ? join(f.blocks) : RTOPK_OK;
   }
   if (parts) {      // first: the gradients may be written over what they are made of
@@ -208,16 +217,13 @@ int layer_norm_gradients(rtopk_matrix* ctx, const NormBackArgs<T>& a, float* dga
     MAT_TRY(join(count));
   }
   if (!a.dresidual && !a.dx) return RTOPK_OK;
-  const LongSplit s(a.rows, a.cols);
-  return launch(ctx, vec ? k_layer_norm_back<T, true, 4> : k_layer_norm_back<T, false, 4>, dim3(s.blocks), 32 * s.warps * s.rows_per, 0, st, a, s.warps, s.rows_per);
+  return launch(ctx, vec ? k_layer_norm_back_long<T, true> : k_layer_norm_back_long<T, false>, dim3((unsigned)a.rows), 32 * kRowWarps, 0, st, a);
 }
 
 }  // namespace
 
 cudaError_t rtopk::mat::allow_layers() {
-  using B = __nv_bfloat16;
-  for (const cudaError_t e : {allow_smem<EPI_MICRO>(), allow_rows<float, true, 1>(), allow_rows<float, true, 2>(), allow_rows<float, true, 4>(), allow_rows<float, false, 1>(), allow_rows<float, false, 2>(),
-                              allow_rows<B, true, 1>(), allow_rows<B, true, 2>(), allow_rows<B, true, 4>(), allow_rows<B, false, 1>(), allow_rows<B, false, 2>()})
+  for (const cudaError_t e : {allow_smem<EPI_MICRO>(), allow_rows<float>(), allow_rows<__nv_bfloat16>()})
     if (e != cudaSuccess) return e;
   return cudaSuccess;
 }
@@ -319,7 +325,7 @@ int rtopk_layer_norm(rtopk_matrix* ctx, const void* x, int64_t ld_x, const void*
     return RTOPK_ERR_INVALID_ARG;
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
-  const bool vec = rows_aligned(x, e, 1, ld_x, 0, 16) && rows_aligned(out, e, 1, ld_out, 0, 16) && (!residual || rows_aligned(residual, e, 1, ld_r, 0, 16)) &&
+  const bool vec = cols % 8 == 0 && rows_aligned(x, e, 1, ld_x, 0, 16) && rows_aligned(out, e, 1, ld_out, 0, 16) && (!residual || rows_aligned(residual, e, 1, ld_r, 0, 16)) &&
                    (!total || rows_aligned(total, e, 1, ld_t, 0, 16)) && aligned_to(gamma, 16) && aligned_to(beta, 16);
   auto go = [&](auto t) {
     using T = decltype(t);
@@ -360,7 +366,7 @@ int rtopk_layer_norm_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy,
     return RTOPK_OK;
   }
   auto aligned = [&](const void* p, int64_t ld) { return !p || rows_aligned(p, e, 1, ld, 0, 16); };
-  const bool vec = aligned(dy, ld_dy) && aligned(total, ld_t) && aligned(dtotal, ld_dt) && aligned(dresidual, ld_dr) && aligned(dx, ld_dx) && aligned_to(gamma, 16);
+  const bool vec = cols % 8 == 0 && aligned(dy, ld_dy) && aligned(total, ld_t) && aligned(dtotal, ld_dt) && aligned(dresidual, ld_dr) && aligned(dx, ld_dx) && aligned_to(gamma, 16);
   auto go = [&](auto t) {
     using T = decltype(t);
     const NormBackArgs<T> a = {(const T*)dy, (const T*)total, (const T*)dtotal, (T*)dresidual, (T*)dx, ld_dy, ld_t, ld_dt, ld_dr, ld_dx, gamma, mean, rstd, (int)rows, (int)cols, m};

@@ -49,17 +49,19 @@ __device__ __forceinline__ uint32_t kept8(const Mask& m, uint32_t step, uint32_t
 }
 
 // ----------------------------------------------------------------------------- eight values of a row in a thread
-// A warp takes 256 columns from `base`.  kVec: a thread has eight neighbours, in vectors; else every 32nd, so that loads and stores
-// of rows without alignment are coalesced.
+// A warp takes 256 columns from `base`.  kVec: rows of whole vectors (a multiple of eight columns), of which a thread has eight neighbours or
+// none; else a thread has every 32nd column, so that loads and stores of rows without alignment are coalesced.
 constexpr int kWarpCols = 256;
 template <bool kVec>
 __device__ __forceinline__ int col_of(int base, int lane, int j) { return kVec ? base + lane * 8 + j : base + j * 32 + lane; }
+// Whether the thread has any of the columns; without kVec the warp does.
+template <bool kVec>
+__device__ __forceinline__ bool has_cols(int base, int lane, int cols) { return kVec ? base + lane * 8 < cols : base < cols; }
 
 template <class T, bool kVec>
 __device__ __forceinline__ void load_cols(const T* row, int base, int lane, int cols, Eight<T>& e) {
   if constexpr (kVec) {
-    const int c = base + lane * 8;
-    e.load(row + (c < cols ? c : 0), cols - c, true);
+    if (has_cols<true>(base, lane, cols)) e.load(row + base + lane * 8, 8, true);
   } else if constexpr (sizeof(T) == 4) {
     float v[8];
 #pragma unroll
@@ -76,29 +78,33 @@ __device__ __forceinline__ void load_cols(const T* row, int base, int lane, int 
 }
 template <bool kVec>
 __device__ __forceinline__ void load_cols(const float* row, int base, int lane, int cols, float (&v)[8]) {
-  Eight<float> e;
+  Eight<float> e = {};
   load_cols<float, kVec>(row, base, lane, cols, e);
   e.widen_to(v);
 }
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  ((float4*)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
+  __nv_bfloat162 q[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) q[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+  uint4 w;
+  memcpy(&w, q, sizeof w);
+  *(uint4*)p = w;
+}
 __device__ __forceinline__ void narrow(float v, float& out) { out = v; }
 __device__ __forceinline__ void narrow(float v, __nv_bfloat16& out) { out = __float2bfloat16_rn(v); }
+// kVec: for threads that have columns.
 template <class T, bool kVec>
 __device__ __forceinline__ void store_cols(T* row, int base, int lane, int cols, const float (&v)[8]) {
-  T q[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) narrow(v[j], q[j]);
-  if (kVec && base + lane * 8 + 8 <= cols) {
-    uint4* to = (uint4*)(row + base + lane * 8);
-    uint4 w[sizeof(T) / 2];
-    memcpy(w, q, sizeof w);
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) to[i] = w[i];
+  if constexpr (kVec) {
+    store8(row + base + lane * 8, v);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int c = col_of<kVec>(base, lane, j);
-      if (c < cols) row[c] = q[j];
-    }
+    for (int j = 0; j < 8; ++j)
+      if (base + j * 32 + lane < cols) narrow(v[j], row[base + j * 32 + lane]);
   }
 }
 // v <- D(v) for the warp's 256 columns from `base`.
@@ -119,16 +125,18 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int k = 16; k; k >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, k);
   return v;
 }
-// The sum over a row's `warps` warps; `part` has a place for each warp of the block and is used once between two barriers.
-__device__ __forceinline__ float row_sum(float v, int warps, int group, float* part) {
+// 1 / sqrt(v), the approximation improved by one Newton step: within 2 steps of binary32.
+__device__ __forceinline__ float inverse_root(float v) {
+  const float r = rsqrtf(v);
+  return fmaf(r * fmaf(-v * r, r, 1.f), 0.5f, r);
+}
+// The sum over the block; `part` has a place for each warp and is used once between two barriers.
+__device__ __forceinline__ float row_sum(float v, float* part) {
+  const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   v = warp_sum(v);
-  if (warps > 1) {
-    const int lane = threadIdx.x & 31;
-    if (lane == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = warp_sum(lane < warps ? part[group * warps + lane] : 0.f);
-  }
-  return v;
+  if (lane == 0) part[threadIdx.x >> 5] = v;
+  __syncthreads();
+  return warp_sum(lane < warps ? part[lane] : 0.f);
 }
 
 // ----------------------------------------------------------------------------- dropout
@@ -137,48 +145,33 @@ __device__ __forceinline__ float row_sum(float v, int warps, int group, float* p
 struct Divisor { uint32_t m, d; int shift; };
 __device__ __forceinline__ uint32_t divide(uint32_t k, const Divisor& v) { return v.d == 1 ? k : __umulhi(k, v.m) >> v.shift; }
 
+// Four rows at a time: a thread takes eight neighbouring columns of them (kVec), or a warp 256, so that what the generator's first
+// rounds make of the column is shared by four rows.  Bands of `band` rows, a multiple of four, along the grid's second side.
 template <class T, bool kVec>
 __global__ void __launch_bounds__(256) k_dropout(const T* x, int64_t ld_x, int64_t rows, int cols, int64_t band, const Divisor units, const __grid_constant__ Mask mask, T* out, int64_t ld_out) {
   constexpr int kEach = 4;
+  const uint32_t k = kVec ? blockIdx.x * 256u + threadIdx.x : blockIdx.x * 8u + (threadIdx.x >> 5);
+  const uint32_t quad = divide(k, units), unit = k - quad * units.d;
+  const int64_t row = blockIdx.y * band + (int64_t)quad * kEach;
+  const int left = (int)min((int64_t)kEach, min(rows, (blockIdx.y + 1) * band) - row);
+  const int base = kVec ? (int)unit * 8 : (int)unit * kWarpCols, lane = kVec ? 0 : threadIdx.x & 31;
   launch_wait();
   launch_next();
+  if (left <= 0) return;
   const uint32_t step = mask_step(mask);
-  const int lane = threadIdx.x & 31;
-  const int64_t row0 = blockIdx.y * band;
-  const int in_band = (int)min(band, rows - row0);
-  if constexpr (kVec) {      // a thread: groups of eight columns, a block apart
-    const uint32_t groups = units.d, all = in_band * groups, first = blockIdx.x * (256u * kEach) + threadIdx.x;
-    Eight<T> e[kEach];
-    uint32_t r[kEach], g[kEach];
+  const T* from = x + row * ld_x;
+  T* to = out + row * ld_out;
+  Eight<T> e[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const uint32_t k = first + 256 * i;
-      r[i] = divide(k, units), g[i] = k - r[i] * groups;
-      if (k < all) e[i].load(x + (row0 + r[i]) * ld_x + g[i] * 8, cols - (int)g[i] * 8, true);
-    }
+  for (int i = 0; i < kEach; ++i)
+    if (i < left) load_cols<T, kVec>(from + i * ld_x, base, lane, cols, e[i]);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      if (first + 256 * i >= all) break;
-      float v[8];
-      e[i].widen_to(v);
-      drop8(mask, mask_words(mask, step, (uint32_t)(row0 + r[i]), g[i]), v);
-      store_cols<T, true>(out + (row0 + r[i]) * ld_out, g[i] * 8, 0, cols, v);
-    }
-  } else {                   // a warp: 256 columns of a row
-    const uint32_t chunks = units.d, all = in_band * chunks;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const uint32_t k = blockIdx.x * (8u * kEach) + (threadIdx.x >> 5) + 8 * i;
-      if (k >= all) break;
-      const uint32_t r = divide(k, units);
-      const int base = (int)(k - r * chunks) * kWarpCols;
-      Eight<T> e;
-      load_cols<T, false>(x + (row0 + r) * ld_x, base, lane, cols, e);
-      float v[8];
-      e.widen_to(v);
-      drop_cols<false>(mask, step, (uint32_t)(row0 + r), base, lane, v);
-      store_cols<T, false>(out + (row0 + r) * ld_out, base, lane, cols, v);
-    }
+  for (int i = 0; i < kEach; ++i) {
+    if (i >= left) break;
+    float v[8];
+    e[i].widen_to(v);
+    drop_cols<kVec>(mask, step, (uint32_t)(row + i), base, lane, v);
+    store_cols<T, kVec>(to + i * ld_out, base, lane, cols, v);
   }
 }
 
@@ -195,82 +188,86 @@ struct NormArgs {
   Mask mask;
 };
 
-// Rows that fit the block are taken in turn: one block per SM, `rows_per` rows of it at a time with `warps` warps each, kKeep pieces of 256 columns
-// a warp.  What a thread needs of the next rows is on its way to its own place in shared memory (kVec: asynchronous copies, `stages`
-// rows deep; else by way of registers), so that no barrier stops the stream of reads.
+// Rows that fit the block are taken in turn: one block per SM, `rows_per` rows of it at a time with `warps` warps each (a group), kKeep pieces of
+// 256 columns a warp.  What a thread needs of the next rows is on its way to its own place in shared memory (kVec: asynchronous copies,
+// kStages rows deep; else by way of registers).  A row's sums meet while the results of the row before are formed, so that neither the
+// barrier nor the sums' latency stops the block; one barrier a row, of the row's warps.
 //
 // The bound is memory as long as the instructions keep up: 16 columns a thread, so that a row's sums, addresses and statistics are shared
-// by 16; numbers of the mask compared two at a time.
+// by 16, and places in shared memory that differ by constants.
 constexpr int kRowWarps = 16, kRowSmem = 216 * 1024;
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {      // the rest of 16 becomes zero
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void copies_wait(int left) {
-  if (left == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
-  else if (left == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
-  else asm volatile("cp.async.wait_group 3;" ::: "memory");
-}
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
 template <class T, bool kVec, int kKeep, int kArrays>
-struct RowPipe {
-  static constexpr int kPlanes = sizeof(T) / 2;      // a thread's eight values lie in pieces of 16 bytes, each thread's next to the others'
-  int warps, group, in_row, lane, stages, arrays, plane, cols;
-  int sets;                    // of rows, of this block
-  int64_t first, step, rows;   // the thread's row of a set is first + set * step
+struct RowShape {
+  static constexpr int kPlanes = sizeof(T) / 2;                       // a thread's eight values lie in pieces of 16 bytes,
+  static constexpr int kPlane = 32 * kRowWarps * 16;                  // each thread's next to the others'
+  static constexpr int kStage = kArrays * kKeep * kPlanes * kPlane;
+  static constexpr int kFit = kRowSmem / kStage, kStages = kVec ? (kFit > 4 ? 4 : kFit) : 1;
+  static constexpr int kSmem = kStages * kStage;
+};
+
+template <class T, bool kVec, int kKeep, int kArrays>
+struct RowPipe : RowShape<T, kVec, kKeep, kArrays> {
+  using S = RowShape<T, kVec, kKeep, kArrays>;
+  using S::kPlanes;
+  using S::kPlane;
+  using S::kStage;
+  using S::kStages;
+  int warps, group, in_row, lane, cols;
+  int count, first, step;      // rows of the group, the first of them, and how far apart they are
+  int fetched, to;             // rows on their way or here, and the stage of the next
   char* mine;
   struct Source {
-    const T* p;      // of the next row to be read
+    const T* p;                // of the next row to be read
     int64_t step;
     Eight<T> next[kVec ? 1 : kKeep];
   } s0, s1, s2;
 
-  __device__ __forceinline__ RowPipe(char* smem, int warps, int rows_per, int stages, int64_t rows, int cols) : warps(warps), stages(stages), cols(cols), rows(rows) {
+  __device__ __forceinline__ RowPipe(char* smem, int warps, int rows_per, int rows, int cols) : warps(warps), cols(cols) {
     lane = threadIdx.x & 31;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0);
     group = warp / warps, in_row = warp - group * warps;
-    plane = warps * 512;
-    arrays = 0;
-    first = (int64_t)blockIdx.x * rows_per + group, step = (int64_t)gridDim.x * rows_per;
-    const int64_t all = (rows + rows_per - 1) / rows_per;
-    sets = blockIdx.x < all ? (int)((all - 1 - blockIdx.x) / gridDim.x) + 1 : 0;
-    mine = smem;
-  }
-  __device__ __forceinline__ void add(Source& s, const T* p, int64_t ld) {      // in the order of s0, s1, s2
-    if (!p) return;
-    s.p = p + first * ld + (kVec ? base(0) + lane * 8 : 0), s.step = ld * step;
-    ++arrays;
-  }
-  __device__ __forceinline__ void start() {
-    mine += group * stages * arrays * kKeep * kPlanes * plane + (in_row * 32 + lane) * 16;
-    if constexpr (kVec)
-      for (int k = 0; k < stages - 1; ++k) fetch(k, k);
-    else fetch(0, 0);
+    first = blockIdx.x * rows_per + group, step = gridDim.x * rows_per;
+    count = first < rows ? (rows - 1 - first) / step + 1 : 0;
+    mine = smem + threadIdx.x * 16;
+    fetched = to = 0;
   }
   __device__ __forceinline__ int base(int i) const { return (i * warps + in_row) * kWarpCols; }
-  __device__ __forceinline__ char* place(int stage, int q, int i) const { return mine + ((stage * arrays + q) * kKeep + i) * kPlanes * plane; }
-  __device__ __forceinline__ void fetch(Source& s, int q, int stage) {
-    const uint32_t to = smem_addr(place(stage, q, 0));
+  __device__ __forceinline__ bool on(int i) const { return has_cols<kVec>(base(i), lane, cols); }
+  __device__ __forceinline__ char* place(int stage, int q, int i) const { return mine + stage * kStage + (q * kKeep + i) * kPlanes * kPlane; }
+  __device__ __forceinline__ void source(Source& s, const T* p, int64_t ld) { s.p = p + first * ld + (kVec ? base(0) + lane * 8 : 0), s.step = ld * step; }
+  __device__ __forceinline__ void fetch(Source& s, int q) {
+    const uint32_t dst = smem_addr(place(to, q, 0));
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
       if constexpr (kVec) {
-        const int left = (cols - base(i) - lane * 8) * (int)sizeof(T);
+        if (on(i))
 #pragma unroll
-        for (int r = 0; r < kPlanes; ++r)
-          if (left > 16 * r) copy16(to + (i * kPlanes + r) * plane, (const char*)(s.p + i * warps * kWarpCols) + 16 * r, min(16, left - 16 * r));
+          for (int r = 0; r < kPlanes; ++r) copy16(dst + (i * kPlanes + r) * kPlane, (const char*)(s.p + i * warps * kWarpCols) + 16 * r);
       } else {
         load_cols<T, false>(s.p, base(i), lane, cols, s.next[i]);
       }
     }
     s.p += s.step;
   }
-  __device__ __forceinline__ void fetch(int k, int stage) {      // called for k = 0, 1, 2, ..
-    if (k < sets && first + k * step < rows) {
-      fetch(s0, 0, stage);
-      if (arrays > 1) fetch(s1, 1, stage);
-      if (kArrays > 2 && arrays > 2) fetch(s2, 2, stage);
+  __device__ __forceinline__ void fetch() {
+    if (fetched < count) {
+      fetch(s0, 0);
+      if (kArrays > 1) fetch(s1, 1);
+      if (kArrays > 2) fetch(s2, 2);
     }
-    if constexpr (kVec) copies_commit();
+    ++fetched;
+    if constexpr (kVec) {
+      copies_commit();
+      to = to + 1 == kStages ? 0 : to + 1;
+    }
+  }
+  __device__ __forceinline__ void start(int rows) {
+    for (int k = 0; k < rows; ++k) fetch();
   }
   __device__ __forceinline__ void land(const Source& s, int q) {
 #pragma unroll
@@ -278,76 +275,44 @@ struct RowPipe {
       uint4 w[kPlanes];
       memcpy(w, &s.next[i], sizeof w);
 #pragma unroll
-      for (int r = 0; r < kPlanes; ++r) *(uint4*)(place(0, q, i) + r * plane) = w[r];
+      for (int r = 0; r < kPlanes; ++r) *(uint4*)(place(0, q, i) + r * kPlane) = w[r];
     }
   }
-  // Brings row k's values in and the row that follows on its way.
-  __device__ __forceinline__ void advance(int k, int stage) {
-    if constexpr (kVec) {
-      fetch(k + stages - 1, stage == 0 ? stages - 1 : stage - 1);
-      copies_wait(stages - 1);
-    } else {
-      if (first + k * step < rows) {
-        land(s0, 0);
-        if (arrays > 1) land(s1, 1);
-        if (kArrays > 2 && arrays > 2) land(s2, 2);
-      }
-      fetch(k + 1, 0);
-    }
+  __device__ __forceinline__ void land() {      // !kVec: the row in the registers comes to its place
+    land(s0, 0);
+    if (kArrays > 1) land(s1, 1);
+    if (kArrays > 2) land(s2, 2);
   }
-  // The thread's values of piece i; pieces that end inside hold zeros beyond.
+  // The thread's values of piece i, which it has.
   __device__ __forceinline__ void values(int stage, int q, int i, float (&v)[8]) const {
     uint4 w[kPlanes];
     Eight<T> e;
 #pragma unroll
-    for (int r = 0; r < kPlanes; ++r) w[r] = *(const uint4*)(place(stage, q, i) + r * plane);
+    for (int r = 0; r < kPlanes; ++r) w[r] = *(const uint4*)(place(stage, q, i) + r * kPlane);
     memcpy(&e, w, sizeof w);
     e.widen_to(v);
   }
-  __device__ __forceinline__ void zero() {      // places that no copy fills
-    if constexpr (kVec) {
-      for (int s = 0; s < stages; ++s)
-        for (int q = 0; q < arrays; ++q)
-#pragma unroll
-          for (int i = 0; i < kKeep; ++i)
-#pragma unroll
-            for (int r = 0; r < kPlanes; ++r)
-              if ((cols - base(i) - lane * 8) * (int)sizeof(T) <= 16 * r) *(uint4*)(place(s, q, i) + r * plane) = make_uint4(0u, 0u, 0u, 0u);
-    }
-  }
-  // Sums over the row's warps; `part` has a place for each warp and is used again after another call's barrier.
-  __device__ __forceinline__ void meet() const { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(warps * 32) : "memory"); }
-  __device__ __forceinline__ float sum(float v, float* part) const {
-    v = warp_sum(v);
-    if (warps == 1) return v;
-    if (lane == 0) part[group * warps + in_row] = v;
-    meet();
-    return warp_sum(lane < warps ? part[group * warps + lane] : 0.f);
-  }
-  __device__ __forceinline__ float2 sum(float2 v, float2* part) const {
-    v = make_float2(warp_sum(v.x), warp_sum(v.y));
-    if (warps == 1) return v;
-    if (lane == 0) part[group * warps + in_row] = v;
-    meet();
-    v = lane < warps ? part[group * warps + lane] : make_float2(0.f, 0.f);
-    return make_float2(warp_sum(v.x), warp_sum(v.y));
+  __device__ __forceinline__ void meet() const {
+    if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(warps * 32) : "memory");
   }
 };
 
-template <class T, bool kVec, int kKeep>
-__global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __grid_constant__ NormArgs<T> a, int warps, int rows_per, int stages) {
+// The mean and the sum of squares around it meet in one exchange: a warp sums its columns, then their squares around its own mean, and of
+// n columns with sum s and squares q the row takes q + n (s / n - mean)^2 (Chan, Golub and LeVeque, 1979).
+template <class T, bool kVec, int kKeep, bool kResidual>
+__global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __grid_constant__ NormArgs<T> a, int warps, int rows_per) {
+  using Pipe = RowPipe<T, kVec, kKeep, kResidual ? 2 : 1>;
   extern __shared__ __align__(16) char norm_smem[];
-  __shared__ float part[4][kRowWarps];
-  RowPipe<T, kVec, kKeep, 2> pipe(norm_smem, warps, rows_per, stages, a.rows, a.cols);
+  __shared__ float2 part[2][kRowWarps];
+  Pipe pipe(norm_smem, warps, rows_per, a.rows, a.cols);
   const int lane = pipe.lane;
   launch_wait();
   launch_next();
   const uint32_t step = mask_step(a.mask);
-  pipe.add(pipe.s0, a.x, a.ld_x);
-  pipe.add(pipe.s1, a.residual, a.ld_r);
-  pipe.start();
-  pipe.zero();
-  constexpr bool kWeights = kKeep <= 2;      // kept in registers
+  pipe.source(pipe.s0, a.x, a.ld_x);
+  if (kResidual) pipe.source(pipe.s1, a.residual, a.ld_r);
+  pipe.start(Pipe::kStages);
+  constexpr bool kWeights = kKeep == 1 || (kVec && kKeep == 2);      // kept in registers
   float gamma[kWeights ? kKeep : 1][8], beta[kWeights ? kKeep : 1][8];
   auto weights = [&](int i, float (&g)[8], float (&b)[8]) {
     if (a.gamma) load_cols<kVec>(a.gamma, pipe.base(i), lane, a.cols, g);
@@ -361,78 +326,97 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __g
   if constexpr (kWeights) {
 #pragma unroll
     for (int i = 0; i < kKeep; ++i)
-      if (pipe.base(i) < a.cols) weights(i, gamma[i], beta[i]);
+      if (pipe.on(i)) weights(i, gamma[i], beta[i]);
   }
-  const float share = 1.f / a.cols;
-  int stage = 0;
+  auto columns_of = [&](int warp) {      // of a row's warps
+    int n = 0;
+    for (int i = 0; i < kKeep; ++i) n += min(kWarpCols, max(0, a.cols - (i * warps + warp) * kWarpCols));
+    return n;
+  };
+  const int n_own = columns_of(pipe.in_row), n_lane = lane < warps ? columns_of(lane) : 0;
+  const float share_own = n_own ? 1.f / n_own : 0.f, share_lane = n_lane ? 1.f / n_lane : 0.f, share = 1.f / a.cols;
+  const bool to_total = a.total != nullptr, masked = a.mask.limit != 0;
+  T *y = a.y + pipe.first * a.ld_y, *total = a.total + (to_total ? pipe.first * a.ld_t : 0);
+  const int64_t y_step = pipe.step * a.ld_y, total_step = pipe.step * a.ld_t;
+  float v[kKeep][8], before[kKeep][8];
+  int row = pipe.first, stage = 0;
 #pragma unroll 1
-  for (int k = 0; k < pipe.sets; ++k) {
-    const int64_t row = pipe.first + k * pipe.step;
-    pipe.advance(k, stage);
-    if (row >= a.rows) break;      // the same for all of a row's warps; only in the block's last set
-    float v[kKeep][8], sum = 0.f;
+  for (int k = 0; k <= pipe.count; ++k) {
+    if (k < pipe.count) {
+      if constexpr (kVec) copies_wait<Pipe::kStages - 1>();
+      else pipe.land();
+      float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < kKeep; ++i) {
-      if (pipe.base(i) >= a.cols) break;
-      pipe.values(stage, 0, i, v[i]);
-      if (a.mask.limit) drop_cols<kVec>(a.mask, step, (uint32_t)row, pipe.base(i), lane, v[i]);
-      if (a.residual) {
-        float r[8];
-        pipe.values(stage, 1, i, r);
+      for (int i = 0; i < kKeep; ++i) {
+        if (!pipe.on(i)) continue;
+        pipe.values(stage, 0, i, v[i]);
+        if (masked) drop_cols<kVec>(a.mask, step, (uint32_t)row, pipe.base(i), lane, v[i]);
+        if constexpr (kResidual) {
+          float r[8];
+          pipe.values(stage, 1, i, r);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] += r[j];
+          for (int j = 0; j < 8; ++j) v[i][j] += r[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += v[i][j];
+        if (to_total) store_cols<T, kVec>(total, pipe.base(i), lane, a.cols, v[i]);
       }
+      if (to_total) total += total_step;
+      pipe.fetch();      // into the place of the row just read
+      if constexpr (kVec) stage = stage + 1 == Pipe::kStages ? 0 : stage + 1;
+      sum = warp_sum(sum);
+      const float own = sum * share_own;
+      float squares = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum += v[i][j];
-    }
-    const float mean = pipe.sum(sum, part[k & 1]) * share;
-    float squares = 0.f;
-#pragma unroll
-    for (int i = 0; i < kKeep; ++i) {
-      const int base = pipe.base(i);
-      if (base >= a.cols) break;
-      if (base + kWarpCols <= a.cols) {
+      for (int i = 0; i < kKeep; ++i) {
+        if (!pipe.on(i)) continue;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float d = v[i][j] - mean;
-          squares = fmaf(d, d, squares);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float d = v[i][j] - mean;
-          if (col_of<kVec>(base, lane, j) < a.cols) squares = fmaf(d, d, squares);
+          const float d = v[i][j] - own;
+          if (kVec || col_of<kVec>(pipe.base(i), lane, j) < a.cols) squares = fmaf(d, d, squares);
         }
       }
+      squares = warp_sum(squares);
+      if (lane == 0) part[k & 1][pipe.group * warps + pipe.in_row] = make_float2(sum, squares);
     }
-    const float rstd = 1.f / sqrtf(pipe.sum(squares, part[2 + (k & 1)]) * share + a.eps);
-    if (pipe.in_row == 0 && lane == 0) {
-      if (a.mean) a.mean[row] = mean;
-      if (a.rstd) a.rstd[row] = rstd;
+    if (k > 0) {      // the row before
+      const int at = row - pipe.step;
+      const float2 p = lane < warps ? part[(k - 1) & 1][pipe.group * warps + lane] : make_float2(0.f, 0.f);
+      const float mean = warp_sum(p.x) * share, off = p.x * share_lane - mean;
+      const float rstd = inverse_root(warp_sum(fmaf(n_lane * off, off, p.y)) * share + a.eps);
+      if (pipe.in_row == 0 && lane == 0) {
+        if (a.mean) a.mean[at] = mean;
+        if (a.rstd) a.rstd[at] = rstd;
+      }
+#pragma unroll
+      for (int i = 0; i < kKeep; ++i) {
+        if (!pipe.on(i)) continue;
+        if constexpr (!kWeights) weights(i, gamma[0], beta[0]);
+        const float(&g)[8] = gamma[kWeights ? i : 0], (&b)[8] = beta[kWeights ? i : 0];
+        float out[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) out[j] = fmaf((before[i][j] - mean) * rstd, g[j], b[j]);
+        store_cols<T, kVec>(y, pipe.base(i), lane, a.cols, out);
+      }
+      y += y_step;
     }
 #pragma unroll
-    for (int i = 0; i < kKeep; ++i) {
-      const int base = pipe.base(i);
-      if (base >= a.cols) break;
-      if (a.total) store_cols<T, kVec>(a.total + row * a.ld_t, base, lane, a.cols, v[i]);
-      if constexpr (!kWeights) weights(i, gamma[0], beta[0]);
-      const float(&g)[8] = gamma[kWeights ? i : 0], (&b)[8] = beta[kWeights ? i : 0];
+    for (int i = 0; i < kKeep; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = fmaf((v[i][j] - mean) * rstd, g[j], b[j]);
-      store_cols<T, kVec>(a.y + row * a.ld_y, base, lane, a.cols, v[i]);
-    }
-    if constexpr (kVec) stage = stage + 1 == stages ? 0 : stage + 1;
+      for (int j = 0; j < 8; ++j) before[i][j] = v[i][j];
+    row += pipe.step;
+    pipe.meet();
   }
 }
 
-// Longer rows: `warps` warps take a row, each kKeep pieces of 256 columns in its registers; what is beyond is read again.
-template <class T, bool kVec, int kKeep>
-__global__ void __launch_bounds__(512) k_layer_norm(const __grid_constant__ NormArgs<T> a, int warps, int rows_per) {
-  __shared__ float part[2][16];
-  const int lane = threadIdx.x & 31, group = (threadIdx.x >> 5) / warps, in_row = (threadIdx.x >> 5) - group * warps, span = warps * kWarpCols;
-  const int64_t at = (int64_t)blockIdx.x * rows_per + group;
-  const bool in = at < a.rows;
-  const int64_t row = in ? at : a.rows - 1;
+// Longer rows: a block takes one, each warp kLongKeep pieces of 256 columns in its registers; what is beyond is read again.
+constexpr int kLongKeep = 4;
+template <class T, bool kVec>
+__global__ void __launch_bounds__(32 * kRowWarps) k_layer_norm_long(const __grid_constant__ NormArgs<T> a) {
+  __shared__ float part[2][kRowWarps];
+  constexpr int span = kRowWarps * kWarpCols;
+  const int lane = threadIdx.x & 31, in_row = threadIdx.x >> 5;
+  const int64_t row = blockIdx.x;
   launch_wait();
   launch_next();
   const uint32_t step = mask_step(a.mask);
@@ -454,31 +438,31 @@ __global__ void __launch_bounds__(512) k_layer_norm(const __grid_constant__ Norm
     if (res) load_cols<T, kVec>(res, base, lane, a.cols, er);
     values(ex, er, base, v);
   };
-  Eight<T> ex[kKeep], er[kKeep];
+  Eight<T> ex[kLongKeep], er[kLongKeep];
 #pragma unroll
-  for (int i = 0; i < kKeep; ++i) {
+  for (int i = 0; i < kLongKeep; ++i) {
     const int base = i * span + in_row * kWarpCols;
-    if (base < a.cols) {
+    if (has_cols<kVec>(base, lane, a.cols)) {
       load_cols<T, kVec>(x, base, lane, a.cols, ex[i]);
       if (res) load_cols<T, kVec>(res, base, lane, a.cols, er[i]);
     }
   }
-  const int rest = kKeep * span + in_row * kWarpCols;
-  float v[kKeep][8], w[8], sum = 0.f;
+  const int rest = kLongKeep * span + in_row * kWarpCols;
+  float v[kLongKeep][8], w[8], sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < kKeep; ++i) {
+  for (int i = 0; i < kLongKeep; ++i) {
     const int base = i * span + in_row * kWarpCols;
-    if (base >= a.cols) break;
+    if (!has_cols<kVec>(base, lane, a.cols)) break;
     values(ex[i], er[i], base, v[i]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += v[i][j];      // past the end they are zero
+    for (int j = 0; j < 8; ++j) sum += v[i][j];
   }
-  for (int base = rest; base < a.cols; base += span) {
+  for (int base = rest; has_cols<kVec>(base, lane, a.cols); base += span) {
     fetch(base, w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum += w[j];
   }
-  const float mean = row_sum(sum, warps, group, part[0]) / a.cols;
+  const float mean = row_sum(sum, part[0]) / a.cols;
   float squares = 0.f;
   auto add_squares = [&](const float (&v)[8], int base) {
 #pragma unroll
@@ -488,17 +472,16 @@ __global__ void __launch_bounds__(512) k_layer_norm(const __grid_constant__ Norm
     }
   };
 #pragma unroll
-  for (int i = 0; i < kKeep; ++i) {
+  for (int i = 0; i < kLongKeep; ++i) {
     const int base = i * span + in_row * kWarpCols;
-    if (base >= a.cols) break;
+    if (!has_cols<kVec>(base, lane, a.cols)) break;
     add_squares(v[i], base);
   }
-  for (int base = rest; base < a.cols; base += span) {
+  for (int base = rest; has_cols<kVec>(base, lane, a.cols); base += span) {
     fetch(base, w);
     add_squares(w, base);
   }
-  const float rstd = 1.f / sqrtf(row_sum(squares, warps, group, part[1]) / a.cols + a.eps);
-  if (!in) return;
+  const float rstd = inverse_root(row_sum(squares, part[1]) / a.cols + a.eps);
   if (in_row == 0 && lane == 0) {
     if (a.mean) a.mean[row] = mean;
     if (a.rstd) a.rstd[row] = rstd;
@@ -517,12 +500,12 @@ __global__ void __launch_bounds__(512) k_layer_norm(const __grid_constant__ Norm
     store_cols<T, kVec>(a.y + row * a.ld_y, base, lane, a.cols, y);
   };
 #pragma unroll
-  for (int i = 0; i < kKeep; ++i) {
+  for (int i = 0; i < kLongKeep; ++i) {
     const int base = i * span + in_row * kWarpCols;
-    if (base >= a.cols) break;
+    if (!has_cols<kVec>(base, lane, a.cols)) break;
     finish(v[i], base);
   }
-  for (int base = rest; base < a.cols; base += span) {
+  for (int base = rest; has_cols<kVec>(base, lane, a.cols); base += span) {
     fetch(base, w);
     finish(w, base);
   }
@@ -538,13 +521,12 @@ struct NormBackArgs {
   Mask mask;
 };
 
-template <class T, bool kVec, int kKeep>
-__global__ void __launch_bounds__(512) k_layer_norm_back(const __grid_constant__ NormBackArgs<T> a, int warps, int rows_per) {
-  __shared__ float part[2][16];
-  const int lane = threadIdx.x & 31, group = (threadIdx.x >> 5) / warps, in_row = (threadIdx.x >> 5) - group * warps, span = warps * kWarpCols;
-  const int64_t at = (int64_t)blockIdx.x * rows_per + group;
-  const bool in = at < a.rows;
-  const int64_t row = in ? at : a.rows - 1;
+template <class T, bool kVec>
+__global__ void __launch_bounds__(32 * kRowWarps) k_layer_norm_back_long(const __grid_constant__ NormBackArgs<T> a) {
+  __shared__ float part[2][kRowWarps];
+  constexpr int span = kRowWarps * kWarpCols;
+  const int lane = threadIdx.x & 31, in_row = threadIdx.x >> 5;
+  const int64_t row = blockIdx.x;
   launch_wait();
   launch_next();
   const uint32_t step = mask_step(a.mask);
@@ -569,35 +551,34 @@ __global__ void __launch_bounds__(512) k_layer_norm_back(const __grid_constant__
     load_cols<T, kVec>(total, base, lane, a.cols, et);
     values(ey, et, base, g, h);
   };
-  Eight<T> ey[kKeep], et[kKeep];
+  Eight<T> ey[kLongKeep], et[kLongKeep];
 #pragma unroll
-  for (int i = 0; i < kKeep; ++i) {
+  for (int i = 0; i < kLongKeep; ++i) {
     const int base = i * span + in_row * kWarpCols;
-    if (base < a.cols) {
+    if (has_cols<kVec>(base, lane, a.cols)) {
       load_cols<T, kVec>(dy, base, lane, a.cols, ey[i]);
       load_cols<T, kVec>(total, base, lane, a.cols, et[i]);
     }
   }
-  const int rest = kKeep * span + in_row * kWarpCols;
+  const int rest = kLongKeep * span + in_row * kWarpCols;
   float g[8], h[8], sum = 0.f, along = 0.f;
   auto add = [&]() {
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum += g[j], along = fmaf(g[j], h[j], along);
   };
 #pragma unroll
-  for (int i = 0; i < kKeep; ++i) {
+  for (int i = 0; i < kLongKeep; ++i) {
     const int base = i * span + in_row * kWarpCols;
-    if (base >= a.cols) break;
+    if (!has_cols<kVec>(base, lane, a.cols)) break;
     values(ey[i], et[i], base, g, h);
     add();
   }
-  for (int base = rest; base < a.cols; base += span) {
+  for (int base = rest; has_cols<kVec>(base, lane, a.cols); base += span) {
     fetch(base, g, h);
     add();
   }
-  sum = row_sum(sum, warps, group, part[0]) / a.cols;
-  along = row_sum(along, warps, group, part[1]) / a.cols;
-  if (!in) return;
+  sum = row_sum(sum, part[0]) / a.cols;
+  along = row_sum(along, part[1]) / a.cols;
   auto finish = [&](int base) {
     float d[8];
 #pragma unroll
@@ -617,35 +598,37 @@ __global__ void __launch_bounds__(512) k_layer_norm_back(const __grid_constant__
     }
   };
 #pragma unroll
-  for (int i = 0; i < kKeep; ++i) {
+  for (int i = 0; i < kLongKeep; ++i) {
     const int base = i * span + in_row * kWarpCols;
-    if (base >= a.cols) break;
+    if (!has_cols<kVec>(base, lane, a.cols)) break;
     values(ey[i], et[i], base, g, h);
     finish(base);
   }
-  for (int base = rest; base < a.cols; base += span) {
+  for (int base = rest; has_cols<kVec>(base, lane, a.cols); base += span) {
     fetch(base, g, h);
     finish(base);
   }
 }
 
 // The gradients of rows that fit the block.  A thread has the same columns of every row, so dgamma's and dbeta's sums stay in its
-// registers; it reads a row in shared memory twice, for the row's two sums, then for the results.  One barrier a row.
-template <class T, bool kVec, int kKeep>
-__global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_back_rows(const __grid_constant__ NormBackArgs<T> a, int warps, int rows_per, int stages, float* parts) {
+// registers; it reads a row in shared memory twice, for the row's two sums, then for the results.
+template <class T, bool kVec, int kKeep, bool kMore>
+__global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_back_rows(const __grid_constant__ NormBackArgs<T> a, int warps, int rows_per, float* parts) {
+  using Pipe = RowPipe<T, kVec, kKeep, kMore ? 3 : 2>;
+  // With three stages a row's results wait until the next row's sums are on their way; with fewer its place is needed before.
+  constexpr bool kLater = Pipe::kStages > 2;
   extern __shared__ __align__(16) char norm_smem[];
   __shared__ float2 part[2][kRowWarps];
-  RowPipe<T, kVec, kKeep, 3> pipe(norm_smem, warps, rows_per, stages, a.rows, a.cols);
+  Pipe pipe(norm_smem, warps, rows_per, a.rows, a.cols);
   const int lane = pipe.lane;
   launch_wait();
   launch_next();
   const uint32_t step = mask_step(a.mask);
-  pipe.add(pipe.s0, a.dy, a.ld_dy);
-  pipe.add(pipe.s1, a.total, a.ld_t);
-  pipe.add(pipe.s2, a.dtotal, a.ld_dt);
-  pipe.start();
-  pipe.zero();
-  constexpr bool kWeights = kKeep <= 2;      // kept in registers
+  pipe.source(pipe.s0, a.dy, a.ld_dy);
+  pipe.source(pipe.s1, a.total, a.ld_t);
+  if (kMore) pipe.source(pipe.s2, a.dtotal, a.ld_dt);
+  pipe.start(kVec ? Pipe::kStages - 1 : 1);
+  constexpr bool kWeights = kKeep == 1 || (kVec && kKeep == 2);      // kept in registers
   float gamma[kWeights ? kKeep : 1][8];
   auto weights = [&](int i, float (&g)[8]) {
     if (a.gamma) load_cols<kVec>(a.gamma, pipe.base(i), lane, a.cols, g);
@@ -656,68 +639,91 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_back_rows(cons
   if constexpr (kWeights) {
 #pragma unroll
     for (int i = 0; i < kKeep; ++i)
-      if (pipe.base(i) < a.cols) weights(i, gamma[i]);
+      if (pipe.on(i)) weights(i, gamma[i]);
   }
   float to_gamma[kKeep][8] = {}, to_beta[kKeep][8] = {};
-  auto stat = [&](const float* p, int k) {
-    const int64_t row = pipe.first + k * pipe.step;
-    return k < pipe.sets && row < a.rows ? p[row] : 0.f;
-  };
-  float next_mean = stat(a.mean, 0), next_rstd = stat(a.rstd, 0);
   const float share = 1.f / a.cols;
-  int stage = 0;
-#pragma unroll 1
-  for (int k = 0; k < pipe.sets; ++k) {
-    const int64_t row = pipe.first + k * pipe.step;
-    pipe.advance(k, stage);
-    if (row >= a.rows) break;      // the same for all of a row's warps; only in the block's last set
-    const float rstd = next_rstd, shift = -next_mean * rstd;
-    next_mean = stat(a.mean, k + 1), next_rstd = stat(a.rstd, k + 1);
-    float2 sums = make_float2(0.f, 0.f);
+  const bool to_residual = a.dresidual != nullptr, to_x = a.dx != nullptr;
+  T *dresidual = a.dresidual + (to_residual ? pipe.first * a.ld_dr : 0), *dx = a.dx + (to_x ? pipe.first * a.ld_dx : 0);
+  const int64_t dresidual_step = pipe.step * a.ld_dr, dx_step = pipe.step * a.ld_dx;
+  int row = pipe.first, stage = 0;
+  float next_mean = pipe.count ? a.mean[row] : 0.f, next_rstd = pipe.count ? a.rstd[row] : 0.f, rstd = 0.f, shift = 0.f, old_rstd = 0.f, old_shift = 0.f;
+  // g and h of piece i of the row in `stage`
+  auto read = [&](int stage, int i, float rstd, float shift, float (&g)[8], float (&h)[8]) {
+    pipe.values(stage, 0, i, g);
+    pipe.values(stage, 1, i, h);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = fmaf(h[j], rstd, shift);
+  };
+  auto weigh = [&](int i, float (&g)[8]) {
+    if constexpr (!kWeights) weights(i, gamma[0]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] *= gamma[kWeights ? i : 0][j];
+  };
+  auto results = [&](int k, int stage, int row, float rstd, float shift) {
+    const float2 p = lane < warps ? part[k & 1][pipe.group * warps + lane] : make_float2(0.f, 0.f);
+    // rstd (g - mean(g) - h mean(g h)) = rstd g + (along h + level)
+    const float along = -rstd * (warp_sum(p.y) * share), level = -rstd * (warp_sum(p.x) * share);
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
-      if (pipe.base(i) >= a.cols) break;
-      float g[8], h[8];
-      pipe.values(stage, 0, i, g);
-      pipe.values(stage, 1, i, h);
-      if constexpr (!kWeights) weights(i, gamma[0]);
-      const float(&w)[8] = gamma[kWeights ? i : 0];
+      if (!pipe.on(i)) continue;
+      float g[8], d[8];
+      read(stage, i, rstd, shift, g, d);
+      weigh(i, g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        h[j] = fmaf(h[j], rstd, shift);
-        to_gamma[i][j] = fmaf(g[j], h[j], to_gamma[i][j]), to_beta[i][j] += g[j];
-        g[j] *= w[j];
-        sums.x += g[j], sums.y = fmaf(g[j], h[j], sums.y);
+      for (int j = 0; j < 8; ++j) d[j] = fmaf(g[j], rstd, fmaf(d[j], along, level));
+      if constexpr (kMore) {
+        pipe.values(stage, 2, i, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[j] += g[j];
+      }
+      if (to_residual) store_cols<T, kVec>(dresidual, pipe.base(i), lane, a.cols, d);
+      if (to_x) {
+        drop_cols<kVec>(a.mask, step, (uint32_t)row, pipe.base(i), lane, d);
+        store_cols<T, kVec>(dx, pipe.base(i), lane, a.cols, d);
       }
     }
-    if (a.dresidual || a.dx) {
-      sums = pipe.sum(sums, part[k & 1]);
-      // rstd (g - mean(g) - h mean(g h)) = rstd g + (along h + level)
-      const float along = -rstd * (sums.y * share), level = -rstd * (sums.x * share);
+    if (to_residual) dresidual += dresidual_step;
+    if (to_x) dx += dx_step;
+  };
+#pragma unroll 1
+  for (int k = 0; k < pipe.count + (kLater ? 1 : 0); ++k) {
+    if (!kLater || k < pipe.count) {
+      rstd = next_rstd, shift = -next_mean * next_rstd;
+      if (k + 1 < pipe.count) next_mean = a.mean[row + pipe.step], next_rstd = a.rstd[row + pipe.step];
+      if constexpr (kVec) {
+        if constexpr (!kLater) pipe.fetch();      // into the place of the row before
+        copies_wait<kLater ? Pipe::kStages - 2 : Pipe::kStages - 1>();
+      } else {
+        pipe.land();
+        pipe.fetch();
+      }
+      float sum = 0.f, along = 0.f;
 #pragma unroll
       for (int i = 0; i < kKeep; ++i) {
-        const int base = pipe.base(i);
-        if (base >= a.cols) break;
-        float g[8], d[8];
-        pipe.values(stage, 0, i, g);
-        pipe.values(stage, 1, i, d);
-        if constexpr (!kWeights) weights(i, gamma[0]);
-        const float(&w)[8] = gamma[kWeights ? i : 0];
+        if (!pipe.on(i)) continue;
+        float g[8], h[8];
+        read(stage, i, rstd, shift, g, h);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = fmaf(g[j] * w[j], rstd, fmaf(fmaf(d[j], rstd, shift), along, level));
-        if (a.dtotal) {
-          pipe.values(stage, 2, i, g);
+        for (int j = 0; j < 8; ++j) to_gamma[i][j] = fmaf(g[j], h[j], to_gamma[i][j]), to_beta[i][j] += g[j];
+        weigh(i, g);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) d[j] += g[j];
-        }
-        if (a.dresidual) store_cols<T, kVec>(a.dresidual + row * a.ld_dr, base, lane, a.cols, d);
-        if (a.dx) {
-          drop_cols<kVec>(a.mask, step, (uint32_t)row, base, lane, d);
-          store_cols<T, kVec>(a.dx + row * a.ld_dx, base, lane, a.cols, d);
-        }
+        for (int j = 0; j < 8; ++j) sum += g[j], along = fmaf(g[j], h[j], along);
       }
+      sum = warp_sum(sum), along = warp_sum(along);
+      if (lane == 0) part[k & 1][pipe.group * warps + pipe.in_row] = make_float2(sum, along);
     }
-    if constexpr (kVec) stage = stage + 1 == stages ? 0 : stage + 1;
+    if constexpr (kLater) {
+      if (k > 0) results(k - 1, stage == 0 ? Pipe::kStages - 1 : stage - 1, row - pipe.step, old_rstd, old_shift);
+      old_rstd = rstd, old_shift = shift;
+      pipe.fetch();      // into the place of the row before
+      pipe.meet();
+    } else {
+      pipe.meet();
+      results(k, stage, row, rstd, shift);
+    }
+    row += pipe.step;
+    if constexpr (kVec) stage = stage + 1 == Pipe::kStages ? 0 : stage + 1;
   }
   if (!parts) return;
   // the groups' sums meet in the rows' places
