@@ -108,13 +108,16 @@ bool as_mask(const rtopk_mask* m, Mask* out) {
   return true;
 }
 
+// Rows of whole vectors of eight values.
+bool whole_vectors(const void* p, int elem, int64_t cols, int64_t ld) { return !p || (cols % 8 == 0 && rows_aligned(p, elem, 1, ld, 0, 8 * elem)); }
+
 int check_rows(const rtopk_matrix* ctx, int64_t rows, int64_t cols, int dtype) {
   return !ctx || rows < 0 || cols < 1 || rows > kDimMax || cols > kDimMax || bad_dtype(dtype) ? RTOPK_ERR_INVALID_ARG : RTOPK_OK;
 }
 
 template <class T>
 int dropout(rtopk_matrix* ctx, const T* x, int64_t ld_x, int64_t rows, int64_t cols, const Mask& mask, T* out, int64_t ld_out, cudaStream_t st) {
-  const bool vec = cols % 8 == 0 && rows_aligned(x, sizeof(T), 1, ld_x, 0, 16) && rows_aligned(out, sizeof(T), 1, ld_out, 0, 16);
+  const bool vec = whole_vectors(x, sizeof(T), cols, ld_x) && whole_vectors(out, sizeof(T), cols, ld_out);
   const int64_t units = ceil_div(cols, vec ? 8 : kWarpCols), per = vec ? 256 : 8;      // of four rows: threads or warps; of a block
   const int64_t band = std::min(up(rows, 4), ((int64_t(1) << 31) / units - 256) / 4 * 4);      // rows whose units 31 bits count
   if (ceil_div(rows, band) > 65535) return RTOPK_ERR_UNSUPPORTED;
@@ -132,28 +135,39 @@ constexpr int kRowBlocks = 160;
 struct RowSplit {
   int warps, rows_per, keep;
   int64_t blocks;
-  bool fits;
+  bool fits, full;
   RowSplit(int sms, int64_t rows, int64_t cols, int most, bool vec) {      // most: pieces a warp, at most
     const int64_t pieces = ceil_div(cols, kWarpCols);
     fits = pieces <= kRowWarps * (vec ? most : 2);
     if (!fits) return;
     keep = pieces > 2 * kRowWarps ? 4 : pieces > kRowWarps || rows * pieces > sms * kRowWarps ? 2 : 1;
     warps = (int)ceil_div(pieces, keep);
+    full = vec && cols == (int64_t)warps * keep * kWarpCols;
     rows_per = (int)std::min<int64_t>(kRowWarps / warps, ceil_div(rows, sms));
     blocks = std::min<int64_t>(std::min(sms, kRowBlocks), ceil_div(rows, rows_per));
   }
 };
 
-template <class T, bool kVec, int kKeep, bool kResidual>
-int norm_rows(rtopk_matrix* ctx, const NormArgs<T>& a, const RowSplit& f, cudaStream_t st) {
-  return launch(ctx, k_layer_norm_rows<T, kVec, kKeep, kResidual>, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, RowShape<T, kVec, kKeep, kResidual ? 2 : 1>::kSmem, st, a, f.warps,
-                f.rows_per);
+// Calls go(kVec, kFull, kKeep) with constants.
+template <class T, int kMost, class F>
+int row_variant(const RowSplit& f, bool vec, F go) {
+  using yes = std::true_type;
+  using no = std::false_type;
+  auto with = [&](auto keep) { return f.full ? go(yes{}, yes{}, keep) : vec ? go(yes{}, no{}, keep) : go(no{}, no{}, keep); };
+  if (f.keep == 1) return with(std::integral_constant<int, 1>{});
+  if (f.keep == 2) return with(std::integral_constant<int, 2>{});
+  if constexpr (kMost == 4) {
+    const std::integral_constant<int, 4> keep;
+    return f.full ? go(yes{}, yes{}, keep) : go(yes{}, no{}, keep);
+  }
+  return RTOPK_ERR_INTERNAL;
 }
 template <class T, bool kResidual>
 int norm_rows(rtopk_matrix* ctx, const NormArgs<T>& a, const RowSplit& f, bool vec, cudaStream_t st) {
-  if (f.keep == 4) return norm_rows<T, true, 4, kResidual>(ctx, a, f, st);
-  if (f.keep == 2) return vec ? norm_rows<T, true, 2, kResidual>(ctx, a, f, st) : norm_rows<T, false, 2, kResidual>(ctx, a, f, st);
-  return vec ? norm_rows<T, true, 1, kResidual>(ctx, a, f, st) : norm_rows<T, false, 1, kResidual>(ctx, a, f, st);
+  return row_variant<T, 4>(f, vec, [&](auto v, auto full, auto keep) {
+    return launch(ctx, k_layer_norm_rows<T, v, full, keep, kResidual>, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, RowShape<T, v, keep, kResidual ? 2 : 1>::kSmem, st, a, f.warps,
+                  f.rows_per);
+  });
 }
 template <class T>
 int layer_norm(rtopk_matrix* ctx, const NormArgs<T>& a, bool vec, cudaStream_t st) {
@@ -165,30 +179,31 @@ int layer_norm(rtopk_matrix* ctx, const NormArgs<T>& a, bool vec, cudaStream_t s
 // The columns' sums of a block's groups meet in its shared memory.
 template <class T, bool kVec, int kKeep, bool kMore>
 constexpr int kBackSmem = std::max(RowShape<T, kVec, kKeep, kMore ? 3 : 2>::kSmem, 2 * kRowWarps * kWarpCols * kKeep * 4);
-template <class T, bool kVec, int kKeep, bool kMore>
-int back_rows(rtopk_matrix* ctx, const NormBackArgs<T>& a, const RowSplit& f, float* parts, cudaStream_t st) {
-  return launch(ctx, k_layer_norm_back_rows<T, kVec, kKeep, kMore>, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, kBackSmem<T, kVec, kKeep, kMore>, st, a, f.warps, f.rows_per, parts);
-}
+template <class T>
+constexpr int kBackMost = sizeof(T) == 2 ? 4 : 2;      // pieces a warp
 template <class T, bool kMore>
 int back_rows(rtopk_matrix* ctx, const NormBackArgs<T>& a, const RowSplit& f, bool vec, float* parts, cudaStream_t st) {
-  if constexpr (sizeof(T) == 2)
-    if (f.keep == 4) return back_rows<T, true, 4, kMore>(ctx, a, f, parts, st);
-  if (f.keep == 2) return vec ? back_rows<T, true, 2, kMore>(ctx, a, f, parts, st) : back_rows<T, false, 2, kMore>(ctx, a, f, parts, st);
-  return vec ? back_rows<T, true, 1, kMore>(ctx, a, f, parts, st) : back_rows<T, false, 1, kMore>(ctx, a, f, parts, st);
+  return row_variant<T, kBackMost<T>>(f, vec, [&](auto v, auto full, auto keep) {
+    return launch(ctx, k_layer_norm_back_rows<T, v, full, keep, kMore>, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, kBackSmem<T, v, keep, kMore>, st, a, f.warps, f.rows_per, parts);
+  });
 }
 
-template <class T, bool kVec, int kKeep, bool kResidual>
+template <class T, bool kSecond>
 cudaError_t allow_rows() {
-  const cudaError_t e = cudaFuncSetAttribute(k_layer_norm_rows<T, kVec, kKeep, kResidual>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem);
-  if constexpr (sizeof(T) == 4 && kKeep == 4) return e;
-  else return e != cudaSuccess ? e : cudaFuncSetAttribute(k_layer_norm_back_rows<T, kVec, kKeep, kResidual>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem);
-}
-template <class T>
-cudaError_t allow_rows() {
-  for (const cudaError_t e : {allow_rows<T, true, 1, false>(), allow_rows<T, true, 1, true>(), allow_rows<T, true, 2, false>(), allow_rows<T, true, 2, true>(), allow_rows<T, true, 4, false>(),
-                              allow_rows<T, true, 4, true>(), allow_rows<T, false, 1, false>(), allow_rows<T, false, 1, true>(), allow_rows<T, false, 2, false>(), allow_rows<T, false, 2, true>()})
-    if (e != cudaSuccess) return e;
-  return cudaSuccess;
+  cudaError_t worst = cudaSuccess;
+  auto allow = [&](auto kernel) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem);
+    if (e != cudaSuccess) worst = e;
+  };
+  for (const int keep : {1, 2, 4})
+    for (const int kind : {0, 1, 2}) {
+      RowSplit f(1, 1, 1, 4, true);
+      f.keep = keep, f.full = kind == 2;
+      if (keep == 4 && kind == 0) continue;
+      row_variant<T, 4>(f, kind > 0, [&](auto v, auto full, auto k) { return allow(k_layer_norm_rows<T, v, full, k, kSecond>), 0; });
+      if (keep <= kBackMost<T>) row_variant<T, kBackMost<T>>(f, kind > 0, [&](auto v, auto full, auto k) { return allow(k_layer_norm_back_rows<T, v, full, k, kSecond>), 0; });
+    }
+  return worst;
 }
 
 // Ranges of rows whose column sums are formed apart: four blocks for each of 148 SMs, but no fewer than 32 rows each.
@@ -204,7 +219,7 @@ int layer_norm_gradients(rtopk_matrix* ctx, const NormBackArgs<T>& a, float* dga
   Carve c{ctx->scratch};
   float* parts = dgamma || dbeta ? NormScratch(c, a.rows, a.cols).parts : nullptr;
   auto join = [&](int64_t count) { return launch(ctx, k_norm_join, dim3((unsigned)ceil_div(2 * (int64_t)a.cols, 32)), 256, 0, st, parts, count, a.cols, dgamma, dbeta); };
-  const RowSplit f(ctx->sms, a.rows, a.cols, sizeof(T) == 2 ? 4 : 2, vec);
+  const RowSplit f(ctx->sms, a.rows, a.cols, kBackMost<T>, vec);
   if (f.fits) {
     MAT_TRY((a.dtotal ? back_rows<T, true>(ctx, a, f, vec, parts, st) : back_rows<T, false>(ctx, a, f, vec, parts, st)));
     return parts ? join(f.blocks) : RTOPK_OK;
@@ -223,7 +238,7 @@ int layer_norm_gradients(rtopk_matrix* ctx, const NormBackArgs<T>& a, float* dga
 }  // namespace
 
 cudaError_t rtopk::mat::allow_layers() {
-  for (const cudaError_t e : {allow_smem<EPI_MICRO>(), allow_rows<float>(), allow_rows<__nv_bfloat16>()})
+  for (const cudaError_t e : {allow_smem<EPI_MICRO>(), allow_rows<float, false>(), allow_rows<float, true>(), allow_rows<__nv_bfloat16, false>(), allow_rows<__nv_bfloat16, true>()})
     if (e != cudaSuccess) return e;
   return cudaSuccess;
 }
@@ -325,8 +340,8 @@ int rtopk_layer_norm(rtopk_matrix* ctx, const void* x, int64_t ld_x, const void*
     return RTOPK_ERR_INVALID_ARG;
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
-  const bool vec = cols % 8 == 0 && rows_aligned(x, e, 1, ld_x, 0, 16) && rows_aligned(out, e, 1, ld_out, 0, 16) && (!residual || rows_aligned(residual, e, 1, ld_r, 0, 16)) &&
-                   (!total || rows_aligned(total, e, 1, ld_t, 0, 16)) && aligned_to(gamma, 16) && aligned_to(beta, 16);
+  auto whole = [&](const void* p, int64_t ld) { return whole_vectors(p, e, cols, ld); };
+  const bool vec = whole(x, ld_x) && whole(out, ld_out) && whole(residual, ld_r) && whole(total, ld_t) && aligned_to(gamma, 32) && aligned_to(beta, 32);
   auto go = [&](auto t) {
     using T = decltype(t);
     const NormArgs<T> a = {(const T*)x, (const T*)residual, (T*)out, (T*)total, ld_x, ld_r, ld_out, ld_t, gamma, beta, mean, rstd, (int)rows, (int)cols, eps, m};
@@ -365,8 +380,8 @@ int rtopk_layer_norm_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy,
     if (dbeta) MAT_CUDA(cudaMemsetAsync(dbeta, 0, cols * sizeof(float), st));
     return RTOPK_OK;
   }
-  auto aligned = [&](const void* p, int64_t ld) { return !p || rows_aligned(p, e, 1, ld, 0, 16); };
-  const bool vec = cols % 8 == 0 && aligned(dy, ld_dy) && aligned(total, ld_t) && aligned(dtotal, ld_dt) && aligned(dresidual, ld_dr) && aligned(dx, ld_dx) && aligned_to(gamma, 16);
+  auto whole = [&](const void* p, int64_t ld) { return whole_vectors(p, e, cols, ld); };
+  const bool vec = whole(dy, ld_dy) && whole(total, ld_t) && whole(dtotal, ld_dt) && whole(dresidual, ld_dr) && whole(dx, ld_dx) && aligned_to(gamma, 32);
   auto go = [&](auto t) {
     using T = decltype(t);
     const NormBackArgs<T> a = {(const T*)dy, (const T*)total, (const T*)dtotal, (T*)dresidual, (T*)dx, ld_dy, ld_t, ld_dt, ld_dr, ld_dx, gamma, mean, rstd, (int)rows, (int)cols, m};

@@ -58,10 +58,19 @@ __device__ __forceinline__ int col_of(int base, int lane, int j) { return kVec ?
 template <bool kVec>
 __device__ __forceinline__ bool has_cols(int base, int lane, int cols) { return kVec ? base + lane * 8 < cols : base < cols; }
 
+// 32 bytes at once, so that a sector is asked for and written in one piece.
+__device__ __forceinline__ void load_vector(const float* p, Eight<float>& e) {
+  asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(e.a.x), "=f"(e.a.y), "=f"(e.a.z), "=f"(e.a.w), "=f"(e.b.x), "=f"(e.b.y), "=f"(e.b.z), "=f"(e.b.w)
+               : "l"(p)
+               : "memory");
+}
+__device__ __forceinline__ void load_vector(const __nv_bfloat16* p, Eight<__nv_bfloat16>& e) { e.load(p, 8, true); }
+
 template <class T, bool kVec>
 __device__ __forceinline__ void load_cols(const T* row, int base, int lane, int cols, Eight<T>& e) {
   if constexpr (kVec) {
-    if (has_cols<true>(base, lane, cols)) e.load(row + base + lane * 8, 8, true);
+    if (has_cols<true>(base, lane, cols)) load_vector(row + base + lane * 8, e);
   } else if constexpr (sizeof(T) == 4) {
     float v[8];
 #pragma unroll
@@ -83,8 +92,8 @@ __device__ __forceinline__ void load_cols(const float* row, int base, int lane, 
   e.widen_to(v);
 }
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-  ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  ((float4*)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
 }
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
   __nv_bfloat162 q[4];
@@ -198,8 +207,12 @@ struct NormArgs {
 constexpr int kRowWarps = 16, kRowSmem = 216 * 1024;
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// For the warp's copies but the last kLeft groups of each thread.
 template <int kLeft>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+  __syncwarp();
+}
 
 template <class T, bool kVec, int kKeep, int kArrays>
 struct RowShape {
@@ -210,7 +223,9 @@ struct RowShape {
   static constexpr int kSmem = kStages * kStage;
 };
 
-template <class T, bool kVec, int kKeep, int kArrays>
+// kFull (with kVec): the row is just what its warps hold, so that every thread has all of its columns and a row's work is one run of code
+// without branches.
+template <class T, bool kVec, bool kFull, int kKeep, int kArrays>
 struct RowPipe : RowShape<T, kVec, kKeep, kArrays> {
   using S = RowShape<T, kVec, kKeep, kArrays>;
   using S::kPlanes;
@@ -237,17 +252,20 @@ struct RowPipe : RowShape<T, kVec, kKeep, kArrays> {
     fetched = to = 0;
   }
   __device__ __forceinline__ int base(int i) const { return (i * warps + in_row) * kWarpCols; }
-  __device__ __forceinline__ bool on(int i) const { return has_cols<kVec>(base(i), lane, cols); }
+  __device__ __forceinline__ bool on(int i) const { return kFull || has_cols<kVec>(base(i), lane, cols); }
   __device__ __forceinline__ char* place(int stage, int q, int i) const { return mine + stage * kStage + (q * kKeep + i) * kPlanes * kPlane; }
-  __device__ __forceinline__ void source(Source& s, const T* p, int64_t ld) { s.p = p + first * ld + (kVec ? base(0) + lane * 8 : 0), s.step = ld * step; }
+  __device__ __forceinline__ void source(Source& s, const T* p, int64_t ld) { s.p = p + first * ld + (kVec ? base(0) : 0), s.step = ld * step; }
   __device__ __forceinline__ void fetch(Source& s, int q) {
-    const uint32_t dst = smem_addr(place(to, q, 0));
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
       if constexpr (kVec) {
-        if (on(i))
+        // Neighbouring lanes copy neighbouring pieces of 16 bytes; of binary32 values that is not the thread's own, but its warp's.
 #pragma unroll
-          for (int r = 0; r < kPlanes; ++r) copy16(dst + (i * kPlanes + r) * kPlane, (const char*)(s.p + i * warps * kWarpCols) + 16 * r);
+        for (int r = 0; r < kPlanes; ++r) {
+          const int piece = r * 32 + lane, owner = piece / kPlanes;
+          if (kFull || base(i) + owner * 8 < cols)
+            copy16(smem_addr(place(to, q, i)) + (owner - lane) * 16 + (piece % kPlanes) * kPlane, (const char*)(s.p + i * warps * kWarpCols) + 16 * piece);
+        }
       } else {
         load_cols<T, false>(s.p, base(i), lane, cols, s.next[i]);
       }
@@ -255,6 +273,7 @@ struct RowPipe : RowShape<T, kVec, kKeep, kArrays> {
     s.p += s.step;
   }
   __device__ __forceinline__ void fetch() {
+    if constexpr (kVec && kPlanes > 1) __syncwarp();      // the place has been read by all of the warp
     if (fetched < count) {
       fetch(s0, 0);
       if (kArrays > 1) fetch(s1, 1);
@@ -299,9 +318,9 @@ struct RowPipe : RowShape<T, kVec, kKeep, kArrays> {
 
 // The mean and the sum of squares around it meet in one exchange: a warp sums its columns, then their squares around its own mean, and of
 // n columns with sum s and squares q the row takes q + n (s / n - mean)^2 (Chan, Golub and LeVeque, 1979).
-template <class T, bool kVec, int kKeep, bool kResidual>
+template <class T, bool kVec, bool kFull, int kKeep, bool kResidual>
 __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __grid_constant__ NormArgs<T> a, int warps, int rows_per) {
-  using Pipe = RowPipe<T, kVec, kKeep, kResidual ? 2 : 1>;
+  using Pipe = RowPipe<T, kVec, kFull, kKeep, kResidual ? 2 : 1>;
   extern __shared__ __align__(16) char norm_smem[];
   __shared__ float2 part[2][kRowWarps];
   Pipe pipe(norm_smem, warps, rows_per, a.rows, a.cols);
@@ -340,73 +359,80 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __g
   const int64_t y_step = pipe.step * a.ld_y, total_step = pipe.step * a.ld_t;
   float v[kKeep][8], before[kKeep][8];
   int row = pipe.first, stage = 0;
-#pragma unroll 1
-  for (int k = 0; k <= pipe.count; ++k) {
-    if (k < pipe.count) {
-      if constexpr (kVec) copies_wait<Pipe::kStages - 1>();
-      else pipe.land();
-      float sum = 0.f;
+  auto sums = [&](int k) {      // of row k, whose values come to v
+    if constexpr (kVec) copies_wait<Pipe::kStages - 1>();
+    else pipe.land();
+    float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < kKeep; ++i) {
-        if (!pipe.on(i)) continue;
-        pipe.values(stage, 0, i, v[i]);
-        if (masked) drop_cols<kVec>(a.mask, step, (uint32_t)row, pipe.base(i), lane, v[i]);
-        if constexpr (kResidual) {
-          float r[8];
-          pipe.values(stage, 1, i, r);
+    for (int i = 0; i < kKeep; ++i) {
+      if (!pipe.on(i)) continue;
+      pipe.values(stage, 0, i, v[i]);
+      if (masked) drop_cols<kVec>(a.mask, step, (uint32_t)row, pipe.base(i), lane, v[i]);
+      if constexpr (kResidual) {
+        float r[8];
+        pipe.values(stage, 1, i, r);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[i][j] += r[j];
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += v[i][j];
-        if (to_total) store_cols<T, kVec>(total, pipe.base(i), lane, a.cols, v[i]);
+        for (int j = 0; j < 8; ++j) v[i][j] += r[j];
       }
-      if (to_total) total += total_step;
-      pipe.fetch();      // into the place of the row just read
-      if constexpr (kVec) stage = stage + 1 == Pipe::kStages ? 0 : stage + 1;
-      sum = warp_sum(sum);
-      const float own = sum * share_own;
-      float squares = 0.f;
-#pragma unroll
-      for (int i = 0; i < kKeep; ++i) {
-        if (!pipe.on(i)) continue;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float d = v[i][j] - own;
-          if (kVec || col_of<kVec>(pipe.base(i), lane, j) < a.cols) squares = fmaf(d, d, squares);
-        }
-      }
-      squares = warp_sum(squares);
-      if (lane == 0) part[k & 1][pipe.group * warps + pipe.in_row] = make_float2(sum, squares);
+      sum += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
+      if (to_total) store_cols<T, kVec>(total, pipe.base(i), lane, a.cols, v[i]);
     }
-    if (k > 0) {      // the row before
-      const int at = row - pipe.step;
-      const float2 p = lane < warps ? part[(k - 1) & 1][pipe.group * warps + lane] : make_float2(0.f, 0.f);
-      const float mean = warp_sum(p.x) * share, off = p.x * share_lane - mean;
-      const float rstd = inverse_root(warp_sum(fmaf(n_lane * off, off, p.y)) * share + a.eps);
-      if (pipe.in_row == 0 && lane == 0) {
-        if (a.mean) a.mean[at] = mean;
-        if (a.rstd) a.rstd[at] = rstd;
-      }
+    total += total_step;
+    pipe.fetch();      // into the place of the row just read
+    if constexpr (kVec) stage = stage + 1 == Pipe::kStages ? 0 : stage + 1;
+    sum = warp_sum(sum);
+    const float own = sum * share_own;
+    float squares[2] = {0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < kKeep; ++i) {
-        if (!pipe.on(i)) continue;
-        if constexpr (!kWeights) weights(i, gamma[0], beta[0]);
-        const float(&g)[8] = gamma[kWeights ? i : 0], (&b)[8] = beta[kWeights ? i : 0];
-        float out[8];
+    for (int i = 0; i < kKeep; ++i) {
+      if (!pipe.on(i)) continue;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) out[j] = fmaf((before[i][j] - mean) * rstd, g[j], b[j]);
-        store_cols<T, kVec>(y, pipe.base(i), lane, a.cols, out);
+      for (int j = 0; j < 8; ++j) {
+        const float d = v[i][j] - own;
+        if (kVec || col_of<kVec>(pipe.base(i), lane, j) < a.cols) squares[j & 1] = fmaf(d, d, squares[j & 1]);
       }
-      y += y_step;
     }
+    const float all = warp_sum(squares[0] + squares[1]);
+    if (lane == 0) part[k & 1][pipe.group * warps + pipe.in_row] = make_float2(sum, all);
+  };
+  auto results = [&](int k, int row) {      // of row k, from `before`
+    const float2 p = lane < warps ? part[k & 1][pipe.group * warps + lane] : make_float2(0.f, 0.f);
+    const float mean = warp_sum(p.x) * share, off = p.x * share_lane - mean;
+    const float rstd = inverse_root(warp_sum(fmaf(n_lane * off, off, p.y)) * share + a.eps);
+    if (pipe.in_row == 0 && lane == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) {
+      if (!pipe.on(i)) continue;
+      if constexpr (!kWeights) weights(i, gamma[0], beta[0]);
+      const float(&g)[8] = gamma[kWeights ? i : 0], (&b)[8] = beta[kWeights ? i : 0];
+      float out[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) out[j] = fmaf((before[i][j] - mean) * rstd, g[j], b[j]);
+      store_cols<T, kVec>(y, pipe.base(i), lane, a.cols, out);
+    }
+    y += y_step;
+  };
+  if (!pipe.count) return;
+  auto next = [&]() {
 #pragma unroll
     for (int i = 0; i < kKeep; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) before[i][j] = v[i][j];
     row += pipe.step;
     pipe.meet();
+  };
+  sums(0);
+  next();
+#pragma unroll 1
+  for (int k = 1; k < pipe.count; ++k) {
+    sums(k);
+    results(k - 1, row - pipe.step);
+    next();
   }
+  results(pipe.count - 1, row - pipe.step);
 }
 
 // Longer rows: a block takes one, each warp kLongKeep pieces of 256 columns in its registers; what is beyond is read again.
@@ -612,9 +638,9 @@ __global__ void __launch_bounds__(32 * kRowWarps) k_layer_norm_back_long(const _
 
 // The gradients of rows that fit the block.  A thread has the same columns of every row, so dgamma's and dbeta's sums stay in its
 // registers; it reads a row in shared memory twice, for the row's two sums, then for the results.
-template <class T, bool kVec, int kKeep, bool kMore>
+template <class T, bool kVec, bool kFull, int kKeep, bool kMore>
 __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_back_rows(const __grid_constant__ NormBackArgs<T> a, int warps, int rows_per, float* parts) {
-  using Pipe = RowPipe<T, kVec, kKeep, kMore ? 3 : 2>;
+  using Pipe = RowPipe<T, kVec, kFull, kKeep, kMore ? 3 : 2>;
   // With three stages a row's results wait until the next row's sums are on their way; with fewer its place is needed before.
   constexpr bool kLater = Pipe::kStages > 2;
   extern __shared__ __align__(16) char norm_smem[];
@@ -686,64 +712,81 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_back_rows(cons
     if (to_residual) dresidual += dresidual_step;
     if (to_x) dx += dx_step;
   };
-#pragma unroll 1
-  for (int k = 0; k < pipe.count + (kLater ? 1 : 0); ++k) {
-    if (!kLater || k < pipe.count) {
-      rstd = next_rstd, shift = -next_mean * next_rstd;
-      if (k + 1 < pipe.count) next_mean = a.mean[row + pipe.step], next_rstd = a.rstd[row + pipe.step];
-      if constexpr (kVec) {
-        if constexpr (!kLater) pipe.fetch();      // into the place of the row before
-        copies_wait<kLater ? Pipe::kStages - 2 : Pipe::kStages - 1>();
-      } else {
-        pipe.land();
-        pipe.fetch();
-      }
-      float sum = 0.f, along = 0.f;
-#pragma unroll
-      for (int i = 0; i < kKeep; ++i) {
-        if (!pipe.on(i)) continue;
-        float g[8], h[8];
-        read(stage, i, rstd, shift, g, h);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) to_gamma[i][j] = fmaf(g[j], h[j], to_gamma[i][j]), to_beta[i][j] += g[j];
-        weigh(i, g);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += g[j], along = fmaf(g[j], h[j], along);
-      }
-      sum = warp_sum(sum), along = warp_sum(along);
-      if (lane == 0) part[k & 1][pipe.group * warps + pipe.in_row] = make_float2(sum, along);
-    }
-    if constexpr (kLater) {
-      if (k > 0) results(k - 1, stage == 0 ? Pipe::kStages - 1 : stage - 1, row - pipe.step, old_rstd, old_shift);
-      old_rstd = rstd, old_shift = shift;
-      pipe.fetch();      // into the place of the row before
-      pipe.meet();
+  auto sums = [&](int k) {
+    rstd = next_rstd, shift = -next_mean * next_rstd;
+    if (k + 1 < pipe.count) next_mean = a.mean[row + pipe.step], next_rstd = a.rstd[row + pipe.step];
+    if constexpr (kVec) {
+      if constexpr (!kLater) pipe.fetch();      // into the place of the row before
+      copies_wait<kLater ? Pipe::kStages - 2 : Pipe::kStages - 1>();
     } else {
-      pipe.meet();
-      results(k, stage, row, rstd, shift);
+      pipe.land();
+      pipe.fetch();
     }
+    float sum[2] = {0.f, 0.f}, along[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) {
+      if (!pipe.on(i)) continue;
+      float g[8], h[8];
+      read(stage, i, rstd, shift, g, h);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) to_gamma[i][j] = fmaf(g[j], h[j], to_gamma[i][j]), to_beta[i][j] += g[j];
+      weigh(i, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j & 1] += g[j], along[j & 1] = fmaf(g[j], h[j], along[j & 1]);
+    }
+    const float2 all = make_float2(warp_sum(sum[0] + sum[1]), warp_sum(along[0] + along[1]));
+    if (lane == 0) part[k & 1][pipe.group * warps + pipe.in_row] = all;
+  };
+  auto next = [&]() {
     row += pipe.step;
     if constexpr (kVec) stage = stage + 1 == Pipe::kStages ? 0 : stage + 1;
+  };
+  if constexpr (kLater) {
+    if (pipe.count) {
+      sums(0);
+      old_rstd = rstd, old_shift = shift;
+      pipe.fetch();
+      pipe.meet();
+      next();
+#pragma unroll 1
+      for (int k = 1; k < pipe.count; ++k) {
+        sums(k);
+        results(k - 1, stage == 0 ? Pipe::kStages - 1 : stage - 1, row - pipe.step, old_rstd, old_shift);
+        old_rstd = rstd, old_shift = shift;
+        pipe.fetch();      // into the place of the row before
+        pipe.meet();
+        next();
+      }
+      results(pipe.count - 1, stage == 0 ? Pipe::kStages - 1 : stage - 1, row - pipe.step, old_rstd, old_shift);
+    }
+  } else {
+#pragma unroll 1
+    for (int k = 0; k < pipe.count; ++k) {
+      sums(k);
+      pipe.meet();
+      results(k, stage, row, rstd, shift);
+      next();
+    }
   }
   if (!parts) return;
   // the groups' sums meet in the rows' places
   if constexpr (kVec) asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
-  float* sums = (float*)norm_smem;
+  float* met = (float*)norm_smem;
   const int width = warps * kWarpCols * kKeep;
 #pragma unroll
   for (int i = 0; i < kKeep; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int c = col_of<kVec>(pipe.base(i), lane, j);
-      sums[(pipe.group * 2) * width + c] = to_gamma[i][j];
-      sums[(pipe.group * 2 + 1) * width + c] = to_beta[i][j];
+      met[(pipe.group * 2) * width + c] = to_gamma[i][j];
+      met[(pipe.group * 2 + 1) * width + c] = to_beta[i][j];
     }
   __syncthreads();
   for (int k = 0; k < 2; ++k)
     for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
       float v = 0.f;
-      for (int r = 0; r < rows_per; ++r) v += sums[(r * 2 + k) * width + c];
+      for (int r = 0; r < rows_per; ++r) v += met[(r * 2 + k) * width + c];
       parts[((int64_t)blockIdx.x * 2 + k) * a.cols + c] = v;
     }
 }
