@@ -52,8 +52,10 @@ enum Epi : int {
   EPI_OUT = 3,     // the last X, into the caller's matrix
   EPI_UPDATE = 4,  // the last X, into the caller's weights
   EPI_CODED = 5,   // 8-bit codes: times the two scales
-  EPI_MICRO = 6    // 4-bit codes with a power of two for every 32 along the contraction, which the tensor core multiplies in
+  EPI_MICRO = 6,   // 4-bit codes with a power of two for every 32 along the contraction, which the tensor core multiplies in
+  EPI_MICRO_ROWS = 7      // the same, a lane's columns being neighbours in the result's rows, which start on multiples of 32 bytes
 };
+__host__ __device__ constexpr bool is_micro(int epi) { return epi == EPI_MICRO || epi == EPI_MICRO_ROWS; }
 
 struct Gemm {
   int lanes, cols, depth;    // D is lanes x cols; depth in elements
@@ -165,6 +167,12 @@ __device__ __forceinline__ void store_strip(T* p, int n, int64_t step, F value) 
   }
 }
 
+// 32 bytes, on a multiple of 32.
+__device__ __forceinline__ void store_sector(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+
 // What the results of 32 columns need beside the products.  Read ahead: for a tile's first columns while its products are
 // still being formed, then for the next columns while the present ones are finished.
 template <int kEpi>
@@ -184,7 +192,7 @@ __device__ __forceinline__ void read_ahead(const Gemm& g, int z, int lane, int c
     load_strip<kFull>((const float*)g.x + z * g.stride + col0 * g.ld + safe, n, g.ld, ahead.at);
   }
   if constexpr (kEpi == EPI_CODED) ahead.col = g.scale_col[my_col];
-  else if constexpr (kEpi != EPI_GRAM && kEpi != EPI_MICRO) ahead.col = g.d_in[z * g.d_stride + my_col];
+  else if constexpr (kEpi != EPI_GRAM && !is_micro(kEpi)) ahead.col = g.d_in[z * g.d_stride + my_col];
 }
 
 // 32 columns (col0 ..) of lane `lane` of one tile; all 32 threads of the warp come here, each with its lane.  kFull: the
@@ -194,8 +202,8 @@ template <int kEpi, bool kFull>
 __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col0, int n, float of_lane, float* cols, const Ahead<kEpi>& ahead, const uint32_t (&acc)[32]) {
   const int me = threadIdx.x & 31;
   bool in = kFull || lane < g.lanes;
-  float of_col[kEpi == EPI_GRAM || kEpi == EPI_MICRO ? 1 : 32];      // every column's number in every thread: by way of the warp's place in shared memory
-  if constexpr (kEpi != EPI_GRAM && kEpi != EPI_MICRO) {
+  float of_col[kEpi == EPI_GRAM || is_micro(kEpi) ? 1 : 32];      // every column's number in every thread: by way of the warp's place in shared memory
+  if constexpr (kEpi != EPI_GRAM && !is_micro(kEpi)) {
     cols[me] = ahead.col;
     __syncwarp();
 #pragma unroll
@@ -234,6 +242,31 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int z, int lane, int col
     for (int c = 0; c < 32; c += 8)
       if (kFull || c < n) store_half8(row + c, v + c);
     if (cb > lb) store_strip<kFull>(g.h + z * g.stride + col0 * g.ld + lane, n, g.ld, [&](int c) { return to_half(v[c]); });
+  } else if constexpr (kEpi == EPI_MICRO_ROWS) {
+    if (!in) return;
+    const int64_t at = lane * g.out_lane + col0;
+    if (kFull || n == 32) {      // a thread writes whole sectors: 16 times fewer stores than along the lanes
+      if (g.out_bf16) {
+        uint32_t w[16];
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+          const __nv_bfloat162 two = __floats2bfloat162_rn(__uint_as_float(acc[2 * c]), __uint_as_float(acc[2 * c + 1]));
+          w[c] = *(const uint32_t*)&two;
+        }
+#pragma unroll
+        for (int c = 0; c < 16; c += 8) store_sector((__nv_bfloat16*)g.out + at + 2 * c, w + c);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 32; c += 8) store_sector((float*)g.out + at + c, acc + c);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < 32; ++c)
+        if (c < n) {
+          if (g.out_bf16) ((__nv_bfloat16*)g.out)[at + c] = __float2bfloat16_rn(__uint_as_float(acc[c]));
+          else ((float*)g.out)[at + c] = __uint_as_float(acc[c]);
+        }
+    }
   } else if constexpr (kEpi == EPI_CODED || kEpi == EPI_MICRO) {
 #pragma unroll
     for (int c = 0; c < 32; ++c) {
@@ -316,15 +349,15 @@ struct GemmShape {
 };
 
 // The scales' maps, for products that have them: words of 32 bits, [128 rows][step of the contraction index][256].
+struct NoScales {};
+struct ScaleMaps { CUtensorMap p, q; };
 template <int kEpi>
-struct Scales {};
-template <>
-struct Scales<EPI_MICRO> { CUtensorMap p, q; };
+using Scales = typename std::conditional<is_micro(kEpi), ScaleMaps, NoScales>::type;
 
 template <int kCols, bool kPair, int kEpi>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 k_gemm(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ Scales<kEpi> scales, const __grid_constant__ Gemm g) {
-  constexpr bool kInt8 = kEpi == EPI_CODED, kMicro = kEpi == EPI_MICRO;
+  constexpr bool kInt8 = kEpi == EPI_CODED, kMicro = is_micro(kEpi);
   using S = GemmShape<kCols, kPair, kMicro>;
   constexpr bool kMnMajor = kEpi == EPI_APPLY || kEpi == EPI_OUT || kEpi == EPI_UPDATE;   // P is stored with its lanes contiguous
   constexpr int kStages = S::kStages;

@@ -40,15 +40,26 @@ int micro_code(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_
                 by_col);
 }
 
-// lanes, cols: the rows of the two code arrays; depth: codes along the contraction
-int micro_gemm(rtopk_matrix* ctx, bool lanes_early, bool free_start, const MicroOut& lane, int64_t lanes, const MicroOut& col, int64_t cols, int64_t depth, void* out, int bf16,
-               int64_t ld_out, cudaStream_t st) {
+// out[r][c] = sum over the contraction of row r of `rows` and row c of `cols`.  Results whose rows start on multiples of 32 bytes are written
+// along the rows by threads that have a row each, where there are rows enough to fill tiles of 128; else along the lanes, which
+// are the result's columns then.  early: `cols` is older than the launch before.
+int micro_gemm(rtopk_matrix* ctx, bool early, bool free_start, const MicroOut& row, int64_t rows, const MicroOut& col, int64_t cols, int64_t depth, void* out, int bf16, int64_t ld_out,
+               cudaStream_t st) {
   Gemm g = {};
   const int64_t bytes = ceil_div(depth, 2);
-  g.lanes = (int)lanes, g.cols = (int)cols, g.depth = (int)bytes, g.batch = 1;
-  g.out = out, g.out_bf16 = bf16, g.out_col = ld_out, g.out_lane = 1;
-  g.p_early = lanes_early, g.free_start = free_start;
-  return gemm<EPI_MICRO>(ctx, {lane.codes, bytes, lanes, lane.ld, 0, lane.scales}, {col.codes, bytes, cols, col.ld, 0, col.scales}, g, st);
+  g.depth = (int)bytes, g.batch = 1;
+  g.out = out, g.out_bf16 = bf16;
+  g.free_start = free_start;
+  const Operand r = {row.codes, bytes, rows, row.ld, 0, row.scales}, c = {col.codes, bytes, cols, col.ld, 0, col.scales};
+  if (rows > 64 && rows_aligned(out, bf16 ? 2 : 4, 1, ld_out, 0, 32)) {
+    g.lanes = (int)rows, g.cols = (int)cols;
+    g.out_col = 1, g.out_lane = ld_out;
+    return gemm<EPI_MICRO_ROWS>(ctx, r, c, g, st);
+  }
+  g.lanes = (int)cols, g.cols = (int)rows;
+  g.out_col = ld_out, g.out_lane = 1;
+  g.p_early = early;
+  return gemm<EPI_MICRO>(ctx, c, r, g, st);
 }
 
 bool bad_micro(const void* codes, int64_t ld, const void* scales, int64_t cols) {
@@ -75,7 +86,7 @@ int micro_product(rtopk_matrix* ctx, const T* x, int64_t ld_x, const MicroOut& w
   Carve c{ctx->scratch};
   MicroScratch s(c, tokens, n_out, n_in);
   MAT_TRY((micro_code<T, true, false, false>(ctx, x, ld_x, tokens, n_in, s.x_rows, s.x_rows, st)));
-  return micro_gemm(ctx, true, false, w, n_out, s.x_rows, tokens, n_in, out, sizeof(T) == 2, ld_out, st);
+  return micro_gemm(ctx, true, false, s.x_rows, tokens, w, n_out, n_in, out, sizeof(T) == 2, ld_out, st);
 }
 
 template <class T>
@@ -87,9 +98,9 @@ int micro_gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, i
   if (dx && dw) MAT_TRY((micro_code<T, true, true, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
   else if (dx) MAT_TRY((micro_code<T, true, false, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
   else MAT_TRY((micro_code<T, false, true, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
-  if (dx) MAT_TRY(micro_gemm(ctx, true, false, w_t, n_in, s.dy_rows, tokens, n_out, dx, sizeof(T) == 2, ld_dx, st));
+  if (dx) MAT_TRY(micro_gemm(ctx, true, false, s.dy_rows, tokens, w_t, n_in, n_out, dx, sizeof(T) == 2, ld_dx, st));
   // The second product does not depend on the first and starts as SMs fall free.
-  if (dw) MAT_TRY(micro_gemm(ctx, false, dx != nullptr, s.x_cols, n_in, s.dy_cols, n_out, tokens, dw, dw_bf16, ld_dw, st));
+  if (dw) MAT_TRY(micro_gemm(ctx, false, dx != nullptr, s.dy_cols, n_out, s.x_cols, n_in, tokens, dw, dw_bf16, ld_dw, st));
   return RTOPK_OK;
 }
 
@@ -238,7 +249,7 @@ int layer_norm_gradients(rtopk_matrix* ctx, const NormBackArgs<T>& a, float* dga
 }  // namespace
 
 cudaError_t rtopk::mat::allow_layers() {
-  for (const cudaError_t e : {allow_smem<EPI_MICRO>(), allow_rows<float, false>(), allow_rows<float, true>(), allow_rows<__nv_bfloat16, false>(), allow_rows<__nv_bfloat16, true>()})
+  for (const cudaError_t e : {allow_smem<EPI_MICRO>(), allow_smem<EPI_MICRO_ROWS>(), allow_rows<float, false>(), allow_rows<float, true>(), allow_rows<__nv_bfloat16, false>(), allow_rows<__nv_bfloat16, true>()})
     if (e != cudaSuccess) return e;
   return cudaSuccess;
 }

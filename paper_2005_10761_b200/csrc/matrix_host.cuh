@@ -137,12 +137,11 @@ inline int scale_map(rtopk_matrix* ctx, CUtensorMap* map, const Operand& o) {
                                  CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? RTOPK_OK : fail(ctx, cudaErrorInvalidValue);
 }
-inline int scale_maps(rtopk_matrix* ctx, Scales<EPI_MICRO>* s, const Operand& p, const Operand& q) {
+inline int scale_maps(rtopk_matrix* ctx, ScaleMaps* s, const Operand& p, const Operand& q) {
   MAT_TRY(scale_map(ctx, &s->p, p));
   return scale_map(ctx, &s->q, q);
 }
-template <int kEpi>
-int scale_maps(rtopk_matrix*, Scales<kEpi>*, const Operand&, const Operand&) { return RTOPK_OK; }
+inline int scale_maps(rtopk_matrix*, NoScales*, const Operand&, const Operand&) { return RTOPK_OK; }
 
 template <int kCols, bool kPair>
 int64_t gemm_tiles(const Gemm& g) {
@@ -156,8 +155,8 @@ int64_t gemm_tiles(const Gemm& g) {
 
 template <int kCols, bool kPair, int kEpi>
 int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int split, cudaStream_t st) {
-  using S = GemmShape<kCols, kPair, kEpi == EPI_MICRO>;
-  constexpr bool kBytes = kEpi == EPI_CODED || kEpi == EPI_MICRO;
+  using S = GemmShape<kCols, kPair, is_micro(kEpi)>;
+  constexpr bool kBytes = kEpi == EPI_CODED || is_micro(kEpi);
   constexpr bool kMnMajor = kEpi == EPI_APPLY || kEpi == EPI_OUT || kEpi == EPI_UPDATE;
   constexpr int kBlocks = kPair ? 2 : 1;
   g.tiles_l = (int)ceil_div(g.lanes, S::kTileLanes), g.tiles_c = (int)ceil_div(g.cols, kCols);
@@ -188,11 +187,11 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
 constexpr int64_t kStepsMax = 1024;
 // The widest tile.  The scales of 4-bit codes need their place in tensor memory beside the accumulators.
 template <int kEpi>
-constexpr int kWidest = kEpi == EPI_MICRO ? 192 : 256;
+constexpr int kWidest = is_micro(kEpi) ? 192 : 256;
 template <int kEpi>
 int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, cudaStream_t st) {
-  constexpr bool kMicro = kEpi == EPI_MICRO;
-  constexpr double kColumn = kEpi == EPI_CODED || kMicro ? 35 : kEpi == EPI_GRAM ? 45 : 75;
+  constexpr bool kMicro = is_micro(kEpi);
+  constexpr double kColumn = kEpi == EPI_MICRO_ROWS ? 15 : kEpi == EPI_CODED || kMicro ? 35 : kEpi == EPI_GRAM ? 45 : 75;
   const int64_t steps = ceil_div((int64_t)g.depth * (kEpi == EPI_CODED || kMicro ? 1 : 2), kDepthBytes);
   double best = 1e300;
   int which = 0, parts = 1;
@@ -221,10 +220,10 @@ int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, c
 
 template <int kEpi>
 cudaError_t allow_smem() {
-  cudaError_t e = cudaFuncSetAttribute(k_gemm<64, false, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<64, false, kEpi == EPI_MICRO>::kSmem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<128, false, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<128, false, kEpi == EPI_MICRO>::kSmem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<128, true, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<128, true, kEpi == EPI_MICRO>::kSmem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<kWidest<kEpi>, true, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<kWidest<kEpi>, true, kEpi == EPI_MICRO>::kSmem);
+  cudaError_t e = cudaFuncSetAttribute(k_gemm<64, false, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<64, false, is_micro(kEpi)>::kSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<128, false, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<128, false, is_micro(kEpi)>::kSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<128, true, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<128, true, is_micro(kEpi)>::kSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<kWidest<kEpi>, true, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<kWidest<kEpi>, true, is_micro(kEpi)>::kSmem);
   return e;
 }
 
