@@ -14,10 +14,10 @@
 namespace rtopk {
 namespace mat {
 
+// From the largest magnitude's bits.  6 = 1.5 2^2: adding just less than half a mantissa carries where the mantissa is above 1.5.
 __device__ __forceinline__ uint32_t micro_scale(uint32_t max_magnitude) {
-  if (max_magnitude >= 0x7F800000u) return 255u;
-  const int e = (int)(max_magnitude >> 23) - 2 + ((max_magnitude & 0x7FFFFFu) > 0x400000u);      // 6 = 1.5 2^2
-  return (uint32_t)max(e, 0);
+  const int e = max((int)((max_magnitude + 0x3FFFFFu) >> 23) - 2, 0);
+  return max_magnitude >= 0x7F800000u ? 255u : (uint32_t)e;
 }
 // 1 / 2^e; NaN's codes are made zero by its caller.
 __device__ __forceinline__ float micro_factor(uint32_t scale) { return __uint_as_float((254u - min(scale, 254u)) << 23); }
@@ -48,6 +48,63 @@ struct MicroOut {
   int64_t ld;            // bytes from row to row of the codes
 };
 
+// Largest magnitudes of eight rows' and eight columns' values in a thread's 8 x 8, then over the lanes that share the rows (1, 2: 32
+// columns) and the columns (8, 16: 32 rows).
+template <class T>
+struct Magnitudes;
+template <>
+struct Magnitudes<float> {
+  static __device__ __forceinline__ void rows(const Eight<float> (&e)[8], uint32_t (&m)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      m[i] = e[i].largest(0u);
+      m[i] = max(m[i], __shfl_xor_sync(0xFFFFFFFFu, m[i], 1));
+      m[i] = max(m[i], __shfl_xor_sync(0xFFFFFFFFu, m[i], 2));
+    }
+  }
+  static __device__ __forceinline__ void columns(const Eight<float> (&e)[8], uint32_t (&m)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m[j] = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float v[8];
+      e[i].widen_to(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m[j] = max(m[j], magnitude(v[j]));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      m[j] = max(m[j], __shfl_xor_sync(0xFFFFFFFFu, m[j], 8));
+      m[j] = max(m[j], __shfl_xor_sync(0xFFFFFFFFu, m[j], 16));
+    }
+  }
+};
+// Two 16-bit magnitudes in a word throughout.
+template <>
+struct Magnitudes<__nv_bfloat16> {
+  static __device__ __forceinline__ void rows(const Eight<__nv_bfloat16> (&e)[8], uint32_t (&m)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const uint32_t a = e[i].largest(0u), b = e[i + 1].largest(0u);
+      uint32_t q = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));      // row i's low, row i + 1's high
+      q = __vmaxu2(q, __shfl_xor_sync(0xFFFFFFFFu, q, 1));
+      q = __vmaxu2(q, __shfl_xor_sync(0xFFFFFFFFu, q, 2));
+      m[i] = q << 16, m[i + 1] = q & 0xFFFF0000u;
+    }
+  }
+  static __device__ __forceinline__ void columns(const Eight<__nv_bfloat16> (&e)[8], uint32_t (&m)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+      uint32_t q = 0u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q = __vmaxu2(q, e[i].w[j / 2] & 0x7FFF7FFFu);
+      q = __vmaxu2(q, __shfl_xor_sync(0xFFFFFFFFu, q, 8));
+      q = __vmaxu2(q, __shfl_xor_sync(0xFFFFFFFFu, q, 16));
+      m[j] = q << 16, m[j + 1] = q & 0xFFFF0000u;
+    }
+  }
+};
+
 // Codes of a tile of 128 x 128 values along its rows (blocks of 32 columns) and, transposed, along its columns (blocks of 32
 // rows), the values read once.  kTile: one scale for each 32 x 32 values, the same codes both ways.  A warp takes 32 rows and 64 columns, a
 // thread eight neighbours in each of eight rows: the maxima along rows meet in four lanes, those along columns in the other four, and the
@@ -62,73 +119,57 @@ k_micro_code(const T* src, int64_t ld, int rows, int cols, int vec, int tiles_c,
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cl = lane & 7, rl = lane >> 3;
   const int wr = (warp & 3) * 32, wc = (warp >> 2) * 64;       // the warp's place in the tile
   const int r0 = tile_r * 128 + wr + rl * 8, c0 = tile_c * 128 + wc + cl * 8;
+  const bool whole = tile_r * 128 + 128 <= rows && tile_c * 128 + 128 <= cols;
   launch_wait();
   launch_next();
   Eight<T> e[8];
+  if (whole && vec) {
+    const T* p = src + (int64_t)r0 * ld + c0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) e[i].load(src + (int64_t)min(r0 + i, rows - 1) * ld + min(c0, cols - 1), r0 + i < rows ? cols - c0 : 0, vec);
-  uint32_t row_scale[8], col_scale[8];
-  if constexpr (kTile) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = e[i].largest(m);
-    m = Eight<T>::as_magnitude(m);
-#pragma unroll
-    for (int k : {1, 2, 8, 16}) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, k));
-    const uint32_t s = micro_scale(m);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) row_scale[i] = col_scale[i] = s;
+    for (int i = 0; i < 8; ++i, p += ld) e[i].load(p, 8, true);
   } else {
-    if constexpr (kRows) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        uint32_t m = Eight<T>::as_magnitude(e[i].largest(0));
-        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-        row_scale[i] = micro_scale(m);
-      }
-    }
-    if constexpr (kColumns) {
-      uint32_t m[8] = {};
+    for (int i = 0; i < 8; ++i) e[i].load(src + (int64_t)min(r0 + i, rows - 1) * ld + min(c0, cols - 1), r0 + i < rows ? cols - c0 : 0, vec);
+  }
+  uint32_t shared = 0u;
+  if constexpr (kTile) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float v[8];
-        e[i].widen_to(v);
+    for (int i = 0; i < 8; ++i) shared = e[i].largest(shared);
+    shared = Eight<T>::as_magnitude(shared);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) m[j] = max(m[j], magnitude(v[j]));
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        m[j] = max(m[j], __shfl_xor_sync(0xFFFFFFFFu, m[j], 8));
-        m[j] = max(m[j], __shfl_xor_sync(0xFFFFFFFFu, m[j], 16));
-        col_scale[j] = micro_scale(m[j]);
-      }
-    }
+    for (int k : {1, 2, 8, 16}) shared = max(shared, __shfl_xor_sync(0xFFFFFFFFu, shared, k));
+    shared = micro_scale(shared);
   }
   if constexpr (kRows) {
+    uint32_t s[8];
+    if constexpr (!kTile) Magnitudes<T>::rows(e, s);
+    uint8_t* out = by_row.codes + (int64_t)r0 * by_row.ld + c0 / 2;
+    // row r0 + i's scale for these 32 columns: the rows of a lane follow one another
+    uint8_t* scale = row_scales + rl * 128 + (wr >> 5) * 4 + (wc + cl * 8) / 32;
+    const bool first = (cl & 3) == 0, on = (c0 & ~31) < cols;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i, out += by_row.ld) {
+      const uint32_t q = kTile ? shared : micro_scale(s[i]);
       float v[8];
       e[i].widen_to(v);
-      const uint32_t w = micro_code8(v, row_scale[i]);
-      const int r = wr + rl * 8 + i;
-      if ((cl & 3) == 0) row_scales[(r & 31) * 16 + (r >> 5) * 4 + (wc + cl * 8) / 32] = (uint8_t)row_scale[i];
-      if (r0 + i < rows && (c0 & ~31) < cols) *(uint32_t*)(by_row.codes + (r0 + i) * by_row.ld + c0 / 2) = w;
+      const uint32_t w = micro_code8(v, q);
+      if (first) scale[i * 16] = (uint8_t)q;
+      if (whole || (r0 + i < rows && on)) *(uint32_t*)out = w;
     }
   }
   if constexpr (kColumns) {
+    uint32_t s[8];
+    if constexpr (!kTile) Magnitudes<T>::columns(e, s);
+    const int c = wc + cl * 8;
+    uint8_t* scale = col_scales + (c & 31) * 16 + (c >> 5) * 4 + (wr >> 5);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
+      const uint32_t q = kTile ? shared : micro_scale(s[j]);
       float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float u[8];
-        e[i].widen_to(u);
-        v[i] = u[j];
-      }
-      const int c = wc + cl * 8 + j;
-      col_codes[c][(wr >> 3) + rl] = micro_code8(v, col_scale[j]);
-      if (rl == 0) col_scales[(c & 31) * 16 + (c >> 5) * 4 + (wr >> 5)] = (uint8_t)col_scale[j];
+      for (int i = 0; i < 8; ++i) v[i] = e[i].at(j);
+      col_codes[c + j][(wr >> 3) + rl] = micro_code8(v, q);
+      if (rl == 0) scale[j * 16] = (uint8_t)q;
     }
   }
   __syncthreads();
@@ -148,7 +189,7 @@ k_micro_code(const T* src, int64_t ld, int rows, int cols, int vec, int tiles_c,
     }
     for (int i = threadIdx.x; i < 512; i += 256) {
       const int c = i >> 2, part = i & 3;      // 16 bytes: a block of 32 rows
-      if (tile_c * 128 + c < cols && tile_r * 128 + part * 32 < rows) {
+      if (whole || (tile_c * 128 + c < cols && tile_r * 128 + part * 32 < rows)) {
         const uint32_t* w = &col_codes[c][part * 4];
         *(uint4*)(by_col.codes + (int64_t)(tile_c * 128 + c) * by_col.ld + tile_r * 64 + part * 16) = make_uint4(w[0], w[1], w[2], w[3]);
       }

@@ -37,6 +37,7 @@ struct Eight<float> {
     return max(max(m, magnitude(b.x)), max(magnitude(b.y), max(magnitude(b.z), magnitude(b.w))));
   }
   static __device__ __forceinline__ uint32_t as_magnitude(uint32_t m) { return m; }
+  __device__ __forceinline__ float at(int j) const { return j < 4 ? (j < 2 ? (j ? a.y : a.x) : (j == 2 ? a.z : a.w)) : (j < 6 ? (j == 4 ? b.x : b.y) : (j == 6 ? b.z : b.w)); }
 };
 template <>
 struct Eight<__nv_bfloat16> {
@@ -62,6 +63,7 @@ struct Eight<__nv_bfloat16> {
     return m;
   }
   static __device__ __forceinline__ uint32_t as_magnitude(uint32_t m) { return max(m << 16, m & 0xFFFF0000u); }
+  __device__ __forceinline__ float at(int j) const { return __uint_as_float(j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16); }
 };
 template <class T>
 __device__ __forceinline__ void load8(const T* p, int left, bool vec, float (&v)[8]) {
