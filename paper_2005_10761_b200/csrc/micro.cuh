@@ -48,62 +48,89 @@ struct MicroOut {
   int64_t ld;            // bytes from row to row of the codes
 };
 
-// Largest magnitudes of eight rows' and eight columns' values in a thread's 8 x 8, then over the lanes that share the rows (1, 2: 32
-// columns) and the columns (8, 16: 32 rows).
+// The larger magnitude, NaN if there is one.  Three numbers at a time; or two 16-bit ones in a word (whose signs mean nothing).
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t other(uint32_t v, int lanes) { return __shfl_xor_sync(0xFFFFFFFFu, v, lanes); }
+
+// Bits of the largest magnitudes of eight rows' and eight columns' values in a thread's 8 x 8, then over the lanes that share the rows (1, 2:
+// 32 columns) and the columns (8, 16: 32 rows); `all`: of all of it.
 template <class T>
 struct Magnitudes;
 template <>
 struct Magnitudes<float> {
-  static __device__ __forceinline__ void rows(const Eight<float> (&e)[8], uint32_t (&m)[8]) {
+  using E = Eight<float>;
+  static __device__ __forceinline__ float row(const E& e, float m) { return max_abs(max_abs(e.a.x, e.a.y, e.a.z), max_abs(e.a.w, e.b.x, e.b.y), max_abs(e.b.z, e.b.w, m)); }
+  static __device__ __forceinline__ void rows(const E (&e)[8], uint32_t (&m)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      m[i] = e[i].largest(0u);
-      m[i] = max(m[i], __shfl_xor_sync(0xFFFFFFFFu, m[i], 1));
-      m[i] = max(m[i], __shfl_xor_sync(0xFFFFFFFFu, m[i], 2));
+      m[i] = __float_as_uint(row(e[i], 0.f));
+      m[i] = max(m[i], other(m[i], 1));
+      m[i] = max(m[i], other(m[i], 2));
     }
   }
-  static __device__ __forceinline__ void columns(const Eight<float> (&e)[8], uint32_t (&m)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m[j] = 0u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float v[8];
-      e[i].widen_to(v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) m[j] = max(m[j], magnitude(v[j]));
-    }
+  static __device__ __forceinline__ void columns(const E (&e)[8], uint32_t (&m)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      m[j] = max(m[j], __shfl_xor_sync(0xFFFFFFFFu, m[j], 8));
-      m[j] = max(m[j], __shfl_xor_sync(0xFFFFFFFFu, m[j], 16));
+      m[j] = __float_as_uint(max_abs(max_abs(e[0].at(j), e[1].at(j), e[2].at(j)), max_abs(e[3].at(j), e[4].at(j), e[5].at(j)), max_abs(e[6].at(j), e[7].at(j), 0.f)));
+      m[j] = max(m[j], other(m[j], 8));
+      m[j] = max(m[j], other(m[j], 16));
     }
   }
+  static __device__ __forceinline__ uint32_t all(const E (&e)[8]) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = row(e[i], m);
+    uint32_t bits = __float_as_uint(m);
+#pragma unroll
+    for (int k : {1, 2, 8, 16}) bits = max(bits, other(bits, k));
+    return bits;
+  }
 };
-// Two 16-bit magnitudes in a word throughout.
 template <>
 struct Magnitudes<__nv_bfloat16> {
-  static __device__ __forceinline__ void rows(const Eight<__nv_bfloat16> (&e)[8], uint32_t (&m)[8]) {
+  using E = Eight<__nv_bfloat16>;
+  static __device__ __forceinline__ uint32_t row(const E& e) { return max_abs2(max_abs2(e.w[0], e.w[1]), max_abs2(e.w[2], e.w[3])); }
+  static __device__ __forceinline__ void rows(const E (&e)[8], uint32_t (&m)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      const uint32_t a = e[i].largest(0u), b = e[i + 1].largest(0u);
-      uint32_t q = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));      // row i's low, row i + 1's high
-      q = __vmaxu2(q, __shfl_xor_sync(0xFFFFFFFFu, q, 1));
-      q = __vmaxu2(q, __shfl_xor_sync(0xFFFFFFFFu, q, 2));
-      m[i] = q << 16, m[i + 1] = q & 0xFFFF0000u;
+      const uint32_t a = row(e[i]), b = row(e[i + 1]);
+      uint32_t q = max_abs2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));      // row i's low, row i + 1's high
+      q = max_abs2(q, other(q, 1));
+      q = max_abs2(q, other(q, 2));
+      m[i] = q << 16 & 0x7FFFFFFFu, m[i + 1] = q & 0x7FFF0000u;
     }
   }
-  static __device__ __forceinline__ void columns(const Eight<__nv_bfloat16> (&e)[8], uint32_t (&m)[8]) {
+  static __device__ __forceinline__ void columns(const E (&e)[8], uint32_t (&m)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
-      uint32_t q = 0u;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) q = __vmaxu2(q, e[i].w[j / 2] & 0x7FFF7FFFu);
-      q = __vmaxu2(q, __shfl_xor_sync(0xFFFFFFFFu, q, 8));
-      q = __vmaxu2(q, __shfl_xor_sync(0xFFFFFFFFu, q, 16));
-      m[j] = q << 16, m[j + 1] = q & 0xFFFF0000u;
+      const int k = j / 2;
+      uint32_t q = max_abs2(max_abs2(max_abs2(e[0].w[k], e[1].w[k]), max_abs2(e[2].w[k], e[3].w[k])), max_abs2(max_abs2(e[4].w[k], e[5].w[k]), max_abs2(e[6].w[k], e[7].w[k])));
+      q = max_abs2(q, other(q, 8));
+      q = max_abs2(q, other(q, 16));
+      m[j] = q << 16 & 0x7FFFFFFFu, m[j + 1] = q & 0x7FFF0000u;
     }
   }
+  static __device__ __forceinline__ uint32_t all(const E (&e)[8]) {
+    uint32_t q = row(e[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) q = max_abs2(q, row(e[i]));
+#pragma unroll
+    for (int k : {1, 2, 8, 16}) q = max_abs2(q, other(q, k));
+    return max(q << 16 & 0x7FFFFFFFu, q & 0x7FFF0000u);
+  }
 };
+// Hides what is known of the values, so that they are widened where they are used and not kept in that form.
+__device__ __forceinline__ void forget(Eight<float>&) {}
+__device__ __forceinline__ void forget(Eight<__nv_bfloat16>& e) { asm volatile("" : "+r"(e.w[0]), "+r"(e.w[1]), "+r"(e.w[2]), "+r"(e.w[3])); }
 
 // Codes of a tile of 128 x 128 values along its rows (blocks of 32 columns) and, transposed, along its columns (blocks of 32
 // rows), the values read once.  kTile: one scale for each 32 x 32 values, the same codes both ways.  A warp takes 32 rows and 64 columns, a
@@ -133,12 +160,7 @@ k_micro_code(const T* src, int64_t ld, int rows, int cols, int vec, int tiles_c,
   }
   uint32_t shared = 0u;
   if constexpr (kTile) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) shared = e[i].largest(shared);
-    shared = Eight<T>::as_magnitude(shared);
-#pragma unroll
-    for (int k : {1, 2, 8, 16}) shared = max(shared, __shfl_xor_sync(0xFFFFFFFFu, shared, k));
-    shared = micro_scale(shared);
+    shared = micro_scale(Magnitudes<T>::all(e));
   }
   if constexpr (kRows) {
     uint32_t s[8];
@@ -157,6 +179,9 @@ k_micro_code(const T* src, int64_t ld, int rows, int cols, int vec, int tiles_c,
       if (whole || (r0 + i < rows && on)) *(uint32_t*)out = w;
     }
   }
+  if constexpr (kRows && kColumns)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) forget(e[i]);
   if constexpr (kColumns) {
     uint32_t s[8];
     if constexpr (!kTile) Magnitudes<T>::columns(e, s);
