@@ -284,14 +284,19 @@ class MatrixContext:
 
     def _rows(self, t: torch.Tensor, what: str, shape=None):
         """(pointer, row stride) of a matrix with contiguous rows."""
-        sizes, strides = t.shape, t.stride()
+        sizes = t.shape
         if shape is not None and sizes != shape:
             raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(sizes)}")
-        if strides[-1] != 1 and sizes[-1] > 1:
-            raise ValueError(f"the rows of {what} must be contiguous")
+        ld = sizes[-1]
+        if not t.is_contiguous():
+            strides = t.stride()
+            if strides[-1] != 1 and ld > 1:
+                raise ValueError(f"the rows of {what} must be contiguous")
+            if sizes[-2] > 1:
+                ld = strides[-2]
         if t.get_device() != self.device:
             raise ValueError(f"{what} must be on device {self.device}")
-        return t.data_ptr(), (strides[-2] if sizes[-2] > 1 else sizes[-1])
+        return t.data_ptr(), ld
 
     def _batch(self, t: torch.Tensor, what: str, shape=None):
         """(pointer, row stride, matrix stride) of a matrix or a batch of them."""
@@ -446,31 +451,47 @@ class MatrixContext:
             self._on_device(mask._step, "the mask's step")
         return C.byref(mask._struct)
 
-    def _like(self, t, what: str, x, shape):
-        """(pointer, row stride) of an optional matrix of x's shape and type."""
+    def _like(self, t, what: str, dtype, shape):
+        """(pointer, row stride) of an optional matrix of that type and shape."""
         if t is None:
             return None, 0
-        if t.dtype != x.dtype:
+        if t.dtype is not dtype:
             raise TypeError(f"{what} must have the other matrices' type")
-        return self._rows(t, what, shape)
+        if t.shape != shape or not t.is_contiguous():
+            return self._rows(t, what, shape)
+        if t.get_device() != self.device:
+            raise ValueError(f"{what} must be on device {self.device}")
+        return t.data_ptr(), shape[1]
 
     def _vector(self, t, what: str, n: int):
         if t is None:
             return None
-        if t.dtype != torch.float32:
+        if t.dtype is not torch.float32:
             raise TypeError(f"{what} must be float32")
-        if t.shape != (n,) or (n > 1 and t.stride()[0] != 1):
+        if t.numel() != n or t.dim() != 1 or not t.is_contiguous():
             raise ValueError(f"{what} must be contiguous and of shape {(n,)}")
-        return self._on_device(t, what)
+        if t.get_device() != self.device:
+            raise ValueError(f"{what} must be on device {self.device}")
+        return t.data_ptr()
+
+    @staticmethod
+    def _matrix(t, what: str):
+        """(shape, torch's type, the library's type) of the matrix that the others are like."""
+        shape, dtype = t.shape, t.dtype
+        if len(shape) != 2:
+            raise ValueError(f"{what} must be a matrix")
+        code = _DTYPES.get(dtype)
+        if code is None:
+            raise TypeError(f"{what} must be float32 or bfloat16")
+        return shape, dtype, code
 
     def dropout(self, x, out, mask: Mask) -> None:
         """out <- x where the mask keeps an element, times 1 / the share that is kept, else 0 ([rows, cols], float32 or bfloat16; out may be
         x).  The gradient is the same call on out's gradient."""
-        if x.dim() != 2:
-            raise ValueError("x must be a matrix")
-        p, ld = self._rows(x, "x")
-        po, ldo = self._like(out, "out", x, x.shape)
-        rc = self._lib.rtopk_dropout(self._h, p, _dtype(x, "x"), ld, x.shape[0], x.shape[1], self._mask(mask), po, ldo, self._stream())
+        shape, dtype, code = self._matrix(x, "x")
+        p, ld = self._like(x, "x", dtype, shape)
+        po, ldo = self._like(out, "out", dtype, shape)
+        rc = self._lib.rtopk_dropout(self._h, p, code, ld, *shape, self._mask(mask), po, ldo, self._stream())
         if rc:
             self._check(rc, "rtopk_dropout")
 
@@ -478,14 +499,13 @@ class MatrixContext:
         """total <- residual + dropout(x); out <- gamma (total - mean) rstd + beta over each row of [rows, cols] matrices, float32 or bfloat16.
         residual, mask, gamma, beta (float32 [cols]) may be None; total, mean and rstd (float32 [rows]) are written where given, for
         :meth:`layer_norm_gradients`."""
-        if x.dim() != 2:
-            raise ValueError("x must be a matrix")
-        rows, cols = shape = x.shape
-        p, ld = self._rows(x, "x")
-        pr, ldr = self._like(residual, "residual", x, shape)
-        po, ldo = self._like(out, "out", x, shape)
-        pt, ldt = self._like(total, "total", x, shape)
-        rc = self._lib.rtopk_layer_norm(self._h, p, ld, pr, ldr, _dtype(x, "x"), rows, cols, self._vector(gamma, "gamma", cols),
+        shape, dtype, code = self._matrix(x, "x")
+        rows, cols = shape
+        p, ld = self._like(x, "x", dtype, shape)
+        pr, ldr = self._like(residual, "residual", dtype, shape)
+        po, ldo = self._like(out, "out", dtype, shape)
+        pt, ldt = self._like(total, "total", dtype, shape)
+        rc = self._lib.rtopk_layer_norm(self._h, p, ld, pr, ldr, code, rows, cols, self._vector(gamma, "gamma", cols),
                                         self._vector(beta, "beta", cols), eps, self._mask(mask), po, ldo, pt, ldt,
                                         self._vector(mean, "mean", rows), self._vector(rstd, "rstd", rows), self._stream())
         if rc:
@@ -496,17 +516,16 @@ class MatrixContext:
         """The gradients of :meth:`layer_norm` for dy (of out) and dtotal (of total, where it is used elsewhere; may be None): dresidual (without
         a mask also that of x), dx with a mask, dgamma and dbeta (float32 [cols]).  total, mean and rstd are the forward call's;
         without residual and mask, total is its x."""
-        if dy.dim() != 2:
-            raise ValueError("dy must be a matrix")
+        shape, dtype, code = self._matrix(dy, "dy")
         if (mask is None) != (dx is None):
             raise ValueError("dx goes with a mask: without one it is dresidual")
-        rows, cols = shape = dy.shape
-        p, ld = self._rows(dy, "dy")
-        pt, ldt = self._like(total, "total", dy, shape)
-        pa, lda = self._like(dtotal, "dtotal", dy, shape)
-        pr, ldr = self._like(dresidual, "dresidual", dy, shape)
-        px, ldx = self._like(dx, "dx", dy, shape)
-        rc = self._lib.rtopk_layer_norm_gradients(self._h, p, ld, pt, ldt, pa, lda, _dtype(dy, "dy"), rows, cols, self._vector(mean, "mean", rows),
+        rows, cols = shape
+        p, ld = self._like(dy, "dy", dtype, shape)
+        pt, ldt = self._like(total, "total", dtype, shape)
+        pa, lda = self._like(dtotal, "dtotal", dtype, shape)
+        pr, ldr = self._like(dresidual, "dresidual", dtype, shape)
+        px, ldx = self._like(dx, "dx", dtype, shape)
+        rc = self._lib.rtopk_layer_norm_gradients(self._h, p, ld, pt, ldt, pa, lda, code, rows, cols, self._vector(mean, "mean", rows),
                                                   self._vector(rstd, "rstd", rows), self._vector(gamma, "gamma", cols), self._mask(mask), pr, ldr,
                                                   px, ldx, self._vector(dgamma, "dgamma", cols), self._vector(dbeta, "dbeta", cols), self._stream())
         if rc:
