@@ -81,8 +81,22 @@ int micro_weights(rtopk_matrix* ctx, const T* w, int64_t ld, int64_t n_out, int6
   return micro_code<T, true, true, true>(ctx, w, ld, n_out, n_in, rows, cols, st);
 }
 
+constexpr int kFewSmem = 96 * 1024;
+template <class T, int kTokens>
+int micro_few(rtopk_matrix* ctx, const T* x, int64_t ld_x, const MicroOut& w, int64_t tokens, int64_t n_out, int64_t n_in, T* out, int64_t ld_out, cudaStream_t st) {
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(n_out, 128) * 4, 2 * ctx->sms));
+  return launch(ctx, k_micro_few<T, kTokens>, grid, 256, few_smem(kTokens, n_in), st, x, ld_x, rows_aligned(x, sizeof(T), 1, ld_x, 0, 16) ? 1 : 0, w, tokens, n_out, n_in, out, ld_out);
+}
+
 template <class T>
 int micro_product(rtopk_matrix* ctx, const T* x, int64_t ld_x, const MicroOut& w, int64_t tokens, int64_t n_out, int64_t n_in, T* out, int64_t ld_out, cudaStream_t st) {
+  // One launch, but its dot products take longer than reading W with several tokens: 4 through 4096 -> 4096 7.4 us against 8.9 of the product
+  // kernel, 2 through 8192 -> 8192 17.3 against 16.5, 4 23.6.
+  if ((tokens == 1 || (tokens <= kFewTokens && tokens * n_in * n_out <= 100000000)) && few_smem(tokens <= 2 ? (int)tokens : 4, n_in) <= kFewSmem) {
+    if (tokens == 1) return micro_few<T, 1>(ctx, x, ld_x, w, tokens, n_out, n_in, out, ld_out, st);
+    if (tokens == 2) return micro_few<T, 2>(ctx, x, ld_x, w, tokens, n_out, n_in, out, ld_out, st);
+    return micro_few<T, 4>(ctx, x, ld_x, w, tokens, n_out, n_in, out, ld_out, st);
+  }
   Carve c{ctx->scratch};
   MicroScratch s(c, tokens, n_out, n_in);
   MAT_TRY((micro_code<T, true, false, false>(ctx, x, ld_x, tokens, n_in, s.x_rows, s.x_rows, st)));
@@ -249,7 +263,9 @@ int layer_norm_gradients(rtopk_matrix* ctx, const NormBackArgs<T>& a, float* dga
 }  // namespace
 
 cudaError_t rtopk::mat::allow_layers() {
-  for (const cudaError_t e : {allow_smem<EPI_MICRO>(), allow_smem<EPI_MICRO_ROWS>(), allow_rows<float, false>(), allow_rows<float, true>(), allow_rows<__nv_bfloat16, false>(), allow_rows<__nv_bfloat16, true>()})
+  auto few = [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem); };
+  for (const cudaError_t e : {few(k_micro_few<float, 1>), few(k_micro_few<float, 2>), few(k_micro_few<float, 4>), few(k_micro_few<__nv_bfloat16, 1>), few(k_micro_few<__nv_bfloat16, 2>),
+                              few(k_micro_few<__nv_bfloat16, 4>), allow_smem<EPI_MICRO>(), allow_smem<EPI_MICRO_ROWS>(), allow_rows<float, false>(), allow_rows<float, true>(), allow_rows<__nv_bfloat16, false>(), allow_rows<__nv_bfloat16, true>()})
     if (e != cudaSuccess) return e;
   return cudaSuccess;
 }

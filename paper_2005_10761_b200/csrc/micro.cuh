@@ -222,5 +222,147 @@ k_micro_code(const T* src, int64_t ld, int rows, int cols, int vec, int tiles_c,
   }
 }
 
+// ----------------------------------------------------------------------------- a few tokens
+// The layer for up to four tokens, where reading W is the work, in one launch.  Every block codes the tokens for itself; then each warp takes four
+// channels at a time, 32 apart, whose scales lie together, and a lane a block of 32 codes of each: integer dot products with the tokens'
+// codes in shared memory, times the two scales, added in binary32.
+//
+// A code is looked up as a byte, twice its value plus 12: one byte permutation takes four codes as selectors into the eight bytes of a table,
+// in which a code's sign bit asks for a byte's sign instead, 0 here; so the positive codes come from one table, the negative ones, their
+// sign bits turned round, from another, and the two are or'ed.  The 12 is taken off the sum: 12 times the sum of the token's codes.
+constexpr int kFewTokens = 4, kFewAhead = 2;
+constexpr uint32_t kFewPositive0 = 0x0F0E0D0Cu, kFewPositive1 = 0x18141210u, kFewNegative0 = 0x090A0B0Cu, kFewNegative1 = 0x00040608u;
+__device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t selectors) {
+  uint32_t r;
+  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(selectors));
+  return r;
+}
+// Two words of four bytes from a word of eight codes.
+__device__ __forceinline__ void few_bytes(uint32_t w, uint32_t& low, uint32_t& high) {
+  const uint32_t turned = w ^ 0x88888888u;
+  low = permute(kFewPositive0, kFewPositive1, w) | permute(kFewNegative0, kFewNegative1, turned);
+  high = permute(kFewPositive0, kFewPositive1, w >> 16) | permute(kFewNegative0, kFewNegative1, turned >> 16);
+}
+// 2^(b - 127); infinity for NaN's 255, which makes NaN of its block's zeros.
+__device__ __forceinline__ float power_of(uint32_t b) { return __uint_as_float(b ? b << 23 : 1u << 22); }
+constexpr int few_smem(int tokens, int64_t n_in) { return (int)((n_in + 31) / 32) * tokens * (32 + 8); }
+
+template <class T, int kTokens>
+__global__ void __launch_bounds__(256)
+k_micro_few(const T* x, int64_t ld_x, int vec, const __grid_constant__ MicroOut w, int tokens, int n_out, int n_in, T* out, int64_t ld_out) {
+  extern __shared__ __align__(16) char few_smem_raw[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int blocks = (n_in + 31) / 32, pieces = (n_in + 255) / 256 * 2;
+  uint4* x_codes = (uint4*)few_smem_raw;                                   // [token][half of a block][block]: twice the codes' values, bytes
+  uint2* x_scales = (uint2*)(x_codes + 2 * kTokens * blocks);              // [token][block]: a quarter of the scale, 12 times the codes' sum
+  const int units = (n_out + 127) / 128 * 32, step = gridDim.x * 8;
+  launch_wait();
+  launch_next();
+  struct Batch { uint4 codes[kFewAhead][4], scales[kFewAhead]; };
+  // of blocks first + lane, + 32, ..: four channels' codes, and four blocks' scales of each
+  auto read = [&](int unit, int first, Batch& v) {
+    const int group = unit >> 5, r = unit & 31;
+#pragma unroll
+    for (int k = 0; k < kFewAhead; ++k) {
+      const int b = first + 32 * k + lane;
+      if (b < blocks) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.codes[k][i] = __ldg((const uint4*)(w.codes + (int64_t)min(group * 128 + r + 32 * i, n_out - 1) * w.ld + b * 16));
+        v.scales[k] = __ldg((const uint4*)(w.scales + ((int64_t)group * pieces + (b >> 2)) * 512 + r * 16));
+      }
+    }
+  };
+  Batch now, next;
+  int unit = blockIdx.x * 8 + warp;
+  if (unit < units) read(unit, 0, now);
+  for (int i = threadIdx.x; i < kTokens * blocks; i += 256) {
+    const int t = i / blocks, b = i - t * blocks;
+    uint32_t bytes[8] = {}, scale = 0u;
+    int sum = 0;
+    if (t < tokens) {
+      Eight<T> e[4];
+      uint32_t m = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) e[k].load(x + t * ld_x + min(b * 32 + k * 8, n_in - 1), n_in - b * 32 - k * 8, vec);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m = e[k].largest(m);
+      scale = micro_scale(Eight<T>::as_magnitude(m));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float v[8];
+        e[k].widen_to(v);
+        uint32_t low, high;
+        few_bytes(micro_code8(v, scale), low, high);
+        bytes[2 * k] = __vsub4(low, 0x0C0C0C0Cu), bytes[2 * k + 1] = __vsub4(high, 0x0C0C0C0Cu);
+        sum = __dp4a((int)bytes[2 * k], 0x0C0C0C0C, __dp4a((int)bytes[2 * k + 1], 0x0C0C0C0C, sum));
+      }
+    }
+    x_codes[2 * t * blocks + b] = make_uint4(bytes[0], bytes[1], bytes[2], bytes[3]);
+    x_codes[(2 * t + 1) * blocks + b] = make_uint4(bytes[4], bytes[5], bytes[6], bytes[7]);
+    x_scales[t * blocks + b] = make_uint2(__float_as_uint(power_of(scale)), (uint32_t)sum);
+  }
+  __syncthreads();
+  for (; unit < units; unit += step) {
+    float acc[4][kTokens] = {};
+    for (int first = 0; first < blocks; first += 32 * kFewAhead) {
+      // what comes next, of this unit or of the warp's next one
+      if (first + 32 * kFewAhead < blocks) read(unit, first + 32 * kFewAhead, next);
+      else if (unit + step < units) read(unit + step, 0, next);
+#pragma unroll
+      for (int k = 0; k < kFewAhead; ++k) {
+        const int b = first + 32 * k + lane;
+        if (b >= blocks) break;
+        const uint32_t s[4] = {now.scales[k].x, now.scales[k].y, now.scales[k].z, now.scales[k].w};
+        int dot[4][kTokens];
+        float w_scale[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w_scale[i] = power_of(s[i] >> 8 * (b & 3) & 255u);
+#pragma unroll
+          for (int t = 0; t < kTokens; ++t) dot[i][t] = 0;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint4 q[kTokens];
+#pragma unroll
+          for (int t = 0; t < kTokens; ++t) q[t] = x_codes[(2 * t + h) * blocks + b];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t a[4];
+            few_bytes(h ? now.codes[k][i].z : now.codes[k][i].x, a[0], a[1]);
+            few_bytes(h ? now.codes[k][i].w : now.codes[k][i].y, a[2], a[3]);
+#pragma unroll
+            for (int t = 0; t < kTokens; ++t)
+              dot[i][t] = __dp4a((int)a[0], (int)q[t].x, __dp4a((int)a[1], (int)q[t].y, __dp4a((int)a[2], (int)q[t].z, __dp4a((int)a[3], (int)q[t].w, dot[i][t]))));
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < kTokens; ++t) {
+          const uint2 m = x_scales[t * blocks + b];
+          const float x_scale = __uint_as_float(m.x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)      // the smaller scale first, so that only what is too large in the end overflows
+            acc[i][t] = fmaf((float)(dot[i][t] - (int)m.y) * 0.25f * fminf(x_scale, w_scale[i]), fmaxf(x_scale, w_scale[i]), acc[i][t]);
+        }
+      }
+      now = next;
+    }
+    float result = 0.f;      // of channel lane & 3 and token lane >> 2
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < kTokens; ++t) {
+#pragma unroll
+        for (int k = 16; k; k >>= 1) acc[i][t] += __shfl_xor_sync(0xFFFFFFFFu, acc[i][t], k);
+        if (lane == t * 4 + i) result = acc[i][t];
+      }
+    const int t = lane >> 2, n = (unit >> 5) * 128 + (unit & 31) + 32 * (lane & 3);
+    if (t < kTokens && t < tokens && n < n_out) {
+      if (sizeof(T) == 2) ((__nv_bfloat16*)out)[t * ld_out + n] = __float2bfloat16_rn(result);
+      else ((float*)out)[t * ld_out + n] = result;
+    }
+  }
+}
+
 }  // namespace mat
 }  // namespace rtopk
