@@ -44,7 +44,7 @@ int micro_code(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_
 // along the rows by threads that have a row each, where there are rows enough to fill tiles of 128; else along the lanes, which
 // are the result's columns then.  early: `cols` is older than the launch before.
 int micro_gemm(rtopk_matrix* ctx, bool early, bool free_start, const MicroOut& row, int64_t rows, const MicroOut& col, int64_t cols, int64_t depth, void* out, int bf16, int64_t ld_out,
-               cudaStream_t st) {
+               cudaStream_t st, bool shares = false) {
   Gemm g = {};
   const int64_t bytes = ceil_div(depth, 2);
   g.depth = (int)bytes, g.batch = 1;
@@ -54,12 +54,12 @@ int micro_gemm(rtopk_matrix* ctx, bool early, bool free_start, const MicroOut& r
   if (rows > 64 && rows_aligned(out, bf16 ? 2 : 4, 1, ld_out, 0, 32)) {
     g.lanes = (int)rows, g.cols = (int)cols;
     g.out_col = 1, g.out_lane = ld_out;
-    return gemm<EPI_MICRO_ROWS>(ctx, r, c, g, st);
+    return gemm<EPI_MICRO_ROWS>(ctx, r, c, g, st, shares);
   }
   g.lanes = (int)cols, g.cols = (int)rows;
   g.out_col = ld_out, g.out_lane = 1;
   g.p_early = early;
-  return gemm<EPI_MICRO>(ctx, c, r, g, st);
+  return gemm<EPI_MICRO>(ctx, c, r, g, st, shares);
 }
 
 bool bad_micro(const void* codes, int64_t ld, const void* scales, int64_t cols) {
@@ -112,7 +112,7 @@ int micro_gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, i
   if (dx && dw) MAT_TRY((micro_code<T, true, true, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
   else if (dx) MAT_TRY((micro_code<T, true, false, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
   else MAT_TRY((micro_code<T, false, true, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
-  if (dx) MAT_TRY(micro_gemm(ctx, true, false, s.dy_rows, tokens, w_t, n_in, n_out, dx, sizeof(T) == 2, ld_dx, st));
+  if (dx) MAT_TRY(micro_gemm(ctx, true, false, s.dy_rows, tokens, w_t, n_in, n_out, dx, sizeof(T) == 2, ld_dx, st, dw != nullptr));
   // The second product does not depend on the first and starts as SMs fall free.
   if (dw) MAT_TRY(micro_gemm(ctx, false, dx != nullptr, s.dy_cols, n_out, s.x_cols, n_in, tokens, dw, dw_bf16, ld_dw, st));
   return RTOPK_OK;
