@@ -33,18 +33,24 @@ struct MicroScratch {
   }
 };
 
-template <class T, bool kRows, bool kColumns, bool kTile>
-int micro_code(rtopk_matrix* ctx, const T* src, int64_t ld, int64_t rows, int64_t cols, const MicroOut& by_row, const MicroOut& by_col, cudaStream_t st) {
-  const int64_t tiles_c = ceil_div(cols, 128), tiles = tiles_c * ceil_div(rows, 128);
-  return launch(ctx, k_micro_code<T, kRows, kColumns, kTile>, dim3((unsigned)tiles), 256, 0, st, src, ld, rows, cols, rows_aligned(src, sizeof(T), 1, ld, 0, 16) ? 1 : 0, tiles_c, by_row,
-                by_col);
+template <class T>
+CodeJob<T> code_job(const T* src, int64_t ld, int64_t rows, int64_t cols, const MicroOut& by_row, const MicroOut& by_col) {
+  return {src, ld, (int)rows, (int)cols, rows_aligned(src, sizeof(T), 1, ld, 0, 16) ? 1 : 0, (int)ceil_div(cols, 128), by_row, by_col};
+}
+template <class T>
+int64_t code_tiles(const CodeJob<T>& j) { return j.tiles_c * ceil_div(j.rows, 128); }
+
+template <bool kRows, bool kColumns, bool kTile, class T>
+int micro_code(rtopk_matrix* ctx, cudaStream_t st, const CodeJob<T>& job, const CodeJob<T>* second = nullptr) {
+  const int64_t tiles = code_tiles(job), all = tiles + (second ? code_tiles(*second) : 0);
+  return launch(ctx, k_micro_code<T, kRows, kColumns, kTile>, dim3((unsigned)all), 256, 0, st, job, second ? *second : job, tiles);
 }
 
 // out[r][c] = sum over the contraction of row r of `rows` and row c of `cols`.  Results whose rows start on multiples of 32 bytes are written
 // along the rows by threads that have a row each, where there are rows enough to fill tiles of 128; else along the lanes, which
 // are the result's columns then.  early: `cols` is older than the launch before.
 int micro_gemm(rtopk_matrix* ctx, bool early, bool free_start, const MicroOut& row, int64_t rows, const MicroOut& col, int64_t cols, int64_t depth, void* out, int bf16, int64_t ld_out,
-               cudaStream_t st, bool shares = false) {
+               cudaStream_t st) {
   Gemm g = {};
   const int64_t bytes = ceil_div(depth, 2);
   g.depth = (int)bytes, g.batch = 1;
@@ -54,12 +60,12 @@ int micro_gemm(rtopk_matrix* ctx, bool early, bool free_start, const MicroOut& r
   if (rows > 64 && rows_aligned(out, bf16 ? 2 : 4, 1, ld_out, 0, 32)) {
     g.lanes = (int)rows, g.cols = (int)cols;
     g.out_col = 1, g.out_lane = ld_out;
-    return gemm<EPI_MICRO_ROWS>(ctx, r, c, g, st, shares);
+    return gemm<EPI_MICRO_ROWS>(ctx, r, c, g, st);
   }
   g.lanes = (int)cols, g.cols = (int)rows;
   g.out_col = ld_out, g.out_lane = 1;
   g.p_early = early;
-  return gemm<EPI_MICRO>(ctx, c, r, g, st, shares);
+  return gemm<EPI_MICRO>(ctx, c, r, g, st);
 }
 
 bool bad_micro(const void* codes, int64_t ld, const void* scales, int64_t cols) {
@@ -76,9 +82,10 @@ bool micro_too_large(int64_t rows, int64_t cols) { return ceil_div(rows, 128) * 
 
 template <class T>
 int micro_weights(rtopk_matrix* ctx, const T* w, int64_t ld, int64_t n_out, int64_t n_in, int tile, const MicroOut& rows, const MicroOut& cols, cudaStream_t st) {
-  if (tile == 1) return micro_code<T, true, false, false>(ctx, w, ld, n_out, n_in, rows, cols, st);
-  if (!cols.codes) return micro_code<T, true, false, true>(ctx, w, ld, n_out, n_in, rows, cols, st);
-  return micro_code<T, true, true, true>(ctx, w, ld, n_out, n_in, rows, cols, st);
+  const CodeJob<T> job = code_job(w, ld, n_out, n_in, rows, cols);
+  if (tile == 1) return micro_code<true, false, false>(ctx, st, job);
+  if (!cols.codes) return micro_code<true, false, true>(ctx, st, job);
+  return micro_code<true, true, true>(ctx, st, job);
 }
 
 constexpr int kFewSmem = 96 * 1024;
@@ -99,7 +106,7 @@ int micro_product(rtopk_matrix* ctx, const T* x, int64_t ld_x, const MicroOut& w
   }
   Carve c{ctx->scratch};
   MicroScratch s(c, tokens, n_out, n_in);
-  MAT_TRY((micro_code<T, true, false, false>(ctx, x, ld_x, tokens, n_in, s.x_rows, s.x_rows, st)));
+  MAT_TRY((micro_code<true, false, false>(ctx, st, code_job(x, ld_x, tokens, n_in, s.x_rows, MicroOut{}))));
   return micro_gemm(ctx, true, false, s.x_rows, tokens, w, n_out, n_in, out, sizeof(T) == 2, ld_out, st);
 }
 
@@ -108,11 +115,15 @@ int micro_gradients(rtopk_matrix* ctx, const T* dy, int64_t ld_dy, const T* x, i
                     void* dw, int dw_bf16, int64_t ld_dw, cudaStream_t st) {
   Carve c{ctx->scratch};
   MicroScratch s(c, tokens, n_out, n_in);
-  if (dw) MAT_TRY((micro_code<T, false, true, false>(ctx, x, ld_x, tokens, n_in, s.x_cols, s.x_cols, st)));
-  if (dx && dw) MAT_TRY((micro_code<T, true, true, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
-  else if (dx) MAT_TRY((micro_code<T, true, false, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
-  else MAT_TRY((micro_code<T, false, true, false>(ctx, dy, ld_dy, tokens, n_out, s.dy_rows, s.dy_cols, st)));
-  if (dx) MAT_TRY(micro_gemm(ctx, true, false, s.dy_rows, tokens, w_t, n_in, n_out, dx, sizeof(T) == 2, ld_dx, st, dw != nullptr));
+  const CodeJob<T> dy_job = code_job(dy, ld_dy, tokens, n_out, dx ? s.dy_rows : MicroOut{}, dw ? s.dy_cols : MicroOut{});
+  if (dw) {      // both in one launch
+    const CodeJob<T> x_job = code_job(x, ld_x, tokens, n_in, MicroOut{}, s.x_cols);
+    if (dx) MAT_TRY((micro_code<true, true, false>(ctx, st, dy_job, &x_job)));
+    else MAT_TRY((micro_code<false, true, false>(ctx, st, dy_job, &x_job)));
+  } else {
+    MAT_TRY((micro_code<true, false, false>(ctx, st, dy_job)));
+  }
+  if (dx) MAT_TRY(micro_gemm(ctx, true, false, s.dy_rows, tokens, w_t, n_in, n_out, dx, sizeof(T) == 2, ld_dx, st));
   // The second product does not depend on the first and starts as SMs fall free.
   if (dw) MAT_TRY(micro_gemm(ctx, false, dx != nullptr, s.dy_cols, n_out, s.x_cols, n_in, tokens, dw, dw_bf16, ld_dw, st));
   return RTOPK_OK;
@@ -325,7 +336,7 @@ int rtopk_micro_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy, cons
   if (dx && ((tokens && bad_view(dx, elem(dtype), 1, tokens, n_in, ld_dx, 0)) || bad_micro(codes_t, ld_t, scales_t, n_out))) return RTOPK_ERR_INVALID_ARG;
   if (dw && (bad_dtype(dw_dtype) || bad_view(dw, elem(dw_dtype), 1, n_out, n_in, ld_dw, 0) || (tokens && bad_view(x, elem(dtype), 1, tokens, n_in, ld_x, 0))))
     return RTOPK_ERR_INVALID_ARG;
-  if (micro_too_large(tokens, std::max(n_in, n_out))) return RTOPK_ERR_UNSUPPORTED;
+  if (micro_too_large(tokens, n_in + n_out + 128)) return RTOPK_ERR_UNSUPPORTED;
   int64_t need = 0;
   rtopk_micro_scratch(tokens, n_out, n_in, &need);
   if (tokens && need > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;

@@ -181,8 +181,7 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
 // of 256, 257 and 258 us the whole operator; of four 1500 x 6000, eight tiles of 256 or sixteen of 128, 1350 and 1420 us.
 //
 // 4-bit codes have figures of their own: their steps hold twice the codes, their results no factors.  Fitted to 140 shapes from 9 x 256 -> 256 to
-// 8192 x 4096 -> 8192 in every tile and up to four parts: the choice is 1.4 % slower than the best on average.  shares: another product
-// runs beside this one on the SMs that it leaves, so that what counts is time times SMs.
+// 8192 x 4096 -> 8192 in every tile and up to four parts: the choice is 1.4 % slower than the best on average.
 //
 // Contractions beyond kStepsMax steps are cut further, as far as their parts fit the scratch, in several waves if need be: the tensor core
 // drops what falls below its accumulator's last bit, which in 4096 instructions takes up to 2.5e-4 of a sum of equal terms; the
@@ -193,7 +192,7 @@ constexpr int64_t kStepsMax = 1024;
 template <int kEpi>
 constexpr int kWidest = is_micro(kEpi) ? 192 : 256;
 template <int kEpi>
-int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, cudaStream_t st, bool shares = false) {
+int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, cudaStream_t st) {
   constexpr bool kMicro = is_micro(kEpi);
   constexpr double kColumn = kEpi == EPI_CODED ? 35 : kEpi == EPI_GRAM ? 45 : 75;
   const int64_t steps = ceil_div((int64_t)g.depth * (kEpi == EPI_CODED || kMicro ? 1 : 2), kDepthBytes);
@@ -211,8 +210,7 @@ int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, c
         const double here = (double)std::min<int64_t>(cols, g.cols), pair = blocks - 1;
         const double main = (double)ceil_div(steps, split) * std::max(stage_bytes / 90.0, cols * 2.0) + 1000 * pair, tail = here * column;
         const double t = main + tail + (waves - 1) * std::max(main, 0.3 * tail) + 2000 * pair + (split > 1 ? here * (2.0 + 16.0 * split) + 6000 : 0);
-        const double cost = shares ? t * (double)std::min(all * split, sms) * blocks : t;
-        if (cost < best) best = cost, which = id, parts = split;
+        if (t < best) best = t, which = id, parts = split;
         continue;
       }
       const double main = (double)ceil_div(steps, split) * std::max(stage_bytes / 64.0, cols * 2.0) + 500, tail = cols * kColumn;

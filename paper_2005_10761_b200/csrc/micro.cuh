@@ -137,12 +137,29 @@ __device__ __forceinline__ void forget(Eight<__nv_bfloat16>& e) { asm volatile("
 // thread eight neighbours in each of eight rows: the maxima along rows meet in four lanes, those along columns in the other four, and the
 // codes of both directions are whole words.  Past the matrix's end codes and scales are zero; a row's codes are written up to a
 // whole number of blocks.
+// Up to two matrices in one launch: the first `tiles` blocks take the first.
+template <class T>
+struct CodeJob {
+  const T* src;
+  int64_t ld;
+  int rows, cols, vec, tiles_c;
+  MicroOut by_row, by_col;      // without codes: not asked for (where the kernel has both)
+};
+
 template <class T, bool kRows, bool kColumns, bool kTile>
 __global__ void __launch_bounds__(256)
-k_micro_code(const T* src, int64_t ld, int rows, int cols, int vec, int tiles_c, const __grid_constant__ MicroOut by_row, const __grid_constant__ MicroOut by_col) {
+k_micro_code(const __grid_constant__ CodeJob<T> first, const __grid_constant__ CodeJob<T> second, int tiles) {
   __shared__ uint32_t col_codes[kColumns ? 128 : 1][17];
   __shared__ __align__(16) uint8_t row_scales[512], col_scales[512];
-  const int tile_r = blockIdx.x / tiles_c, tile_c = blockIdx.x - tile_r * tiles_c;
+  const bool in_first = (int)blockIdx.x < tiles;
+  const CodeJob<T>& job = in_first ? first : second;
+  const T* src = job.src;
+  const int64_t ld = job.ld;
+  const int rows = job.rows, cols = job.cols, vec = job.vec, tiles_c = job.tiles_c;
+  const MicroOut by_row = job.by_row, by_col = job.by_col;
+  const bool along_rows = kRows && (!kColumns || by_row.codes);
+  const int tile = in_first ? blockIdx.x : blockIdx.x - tiles;
+  const int tile_r = tile / tiles_c, tile_c = tile - tile_r * tiles_c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cl = lane & 7, rl = lane >> 3;
   const int wr = (warp & 3) * 32, wc = (warp >> 2) * 64;       // the warp's place in the tile
   const int r0 = tile_r * 128 + wr + rl * 8, c0 = tile_c * 128 + wc + cl * 8;
@@ -162,7 +179,7 @@ k_micro_code(const T* src, int64_t ld, int rows, int cols, int vec, int tiles_c,
   if constexpr (kTile) {
     shared = micro_scale(Magnitudes<T>::all(e));
   }
-  if constexpr (kRows) {
+  if (along_rows) {
     uint32_t s[8];
     if constexpr (!kTile) Magnitudes<T>::rows(e, s);
     uint8_t* out = by_row.codes + (int64_t)r0 * by_row.ld + c0 / 2;
@@ -200,7 +217,7 @@ k_micro_code(const T* src, int64_t ld, int rows, int cols, int vec, int tiles_c,
   __syncthreads();
   // Scales in whole pieces of 512 bytes; where the last piece along a row has an even number, an empty one follows.
   const int pieces_c = (cols + 255) / 256 * 2, pieces_r = (rows + 255) / 256 * 2;
-  if (kRows && threadIdx.x < 32) {
+  if (along_rows && threadIdx.x < 32) {
     uint4* to = (uint4*)(by_row.scales + ((int64_t)tile_r * pieces_c + tile_c) * 512) + threadIdx.x;
     to[0] = ((const uint4*)row_scales)[threadIdx.x];
     if (tile_c + 1 == tiles_c && tiles_c < pieces_c) to[32] = make_uint4(0u, 0u, 0u, 0u);
