@@ -43,7 +43,8 @@ int64_t code_tiles(const CodeJob<T>& j) { return j.tiles_c * ceil_div(j.rows, 12
 template <bool kRows, bool kColumns, bool kTile, class T>
 int micro_code(rtopk_matrix* ctx, cudaStream_t st, const CodeJob<T>& job, const CodeJob<T>* second = nullptr) {
   const int64_t tiles = code_tiles(job), all = tiles + (second ? code_tiles(*second) : 0);
-  return launch(ctx, k_micro_code<T, kRows, kColumns, kTile>, dim3((unsigned)all), 256, 0, st, job, second ? *second : job, tiles);
+  if (job.vec && (!second || second->vec)) return launch(ctx, k_micro_code<T, kRows, kColumns, kTile, true>, dim3((unsigned)all), 256, 0, st, job, second ? *second : job, tiles);
+  return launch(ctx, k_micro_code<T, kRows, kColumns, kTile, false>, dim3((unsigned)all), 256, 0, st, job, second ? *second : job, tiles);
 }
 
 // out[r][c] = sum over the contraction of row r of `rows` and row c of `cols`.  Results whose rows start on multiples of 32 bytes are written

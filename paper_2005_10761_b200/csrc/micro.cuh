@@ -132,6 +132,45 @@ struct Magnitudes<__nv_bfloat16> {
 __device__ __forceinline__ void forget(Eight<float>&) {}
 __device__ __forceinline__ void forget(Eight<__nv_bfloat16>& e) { asm volatile("" : "+r"(e.w[0]), "+r"(e.w[1]), "+r"(e.w[2]), "+r"(e.w[3])); }
 
+// Eight neighbours of a row without alignment, of which `left` exist (the others count as zero): the aligned vectors that hold any of them
+// are read whole and shifted.  Loads of single values would touch a sector for each lane; words copied to shared memory one by one took
+// 79 us for 7124 x 7499 binary32 values, this takes WHAT.
+__device__ __forceinline__ uint4 vector_if(const uint4* p, bool there) { return there ? *p : make_uint4(0u, 0u, 0u, 0u); }
+template <class T>
+struct Shifted {
+  static constexpr int kVectors = sizeof(T) == 4 ? 3 : 2;
+  uint4 v[kVectors];
+  uint32_t m;      // bytes of the first vector before the first value
+  __device__ __forceinline__ void load(const T* p, int left) {
+    m = (uint32_t)(uintptr_t)p & 15u;
+    const uint4* at = (const uint4*)((uintptr_t)p & ~(uintptr_t)15);
+    const int bytes = left > 0 ? (int)m + min(left, 8) * (int)sizeof(T) : 0;      // up to the last one, from the first vector's start
+#pragma unroll
+    for (int k = 0; k < kVectors; ++k) v[k] = vector_if(at + k, bytes > 16 * k);
+  }
+  __device__ __forceinline__ void shift(int left, Eight<T>& e) const {
+    uint32_t w[4 * kVectors];
+    memcpy(w, v, sizeof w);
+    constexpr int kWords = 2 * (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < kWords + 2; ++i) w[i] = m & 8u ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < kWords + 1; ++i) w[i] = m & 4u ? w[i + 1] : w[i];
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t half = m & 2u ? 0x5432u : 0x3210u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __byte_perm(w[i], w[i + 1], half);
+    }
+    if (left < 8)
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        if (sizeof(T) == 4) w[i] = i < left ? w[i] : 0u;
+        else if (2 * i + 1 >= left) w[i] &= 2 * i < left ? 0xFFFFu : 0u;
+      }
+    memcpy(&e, w, sizeof e);
+  }
+};
+
 // Codes of a tile of 128 x 128 values along its rows (blocks of 32 columns) and, transposed, along its columns (blocks of 32
 // rows), the values read once.  kTile: one scale for each 32 x 32 values, the same codes both ways.  A warp takes 32 rows and 64 columns, a
 // thread eight neighbours in each of eight rows: the maxima along rows meet in four lanes, those along columns in the other four, and the
@@ -146,11 +185,13 @@ struct CodeJob {
   MicroOut by_row, by_col;      // without codes: not asked for (where the kernel has both)
 };
 
-template <class T, bool kRows, bool kColumns, bool kTile>
+// kAligned: both matrices' rows start on multiples of 16 bytes.
+template <class T, bool kRows, bool kColumns, bool kTile, bool kAligned>
 __global__ void __launch_bounds__(256)
 k_micro_code(const __grid_constant__ CodeJob<T> first, const __grid_constant__ CodeJob<T> second, int tiles) {
   __shared__ uint32_t col_codes[kColumns ? 128 : 1][17];
   __shared__ __align__(16) uint8_t row_scales[512], col_scales[512];
+  constexpr int kTogether = sizeof(T) == 4 ? 4 : 8;
   const bool in_first = (int)blockIdx.x < tiles;
   const CodeJob<T>& job = in_first ? first : second;
   const T* src = job.src;
@@ -167,13 +208,24 @@ k_micro_code(const __grid_constant__ CodeJob<T> first, const __grid_constant__ C
   launch_wait();
   launch_next();
   Eight<T> e[8];
-  if (whole && vec) {
+  if (kAligned && whole) {
     const T* p = src + (int64_t)r0 * ld + c0;
 #pragma unroll
     for (int i = 0; i < 8; ++i, p += ld) e[i].load(p, 8, true);
-  } else {
+  } else if (kAligned || vec) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e[i].load(src + (int64_t)min(r0 + i, rows - 1) * ld + min(c0, cols - 1), r0 + i < rows ? cols - c0 : 0, vec);
+    for (int i = 0; i < 8; ++i) e[i].load(src + (int64_t)min(r0 + i, rows - 1) * ld + min(c0, cols - 1), r0 + i < rows ? cols - c0 : 0, true);
+  } else {
+    const T* p = src + (int64_t)r0 * ld + c0;
+#pragma unroll
+    for (int h = 0; h < 8; h += kTogether) {      // rows whose loads are all under way before the first is used
+      Shifted<T> v[kTogether];
+#pragma unroll
+      for (int i = 0; i < kTogether; ++i, p += ld) v[i].load(p, r0 + h + i < rows ? cols - c0 : 0);
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < kTogether; ++i) v[i].shift(r0 + h + i < rows ? cols - c0 : 0, e[h + i]);
+    }
   }
   uint32_t shared = 0u;
   if constexpr (kTile) {
