@@ -687,6 +687,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_back_rows(cons
     for (int j = 0; j < 8; ++j) g[j] *= gamma[kWeights ? i : 0][j];
   };
   auto results = [&](int k, int stage, int row, float rstd, float shift) {
+    if (!to_residual && !to_x) return;
     const float2 p = lane < warps ? part[k & 1][pipe.group * warps + lane] : make_float2(0.f, 0.f);
     // rstd (g - mean(g) - h mean(g h)) = rstd g + (along h + level)
     const float along = -rstd * (warp_sum(p.y) * share), level = -rstd * (warp_sum(p.x) * share);

@@ -211,12 +211,15 @@ class Mask:
         if isinstance(step, torch.Tensor):
             if step.dtype != torch.int32 or step.numel() != 1:
                 raise ValueError("step must be a number or one int32")
-            self._struct.step, self._struct.step_ptr = 0, step.data_ptr()
+            self._struct.step = 0
         else:
             if not 0 <= step < 1 << 32:
                 raise ValueError("step must be a number of 32 bits")
             self._struct.step, self._struct.step_ptr = step, None
         self._step = step
+
+    def __reduce__(self):
+        return Mask, (self.p, self.seed, self._step, self.worker, self.site)
 
 
 class MatrixContext:
@@ -448,7 +451,7 @@ class MatrixContext:
         if mask is None:
             return None
         if isinstance(mask._step, torch.Tensor):
-            self._on_device(mask._step, "the mask's step")
+            mask._struct.step_ptr = self._on_device(mask._step, "the mask's step")
         return C.byref(mask._struct)
 
     def _like(self, t, what: str, dtype, shape):

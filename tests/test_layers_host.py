@@ -99,6 +99,10 @@ def test_a_mask_reaches_the_library_as_it_is_when_the_call_is_made():
     word = torch.zeros(1, dtype=torch.int32)
     mask.step = word
     ctx.dropout(x, x, mask)
+    for copied in (copy.deepcopy(mask), pickle.loads(pickle.dumps(mask))):
+        seen_before = len(seen)
+        ctx.dropout(x, x, copied)
+        assert seen.pop(seen_before)[2] == copied.step.data_ptr() != word.data_ptr()
     assert seen == [(0.25, (1 << 64) - 1, None, 7, 3, 2), (0.25, (1 << 64) - 1, None, 8, 3, 2), (0.25, (1 << 64) - 1, word.data_ptr(), 0, 3, 2)]
     assert ctypes.sizeof(mask._struct) == 40
 
