@@ -255,7 +255,7 @@ template <class T>
 int layer_norm_gradients(rtopk_matrix* ctx, const NormBackArgs<T>& a, float* dgamma, float* dbeta, bool vec, cudaStream_t st) {
   Carve c{ctx->scratch};
   float* parts = dgamma || dbeta ? NormScratch(c, a.rows, a.cols).parts : nullptr;
-  auto join = [&](int64_t count) { return launch(ctx, k_norm_join, dim3((unsigned)ceil_div(2 * (int64_t)a.cols, 32)), 256, 0, st, parts, count, a.cols, dgamma, dbeta); };
+  auto join = [&](int64_t count) { return launch(ctx, k_norm_join, dim3((unsigned)ceil_div(2 * (int64_t)a.cols, 32)), 32 * kJoinSlices, 0, st, parts, count, a.cols, dgamma, dbeta); };
   const RowSplit f(ctx->sms, a.rows, a.cols, kBackMost<T>, vec);
   if (f.fits) {
     MAT_TRY((a.dtotal ? back_rows<T, true>(ctx, a, f, vec, parts, st) : back_rows<T, false>(ctx, a, f, vec, parts, st)));

@@ -829,23 +829,30 @@ __global__ void __launch_bounds__(256) k_norm_columns(const T* dy, int64_t ld_dy
     if (c < cols) parts[((int64_t)blockIdx.y * 2 + k) * cols + c] = v;
   }
 }
-// Adds the parts in binary64: 32 columns a block, eight slices of the parts in turn, then the slices in their order.
-__global__ void __launch_bounds__(256) k_norm_join(const float* parts, int count, int cols, float* dgamma, float* dbeta) {
-  __shared__ double sums[8][32];
+// Adds the parts in binary64: 32 columns a block, 16 slices of the parts, each of whose loads are under way together, then the slices in
+// their order.
+constexpr int kJoinSlices = 16, kJoinTogether = 10;
+__global__ void __launch_bounds__(32 * kJoinSlices) k_norm_join(const float* parts, int count, int cols, float* dgamma, float* dbeta) {
+  __shared__ double sums[kJoinSlices][32];
   const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
   const int64_t i = (int64_t)blockIdx.x * 32 + lane, all = 2 * (int64_t)cols;
   launch_wait();
   launch_next();
   double s = 0.0;
   if (i < all) {
-#pragma unroll 4
-    for (int k = slice; k < count; k += 8) s += parts[k * all + i];
+    for (int k = slice; k < count; k += kJoinSlices * kJoinTogether) {
+      float v[kJoinTogether];
+#pragma unroll
+      for (int j = 0; j < kJoinTogether; ++j) v[j] = k + kJoinSlices * j < count ? parts[(k + kJoinSlices * j) * all + i] : 0.f;
+#pragma unroll
+      for (int j = 0; j < kJoinTogether; ++j) s += v[j];
+    }
   }
   sums[slice][lane] = s;
   __syncthreads();
   if (slice || i >= all) return;
 #pragma unroll
-  for (int k = 1; k < 8; ++k) s += sums[k][lane];
+  for (int k = 1; k < kJoinSlices; ++k) s += sums[k][lane];
   if (i < cols) {
     if (dgamma) dgamma[i] = (float)s;
   } else if (dbeta) {
