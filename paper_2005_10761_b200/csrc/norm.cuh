@@ -223,8 +223,8 @@ struct RowShape {
   static constexpr int kSmem = kStages * kStage;
 };
 
-// kFull (with kVec): the row is just what its warps hold, so that every thread has all of its columns and a row's work is one run of code
-// without branches.
+// kFull (with kVec): the row is just what its warps hold, so that every thread has all of its columns.  With kVec a row's work is one run of code
+// without branches: threads without columns go along with zeros.
 template <class T, bool kVec, bool kFull, int kKeep, int kArrays>
 struct RowPipe : RowShape<T, kVec, kKeep, kArrays> {
   using S = RowShape<T, kVec, kKeep, kArrays>;
@@ -252,6 +252,8 @@ struct RowPipe : RowShape<T, kVec, kKeep, kArrays> {
     fetched = to = 0;
   }
   __device__ __forceinline__ int base(int i) const { return (i * warps + in_row) * kWarpCols; }
+  // Whether piece i is to be worked on: without kVec where the warp has columns of it.
+  __device__ __forceinline__ bool works(int i) const { return kVec || on(i); }
   __device__ __forceinline__ bool on(int i) const { return kFull || has_cols<kVec>(base(i), lane, cols); }
   __device__ __forceinline__ char* place(int stage, int q, int i) const { return mine + stage * kStage + (q * kKeep + i) * kPlanes * kPlane; }
   __device__ __forceinline__ void source(Source& s, const T* p, int64_t ld) { s.p = p + first * ld + (kVec ? base(0) : 0), s.step = ld * step; }
@@ -286,6 +288,15 @@ struct RowPipe : RowShape<T, kVec, kKeep, kArrays> {
     }
   }
   __device__ __forceinline__ void start(int rows) {
+    if constexpr (kVec && !kFull) {      // places that no copy fills: threads without columns go along with zeros
+#pragma unroll
+      for (int i = 0; i < kKeep; ++i)
+        if (!on(i))
+          for (int s = 0; s < kStages; ++s)
+#pragma unroll
+            for (int q = 0; q < kArrays * kPlanes; ++q) *(uint4*)(place(s, q / kPlanes, i) + q % kPlanes * kPlane) = make_uint4(0u, 0u, 0u, 0u);
+      __syncwarp();
+    }
     for (int k = 0; k < rows; ++k) fetch();
   }
   __device__ __forceinline__ void land(const Source& s, int q) {
@@ -332,7 +343,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __g
   if (kResidual) pipe.source(pipe.s1, a.residual, a.ld_r);
   pipe.start(Pipe::kStages);
   constexpr bool kWeights = kKeep == 1 || (kVec && kKeep == 2);      // kept in registers
-  float gamma[kWeights ? kKeep : 1][8], beta[kWeights ? kKeep : 1][8];
+  float gamma[kWeights ? kKeep : 1][8] = {}, beta[kWeights ? kKeep : 1][8] = {};
   auto weights = [&](int i, float (&g)[8], float (&b)[8]) {
     if (a.gamma) load_cols<kVec>(a.gamma, pipe.base(i), lane, a.cols, g);
     if (a.beta) load_cols<kVec>(a.beta, pipe.base(i), lane, a.cols, b);
@@ -365,7 +376,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __g
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
-      if (!pipe.on(i)) continue;
+      if (!pipe.works(i)) continue;
       pipe.values(stage, 0, i, v[i]);
       if (masked) drop_cols<kVec>(a.mask, step, (uint32_t)row, pipe.base(i), lane, v[i]);
       if constexpr (kResidual) {
@@ -375,7 +386,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __g
         for (int j = 0; j < 8; ++j) v[i][j] += r[j];
       }
       sum += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
-      if (to_total) store_cols<T, kVec>(total, pipe.base(i), lane, a.cols, v[i]);
+      if (to_total && pipe.on(i)) store_cols<T, kVec>(total, pipe.base(i), lane, a.cols, v[i]);
     }
     total += total_step;
     pipe.fetch();      // into the place of the row just read
@@ -385,11 +396,11 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __g
     float squares[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
-      if (!pipe.on(i)) continue;
+      if (!pipe.works(i)) continue;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float d = v[i][j] - own;
-        if (kVec || col_of<kVec>(pipe.base(i), lane, j) < a.cols) squares[j & 1] = fmaf(d, d, squares[j & 1]);
+        const float d = (kVec ? pipe.on(i) : col_of<kVec>(pipe.base(i), lane, j) < a.cols) ? v[i][j] - own : 0.f;
+        squares[j & 1] = fmaf(d, d, squares[j & 1]);
       }
     }
     const float all = warp_sum(squares[0] + squares[1]);
@@ -405,13 +416,13 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __g
     }
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
-      if (!pipe.on(i)) continue;
+      if (!pipe.works(i)) continue;
       if constexpr (!kWeights) weights(i, gamma[0], beta[0]);
       const float(&g)[8] = gamma[kWeights ? i : 0], (&b)[8] = beta[kWeights ? i : 0];
       float out[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) out[j] = fmaf((before[i][j] - mean) * rstd, g[j], b[j]);
-      store_cols<T, kVec>(y, pipe.base(i), lane, a.cols, out);
+      if (pipe.on(i)) store_cols<T, kVec>(y, pipe.base(i), lane, a.cols, out);
     }
     y += y_step;
   };
@@ -655,7 +666,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_back_rows(cons
   if (kMore) pipe.source(pipe.s2, a.dtotal, a.ld_dt);
   pipe.start(kVec ? Pipe::kStages - 1 : 1);
   constexpr bool kWeights = kKeep == 1 || (kVec && kKeep == 2);      // kept in registers
-  float gamma[kWeights ? kKeep : 1][8];
+  float gamma[kWeights ? kKeep : 1][8] = {};
   auto weights = [&](int i, float (&g)[8]) {
     if (a.gamma) load_cols<kVec>(a.gamma, pipe.base(i), lane, a.cols, g);
     else
@@ -693,7 +704,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_back_rows(cons
     const float along = -rstd * (warp_sum(p.y) * share), level = -rstd * (warp_sum(p.x) * share);
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
-      if (!pipe.on(i)) continue;
+      if (!pipe.works(i)) continue;
       float g[8], d[8];
       read(stage, i, rstd, shift, g, d);
       weigh(i, g);
@@ -704,10 +715,10 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_back_rows(cons
 #pragma unroll
         for (int j = 0; j < 8; ++j) d[j] += g[j];
       }
-      if (to_residual) store_cols<T, kVec>(dresidual, pipe.base(i), lane, a.cols, d);
+      if (to_residual && pipe.on(i)) store_cols<T, kVec>(dresidual, pipe.base(i), lane, a.cols, d);
       if (to_x) {
         drop_cols<kVec>(a.mask, step, (uint32_t)row, pipe.base(i), lane, d);
-        store_cols<T, kVec>(dx, pipe.base(i), lane, a.cols, d);
+        if (pipe.on(i)) store_cols<T, kVec>(dx, pipe.base(i), lane, a.cols, d);
       }
     }
     if (to_residual) dresidual += dresidual_step;
@@ -726,7 +737,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_back_rows(cons
     float sum[2] = {0.f, 0.f}, along[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kKeep; ++i) {
-      if (!pipe.on(i)) continue;
+      if (!pipe.works(i)) continue;
       float g[8], h[8];
       read(stage, i, rstd, shift, g, h);
 #pragma unroll
