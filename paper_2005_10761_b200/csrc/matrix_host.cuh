@@ -182,6 +182,8 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
 //
 // 4-bit codes have figures of their own: their steps hold twice the codes, their results no factors.  Fitted to 140 shapes from 9 x 256 -> 256 to
 // 8192 x 4096 -> 8192 in every tile and up to four parts: the choice is 1.4 % slower than the best on average.
+// They have no pair of 128 columns: of 63 such shapes and types it was the fastest for three, by 1.1 % at most, and mostly far behind
+// (8192 x 8192 -> 8192, bfloat16: 234 us, in 192 columns 206).
 //
 // Contractions beyond kStepsMax steps are cut further, as far as their parts fit the scratch, in several waves if need be: the tensor core
 // drops what falls below its accumulator's last bit, which in 4096 instructions takes up to 2.5e-4 of a sum of equal terms; the
@@ -220,12 +222,14 @@ int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, c
   };
   consider(0, gemm_tiles<64, false>(g), 64, 1, GemmShape<64, false, kMicro>::kStageBytes);
   consider(1, gemm_tiles<128, false>(g), 128, 1, GemmShape<128, false, kMicro>::kStageBytes);
-  consider(2, gemm_tiles<128, true>(g), 128, 2, GemmShape<128, true, kMicro>::kStageBytes);
+  if constexpr (!kMicro) consider(2, gemm_tiles<128, true>(g), 128, 2, GemmShape<128, true, kMicro>::kStageBytes);
   consider(3, gemm_tiles<kWidest<kEpi>, true>(g), kWidest<kEpi>, 2, GemmShape<kWidest<kEpi>, true, kMicro>::kStageBytes);
   switch (which) {
     case 0: return gemm_tile<64, false, kEpi>(ctx, p, q, g, parts, st);
     case 1: return gemm_tile<128, false, kEpi>(ctx, p, q, g, parts, st);
-    case 2: return gemm_tile<128, true, kEpi>(ctx, p, q, g, parts, st);
+    case 2:      // never chosen for 4-bit codes
+      if constexpr (!kMicro) return gemm_tile<128, true, kEpi>(ctx, p, q, g, parts, st);
+      [[fallthrough]];
     default: return gemm_tile<kWidest<kEpi>, true, kEpi>(ctx, p, q, g, parts, st);
   }
 }
@@ -234,7 +238,8 @@ template <int kEpi>
 cudaError_t allow_smem() {
   cudaError_t e = cudaFuncSetAttribute(k_gemm<64, false, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<64, false, is_micro(kEpi)>::kSmem);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<128, false, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<128, false, is_micro(kEpi)>::kSmem);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<128, true, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<128, true, is_micro(kEpi)>::kSmem);
+  if constexpr (!is_micro(kEpi))
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<128, true, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<128, true, is_micro(kEpi)>::kSmem);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(k_gemm<kWidest<kEpi>, true, kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmShape<kWidest<kEpi>, true, is_micro(kEpi)>::kSmem);
   return e;
 }
