@@ -177,6 +177,9 @@ struct Shifted {
 // codes of both directions are whole words.  Past the matrix's end codes and scales are zero; a row's codes are written up to a
 // whole number of blocks.
 // Up to two matrices in one launch: the first `tiles` blocks take the first.
+//
+// Bound by memory along rows (4096 x 4096 bfloat16 11 us from DRAM under a profiler), both ways by the instructions, issued in 70 % of the cycles
+// (two such matrices, one of them both ways, 20 us).
 template <class T>
 struct CodeJob {
   const T* src;
@@ -299,6 +302,8 @@ k_micro_code(const __grid_constant__ CodeJob<T> first, const __grid_constant__ C
 // A code is looked up as a byte, twice its value plus 12: one byte permutation takes four codes as selectors into the eight bytes of a table,
 // in which a code's sign bit asks for a byte's sign instead, 0 here; so the positive codes come from one table, the negative ones, their
 // sign bits turned round, from another, and the two are or'ed.  The 12 is taken off the sum: 12 times the sum of the token's codes.
+// 1 token through 1500 -> 6000 takes 5.7 us, most of it the call; through 8192 -> 8192 12.2 (36 MB of codes and scales: 5.5 at memory's rate),
+// where the look-ups and products are half of the cycles.
 constexpr int kFewTokens = 4, kFewAhead = 2;
 constexpr uint32_t kFewPositive0 = 0x0F0E0D0Cu, kFewPositive1 = 0x18141210u, kFewNegative0 = 0x090A0B0Cu, kFewNegative1 = 0x00040608u;
 __device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t selectors) {
