@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librtopk.so")
 SOURCES = ["rtopk.cu", "matrix.cu", "layers.cu"]
 HEADERS = ["common.cuh", "element.cuh", "select.cuh", "stream.cuh", "sampler.cuh", "aggregate.cuh", "codec.cuh", "threshold.cuh", "finish.cuh",
-           "tensorcore.cuh", "gemm.cuh", "matrix_host.cuh", "values.cuh", "coded.cuh", "orthogonal.cuh", "micro.cuh", "norm.cuh"]
+           "tensorcore.cuh", "gemm.cuh", "matrix_host.cuh", "grids.h", "values.cuh", "coded.cuh", "orthogonal.cuh", "micro.cuh", "norm.cuh"]
 
 
 def nvcc() -> str:

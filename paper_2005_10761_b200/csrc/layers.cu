@@ -156,13 +156,9 @@ template <class T>
 int dropout(rtopk_matrix* ctx, const T* x, int64_t ld_x, int64_t rows, int64_t cols, const Mask& mask, T* out, int64_t ld_out, cudaStream_t st) {
   const bool vec = whole_vectors(x, sizeof(T), cols, ld_x) && whole_vectors(out, sizeof(T), cols, ld_out);
   const int64_t units = ceil_div(cols, vec ? 8 : kWarpCols), per = vec ? 256 : 8;      // of four rows: threads or warps; of a block
-  const int64_t band = std::min(up(rows, 4), ((int64_t(1) << 31) / units - 256) / 4 * 4);      // rows whose units 31 bits count
-  if (ceil_div(rows, band) > 65535) return RTOPK_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)ceil_div(band / 4 * units, per), (unsigned)ceil_div(rows, band));
-  Divisor d = {0, (uint32_t)units, 0};
-  while (units > int64_t(2) << d.shift) ++d.shift;
-  d.m = (uint32_t)((uint64_t(1) << (32 + d.shift)) / units + 1);
-  return launch(ctx, vec ? k_dropout<T, true> : k_dropout<T, false>, grid, 256, 0, st, x, ld_x, rows, cols, band, d, mask, out, ld_out);
+  const DropoutGrid f(rows, units, per);
+  if (f.bands > 65535) return RTOPK_ERR_UNSUPPORTED;
+  return launch(ctx, vec ? k_dropout<T, true> : k_dropout<T, false>, dim3((unsigned)f.blocks, (unsigned)f.bands), 256, 0, st, x, ld_x, rows, cols, f.band, divisor((uint32_t)units), mask, out, ld_out);
 }
 
 // How a block takes rows: `warps` warps for each, `keep` pieces of 256 columns a warp, `rows_per` rows at a time.  Two pieces, so that what is

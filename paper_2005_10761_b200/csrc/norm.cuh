@@ -9,6 +9,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "grids.h"
 #include "values.cuh"
 
 namespace rtopk {
@@ -149,9 +150,6 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
 }
 
 // ----------------------------------------------------------------------------- dropout
-// Quotients of numbers below 2^31 by d: (k m / 2^32) / 2^shift with m = floor(2^(32 + shift) / d) + 1, 2^shift < d <= 2^(shift + 1); m is
-// off by less than 1, which k times 2^-(32 + shift) keeps below 1 / d.
-struct Divisor { uint32_t m, d; int shift; };
 __device__ __forceinline__ uint32_t divide(uint32_t k, const Divisor& v) { return v.d == 1 ? k : __umulhi(k, v.m) >> v.shift; }
 
 // Four rows at a time: a thread takes eight neighbouring columns of them (kVec), or a warp 256, so that what the generator's first
