@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_layers import rt  # noqa: F401
+from test_gpu_layers import TYPES, U, back64, close, normal, rounding, rt  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -48,4 +48,32 @@ def test_dropout_of_very_wide_rows(rt, ty, rows, cols):  # noqa: F811
         assert abs(dropped - p * cols) < 8 * (p * (1 - p) * cols) ** 0.5
     ctx.dropout(x, x, spec)
     assert torch.equal(x, out)
+    ctx.close()
+
+
+# ------------------------------------------------------------------------------------------------- large means
+@pytest.mark.parametrize("rows,cols", [(700, 200), (64, 256), (700, 1500), (300, 1504), (170, 4096), (170, 4099), (160, 10000), (40, 16384), (5, 20001)])
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("far", [10.0, 1000.0])
+def test_layer_norm_gradients_of_rows_with_large_means(rt, rows, cols, ty, far):  # noqa: F811
+    """With mean and rstd given, h = (total - mean) rstd has two roundings: it is within 2 u of itself, whatever the mean is."""
+    total = (normal(rows, cols) + far * (1 + normal(rows, 1, seed=2).abs())).to(ty)
+    dy, gamma = normal(rows, cols, seed=1).to(ty), 1 + 0.3 * normal(cols, seed=3)
+    mean = total.double().mean(1).float()
+    rstd = (total.double().var(1, correction=0) + 1e-5).rsqrt().float()
+    ctx = rt.MatrixContext(rt.layer_norm_scratch(rows, cols))
+    dr, dgamma, dbeta = torch.full((rows, cols), 7.0, dtype=ty, device="cuda"), torch.full((cols,), 7.0, device="cuda"), torch.full((cols,), 7.0, device="cuda")
+    ctx.layer_norm_gradients(dy, total, mean, rstd, gamma, dr, dgamma=dgamma, dbeta=dbeta)
+    d, _, wg, wb = back64(dy, total, mean, rstd, gamma, None, None)
+    r = rstd.double()[:, None]
+    h = (total.double() - mean.double()[:, None]) * r
+    gg, eh = (dy.double() * gamma.double()).abs(), 2.01 * U * h.abs()
+    adds = (64 + cols / 4096) * U
+    along = (gg * h.abs()).mean(1, keepdim=True)
+    tol = r * (4 * U * gg + adds * gg.mean(1, keepdim=True) + h.abs() * (adds * along + (gg * eh).mean(1, keepdim=True)) + eh * along)
+    tol = tol + 4 * U * d.abs() + 4 * U * r * (gg + along * h.abs())
+    close(dr, d, tol + rounding(ty, d), "dresidual")
+    adds = (64 + rows / 4096) * U
+    close(dgamma, wg.sum(0), adds * wg.abs().sum(0) + (dy.double().abs() * eh).sum(0) + U * wg.sum(0).abs(), "dgamma")
+    close(dbeta, wb.sum(0), adds * wb.abs().sum(0), "dbeta")
     ctx.close()
