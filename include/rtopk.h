@@ -673,7 +673,9 @@ int rtopk_dropout(rtopk_matrix* ctx, const void* x, int dtype, int64_t ld_x, int
  *   gamma, beta  cols binary32 each, may be null (1 and 0);
  *   total [out]  t rounded to dtype, may be null;   mean, rstd [out]  rows binary32 each, may be null.  Both are of t before it is rounded.
  * x, residual, out, total rows x cols of dtype; out and total may each be x or residual itself, with its row stride.  eps finite, >= 0.
- * A row with a NaN or an infinity gives NaN.  Needs no scratch.  Errors: INVALID_ARG, CUDA.
+ * A row with a NaN or an infinity gives NaN.  So does a row whose sum leaves binary32; where only the squares of t - mean do, rstd is 0
+ * and out is beta.  With eps = 0 a row whose variance comes out as 0, like one of zeros, has the rstd infinity and gives NaN.
+ * Needs no scratch.  Errors: INVALID_ARG, CUDA.
  */
 int rtopk_layer_norm(rtopk_matrix* ctx, const void* x, int64_t ld_x, const void* residual, int64_t ld_r, int dtype, int64_t rows,
                      int64_t cols, const float* gamma, const float* beta, float eps, const rtopk_mask* mask, void* out, int64_t ld_out,

@@ -135,10 +135,11 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int k = 16; k; k >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, k);
   return v;
 }
-// 1 / sqrt(v), the approximation improved by one Newton step: within 2 steps of binary32.
+// 1 / sqrt(v), the approximation improved by one Newton step: within 2 steps of binary32.  0 of infinity and infinity of 0: there the step's
+// residual is NaN, of which fminf makes a number that changes neither.
 __device__ __forceinline__ float inverse_root(float v) {
   const float r = rsqrtf(v);
-  return fmaf(r * fmaf(-v * r, r, 1.f), 0.5f, r);
+  return fmaf(r * fminf(fmaf(-v * r, r, 1.f), 1.f), 0.5f, r);
 }
 // The sum over the block; `part` has a place for each warp and is used once between two barriers.
 __device__ __forceinline__ float row_sum(float v, float* part) {

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_layers import TYPES, U, back64, close, normal, rounding, rt  # noqa: F401
+from test_gpu_layers import TYPES, U, back64, close, norm64, normal, rounding, rt  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -76,4 +76,45 @@ def test_layer_norm_gradients_of_rows_with_large_means(rt, rows, cols, ty, far):
     adds = (64 + rows / 4096) * U
     close(dgamma, wg.sum(0), adds * wg.abs().sum(0) + (dy.double().abs() * eh).sum(0) + U * wg.sum(0).abs(), "dgamma")
     close(dbeta, wb.sum(0), adds * wb.abs().sum(0), "dbeta")
+    ctx.close()
+
+
+# ------------------------------------------------------------------------------------------------- the ends of the range
+@pytest.mark.parametrize("cols", [1, 200, 1500, 1504, 10000, 20001])
+@pytest.mark.parametrize("ty", TYPES)
+def test_layer_norm_at_the_ends_of_the_range(rt, cols, ty):  # noqa: F811
+    """1 / sqrt is 0 of infinity and infinity of 0: finite rows whose squares leave binary32 come out as beta, and without an eps a row whose
+    variance is 0 has an infinite rstd, and no results."""
+    ctx = rt.MatrixContext(rt.layer_norm_scratch(4, cols))
+    x = normal(4, cols).to(ty)
+    x[1] = torch.where(torch.arange(cols, device="cuda") % 2 == 0, 3e30, -3e30).to(ty)
+    x[2] = 3.0
+    gamma, beta = 1 + 0.3 * normal(cols, seed=3), normal(cols, seed=4)
+    y, mean, rstd = torch.empty_like(x), torch.empty(4, device="cuda"), torch.empty(4, device="cuda")
+    for eps in (1e-5, 0.0):
+        ctx.layer_norm(x, gamma, beta, y, mean=mean, rstd=rstd, eps=eps)
+        if cols > 1:
+            assert float(rstd[1]) == 0.0 and bool(mean[1].isfinite())
+            assert torch.equal(y[1], beta.to(ty))
+        if eps == 0.0:      # equal values: mean and differences are within adds u of them, so the variance is at most the square of that
+            adds = 64 + cols / 4096
+            assert float(rstd[2]) >= (1 - adds * U) / (adds * U * 3)
+        if cols > 1:
+            for i in (0, 3):
+                t, m, r, h, want = norm64(x[i:i + 1], None, gamma, beta, eps, None)
+                adds = 64 + cols / 4096
+                d = adds * U * t.abs().amax(1) * r
+                close(rstd[i:i + 1], r, r * (2 * d + adds * U))
+                tol = gamma.double().abs() * (d[:, None] * (1 + 2 * h.abs()) + 64 * U * h.abs()) + 4 * U * want.abs() + 4 * U * (h * gamma.double()).abs()
+                close(y[i:i + 1], want, tol + rounding(ty, want))
+    x[2] = 0.0
+    ctx.layer_norm(x, gamma, beta, y, rstd=rstd, eps=0.0)
+    assert float(rstd[2]) == float("inf") and bool(y[2].isnan().all())
+    # the gradients of the rows with rstd = 0: what reaches t on its other way, and nothing for gamma
+    dy, dt = normal(4, cols, seed=5).to(ty), normal(4, cols, seed=6).to(ty)
+    m1, zero = x[1].double().mean().float().expand(4).contiguous(), torch.zeros(4, device="cuda")
+    dr, dgamma = torch.empty_like(x), torch.empty(cols, device="cuda")
+    rows = x[1:2].expand(4, cols).contiguous()
+    ctx.layer_norm_gradients(dy, rows, m1, zero, gamma, dr, dgamma=dgamma, dtotal=dt)
+    assert torch.equal(dr, dt) and not bool(dgamma.any())
     ctx.close()
