@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(32 * kRowWarps) k_layer_norm_back_long(const _
   const uint32_t step = mask_step(a.mask);
   const T *dy = a.dy + row * a.ld_dy, *total = a.total + row * a.ld_t;
   const float mean = a.mean[row], rstd = a.rstd[row];
-  // g and h of 256 columns; past the end g is zero
+  // g and h of 256 columns, zero past the end
   auto values = [&](const Eight<T>& ey, const Eight<T>& et, int base, float (&g)[8], float (&h)[8]) {
     ey.widen_to(g);
     et.widen_to(h);
@@ -583,7 +583,7 @@ __global__ void __launch_bounds__(32 * kRowWarps) k_layer_norm_back_long(const _
       for (int j = 0; j < 8; ++j) g[j] *= w[j];
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = (h[j] - mean) * rstd;
+    for (int j = 0; j < 8; ++j) h[j] = kVec || col_of<kVec>(base, lane, j) < a.cols ? (h[j] - mean) * rstd : 0.f;
   };
   auto fetch = [&](int base, float (&g)[8], float (&h)[8]) {
     Eight<T> ey, et;
@@ -692,11 +692,15 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_back_rows(cons
   auto read = [&](int stage, int i, float mean, float rstd, float (&g)[8], float (&h)[8]) {
     pipe.values(stage, 0, i, g);
     pipe.values(stage, 1, i, h);
+    if (kVec && !pipe.on(i)) mean = 0.f;      // where there are no columns h is 0 like g, and not what -mean rstd may overflow to
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {      // in pairs, an instruction each: 227 us where single ones took 240 (gradients of 16384 x 8192, bfloat16)
       const float2 two = __fmul2_rn(__fadd2_rn(make_float2(h[j], h[j + 1]), make_float2(-mean, -mean)), make_float2(rstd, rstd));
       h[j] = two.x, h[j + 1] = two.y;
     }
+    if (!kVec && !isfinite(mean * rstd))
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[j] = col_of<kVec>(pipe.base(i), lane, j) < a.cols ? h[j] : 0.f;
   };
   auto weigh = [&](int i, float (&g)[8]) {
     if constexpr (!kWeights) weights(i, gamma[0]);

@@ -118,3 +118,22 @@ def test_layer_norm_at_the_ends_of_the_range(rt, cols, ty):  # noqa: F811
     ctx.layer_norm_gradients(dy, rows, m1, zero, gamma, dr, dgamma=dgamma, dtotal=dt)
     assert torch.equal(dr, dt) and not bool(dgamma.any())
     ctx.close()
+
+
+@pytest.mark.parametrize("cols", [3, 200, 256, 1500, 1504, 10000, 20001])
+@pytest.mark.parametrize("ty", TYPES)
+def test_layer_norm_gradients_of_huge_equal_rows(rt, cols, ty):  # noqa: F811
+    """h is 0 in every column; a column that is not there, with a total of 0, would have -mean rstd, beyond binary32."""
+    rows, rstd = 300, torch.full((300,), 1e6, device="cuda")      # eps = 1e-12
+    total = torch.full((rows, cols), 1e33, device="cuda").to(ty)
+    mean = total[:, 0].float().contiguous()
+    dy = normal(rows, cols, seed=1).to(ty)
+    ctx = rt.MatrixContext(rt.layer_norm_scratch(rows, cols))
+    dr, dgamma, dbeta = torch.empty_like(dy), torch.full((cols,), 7.0, device="cuda"), torch.full((cols,), 7.0, device="cuda")
+    ctx.layer_norm_gradients(dy, total, mean, rstd, None, dr, dgamma=dgamma, dbeta=dbeta)
+    g = dy.double()
+    want = 1e6 * (g - g.mean(1, keepdim=True))
+    close(dr, want, 1e6 * ((64 + cols / 4096) * U * g.abs().mean(1, keepdim=True) + 4 * U * g.abs()) + 4 * U * want.abs() + rounding(ty, want))
+    assert not bool(dgamma.any())
+    close(dbeta, g.sum(0), 65 * U * g.abs().sum(0))
+    ctx.close()
