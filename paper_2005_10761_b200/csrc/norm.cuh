@@ -130,6 +130,7 @@ __device__ __forceinline__ void drop_cols(const Mask& m, uint32_t step, uint32_t
   }
 }
 
+__device__ __forceinline__ float sum8(const float (&v)[8]) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int k = 16; k; k >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, k);
@@ -388,7 +389,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __g
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] += r[j];
       }
-      sum += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
+      sum += sum8(v[i]);
       if (to_total && pipe.on(i)) store_cols<T, kVec>(total, pipe.base(i), lane, a.cols, v[i]);
     }
     total += total_step;
@@ -449,7 +450,9 @@ __global__ void __launch_bounds__(32 * kRowWarps, 1) k_layer_norm_rows(const __g
   results(pipe.count - 1, row - pipe.step);
 }
 
-// Longer rows: a block takes one, each warp kLongKeep pieces of 256 columns in its registers; what is beyond is read again.
+// Longer rows: a block takes one, each warp kLongKeep pieces of 256 columns in its registers; what is beyond is read again.  A thread adds eight
+// values before they join its sum, so that of n columns n / 4096 follow one another there, not n / 512 (2^24 equal values: mean off by
+// up to 6e-5 of itself, not 5e-4).
 constexpr int kLongKeep = 4;
 template <class T, bool kVec>
 __global__ void __launch_bounds__(32 * kRowWarps) k_layer_norm_long(const __grid_constant__ NormArgs<T> a) {
@@ -494,22 +497,22 @@ __global__ void __launch_bounds__(32 * kRowWarps) k_layer_norm_long(const __grid
     const int base = i * span + in_row * kWarpCols;
     if (!has_cols<kVec>(base, lane, a.cols)) break;
     values(ex[i], er[i], base, v[i]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum += v[i][j];
+    sum += sum8(v[i]);
   }
   for (int base = rest; has_cols<kVec>(base, lane, a.cols); base += span) {
     fetch(base, w);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum += w[j];
+    sum += sum8(w);
   }
   const float mean = row_sum(sum, part[0]) / a.cols;
   float squares = 0.f;
   auto add_squares = [&](const float (&v)[8], int base) {
+    float here = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float d = v[j] - mean;
-      if (col_of<kVec>(base, lane, j) < a.cols) squares = fmaf(d, d, squares);
+      if (col_of<kVec>(base, lane, j) < a.cols) here = fmaf(d, d, here);
     }
+    squares += here;
   };
 #pragma unroll
   for (int i = 0; i < kLongKeep; ++i) {
@@ -603,8 +606,10 @@ __global__ void __launch_bounds__(32 * kRowWarps) k_layer_norm_back_long(const _
   const int rest = kLongKeep * span + in_row * kWarpCols;
   float g[8], h[8], sum = 0.f, along = 0.f;
   auto add = [&]() {
+    float here = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += g[j], along = fmaf(g[j], h[j], along);
+    for (int j = 0; j < 8; ++j) here = fmaf(g[j], h[j], here);
+    sum += sum8(g), along += here;
   };
 #pragma unroll
   for (int i = 0; i < kLongKeep; ++i) {

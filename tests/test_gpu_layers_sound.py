@@ -137,3 +137,33 @@ def test_layer_norm_gradients_of_huge_equal_rows(rt, cols, ty):  # noqa: F811
     assert not bool(dgamma.any())
     close(dbeta, g.sum(0), 65 * U * g.abs().sum(0))
     ctx.close()
+
+
+# ------------------------------------------------------------------------------------------------- long rows
+@pytest.mark.parametrize("cols", [(1 << 24) + 8, (1 << 24) + 1])
+def test_long_rows_of_equal_values(rt, cols):  # noqa: F811
+    """Sums of equal terms lose the most: each addition's rounding has the same sign."""
+    rows, v = 2, 0.5141598582267761
+    x = torch.full((rows, cols), v, device="cuda")
+    x[1, 1::2] = -v
+    adds = (64 + cols / 4096) * U
+    ctx = rt.MatrixContext(rt.layer_norm_scratch(rows, cols))
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    ctx.layer_norm(x, None, None, y, mean=mean, rstd=rstd)
+    t, m, r, h, want = norm64(x, None, None, None, 1e-5, None)
+    d = adds * v * r
+    close(mean, m, torch.full_like(m, adds * v), "mean")
+    close(rstd, r, r * (2 * d + adds), "rstd")
+    close(y, want, d[:, None] * (1 + 2 * h.abs()) + 64 * U * h.abs() + 8 * U * want.abs(), "y")
+    # gradients: equal terms in the sums of g, then of g h
+    mean, rstd = m.float(), r.float()
+    dr = torch.empty_like(x)
+    for dy in (torch.full_like(x, v), x):
+        ctx.layer_norm_gradients(dy, x, mean, rstd, None, dr)
+        d, _, _, _ = back64(dy, x, mean, rstd, None, None, None)
+        r1, h = rstd.double()[:, None], (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+        gg = dy.double().abs()
+        eh, along = 2.01 * U * h.abs(), (gg * h.abs()).mean(1, keepdim=True)
+        tol = r1 * (4 * U * gg + adds * gg.mean(1, keepdim=True) + h.abs() * (adds * along + (gg * eh).mean(1, keepdim=True)) + eh * along)
+        close(dr, d, tol + 4 * U * d.abs() + 4 * U * r1 * (gg + along * h.abs()), "dresidual")
+    ctx.close()
