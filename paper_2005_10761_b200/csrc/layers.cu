@@ -10,6 +10,19 @@ using namespace rtopk::mat;
 
 namespace {
 
+// Kernels get their shared memory at a context's first call of their family: each is loaded for that, which took a program's first context 17 ms
+// for all of them, also where it only codes or orthogonalises.
+enum Family : uint32_t { MICRO = 1, NORM = 2, NORM_BACK = NORM << 4 };      // of the normalisation, four each: by type and by what is read
+template <class F>
+int allow_once(rtopk_matrix* ctx, uint32_t family, F allow) {
+  if (ctx->allowed & family) return RTOPK_OK;
+  MAT_CUDA(allow());
+  ctx->allowed |= family;
+  return RTOPK_OK;
+}
+template <class T>
+constexpr uint32_t norm_family(Family first, bool second) { return first << (2 * (sizeof(T) == 2) + second); }
+
 // ----------------------------------------------------------------------------- 4-bit codes
 int64_t micro_ld(int64_t cols) { return up(ceil_div(cols, 2), 16); }                                  // bytes of a row of codes, at least
 int64_t micro_scale_bytes(int64_t rows, int64_t cols) { return ceil_div(rows, 128) * ceil_div(cols, 256) * 1024; }
@@ -94,6 +107,14 @@ template <class T, int kTokens>
 int micro_few(rtopk_matrix* ctx, const T* x, int64_t ld_x, const MicroOut& w, int64_t tokens, int64_t n_out, int64_t n_in, T* out, int64_t ld_out, cudaStream_t st) {
   const dim3 grid((unsigned)std::min<int64_t>(ceil_div(n_out, 128) * 4, 2 * ctx->sms));
   return launch(ctx, k_micro_few<T, kTokens>, grid, 256, few_smem(kTokens, n_in), st, x, ld_x, rows_aligned(x, sizeof(T), 1, ld_x, 0, 16) ? 1 : 0, w, tokens, n_out, n_in, out, ld_out);
+}
+
+cudaError_t allow_micro() {
+  auto few = [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem); };
+  for (const cudaError_t e : {few(k_micro_few<float, 1>), few(k_micro_few<float, 2>), few(k_micro_few<float, 4>), few(k_micro_few<__nv_bfloat16, 1>), few(k_micro_few<__nv_bfloat16, 2>),
+                              few(k_micro_few<__nv_bfloat16, 4>), allow_smem<EPI_MICRO>(), allow_smem<EPI_MICRO_ROWS>()})
+    if (e != cudaSuccess) return e;
+  return cudaSuccess;
 }
 
 template <class T>
@@ -195,10 +216,30 @@ int row_variant(const RowSplit& f, bool vec, F go) {
   }
   return RTOPK_ERR_INTERNAL;
 }
+// For every variant with up to kMost pieces a warp.
+template <class T, int kMost, class F>
+cudaError_t allow_rows(F kernel_of) {
+  cudaError_t worst = cudaSuccess;
+  for (const int keep : {1, 2, 4})
+    for (const int kind : {0, 1, 2}) {      // without alignment, with it, full rows
+      if (keep > (kind ? kMost : 2)) continue;
+      RowSplit f(1, 1, 1, 4, true);
+      f.keep = keep, f.full = kind == 2;
+      row_variant<T, kMost>(f, kind > 0, [&](auto v, auto full, auto k) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel_of(v, full, k), cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem);
+        if (e != cudaSuccess) worst = e;
+        return RTOPK_OK;
+      });
+    }
+  return worst;
+}
+
 template <class T, bool kResidual>
 int norm_rows(rtopk_matrix* ctx, const NormArgs<T>& a, const RowSplit& f, bool vec, cudaStream_t st) {
+  auto kernel_of = [](auto v, auto full, auto keep) { return k_layer_norm_rows<T, v, full, keep, kResidual>; };
+  MAT_TRY(allow_once(ctx, norm_family<T>(NORM, kResidual), [&] { return allow_rows<T, 4>(kernel_of); }));
   return row_variant<T, 4>(f, vec, [&](auto v, auto full, auto keep) {
-    return launch(ctx, k_layer_norm_rows<T, v, full, keep, kResidual>, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, RowShape<T, v, keep, kResidual ? 2 : 1>::kSmem, st, a, f.warps,
+    return launch(ctx, kernel_of(v, full, keep), dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, RowShape<T, v, keep, kResidual ? 2 : 1>::kSmem, st, a, f.warps,
                   f.rows_per);
   });
 }
@@ -216,27 +257,11 @@ template <class T>
 constexpr int kBackMost = sizeof(T) == 2 ? 4 : 2;      // pieces a warp
 template <class T, bool kMore>
 int back_rows(rtopk_matrix* ctx, const NormBackArgs<T>& a, const RowSplit& f, bool vec, float* parts, cudaStream_t st) {
+  auto kernel_of = [](auto v, auto full, auto keep) { return k_layer_norm_back_rows<T, v, full, keep, kMore>; };
+  MAT_TRY(allow_once(ctx, norm_family<T>(NORM_BACK, kMore), [&] { return allow_rows<T, kBackMost<T>>(kernel_of); }));
   return row_variant<T, kBackMost<T>>(f, vec, [&](auto v, auto full, auto keep) {
-    return launch(ctx, k_layer_norm_back_rows<T, v, full, keep, kMore>, dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, kBackSmem<T, v, keep, kMore>, st, a, f.warps, f.rows_per, parts);
+    return launch(ctx, kernel_of(v, full, keep), dim3((unsigned)f.blocks), 32 * f.warps * f.rows_per, kBackSmem<T, v, keep, kMore>, st, a, f.warps, f.rows_per, parts);
   });
-}
-
-template <class T, bool kSecond>
-cudaError_t allow_rows() {
-  cudaError_t worst = cudaSuccess;
-  auto allow = [&](auto kernel) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem);
-    if (e != cudaSuccess) worst = e;
-  };
-  for (const int keep : {1, 2, 4})
-    for (const int kind : {0, 1, 2}) {
-      RowSplit f(1, 1, 1, 4, true);
-      f.keep = keep, f.full = kind == 2;
-      if (keep == 4 && kind == 0) continue;
-      row_variant<T, 4>(f, kind > 0, [&](auto v, auto full, auto k) { return allow(k_layer_norm_rows<T, v, full, k, kSecond>), 0; });
-      if (keep <= kBackMost<T>) row_variant<T, kBackMost<T>>(f, kind > 0, [&](auto v, auto full, auto k) { return allow(k_layer_norm_back_rows<T, v, full, k, kSecond>), 0; });
-    }
-  return worst;
 }
 
 // Ranges of rows whose column sums are formed apart: four blocks for each of 148 SMs, but no fewer than 32 rows each.
@@ -269,14 +294,6 @@ int layer_norm_gradients(rtopk_matrix* ctx, const NormBackArgs<T>& a, float* dga
 }
 
 }  // namespace
-
-cudaError_t rtopk::mat::allow_layers() {
-  auto few = [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem); };
-  for (const cudaError_t e : {few(k_micro_few<float, 1>), few(k_micro_few<float, 2>), few(k_micro_few<float, 4>), few(k_micro_few<__nv_bfloat16, 1>), few(k_micro_few<__nv_bfloat16, 2>),
-                              few(k_micro_few<__nv_bfloat16, 4>), allow_smem<EPI_MICRO>(), allow_smem<EPI_MICRO_ROWS>(), allow_rows<float, false>(), allow_rows<float, true>(), allow_rows<__nv_bfloat16, false>(), allow_rows<__nv_bfloat16, true>()})
-    if (e != cudaSuccess) return e;
-  return cudaSuccess;
-}
 
 extern "C" {
 
@@ -321,6 +338,7 @@ int rtopk_micro_product(rtopk_matrix* ctx, const void* x, int dtype, int64_t ld_
   if (need > ctx->scratch_bytes) return RTOPK_ERR_INVALID_ARG;
   OnDevice on(ctx->device);
   if (!on.ok) return fail(ctx, cudaErrorInvalidDevice);
+  MAT_TRY(allow_once(ctx, MICRO, allow_micro));
   const MicroOut w = as_micro(codes, ld_codes, scales);
   if (dtype == RTOPK_F32) return micro_product(ctx, (const float*)x, ld_x, w, tokens, n_out, n_in, (float*)out, ld_out, (cudaStream_t)stream);
   return micro_product(ctx, (const __nv_bfloat16*)x, ld_x, w, tokens, n_out, n_in, (__nv_bfloat16*)out, ld_out, (cudaStream_t)stream);
@@ -344,6 +362,7 @@ int rtopk_micro_gradients(rtopk_matrix* ctx, const void* dy, int64_t ld_dy, cons
     if (dw) MAT_CUDA(cudaMemset2DAsync(dw, ld_dw * elem(dw_dtype), 0, n_in * elem(dw_dtype), n_out, st));
     return RTOPK_OK;
   }
+  MAT_TRY(allow_once(ctx, MICRO, allow_micro));
   const MicroOut w_t = as_micro(codes_t, ld_t, scales_t);
   if (dtype == RTOPK_F32)
     return micro_gradients(ctx, (const float*)dy, ld_dy, (const float*)x, ld_x, w_t, tokens, n_out, n_in, (float*)dx, ld_dx, dw, dw_dtype == RTOPK_BF16, ld_dw, st);

@@ -253,8 +253,7 @@ int rtopk_matrix_create(rtopk_matrix** out, int device, void* scratch, int64_t s
                              allow_smem<EPI_GRAM>() != cudaSuccess || allow_smem<EPI_POLY>() != cudaSuccess || allow_smem<EPI_APPLY>() != cudaSuccess ||
                              allow_smem<EPI_OUT>() != cudaSuccess || allow_smem<EPI_UPDATE>() != cudaSuccess || allow_smem<EPI_CODED>() != cudaSuccess ||
                              cudaFuncSetAttribute(k_orth_small, cudaFuncAttributeMaxDynamicSharedMemorySize, small_bytes(kSmallLong)) != cudaSuccess ||
-                             cudaFuncSetAttribute(k_orth_cluster, cudaFuncAttributeMaxDynamicSharedMemorySize, kMidBytes) != cudaSuccess ||
-                             allow_layers() != cudaSuccess))
+                             cudaFuncSetAttribute(k_orth_cluster, cudaFuncAttributeMaxDynamicSharedMemorySize, kMidBytes) != cudaSuccess))
     status = RTOPK_ERR_CUDA;
   ctx->encode = (EncodeTiled)fn;
   ctx->scratch = (char*)scratch;

@@ -26,6 +26,7 @@ struct rtopk_matrix {
   EncodeTiled encode = nullptr;
   uint64_t launches = 0;
   int test_giveup = 0;              // RTOPK_MATRIX_OPT_TEST_GIVEUP
+  uint32_t allowed = 0;             // which families of layers.cu have their shared memory
 };
 
 namespace rtopk {
@@ -256,9 +257,6 @@ inline bool bad_view(const void* p, size_t elem, int64_t batch, int64_t m, int64
 }
 inline bool bad_dtype(int t) { return t != RTOPK_F32 && t != RTOPK_BF16; }
 inline size_t elem(int t) { return t == RTOPK_F32 ? 4 : 2; }
-
-
-cudaError_t allow_layers();      // the kernels of layers.cu: their shared memory
 
 }  // namespace mat
 }  // namespace rtopk

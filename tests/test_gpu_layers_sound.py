@@ -1,4 +1,8 @@
 """A worker's layers in calls that once went wrong.  Tolerances as derived in test_gpu_layers.py (u = 2^-24) unless a test says otherwise."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -167,3 +171,54 @@ def test_long_rows_of_equal_values(rt, cols):  # noqa: F811
         tol = r1 * (4 * U * gg + adds * gg.mean(1, keepdim=True) + h.abs() * (adds * along + (gg * eh).mean(1, keepdim=True)) + eh * along)
         close(dr, d, tol + 4 * U * d.abs() + 4 * U * r1 * (gg + along * h.abs()), "dresidual")
     ctx.close()
+
+
+FIRST = """
+import torch
+import paper_2005_10761_b200 as rt
+tokens, d, hidden = 70, 96, 200
+def buffers():
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, dy = (torch.randn((tokens, d), generator=g, device="cuda").to(ty) for _ in range(2))
+    io = dict(x=x, dy=dy, w=torch.randn((d, d), generator=g, device="cuda"), m=rt.MicroWeights(d, d))
+    for k in "o1", "h", "y", "t", "dr", "dh", "dx":
+        io[k] = torch.zeros_like(x)
+    io["o1"] = io["o1"][:1]
+    for k, n in (("mean", tokens), ("rstd", tokens), ("dgamma", d), ("dbeta", d)):
+        io[k] = torch.zeros(n, device="cuda")
+    io["dw"] = torch.zeros((d, d), device="cuda")
+    return io
+def calls(ctx, io):
+    spec = rt.Mask(0.2, 9, 1)
+    ctx.micro_weights(io["w"], io["m"])
+    ctx.micro_product(io["x"][:1], io["m"], io["o1"])
+    ctx.micro_product(io["x"], io["m"], io["h"])
+    ctx.dropout(io["h"], io["h"], spec)
+    ctx.layer_norm(io["h"], None, None, io["y"], residual=io["x"], total=io["t"], mean=io["mean"], rstd=io["rstd"], mask=spec)
+    ctx.layer_norm_gradients(io["dy"], io["t"], io["mean"], io["rstd"], None, io["dr"], dgamma=io["dgamma"], dbeta=io["dbeta"], dtotal=io["x"], dx=io["dh"], mask=spec)
+    ctx.micro_gradients(io["dh"], io["x"], io["m"], io["dx"], io["dw"])
+for ty in torch.float32, torch.bfloat16:
+    io, again = buffers(), buffers()
+    ctx = rt.MatrixContext(max(rt.micro_scratch(tokens, d, d), rt.layer_norm_scratch(tokens, d)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(ctx, io)
+    graph.replay()
+    torch.cuda.synchronize()
+    ctx.poll_status()
+    calls(ctx, again)
+    torch.cuda.synchronize()
+    for k in io:
+        if isinstance(io[k], torch.Tensor):
+            assert torch.equal(io[k], again[k]) and bool(io[k].any()), k
+    del graph
+    ctx.close()
+print("as later calls")
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured(rt):  # noqa: F811
+    """Kernels are loaded and given their shared memory at a context's first call of their kind, in a capture too."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    ran = subprocess.run([sys.executable, "-c", FIRST], cwd=root, capture_output=True, text=True, timeout=300)
+    assert ran.returncode == 0 and ran.stdout.strip() == "as later calls", ran.stdout + ran.stderr
