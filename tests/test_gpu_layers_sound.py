@@ -1,4 +1,4 @@
-"""A worker's layers in calls that once went wrong.  Tolerances as derived in test_gpu_layers.py (u = 2^-24) unless a test says otherwise."""
+"""A worker's layers in calls that once went wrong or that no test made.  Tolerances as derived in test_gpu_layers.py (u = 2^-24) unless a test says otherwise."""
 import os
 import subprocess
 import sys
@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+import test_gpu_layers as base
 from test_gpu_layers import TYPES, U, back64, close, norm64, normal, rounding, rt  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -170,6 +171,31 @@ def test_long_rows_of_equal_values(rt, cols):  # noqa: F811
         eh, along = 2.01 * U * h.abs(), (gg * h.abs()).mean(1, keepdim=True)
         tol = r1 * (4 * U * gg + adds * gg.mean(1, keepdim=True) + h.abs() * (adds * along + (gg * eh).mean(1, keepdim=True)) + eh * along)
         close(dr, d, tol + 4 * U * d.abs() + 4 * U * r1 * (gg + along * h.abs()), "dresidual")
+    ctx.close()
+
+
+# ------------------------------------------------------------------------------------------------- wide rows, several to a block
+@pytest.mark.parametrize("cols", [10000, 16384])
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("residual,p", [(False, 0.0), (True, 0.0), (True, 0.3)])
+def test_blocks_that_take_several_wide_rows(rt, cols, ty, residual, p):  # noqa: F811
+    rows = 700
+    base.test_layer_norm(rt, rows, cols, ty, residual, p)
+    base.test_layer_norm_gradients(rt, rows, cols, ty, residual, p)
+    # the same bits in place
+    ctx, spec = rt.MatrixContext(0), rt.Mask(p, 11, 3) if p else None
+    x, res, gamma = normal(rows, cols).to(ty), normal(rows, cols, seed=1).to(ty) if residual else None, 1 + 0.3 * normal(cols, seed=3)
+    y, total, mean, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    ctx.layer_norm(x, gamma, None, y, residual=res, total=total, mean=mean, rstd=rstd, mask=spec)
+    a, b = x.clone(), res.clone() if residual else torch.empty_like(x)
+    ctx.layer_norm(a, gamma, None, a, residual=b if residual else None, total=b, mask=spec)
+    assert torch.equal(a, y) and torch.equal(b, total)
+    dy, dt = normal(rows, cols, seed=5).to(ty), normal(rows, cols, seed=6).to(ty) if residual else None
+    dr, dx = torch.empty_like(x), torch.empty_like(x) if p else None
+    ctx.layer_norm_gradients(dy, total, mean, rstd, gamma, dr, dtotal=dt, dx=dx, mask=spec)
+    a, b = dy.clone(), dt.clone() if residual else None
+    ctx.layer_norm_gradients(a, total, mean, rstd, gamma, a, dtotal=b, dx=b if p else None, mask=spec)
+    assert torch.equal(a, dr) and (not p or torch.equal(b, dx))
     ctx.close()
 
 
