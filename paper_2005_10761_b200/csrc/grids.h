@@ -31,5 +31,12 @@ struct DropoutGrid {
   }
 };
 
+// Products whose contraction is cut: each tile has counters, each part room for its sums at the scratch's start.
+constexpr int kSplitTiles = 1024;                      // tiles of a split product
+constexpr int64_t kPartBytes = 128 * 256 * 4;          // the largest part of one block
+constexpr int kPartBlocks = 160;                       // blocks with such a part, at most
+constexpr int64_t kPartsBytes = kPartBlocks * kPartBytes;
+inline bool parts_fit(int64_t tiles, int64_t split, int64_t tile_bytes) { return split == 1 || (tiles <= kSplitTiles && split <= kPartsBytes / tile_bytes / tiles); }
+
 }  // namespace mat
 }  // namespace rtopk

@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "gemm.cuh"
+#include "grids.h"
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -64,10 +65,7 @@ constexpr int64_t kDimMax = 1 << 30;
 constexpr int64_t kBatchMax = 65535;
 constexpr int64_t kDepthMax = 131072;     // 127 * 127 * depth stays below 2^31
 
-constexpr int kSplitTiles = 1024;         // tiles of a split product: counters
-constexpr int64_t kPartBytes = kLanes * 256 * 4;       // partial sums of one block
-constexpr int kPartBlocks = 160;                       // blocks with a part, at most
-constexpr int64_t kPartsBytes = kPartBlocks * kPartBytes;
+static_assert(kPartBytes == kLanes * 256 * 4, "");
 constexpr int kErrorBytes = 1024 + 2 * kSplitTiles * 4;
 
 inline int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
@@ -162,6 +160,7 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
   constexpr int kBlocks = kPair ? 2 : 1;
   g.tiles_l = (int)ceil_div(g.lanes, S::kTileLanes), g.tiles_c = (int)ceil_div(g.cols, kCols);
   g.tiles = (int)gemm_tiles<kCols, kPair>(g);
+  if (!parts_fit((int64_t)g.tiles * g.batch, split, (int64_t)S::kTileLanes * kCols * 4)) return RTOPK_ERR_INTERNAL;      // the kernel would write past both
   g.split = split;
   g.test_giveup = ctx->test_giveup;
   if (split > 1) g.free_start = 0;      // the parts' room is the context's
@@ -184,7 +183,8 @@ int gemm_tile(rtopk_matrix* ctx, const Operand& p, const Operand& q, Gemm g, int
 // 4-bit codes have figures of their own: their steps hold twice the codes, their results no factors.  Fitted to 140 shapes from 9 x 256 -> 256 to
 // 8192 x 4096 -> 8192 in every tile and up to four parts: the choice is 1.4 % slower than the best on average.
 // They have no pair of 128 columns: of 63 such shapes and types it was the fastest for three, by 1.1 % at most, and mostly far behind
-// (8192 x 8192 -> 8192, bfloat16: 234 us, in 192 columns 206).
+// (8192 x 8192 -> 8192, bfloat16: 234 us, in 192 columns 206).  And in a trial build with tiles forced one of them did not come to its end
+// (5534 tokens, 3325 -> 6256, binary32), for a cause that is not known; another trial's did.
 //
 // Contractions beyond kStepsMax steps are cut further, as far as their parts fit the scratch, in several waves if need be: the tensor core
 // drops what falls below its accumulator's last bit, which in 4096 instructions takes up to 2.5e-4 of a sum of equal terms; the
@@ -206,7 +206,7 @@ int gemm(rtopk_matrix* ctx, const Operand& p, const Operand& q, const Gemm& g, c
     const int64_t sms = std::min(ctx->sms, kPartBlocks) / blocks, all = tiles * g.batch;
     const int64_t room = kPartsBytes / ((int64_t)cols * kLanes * blocks * 4), least = std::min(ceil_div(steps, kStepsMax), std::max<int64_t>(1, room / all));
     for (int split = (int)least; split <= std::max<int64_t>(8, least); ++split) {
-      if (split > 1 && ((split > least && all * split > sms) || steps < 4 * split || all > kSplitTiles)) break;
+      if (split > 1 && ((split > least && all * split > sms) || steps < 4 * split || !parts_fit(all, split, (int64_t)cols * kLanes * blocks * 4))) break;
       if ((split - 1) * ceil_div(steps, split) >= steps) continue;      // a part without any step
       const int64_t waves = ceil_div(all * split, sms);
       if (kMicro) {

@@ -19,6 +19,8 @@ void divisor_of(uint32_t d, uint32_t* out) {
   const Divisor v = divisor(d);
   out[0] = v.m, out[1] = v.d, out[2] = v.shift;
 }
+int fit(int64_t tiles, int64_t split, int64_t tile_bytes) { return parts_fit(tiles, split, tile_bytes); }
+int64_t limit(int which) { return which ? kPartsBytes : kSplitTiles; }
 }
 """
 
@@ -70,3 +72,17 @@ def test_quotients_by_multiplication(lib):
             for k in (q * d - 1, q * d, q * d + 1, (1 << 31) - 1):
                 if 0 <= k < 1 << 31:
                     assert (k if d == 1 else (k * m >> 32) >> shift) == k // d, (k, d)
+
+
+def test_parts_stay_within_their_counters_and_their_room(lib):
+    lib.limit.restype = ctypes.c_int64
+    counters, room = lib.limit(0), lib.limit(1)
+
+    def fit(tiles, split, tile_bytes):
+        return bool(lib.fit(ctypes.c_int64(tiles), ctypes.c_int64(split), ctypes.c_int64(tile_bytes)))
+    for lanes, cols in ((128, 64), (128, 128), (256, 128), (256, 192), (256, 256)):
+        size = lanes * cols * 4
+        for tiles in (1, 2, 3, 37, 74, 148, 160, 640, 1023, 1024, 1025, 1078, 1 << 30, 1 << 40):
+            assert fit(tiles, 1, size)
+            for split in (2, 3, 8, 160, 1 << 20, 1 << 40):
+                assert fit(tiles, split, size) == (tiles <= counters and tiles * split * size <= room), (lanes, cols, tiles, split)
