@@ -183,8 +183,8 @@ int dropout(rtopk_matrix* ctx, const T* x, int64_t ld_x, int64_t rows, int64_t c
 }
 
 // How a block takes rows: `warps` warps for each, `keep` pieces of 256 columns a warp, `rows_per` rows at a time.  Two pieces, so that what is
-// done once a row is shared by 16 columns of a thread; one where there are too few rows to fill the SMs, four where two do not
-// reach.  Without alignment the next row waits in registers, which four pieces would not leave.
+// done once a row is shared by 16 columns of a thread (many rows of one piece get two as well, the second empty); one where there are too few
+// rows to fill the SMs, four where two do not reach.  Without alignment the next row waits in registers, which four pieces would not leave.
 constexpr int kRowBlocks = 160;
 struct RowSplit {
   int warps, rows_per, keep;

@@ -5,7 +5,8 @@
 //   dt = rstd (g - mean(g) - h mean(g h)) + dtotal,  g = gamma dy, h = (t - mean) rstd;   dx = D(dt)
 //   dgamma = sum over the rows of dy h,   dbeta = sum over the rows of dy
 //
-// All of it is bound by memory: a row is read once and kept in registers between its sums and its results.
+// All of it is bound by memory.  Forwards a row that fits a block is read once and kept in registers between its sums and its results; the gradients
+// read it from shared memory for its sums and again for its results; of longer rows what does not fit is read from memory again.
 #pragma once
 
 #include "common.cuh"
@@ -206,8 +207,11 @@ struct NormArgs {
 // barrier nor the sums' latency stops the block; one barrier a row, of the row's warps.
 //
 // The bound is memory as long as the instructions keep up: 16 columns a thread, so that a row's sums, addresses and statistics are shared
-// by 16, and places in shared memory that differ by constants.  Bfloat16 with dropout and residual sum: 8192 x 4096 51.5 us; gradients of
-// 16384 x 8192 259 us (5.2 TB/s both; instructions are issued in 62 % of the cycles).  A block for each row took 417 for the latter.
+// by 16, and places in shared memory that differ by constants.  Bfloat16 with dropout and residual sum: 8192 x 4096 51.8 us; gradients of
+// 16384 x 8192 258 us (5.2 TB/s both; instructions are issued in 61 and 64 % of the cycles).  A block for each row took 417 for the latter.
+// Widths that do not fill the block's 16 warps leave some of that: 8192 x 4608, 9 warps, 79 us, and rows of one piece most of it: 262144 x 64
+// without dropout and residual 106 us.  Without alignment values are loaded one by one: 8192 x 4095 121 us.  Binary32 rows of 8193 to 16384 columns
+// with a residual have one stage, so that nothing is on its way during a row's sums: 4096 x 16384 294 us, 3.7 TB/s.
 constexpr int kRowWarps = 16, kRowSmem = 216 * 1024;
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
