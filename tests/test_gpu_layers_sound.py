@@ -199,6 +199,40 @@ def test_blocks_that_take_several_wide_rows(rt, cols, ty, residual, p):  # noqa:
     ctx.close()
 
 
+def test_two_contexts_at_once(rt):  # noqa: F811
+    """Blocks of two workers on streams of their own, eager and replayed: the same bits as one after another."""
+    workers, spec = [], rt.Mask(0.2, 99, 4, worker=1)
+    for tokens, d, hidden, ty, seed in ((300, 515, 1029, torch.bfloat16, 40), (700, 1024, 2048, torch.float32, 80)):
+        ctx = rt.MatrixContext(max(rt.micro_scratch(tokens, hidden, d), rt.layer_norm_scratch(tokens, d)))
+        io = base.block_buffers(rt, ctx, tokens, d, hidden, ty, seed)
+        base.block(rt, ctx, spec, io)
+        torch.cuda.synchronize()
+        want = {k: io[k].clone() for k in base.RESULTS}
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            base.block(rt, ctx, spec, io)
+        workers.append((ctx, io, want, torch.cuda.Stream(), graph))
+    for replayed in (False, True):
+        for _, io, _, _, _ in workers:
+            for k in base.RESULTS:
+                io[k].fill_(5.0)
+        torch.cuda.synchronize()
+        for _ in range(30):
+            for ctx, io, _, stream, graph in workers:
+                with torch.cuda.stream(stream):
+                    if replayed:
+                        graph.replay()
+                    else:
+                        base.block(rt, ctx, spec, io)
+        torch.cuda.synchronize()
+        for ctx, io, want, _, _ in workers:
+            ctx.poll_status()
+            for k in base.RESULTS:
+                assert torch.equal(io[k], want[k]), (replayed, k)
+    while workers:
+        workers.pop()[0].close()
+
+
 FIRST = """
 import torch
 import paper_2005_10761_b200 as rt
